@@ -21,9 +21,10 @@
  * --------------------------------
  *   Hkv = num_kv_heads, g = group_size, Hq = Hkv * g, d = head_dim,
  *   P = page_size, w = window.  Query head q attends with KV head q / g.
- *   Keys and queries are passed after any positional encoding; the library
- *   never applies positions (keys "carry positional information", Sec. 3.2),
- *   so the order of retained slots is irrelevant to attention.
+ *   Keys and queries are passed after any positional encoding; the cache and
+ *   attention calls never apply positions (keys "carry positional
+ *   information", Sec. 3.2), so the order of retained slots is irrelevant to
+ *   attention.  dms_rope_fwd rotates projected queries and keys beforehand.
  *
  *   bf16 tensors are IEEE bfloat16 bit patterns (uint16), row-major, densely
  *   packed.  Decode inputs: q [n, Hq, d], k / v [n, Hkv, d], flags [n, Hkv]
@@ -265,6 +266,33 @@ int dms_init_state(dms_ctx* ctx, void* stream);
  * ring are cleared.  seq_ids_dev: int32 [n]. */
 int dms_seq_reset(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev, void* stream);
 
+/* Copy sequences in every layer (layer = -1) or one layer: dst_ids[i] becomes a
+ * copy of src_ids[i] -- position, retained lengths, ring, slots and the live
+ * tiles (32 slots) of its pages, page bounds included -- on pages of its own.
+ * The paper scales inference by sampling many chains from one prompt (Sec. 2.1);
+ * a chain recycles slots in place (Sec. 3.2), so chains share no pages.
+ * A source may be listed any number of times (copies listed next to each other
+ * share its reads) and may be empty.  Destinations must be distinct, empty in
+ * every layer of the call (dms_seq_reset) and no sources: DMS_ERR_BAD_SEQ in
+ * the sticky status otherwise, DMS_ERR_OUT_OF_PAGES where a layer's free pages
+ * do not suffice; then no layer changes.  A layer's copies take their pages
+ * off its stack as one block, the block's lowest entry first, in the order
+ * (pair in call order, head, page-table index): releasing the copies in call
+ * order and forking again gives the same pages, also on replays of a captured
+ * graph.  src_ids_dev, dst_ids_dev: int32 [n]. */
+int dms_seq_fork(dms_ctx* ctx, int layer, int n, const int32_t* src_ids_dev,
+                 const int32_t* dst_ids_dev, void* stream);
+
+/* Move the live pages of every layer (layer = -1) or one layer to the front of
+ * its pool: with U live pages, the pages with ids >= U move, in ascending order,
+ * to the free ids below U in ascending order; page tables (and page bounds)
+ * follow, and the free pages U .. num_pages-1 are stacked as by dms_init_state
+ * (popped U, U+1, ...).  Attention is unchanged.  The first U pages are then all
+ * that a snapshot or an offload of the pool has to hold.
+ * pages_used_out_dev: int32 [num_layers] (layer = -1) or [1], may be NULL:
+ * receives U per layer. */
+int dms_compact(dms_ctx* ctx, int layer, int32_t* pages_used_out_dev, void* stream);
+
 /* Append one token per listed sequence to one layer (Sec. 3.2 cache
  * management).  For each (sequence, KV head), with t = pos:
  *   if t >= w and the token at t - w was flagged, the new token takes that
@@ -466,6 +494,124 @@ int dms_gumbel_sigmoid_fwd(int n, const float* logits_dev, const float* u_dev, f
 /* dlogit = dalpha * alpha (1 - alpha) / tau. */
 int dms_gumbel_sigmoid_bwd(int n, const float* alpha_dev, const float* dalpha_dev, float tau,
                            float* dlogits_dev, void* stream);
+
+/*
+ * Rotary positions of queries and keys
+ * ------------------------------------
+ * Each head's elements rotary_offset .. rotary_offset + rotary_dim - 1 form
+ * rotary_dim / 2 pairs; pair i of a token turns by the angle
+ * pos[axis(i)] * inv_freq[i]:
+ *   y1 = f (x1 cos - x2 sin),  y2 = f (x1 sin + x2 cos),  f = factor;
+ * the other elements are copied.  A token has a position on each of num_axes
+ * axes (one: text; three: the time, height and width of image and video
+ * tokens), and axis(i) follows from `sections`, the pairs of each axis:
+ *   DMS_ROPE_SECTIONS: the first sections[0] pairs belong to axis 0, the next
+ *     sections[1] to axis 1, ...;
+ *   DMS_ROPE_INTERLEAVED: pair i belongs to axis a = i % num_axes if
+ *     i / num_axes < sections[a], else to axis 0 (sections[0] is the largest).
+ * Angles are formed in float64 (positions anywhere in int32), rotations in
+ * float32 and rounded once to the output type.
+ *
+ * borrow = 1 takes the decision neuron of App. C before it is rotated: element 0
+ * of the first query head of each KV head's group is written out (logits_out)
+ * and, with decision_bias added in float32, compared with 0 (decisions_out, the
+ * flags of the cache calls), then treated as 0.  A context that receives such
+ * queries is configured with DMS_DECIDE_CALLER.
+ */
+enum { DMS_TYPE_BF16 = 0, DMS_TYPE_F32 = 1 };
+enum { DMS_ROPE_SECTIONS = 0, DMS_ROPE_INTERLEAVED = 1 };
+enum { DMS_ROPE_HALVES = 0,     /* pair i: elements i and i + rotary_dim / 2 */
+       DMS_ROPE_ADJACENT = 1 }; /* pair i: elements 2 i and 2 i + 1 */
+
+typedef struct dms_rope_config {
+  int32_t num_kv_heads;   /* Hkv >= 1 */
+  int32_t group_size;     /* g = Hq / Hkv >= 1 */
+  int32_t head_dim;       /* d; a row of all query heads has at most 2^20 elements */
+  int32_t rotary_dim;     /* even, 2 .. min(d, 512) */
+  int32_t rotary_offset;  /* first rotated element (latent rows: 512) */
+  int32_t num_axes;       /* 1 .. 4 */
+  int32_t sections[4];    /* pairs of each axis, adding to rotary_dim / 2 */
+  int32_t axis_order;     /* DMS_ROPE_SECTIONS or DMS_ROPE_INTERLEAVED */
+  int32_t pairing;        /* DMS_ROPE_HALVES or DMS_ROPE_ADJACENT */
+  int32_t in_type;        /* DMS_TYPE_*: what a call reads */
+  int32_t out_type;       /* DMS_TYPE_*: what a call writes */
+  int32_t borrow;         /* 0 or 1 */
+  float decision_bias;    /* b added to the borrowed neuron */
+  float factor;           /* <= 0 selects 1 */
+} dms_rope_config;
+
+/* Rotate `tokens` tokens.  q_dev [tokens][Hq][d] and k_dev [tokens][Hkv][d] (in_type)
+ * have q_stride / k_stride elements from a token to the next (>= Hq d / Hkv d: they
+ * may be parts of the rows of one projection); q_out_dev, k_out_dev (out_type) are
+ * dense.  Either of q and k may be NULL together with its output.
+ * positions_dev: int32 [num_axes][tokens]; inv_freq_dev: float64 [rotary_dim / 2].
+ * logits_out_dev float32 [tokens][Hkv], decisions_out_dev uint8 [tokens][Hkv]: with
+ * borrow and q only, each may be NULL.  An output may be its input (dense, same
+ * type) and must not overlap one otherwise. */
+int dms_rope_fwd(const dms_rope_config* cfg, int tokens, const void* q_dev, int64_t q_stride,
+                 const void* k_dev, int64_t k_stride, const int32_t* positions_dev,
+                 const double* inv_freq_dev, void* q_out_dev, void* k_out_dev,
+                 float* logits_out_dev, uint8_t* decisions_out_dev, void* stream);
+
+/* Gradients of q and k from those of the rotated q and k (dq_dev, dk_dev: in_type,
+ * dense), rotated back.  With borrow the neuron's gradient is dlogits_dev (float32
+ * [tokens][Hkv]; NULL: 0).  dq_out_dev, dk_out_dev (out_type) have dq_stride /
+ * dk_stride elements from a token to the next; what lies between is left alone. */
+int dms_rope_bwd(const dms_rope_config* cfg, int tokens, const void* dq_dev, const void* dk_dev,
+                 const int32_t* positions_dev, const double* inv_freq_dev,
+                 const float* dlogits_dev, void* dq_out_dev, int64_t dq_stride,
+                 void* dk_out_dev, int64_t dk_stride, void* stream);
+
+/*
+ * Attention with a sliding window and sinks (training layers)
+ * -----------------------------------------------------------
+ * Window attention that keeps the first tokens of a sequence visible: key j is
+ * visible to query t iff j <= t and (j > t - w or j < sinks), positions counted
+ * inside the sequence.  It is the DMS mask of decisions that are 0 for the first
+ * `sinks` tokens and 1 for all others, so that the cache calls serve a layer
+ * trained with it (flags 0 / 1); work grows with T w instead of T^2.
+ * Sequences are packed: sequence i owns tokens cu_seqlens[i] .. cu_seqlens[i+1]-1
+ * (int32 [num_seqs + 1] on the device, cu[0] = 0, non-decreasing, cu[num_seqs] <=
+ * total_tokens, no sequence longer than max_seqlen; sequences may be empty).
+ * Rows from cu[num_seqs] on belong to no sequence and are left as they are.
+ * Layouts (row-major, dense; bf16 tensors 16-byte aligned):
+ *   q, out, dout, dq  bf16 [total_tokens, Hq, d]
+ *   k, v, dk, dv      bf16 [total_tokens, Hkv, d]
+ *   lse               f32  [Hq, total_tokens]   natural log of each softmax denominator
+ * Products take bf16 operands (probabilities and score gradients are rounded to
+ * bf16 for them) and accumulate in float32; softmax statistics and all sums are
+ * float32, outputs are rounded once.  Gradients are of sum(out * dout) and
+ * overwrite their buffers; their sums have a fixed order.  Every call reads and
+ * writes inside its tensors whatever cu_seqlens_dev holds; values that break its
+ * rules make the rows of the sequences concerned undefined.  One workspace
+ * (dms_window_workspace bytes, 256-byte aligned, contents of no meaning between
+ * calls) serves one stream at a time.
+ */
+typedef struct dms_window_config {
+  int32_t num_seqs;       /* n >= 1, at most 65535 */
+  int32_t total_tokens;   /* rows of the tensors, >= 0 */
+  int32_t max_seqlen;     /* longest sequence, 0 .. total_tokens */
+  int32_t num_kv_heads;   /* Hkv >= 1 */
+  int32_t group_size;     /* g = Hq / Hkv, 1 .. 16 */
+  int32_t head_dim;       /* d: 64 or 128 */
+  int32_t window;         /* w >= 1 */
+  int32_t sinks;          /* first tokens that stay visible, >= 0 */
+  float softmax_scale;    /* <= 0 selects 1 / sqrt(head_dim) */
+} dms_window_config;
+
+int dms_window_workspace(const dms_window_config* cfg, size_t* workspace_bytes);
+
+/* Forward: out and lse. */
+int dms_window_attention_fwd(const dms_window_config* cfg, const int32_t* cu_seqlens_dev,
+                             const void* q_dev, const void* k_dev, const void* v_dev,
+                             void* out_dev, float* lse_dev, void* workspace_dev, void* stream);
+
+/* Backward: dq, dk, dv from the forward's inputs, out, lse and dout. */
+int dms_window_attention_bwd(const dms_window_config* cfg, const int32_t* cu_seqlens_dev,
+                             const void* q_dev, const void* k_dev, const void* v_dev,
+                             const void* out_dev, const float* lse_dev, const void* dout_dev,
+                             void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
+                             void* stream);
 
 #ifdef __cplusplus
 }

@@ -9,3 +9,5 @@ from .latency_model import *  # noqa: F401,F403
 from .train_oracle import *  # noqa: F401,F403
 from .kv_fp8 import *  # noqa: F401,F403
 from .quest import *  # noqa: F401,F403
+from .window_oracle import *  # noqa: F401,F403
+from .rope_oracle import *  # noqa: F401,F403

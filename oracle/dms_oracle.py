@@ -434,6 +434,48 @@ class PagedKVOracle:
             self.ring_flag[s] = 0
 
     # -- attention over the live slots (compact route) -------------------------
+    # -- copies and compaction ------------------------------------------------
+    def seq_fork(self, src_ids, dst_ids):
+        """Every dst becomes a copy of its src; the call's pages are one block off the stack, the
+        block's lowest entry first, by (pair, head, page index)."""
+        D = self.dims
+        P = D.page_size
+        src, dst = [int(s) for s in src_ids], [int(s) for s in dst_ids]
+        if len(set(dst)) < len(dst) or set(src) & set(dst) or any(self.pos[s] for s in dst):
+            raise ValueError("destinations must be distinct, empty and no sources")
+        need = [(s, d, h, i) for s, d in zip(src, dst) for h in range(D.num_kv_heads)
+                for i in range(-(-int(self.L[s, h]) // P))]
+        if len(need) > self.top:
+            raise OutOfPages(f"needs {len(need)} pages, {self.top} free")
+        self.top -= len(need)
+        for at, (s, d, h, i) in enumerate(need):
+            self.page_table[d, h, i] = self.stack[self.top + at]
+        for s, d in zip(src, dst):
+            self.pos[d], self.L[d] = self.pos[s], self.L[s]
+            self.ring_slot[d], self.ring_flag[d] = self.ring_slot[s], self.ring_flag[s]
+            self.slot_pos[d], self.slot_flag[d] = self.slot_pos[s], self.slot_flag[s]
+            if self.store_values:
+                self.k_store[d], self.v_store[d] = self.k_store[s], self.v_store[s]
+                if self.kv_format == "fp8":
+                    for x in (self.k_codes, self.v_codes, self.k_exp, self.v_exp):
+                        x[d] = x[s]
+
+    def compact(self):
+        """Live pages past the live count move, ascending, to the free ids below it, ascending; the
+        free pages are stacked so that the lowest is popped first.  Returns the live count."""
+        D = self.dims
+        used = D.num_pages - self.top
+        free = {int(x) for x in self.stack[:self.top]}
+        holes = [i for i in range(used) if i in free]
+        moved = [i for i in range(used, D.num_pages) if i not in free]
+        to = dict(zip(moved, holes))
+        for s in range(D.max_seqs):
+            for h in range(D.num_kv_heads):
+                for i in range(-(-int(self.L[s, h]) // D.page_size)):
+                    self.page_table[s, h, i] = to.get(int(self.page_table[s, h, i]), self.page_table[s, h, i])
+        self.stack[:self.top] = np.arange(D.num_pages - 1, used - 1, -1)
+        return used
+
     def live_positions(self, s, h):
         return self.slot_pos[s, h, : self.L[s, h]].copy()
 

@@ -4,11 +4,13 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <initializer_list>
 #include <mutex>
 #include <vector>
 
 #include "dms_common.h"
 #include "dms_fp8.h"
+#include "dms_ops.h"
 #include "dms_train.h"
 
 namespace dms {
@@ -124,6 +126,11 @@ Layout make_layout(const dms_config& c) {
   lo.ws_q_sel = take(NH * static_cast<size_t>(c.quest_page_budget) * 4);
   lo.ws_q_page = take(NH * static_cast<size_t>(c.quest_page_budget) * 4);
   lo.ws_q_len = take(NH * 4);
+  const size_t Ly = c.num_layers;
+  lo.ws_fk_base = take(Ly * NH * 4);
+  lo.ws_fk_tiles = take(Ly * (NH + 1) * 4);
+  lo.ws_fk_block = take(Ly * 8);
+  lo.ws_cp_map = take(Ly * static_cast<size_t>(c.num_pages) * 4);
   lo.workspace_bytes = off;
   return lo;
 }
@@ -339,6 +346,24 @@ int dms_seq_reset(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev, vo
   if (n < 1 || n > ctx->c.cfg.max_seqs || !seq_ids_dev) return DMS_ERR_INVALID;
   return hip_rc(dms::launch_seq_reset(ctx->c.cfg, ctx->c.lo, ctx->c.meta, layer, n, seq_ids_dev,
                                       as_stream(stream)));
+}
+
+int dms_seq_fork(dms_ctx* ctx, int layer, int n, const int32_t* src_ids_dev, const int32_t* dst_ids_dev,
+                 void* stream) {
+  if (!ctx) return DMS_ERR_INVALID;
+  if (layer < -1 || layer >= ctx->c.cfg.num_layers) return DMS_ERR_INVALID;
+  if (n < 1 || n > ctx->c.cfg.max_seqs || !src_ids_dev || !dst_ids_dev) return DMS_ERR_INVALID;
+  const Ctx& c = ctx->c;
+  return hip_rc(dms::launch_seq_fork(c.cfg, c.lo, c.meta, c.ws, c.pools.data(), layer, n, src_ids_dev,
+                                     dst_ids_dev, as_stream(stream)));
+}
+
+int dms_compact(dms_ctx* ctx, int layer, int32_t* pages_used_out_dev, void* stream) {
+  if (!ctx) return DMS_ERR_INVALID;
+  if (layer < -1 || layer >= ctx->c.cfg.num_layers) return DMS_ERR_INVALID;
+  const Ctx& c = ctx->c;
+  return hip_rc(dms::launch_compact(c.cfg, c.lo, c.meta, c.ws, c.pools.data(), layer, pages_used_out_dev,
+                                    as_stream(stream)));
 }
 
 int dms_append(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev, const void* k_dev,
@@ -756,6 +781,140 @@ int dms_gumbel_sigmoid_bwd(int n, const float* alpha_dev, const float* dalpha_de
   if (n == 0) return DMS_OK;
   if (!alpha_dev || !dalpha_dev || !dlogits_dev) return DMS_ERR_INVALID;
   return hip_rc(dms::launch_gumbel_bwd(n, alpha_dev, dalpha_dev, tau, dlogits_dev, as_stream(stream)));
+}
+
+// ---------------------------------------------------------------------------
+// Rotary positions
+// ---------------------------------------------------------------------------
+
+static int validate_rope_config(const dms_rope_config* c) {
+  if (!c) return DMS_ERR_INVALID;
+  if (c->num_kv_heads < 1 || c->group_size < 1 || c->head_dim < 2) return DMS_ERR_INVALID;
+  // products of two int32 fit an int64; of three of them only once two are known to be small
+  const int64_t heads = static_cast<int64_t>(c->num_kv_heads) * c->group_size;
+  if (heads > (int64_t(1) << 20) || heads * c->head_dim > (int64_t(1) << 20)) return DMS_ERR_UNSUPPORTED;
+  if (c->rotary_dim < 2 || c->rotary_dim % 2 || c->rotary_offset < 0) return DMS_ERR_INVALID;
+  if (c->rotary_dim > c->head_dim || c->rotary_offset > c->head_dim - c->rotary_dim) return DMS_ERR_INVALID;
+  if (c->rotary_dim > dms::kMaxRotary) return DMS_ERR_UNSUPPORTED;
+  if (c->num_axes < 1 || c->num_axes > dms::kRopeAxes) return DMS_ERR_INVALID;
+  if (c->axis_order != DMS_ROPE_SECTIONS && c->axis_order != DMS_ROPE_INTERLEAVED) return DMS_ERR_INVALID;
+  if (c->pairing != DMS_ROPE_HALVES && c->pairing != DMS_ROPE_ADJACENT) return DMS_ERR_INVALID;
+  int64_t pairs = 0;
+  for (int x = 0; x < c->num_axes; ++x) {
+    if (c->sections[x] < 0) return DMS_ERR_INVALID;
+    if (c->axis_order == DMS_ROPE_INTERLEAVED && c->sections[x] > c->sections[0]) return DMS_ERR_INVALID;
+    pairs += c->sections[x];
+  }
+  if (pairs != c->rotary_dim / 2) return DMS_ERR_INVALID;
+  if (c->in_type != DMS_TYPE_BF16 && c->in_type != DMS_TYPE_F32) return DMS_ERR_INVALID;
+  if (c->out_type != DMS_TYPE_BF16 && c->out_type != DMS_TYPE_F32) return DMS_ERR_INVALID;
+  if (c->borrow != 0 && c->borrow != 1) return DMS_ERR_INVALID;
+  if (c->borrow && !isfinite(c->decision_bias)) return DMS_ERR_INVALID;
+  if (isnan(c->factor) || isinf(c->factor)) return DMS_ERR_INVALID;
+  return DMS_OK;
+}
+
+// Tensors of one call: q and k each present with their output or both absent,
+// strides no shorter than a row.
+static int check_rope_call(const dms_rope_config* c, int tokens, const dms::RopeTensors& t, const void* positions,
+                           const void* inv_freq) {
+  if (tokens < 0) return DMS_ERR_INVALID;
+  const int64_t kv = static_cast<int64_t>(c->num_kv_heads) * c->head_dim, qr = kv * c->group_size;
+  if (t.q_stride < qr || t.k_stride < kv || t.q_out_stride < qr || t.k_out_stride < kv) return DMS_ERR_INVALID;
+  // one thread per pair and a grid of fewer than 2^31 workgroups
+  if (tokens * (qr + kv) >= int64_t(1) << 38) return DMS_ERR_UNSUPPORTED;
+  if (tokens == 0) return DMS_OK;
+  if (!t.q != !t.q_out || !t.k != !t.k_out || (!t.q && !t.k) || !positions || !inv_freq) return DMS_ERR_INVALID;
+  return DMS_OK;
+}
+
+int dms_rope_fwd(const dms_rope_config* cfg, int tokens, const void* q_dev, int64_t q_stride, const void* k_dev,
+                 int64_t k_stride, const int32_t* positions_dev, const double* inv_freq_dev, void* q_out_dev,
+                 void* k_out_dev, float* logits_out_dev, uint8_t* decisions_out_dev, void* stream) {
+  int rc = validate_rope_config(cfg);
+  if (rc) return rc;
+  const int64_t kv = static_cast<int64_t>(cfg->num_kv_heads) * cfg->head_dim, qr = kv * cfg->group_size;
+  const dms::RopeTensors t{q_dev, k_dev, q_out_dev, k_out_dev, q_dev ? q_stride : qr, k_dev ? k_stride : kv, qr, kv};
+  if ((rc = check_rope_call(cfg, tokens, t, positions_dev, inv_freq_dev))) return rc;
+  if ((logits_out_dev || decisions_out_dev) && !(cfg->borrow && (q_dev || tokens == 0))) return DMS_ERR_INVALID;
+  if (tokens == 0) return DMS_OK;
+  return hip_rc(dms::launch_rope(*cfg, tokens, t, positions_dev, inv_freq_dev, false, logits_out_dev,
+                                 decisions_out_dev, nullptr, as_stream(stream)));
+}
+
+int dms_rope_bwd(const dms_rope_config* cfg, int tokens, const void* dq_dev, const void* dk_dev,
+                 const int32_t* positions_dev, const double* inv_freq_dev, const float* dlogits_dev,
+                 void* dq_out_dev, int64_t dq_stride, void* dk_out_dev, int64_t dk_stride, void* stream) {
+  int rc = validate_rope_config(cfg);
+  if (rc) return rc;
+  const int64_t kv = static_cast<int64_t>(cfg->num_kv_heads) * cfg->head_dim, qr = kv * cfg->group_size;
+  const dms::RopeTensors t{dq_dev, dk_dev, dq_out_dev, dk_out_dev, qr, kv, dq_dev ? dq_stride : qr,
+                           dk_dev ? dk_stride : kv};
+  if ((rc = check_rope_call(cfg, tokens, t, positions_dev, inv_freq_dev))) return rc;
+  if (dlogits_dev && !(cfg->borrow && (dq_dev || tokens == 0))) return DMS_ERR_INVALID;
+  if (tokens == 0) return DMS_OK;
+  return hip_rc(dms::launch_rope(*cfg, tokens, t, positions_dev, inv_freq_dev, true, nullptr, nullptr, dlogits_dev,
+                                 as_stream(stream)));
+}
+
+// ---------------------------------------------------------------------------
+// Attention with a sliding window and sinks
+// ---------------------------------------------------------------------------
+
+static int validate_window_config(const dms_window_config* c) {
+  if (!c) return DMS_ERR_INVALID;
+  if (c->num_seqs < 1 || c->num_seqs > 65535 || c->total_tokens < 0) return DMS_ERR_INVALID;
+  if (c->max_seqlen < 0 || c->max_seqlen > c->total_tokens) return DMS_ERR_INVALID;
+  if (c->total_tokens > 0 && c->max_seqlen == 0) return DMS_ERR_INVALID;
+  if (c->num_kv_heads < 1 || c->group_size < 1 || c->window < 1 || c->sinks < 0) return DMS_ERR_INVALID;
+  if (c->group_size > dms::kMaxGroup) return DMS_ERR_UNSUPPORTED;
+  if (c->head_dim != 64 && c->head_dim != 128) return DMS_ERR_UNSUPPORTED;
+  if (isnan(c->softmax_scale) || (c->softmax_scale > 0.0f && !isfinite(c->softmax_scale))) return DMS_ERR_INVALID;
+  // rows of the query tensors; a grid row per KV head; a token's bytes in 32 bits
+  const int64_t heads = static_cast<int64_t>(c->num_kv_heads) * c->group_size;
+  if (c->num_kv_heads > 4096 || heads * c->total_tokens >= int64_t(1) << 31) return DMS_ERR_UNSUPPORTED;
+  return DMS_OK;
+}
+
+int dms_window_workspace(const dms_window_config* cfg, size_t* workspace_bytes) {
+  const int rc = validate_window_config(cfg);
+  if (rc) return rc;
+  if (workspace_bytes) *workspace_bytes = dms::window_workspace_bytes(*cfg);
+  return DMS_OK;
+}
+
+// Every tensor present and aligned for 16-byte accesses.
+static int check_aligned(std::initializer_list<const void*> tensors) {
+  for (const void* p : tensors)
+    if (!p || reinterpret_cast<uintptr_t>(p) % 16) return DMS_ERR_INVALID;
+  return DMS_OK;
+}
+
+int dms_window_attention_fwd(const dms_window_config* cfg, const int32_t* cu_seqlens_dev, const void* q_dev,
+                             const void* k_dev, const void* v_dev, void* out_dev, float* lse_dev,
+                             void* workspace_dev, void* stream) {
+  int rc = validate_window_config(cfg);
+  if (rc) return rc;
+  if (cfg->total_tokens == 0) return DMS_OK;
+  if (!cu_seqlens_dev || !lse_dev || !workspace_dev || reinterpret_cast<uintptr_t>(workspace_dev) % dms::kAlign)
+    return DMS_ERR_INVALID;
+  if ((rc = check_aligned({q_dev, k_dev, v_dev, out_dev}))) return rc;
+  return hip_rc(dms::launch_window_fwd(*cfg, cu_seqlens_dev, q_dev, k_dev, v_dev, out_dev, lse_dev, workspace_dev,
+                                       as_stream(stream)));
+}
+
+int dms_window_attention_bwd(const dms_window_config* cfg, const int32_t* cu_seqlens_dev, const void* q_dev,
+                             const void* k_dev, const void* v_dev, const void* out_dev, const float* lse_dev,
+                             const void* dout_dev, void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
+                             void* stream) {
+  int rc = validate_window_config(cfg);
+  if (rc) return rc;
+  if (cfg->total_tokens == 0) return DMS_OK;
+  if (!cu_seqlens_dev || !lse_dev || !workspace_dev || reinterpret_cast<uintptr_t>(workspace_dev) % dms::kAlign)
+    return DMS_ERR_INVALID;
+  if ((rc = check_aligned({q_dev, k_dev, v_dev, out_dev, dout_dev, dq_dev, dk_dev, dv_dev}))) return rc;
+  return hip_rc(dms::launch_window_bwd(*cfg, cu_seqlens_dev, q_dev, k_dev, v_dev, out_dev, lse_dev, dout_dev, dq_dev,
+                                       dk_dev, dv_dev, workspace_dev, as_stream(stream)));
 }
 
 }  // extern "C"

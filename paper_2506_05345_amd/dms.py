@@ -73,6 +73,47 @@ MLA_ROW_DIM = 576      # latent (512) + rotary key (64)
 MLA_LATENT_DIM = 512
 
 
+class DmsRopeConfig(ctypes.Structure):
+    _fields_ = [
+        ("num_kv_heads", ctypes.c_int32),
+        ("group_size", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("rotary_offset", ctypes.c_int32),
+        ("num_axes", ctypes.c_int32),
+        ("sections", ctypes.c_int32 * 4),
+        ("axis_order", ctypes.c_int32),
+        ("pairing", ctypes.c_int32),
+        ("in_type", ctypes.c_int32),
+        ("out_type", ctypes.c_int32),
+        ("borrow", ctypes.c_int32),
+        ("decision_bias", ctypes.c_float),
+        ("factor", ctypes.c_float),
+    ]
+
+
+class DmsWindowConfig(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32),
+        ("total_tokens", ctypes.c_int32),
+        ("max_seqlen", ctypes.c_int32),
+        ("num_kv_heads", ctypes.c_int32),
+        ("group_size", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("window", ctypes.c_int32),
+        ("sinks", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float),
+    ]
+
+
+DMS_TYPE_BF16 = 0
+DMS_TYPE_F32 = 1
+DMS_ROPE_SECTIONS = 0
+DMS_ROPE_INTERLEAVED = 1
+DMS_ROPE_HALVES = 0
+DMS_ROPE_ADJACENT = 1
+
+
 class DmsStateOffsets(ctypes.Structure):
     _fields_ = [(n, ctypes.c_size_t) for n in
                 ("status", "layer0", "layer_stride", "pos", "len", "ring", "page_table",
@@ -89,6 +130,7 @@ _lib = None
 _VP = ctypes.c_void_p
 _I = ctypes.c_int
 _SZ = ctypes.c_size_t
+_I64 = ctypes.c_int64
 
 _SIGS = {
     "dms_layout": (_I, [ctypes.POINTER(DmsConfig), ctypes.POINTER(_SZ), ctypes.POINTER(_SZ),
@@ -99,6 +141,8 @@ _SIGS = {
     "dms_destroy": (_I, [_VP]),
     "dms_init_state": (_I, [_VP, _VP]),
     "dms_seq_reset": (_I, [_VP, _I, _I, _VP, _VP]),
+    "dms_seq_fork": (_I, [_VP, _I, _I, _VP, _VP, _VP]),
+    "dms_compact": (_I, [_VP, _I, _VP, _VP]),
     "dms_append": (_I, [_VP, _I, _I, _VP, _VP, _VP, _VP, _VP]),
     "dms_decode": (_I, [_VP, _I, _I, _VP, _VP, _VP, _VP]),
     "dms_decode_step": (_I, [_VP, _I, _I, _VP, _VP, _VP, _VP, _VP, _VP, _VP]),
@@ -122,6 +166,11 @@ _SIGS = {
                                      _VP, _VP, _VP, _VP, _VP, _VP, _VP]),
     "dms_gumbel_sigmoid_fwd": (_I, [_I, _VP, _VP, ctypes.c_float, _VP, _VP]),
     "dms_gumbel_sigmoid_bwd": (_I, [_I, _VP, _VP, ctypes.c_float, _VP, _VP]),
+    "dms_rope_fwd": (_I, [ctypes.POINTER(DmsRopeConfig), _I, _VP, _I64, _VP, _I64] + [_VP] * 7),
+    "dms_rope_bwd": (_I, [ctypes.POINTER(DmsRopeConfig), _I] + [_VP] * 6 + [_I64, _VP, _I64, _VP]),
+    "dms_window_workspace": (_I, [ctypes.POINTER(DmsWindowConfig), ctypes.POINTER(_SZ)]),
+    "dms_window_attention_fwd": (_I, [ctypes.POINTER(DmsWindowConfig)] + [_VP] * 8),
+    "dms_window_attention_bwd": (_I, [ctypes.POINTER(DmsWindowConfig)] + [_VP] * 12),
 }
 
 
@@ -171,6 +220,7 @@ _BF16 = "bf16"
 _U8 = "uint8"
 _I32 = "int32"
 _F32 = "float32"
+_F64 = "float64"
 
 
 def _args(where, *specs):
@@ -182,7 +232,8 @@ def _args(where, *specs):
     if all(x is None or isinstance(x, int) for x, *_ in specs):
         return
     import torch
-    kinds = {_BF16: torch.bfloat16, _U8: torch.uint8, _I32: torch.int32, _F32: torch.float32}
+    kinds = {_BF16: torch.bfloat16, _U8: torch.uint8, _I32: torch.int32, _F32: torch.float32,
+             _F64: torch.float64}
     live = []
     for x, name, kind, count in specs:
         if x is None or isinstance(x, int):
@@ -204,6 +255,29 @@ def _args(where, *specs):
 
 def _arg(x, name, kind, count, where):
     _args(where, (x, name, kind, count))
+
+
+def _one_device(where, *tensors):
+    """Tensors of one call lie on the current device, where its kernels run."""
+    devices = {x.device for x in tensors if hasattr(x, "data_ptr")}
+    if not devices:
+        return
+    import torch
+    if len(devices) > 1 or devices.pop().index != torch.cuda.current_device():
+        raise DmsError(DMS_ERR_INVALID, f"{where}: tensors must be on the current device")
+
+
+def _rows_stride(x, heads, dim, stride):
+    """Elements from a token's row to the next: `stride` if given; of a tensor [tokens, heads, dim]
+    whose rows are dense, its own; None where the rows are not dense."""
+    if stride is not None:
+        return stride
+    if x is None or isinstance(x, int) or x.is_contiguous():
+        return heads * dim
+    if x.dim() != 3 or x.shape[1:] != (heads, dim) or x.stride(2) != 1 or \
+            (heads > 1 and x.stride(1) != dim):
+        return None
+    return x.stride(0) if x.shape[0] > 1 else heads * dim
 
 
 def _dims(ctx):
@@ -279,6 +353,21 @@ def dms_init_state(ctx, stream=None):
 def dms_seq_reset(ctx, layer, n, seq_ids, stream=None):
     _arg(seq_ids, "seq_ids", _I32, n, "dms_seq_reset")
     _check(lib().dms_seq_reset(ctx, layer, n, _ptr(seq_ids), _stream(stream)), "dms_seq_reset")
+
+
+def dms_seq_fork(ctx, layer, n, src_ids, dst_ids, stream=None):
+    _args("dms_seq_fork", (src_ids, "src_ids", _I32, n), (dst_ids, "dst_ids", _I32, n))
+    _one_device("dms_seq_fork", src_ids, dst_ids)
+    _check(lib().dms_seq_fork(ctx, layer, n, _ptr(src_ids), _ptr(dst_ids), _stream(stream)),
+           "dms_seq_fork")
+
+
+def dms_compact(ctx, layer, pages_used_out=None, stream=None):
+    c = _CTX_CFG.get(ctx)
+    _arg(pages_used_out, "pages_used_out", _I32, c.num_layers if c is not None and layer < 0 else 1,
+         "dms_compact")
+    _one_device("dms_compact", pages_used_out)
+    _check(lib().dms_compact(ctx, layer, _ptr(pages_used_out), _stream(stream)), "dms_compact")
 
 
 def dms_append(ctx, layer, n, seq_ids, k, v, flags, stream=None):
@@ -583,3 +672,126 @@ def dms_gumbel_sigmoid_bwd(n, alpha, dalpha, tau, dlogits, stream=None):
           (dlogits, "dlogits", _F32, n))
     _check(lib().dms_gumbel_sigmoid_bwd(n, _ptr(alpha), _ptr(dalpha), tau, _ptr(dlogits),
                                         _stream(stream)), "dms_gumbel_sigmoid_bwd")
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions
+# ---------------------------------------------------------------------------
+
+def make_rope_config(num_kv_heads, group_size, head_dim, rotary_dim, sections, rotary_offset=0,
+                     axis_order=DMS_ROPE_SECTIONS, pairing=DMS_ROPE_HALVES, in_type=DMS_TYPE_BF16,
+                     out_type=DMS_TYPE_BF16, borrow=0, decision_bias=-5.0, factor=0.0) -> DmsRopeConfig:
+    """`sections`: the pairs of each axis, one entry per axis."""
+    sec = (ctypes.c_int32 * 4)(*list(sections)[:4])
+    return DmsRopeConfig(num_kv_heads, group_size, head_dim, rotary_dim, rotary_offset,
+                         len(sections), sec, axis_order, pairing, in_type, out_type, borrow,
+                         decision_bias, factor)
+
+
+def _rope_strided(where, x, name, tokens, heads, dim, kind, stride):
+    """Checks a tensor of rows that may lie apart and returns the rows' stride."""
+    if x is None or isinstance(x, int):
+        return heads * dim if stride is None else stride
+    import torch
+    want = {_BF16: torch.bfloat16, _F32: torch.float32}.get(kind)
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{where}: {name} must be a tensor or a device address, got {type(x)}")
+    if want is not None and x.dtype != want:
+        raise DmsError(DMS_ERR_INVALID, f"{where}: {name} must be {kind}, got {x.dtype}")
+    if not x.is_cuda:
+        raise DmsError(DMS_ERR_INVALID, f"{where}: {name} must be a GPU tensor")
+    got = _rows_stride(x, heads, dim, stride)
+    if got is None:
+        raise DmsError(DMS_ERR_INVALID, f"{where}: {name} must have dense rows of [{heads}, {dim}]")
+    # elements from the first to the end of the last row inside the tensor's own extent
+    have = 1 + sum((n - 1) * st for n, st in zip(x.shape, x.stride())) if x.numel() else 0
+    if tokens > 0 and have < (tokens - 1) * got + heads * dim:
+        raise DmsError(DMS_ERR_INVALID, f"{where}: {name} holds fewer than {tokens} rows")
+    return got
+
+
+_TYPE_KIND = {DMS_TYPE_BF16: _BF16, DMS_TYPE_F32: _F32}
+
+
+def dms_rope_fwd(cfg, tokens, q, k, positions, inv_freq, q_out, k_out, logits_out=None,
+                 decisions_out=None, q_stride=None, k_stride=None, stream=None):
+    """q [tokens, Hq, d] and k [tokens, Hkv, d] may be parts of wider rows: the stride is theirs, or
+    given (device addresses)."""
+    w = "dms_rope_fwd"
+    H, Hq, d = cfg.num_kv_heads, cfg.num_kv_heads * cfg.group_size, cfg.head_dim
+    tin, tout = _TYPE_KIND.get(cfg.in_type), _TYPE_KIND.get(cfg.out_type, _F32)
+    qs = _rope_strided(w, q, "q", tokens, Hq, d, tin, q_stride)
+    ks = _rope_strided(w, k, "k", tokens, H, d, tin, k_stride)
+    _args(w, (positions, "positions", _I32, cfg.num_axes * tokens),
+          (inv_freq, "inv_freq", _F64, cfg.rotary_dim // 2),
+          (q_out, "q_out", tout, tokens * Hq * d), (k_out, "k_out", tout, tokens * H * d),
+          (logits_out, "logits_out", _F32, tokens * H), (decisions_out, "decisions_out", _U8, tokens * H))
+    _one_device(w, q, k, positions, inv_freq, q_out, k_out, logits_out, decisions_out)
+    _check(lib().dms_rope_fwd(ctypes.byref(cfg), tokens, _ptr(q), qs, _ptr(k), ks, _ptr(positions),
+                              _ptr(inv_freq), _ptr(q_out), _ptr(k_out), _ptr(logits_out),
+                              _ptr(decisions_out), _stream(stream)), w)
+
+
+def dms_rope_bwd(cfg, tokens, dq, dk, positions, inv_freq, dlogits, dq_out, dk_out, dq_stride=None,
+                 dk_stride=None, stream=None):
+    """dq_out [tokens, Hq, d] and dk_out [tokens, Hkv, d] may be parts of wider rows."""
+    w = "dms_rope_bwd"
+    H, Hq, d = cfg.num_kv_heads, cfg.num_kv_heads * cfg.group_size, cfg.head_dim
+    tin, tout = _TYPE_KIND.get(cfg.in_type, _F32), _TYPE_KIND.get(cfg.out_type)
+    qs = _rope_strided(w, dq_out, "dq_out", tokens, Hq, d, tout, dq_stride)
+    ks = _rope_strided(w, dk_out, "dk_out", tokens, H, d, tout, dk_stride)
+    _args(w, (positions, "positions", _I32, cfg.num_axes * tokens),
+          (inv_freq, "inv_freq", _F64, cfg.rotary_dim // 2),
+          (dq, "dq", tin, tokens * Hq * d), (dk, "dk", tin, tokens * H * d),
+          (dlogits, "dlogits", _F32, tokens * H))
+    _one_device(w, dq, dk, positions, inv_freq, dlogits, dq_out, dk_out)
+    _check(lib().dms_rope_bwd(ctypes.byref(cfg), tokens, _ptr(dq), _ptr(dk), _ptr(positions),
+                              _ptr(inv_freq), _ptr(dlogits), _ptr(dq_out), qs, _ptr(dk_out), ks,
+                              _stream(stream)), w)
+
+
+# ---------------------------------------------------------------------------
+# Attention with a sliding window and sinks
+# ---------------------------------------------------------------------------
+
+def make_window_config(num_seqs, total_tokens, max_seqlen, num_kv_heads, group_size, head_dim, window,
+                       sinks=0, softmax_scale=0.0) -> DmsWindowConfig:
+    return DmsWindowConfig(num_seqs, total_tokens, max_seqlen, num_kv_heads, group_size, head_dim,
+                           window, sinks, softmax_scale)
+
+
+def dms_window_workspace(cfg: DmsWindowConfig) -> int:
+    n = _SZ()
+    _check(lib().dms_window_workspace(ctypes.byref(cfg), ctypes.byref(n)), "dms_window_workspace")
+    return n.value
+
+
+def _check_window_args(cfg, where, workspace, cu_seqlens, **t):
+    T, H, D = cfg.total_tokens, cfg.num_kv_heads, cfg.head_dim
+    rows = {"k": T * H, "v": T * H, "dk": T * H, "dv": T * H}
+    specs = [(cu_seqlens, "cu_seqlens", _I32, cfg.num_seqs + 1)]
+    for name, x in t.items():
+        n = rows.get(name, T * H * cfg.group_size)
+        specs.append((x, name, _F32, n) if name == "lse" else (x, name, _BF16, n * D))
+    if workspace is not None and not isinstance(workspace, int):
+        specs.append((workspace, "workspace", _U8, dms_window_workspace(cfg)))
+    _args(where, *specs)
+    _one_device(where, workspace, cu_seqlens, *t.values())
+
+
+def dms_window_attention_fwd(cfg, cu_seqlens, q, k, v, out, lse, workspace, stream=None):
+    _check_window_args(cfg, "dms_window_attention_fwd", workspace, cu_seqlens, q=q, k=k, v=v, out=out,
+                       lse=lse)
+    _check(lib().dms_window_attention_fwd(ctypes.byref(cfg), _ptr(cu_seqlens), _ptr(q), _ptr(k),
+                                          _ptr(v), _ptr(out), _ptr(lse), _ptr(workspace),
+                                          _stream(stream)), "dms_window_attention_fwd")
+
+
+def dms_window_attention_bwd(cfg, cu_seqlens, q, k, v, out, lse, dout, dq, dk, dv, workspace,
+                             stream=None):
+    _check_window_args(cfg, "dms_window_attention_bwd", workspace, cu_seqlens, q=q, k=k, v=v, out=out,
+                       lse=lse, dout=dout, dq=dq, dk=dk, dv=dv)
+    _check(lib().dms_window_attention_bwd(ctypes.byref(cfg), _ptr(cu_seqlens), _ptr(q), _ptr(k),
+                                          _ptr(v), _ptr(out), _ptr(lse), _ptr(dout), _ptr(dq),
+                                          _ptr(dk), _ptr(dv), _ptr(workspace), _stream(stream)),
+           "dms_window_attention_bwd")
