@@ -237,4 +237,17 @@ __device__ inline u32x4 col_operand(int tile, const LaneAddresses<D>& r, int b, 
 // keeps the compiler from forming (and holding) every operand address ahead of the loop
 __device__ inline void refresh(LaneOffsets& o) { asm volatile("" : "+v"(o.row), "+v"(o.col), "+v"(o.src)); }
 
+// Scheduling order of a stretch of M MFMAs: P LDS reads ahead, then R reads
+// beside each (bounds the operands in flight, so that the accumulators and the
+// resident operands fit without spills).
+template <int P, int M, int R>
+__device__ __forceinline__ void paced() {
+  __builtin_amdgcn_sched_group_barrier(0x100, P, 0);
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
+  }
+}
+
 }  // namespace dms

@@ -60,18 +60,6 @@ constexpr float kLn2 = 0.6931471805599453f;
 // by step (sched_barrier): left alone the compiler reads most operands right
 // before their MFMA and waits out the LDS latency every time.
 constexpr int kAhead = 4;
-// Scheduling order of a stretch of M MFMAs: P LDS reads ahead, then R reads
-// beside each (bounds the operands in flight, so that the accumulators and the
-// resident operands fit without spills).
-template <int P, int M, int R>
-__device__ __forceinline__ void paced() {
-  __builtin_amdgcn_sched_group_barrier(0x100, P, 0);
-#pragma unroll
-  for (int i = 0; i < M; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
-  }
-}
 // Key-major pass, whose sums and operands leave few registers: its score
 // products are paced (pinned, they ran 2680 against 2437 us), its sums pinned
 // with two operands ahead (2437 against 2495 us paced, and 72 against 84 where

@@ -20,6 +20,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kCols = 128;            // (position, query head) columns of a query block, 32 per wave
 constexpr int kAhead = 4;              // operands are read this many MFMAs ahead, in pinned order
+constexpr int kFew = 2;                // the same for the key-major pass, whose registers are short
 constexpr float kRescale = 8.0f;      // lazy rescale threshold, log2 units
 constexpr float kMInit = -1.0e30f;    // running max before the first visible key
 constexpr float kLog2e = 1.4426950408889634f;
@@ -27,14 +28,18 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 struct WindowArgs {
   const int32_t* cu;
-  const __bf16 *q, *k, *v, *dout;
+  const __bf16 *q, *k, *v, *o, *dout;
   const float* lse;
   __bf16 *out, *dq, *dk, *dv;
   float* lse_out;
-  float* row;              // [Hq][T] D_t (workspace)
+  f32x2* rows;             // [Hq][Ts]: -lse / scale (raw score units) and -D of each query (workspace)
+  float* part;             // sinks' sums: [slots][tiles][H] of (dk, dv) [32][D] of the far queries, then
+                           // [slots] of the same from the key blocks (workspace)
+  int64_t Ts;              // rows of a head in `rows`: T + 32, whole tiles are read past a sequence
   int n, T, H, g, w, sinks;
   int single;              // every row sees one key: P = 1 and dS = 0
   int PB;                  // positions of a query block: kCols / g
+  int sink_tiles;          // 32-key tiles of sinks whose far queries go to workgroups of their own (else 0)
   float scale_log2;
 };
 
@@ -42,18 +47,6 @@ struct WindowArgs {
 __device__ inline int2 bounds_of(const WindowArgs& a, int i) {
   const int lo = min(max(a.cu[i], 0), a.T);
   return make_int2(lo, min(max(a.cu[i + 1], lo), a.T));
-}
-
-// Bounds of the sequence that owns packed token t (x > t: none).
-__device__ inline int2 sequence_of(const WindowArgs& a, int t) {
-  int lo = 0, hi = a.n;   // first i with cu[i + 1] > t
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (a.cu[mid + 1] > t) hi = mid; else lo = mid + 1;
-  }
-  if (lo == a.n) return make_int2(t + 1, t + 1);
-  const int2 b = bounds_of(a, lo);
-  return b.x <= t && t < b.y ? b : make_int2(t + 1, t + 1);
 }
 
 __device__ inline float wave_sum(float x) {
@@ -64,24 +57,25 @@ __device__ inline float wave_sum(float x) {
 
 // Block b of a packed launch whose blocks hold PB tokens each: sequence i owns blocks
 // cu[i] / PB + i .. cu[i + 1] / PB + i, at least as many as it needs, so that a block finds its sequence
-// by a search over cu (64 candidates a round) and the host needs no prefix sums.
+// by a search over cu (64 candidates a round) and the host needs no prefix sums.  With per_seq = 0 the
+// blocks are cu[i] / PB + 0, 1, ... instead, which is unambiguous for sequences longer than PB.
 struct Block {
   int s0, len, p0;   // first token and length of the sequence, first position of the block (>= len: no block)
 };
-__device__ inline Block block_of(const WindowArgs& a, int b, int PB) {
+__device__ inline Block block_of(const WindowArgs& a, int b, int PB, int per_seq = 1) {
   const int lane = threadIdx.x & 63;
   int lo = 0, cnt = a.n;
   while (cnt > 1) {
     const int step = (cnt + 63) >> 6;
     const int i = min(lo + lane * step, a.n);
-    const bool le = lane * step < cnt && min(max(a.cu[i], 0), a.T) / PB + i <= b;
+    const bool le = lane * step < cnt && min(max(a.cu[i], 0), a.T) / PB + per_seq * i <= b;
     const int k = max(1, __builtin_popcountll(__builtin_amdgcn_ballot_w64(le)));
     lo += (k - 1) * step;
     cnt = min(step, cnt - (k - 1) * step);
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   const int2 r = bounds_of(a, lo);
-  return Block{r.x, r.y - r.x, max(b - (r.x / PB + lo), 0) * PB};
+  return Block{r.x, r.y - r.x, max(b - (r.x / PB + per_seq * lo), 0) * PB};
 }
 
 // Keys that queries [p0, p1) of a sequence see, as tiles of 32: `nsk` tiles of sinks from position 0
@@ -333,85 +327,590 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(WindowArgs a) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// dQ pass.  Workgroups, columns and tiles as in the forward.  Per key tile:
+// S^T = K Q^T and dP^T = V dO^T over rows, dQ^T += K^T dS^T over columns.  It
+// also leaves -lse and -D of every row to the key-major pass.  EXACT: D_t is
+// summed from P and dP in a first walk over the tiles (two more products and no
+// reading of `out`), else formed from dO and the rounded `out`.
+// ---------------------------------------------------------------------------
+// A dQ row as exact_row above.
 template <int D>
-__global__ __launch_bounds__(kThreads) void window_dq_kernel(WindowArgs a) {
+__device__ inline void exact_dq_row(const WindowArgs& a, int s0, int t, int hq) {
   constexpr int E = D / 64;
-  const int Hq = a.H * a.g, lane = threadIdx.x & 63;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
-  if (row >= static_cast<int64_t>(a.T) * Hq) return;
-  const int t = static_cast<int>(row / Hq), hq = static_cast<int>(row % Hq), h = hq / a.g;
-  const int2 b = sequence_of(a, t);
-  if (b.x > t) return;
+  const int lane = threadIdx.x & 63, Hq = a.H * a.g, h = hq / a.g;
+  const size_t row = (static_cast<size_t>(s0 + t) * Hq + hq) * D + E * lane;
   float q[E], dO[E], dq[E] = {}, d = 0.f, sum = 0.f;
+#pragma unroll
   for (int e = 0; e < E; ++e) {
-    q[e] = static_cast<float>(a.q[row * D + E * lane + e]);
-    dO[e] = static_cast<float>(a.dout[row * D + E * lane + e]);
+    q[e] = static_cast<float>(a.q[row + e]);
+    dO[e] = static_cast<float>(a.dout[row + e]);
   }
-  const float lse2 = a.lse[static_cast<size_t>(hq) * a.T + t] * kLog2e;
-  bool second = false;
-  auto key = [&](int j) {
-    const size_t kr = (static_cast<size_t>(j) * a.H + h) * D + E * lane;
-    float s = 0.f, dp = 0.f;
-    for (int e = 0; e < E; ++e) {
-      s += q[e] * static_cast<float>(a.k[kr + e]);
-      dp += dO[e] * static_cast<float>(a.v[kr + e]);
-    }
-    const float p = exp2f(wave_sum(s) * a.scale_log2 - lse2);
-    dp = wave_sum(dp);
-    if (second) {
-      const float ds = p * (dp - d);
-      for (int e = 0; e < E; ++e) dq[e] += ds * static_cast<float>(a.k[kr + e]);
-    } else {
-      d += p * dp;
-      sum += p;
-    }
-  };
-  const int band = max(b.x, t - a.w + 1);
+  const float lse2 = a.lse[static_cast<size_t>(hq) * a.T + s0 + t] * kLog2e;
+  const int band = max(0, t - a.w + 1);
+#pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
-    for (int j = b.x; j < min(band, b.x + a.sinks); ++j) key(j);
-    for (int j = band; j <= t; ++j) key(j);
-    if (!second) d /= sum;
-    second = true;
+    int j = a.sinks > 0 ? 0 : band;
+#pragma unroll 1
+    while (j <= t) {
+      const size_t kr = (static_cast<size_t>(s0 + j) * a.H + h) * D + E * lane;
+      float k[E], s = 0.f, dp = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        k[e] = static_cast<float>(a.k[kr + e]);
+        s += q[e] * k[e];
+        dp += dO[e] * static_cast<float>(a.v[kr + e]);
+      }
+      const float p = exp2f(wave_sum(s) * a.scale_log2 - lse2);
+      dp = wave_sum(dp);
+      if (pass) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) dq[e] += p * (dp - d) * k[e];
+      } else {
+        d += p * dp;
+        sum += p;
+      }
+      j = j + 1 >= a.sinks ? max(j + 1, band) : j + 1;
+    }
+    if (!pass) d /= sum;
   }
-  if (lane == 0) a.row[static_cast<size_t>(hq) * a.T + t] = d;
-  for (int e = 0; e < E; ++e) a.dq[row * D + E * lane + e] = static_cast<__bf16>(a.single ? 0.f : dq[e] * a.scale_log2 / kLog2e);
+#pragma unroll
+  for (int e = 0; e < E; ++e) a.dq[row + e] = static_cast<__bf16>(a.single ? 0.f : dq[e] * a.scale_log2 / kLog2e);
+  if (lane == 0) a.rows[hq * a.Ts + s0 + t] = f32x2{-lse2 / a.scale_log2, -d};
 }
 
-// A wave per key; it walks the queries that see the key, every head of the group.
-template <int D>
-__global__ __launch_bounds__(kThreads) void window_dkv_kernel(WindowArgs a) {
-  constexpr int E = D / 64;
-  const int Hq = a.H * a.g, lane = threadIdx.x & 63;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
-  if (row >= static_cast<int64_t>(a.T) * a.H) return;
-  const int j = static_cast<int>(row / a.H), h = static_cast<int>(row % a.H);
-  const int2 b = sequence_of(a, j);
-  if (b.x > j) return;
-  float k[E], v[E], dk[E] = {}, dv[E] = {};
-  for (int e = 0; e < E; ++e) {
-    k[e] = static_cast<float>(a.k[row * D + E * lane + e]);
-    v[e] = static_cast<float>(a.v[row * D + E * lane + e]);
+template <int D, bool EXACT>
+__global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
+  using Tile = TileOf<D>;
+  constexpr int kUnit = Tile::kUnit, kStage = 4 * kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
+  __shared__ __attribute__((aligned(256))) char tile_lds[2][kStage];
+  const int2 wg = xcd_order();
+  const int h = wg.y;
+  const Block blk = block_of(a, wg.x, a.PB);
+  if (blk.p0 >= blk.len) return;
+  const int s0 = blk.s0, p0 = blk.p0, p1 = min(blk.len, p0 + a.PB);
+  const KeyTiles kt = key_tiles(a, p0, p1);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hf = lane >> 5;
+  const int Hq = a.H * a.g;
+
+  const uint32_t stride = a.H * Tile::kRowB;
+  const LaneOffsets lo = lane_offsets<D>(lane, stride);
+  const uint32_t tiles = lds_addr(tile_lds);
+  const char* kv = reinterpret_cast<const char*>((wave >> 1 ? a.v : a.k) + (static_cast<size_t>(s0) * a.H + h) * D);
+  const int steps = (kt.nt + 1) >> 1, walk = EXACT ? 2 * steps : steps;
+  auto issue = [&](int st, int buf) {
+    const int i = 2 * (EXACT && st >= steps ? st - steps : st) + (wave & 1);
+    copy_tile<D>(kv, i < kt.nt ? kt.first(i) : p1, p1, stride, lo, lane,
+                 tiles + buf * kStage + 2 * kUnit * (wave & 1) + kUnit * (wave >> 1), &kZeros);
+  };
+  issue(0, 0);
+
+  const int col = wave * 32 + (lane & 31);
+  const int pl = col / a.g, qh = col % a.g;
+  const bool ok = pl < a.PB && p0 + pl < p1;
+  const int t = ok ? p0 + pl : p0;
+  const size_t row = static_cast<size_t>(s0 + t) * Hq + h * a.g + qh;
+  u32x4 qf[kKS], df[kKS];
+  float dcol = 0.f, psum = 0.f;
+#pragma unroll
+  for (int x = 0; x < kKS; ++x) {
+    qf[x] = ok ? ld16(a.q + row * D + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
+    df[x] = ok ? ld16(a.dout + row * D + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
+    if (!EXACT && ok) {
+      const u32x4 ov = ld16(a.o + row * D + 16 * x + 8 * hf);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        dcol += __uint_as_float(df[x][i] << 16) * __uint_as_float(ov[i] << 16) +
+                __uint_as_float(df[x][i] & 0xFFFF0000u) * __uint_as_float(ov[i] & 0xFFFF0000u);
+    }
   }
-  const int end = j - b.x < a.sinks ? b.y : static_cast<int>(min<int64_t>(b.y, static_cast<int64_t>(j) + a.w));
-  for (int t = j; t < end; ++t)
-    for (int hq = h * a.g; hq < (h + 1) * a.g; ++hq) {
-      const size_t qr = (static_cast<size_t>(t) * Hq + hq) * D + E * lane;
-      float s = 0.f, dp = 0.f;
-      for (int e = 0; e < E; ++e) {
-        const float dO = static_cast<float>(a.dout[qr + e]);
-        s += k[e] * static_cast<float>(a.q[qr + e]);
-        dp += v[e] * dO;
+  if (!EXACT) dcol = col_sum(dcol);
+  const size_t at = static_cast<size_t>(h * a.g + qh) * a.T + s0 + t;
+  const float lse2 = ok ? a.lse[at] * kLog2e : 0.f;
+  const int q0 = p0 + wave * 32 / a.g, q1 = min(p1 - 1, p0 + (wave * 32 + 31) / a.g);
+  const LaneAddresses<D> ad = lane_addresses<D>(tiles, lo);
+
+  f32x16 dqa[kDB];
+#pragma unroll
+  for (int x = 0; x < kDB; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dqa[x][i] = 0.f;
+
+  auto attend = [&](int v, auto buf_c) {
+    constexpr int buf = decltype(buf_c)::value;
+    wait_copies();
+    __syncthreads();
+    if (v + 1 < walk) issue(v + 1, buf ^ 1);
+    const bool first = EXACT && v < steps;   // summing D
+    const int st = EXACT && v >= steps ? v - steps : v;
+    if (EXACT && v == steps) dcol = col_sum(dcol) / col_sum(psum);
+    const float start = first ? 0.f : -dcol;   // -D in every row starts the dP products
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      const int i = 2 * st + sub, j0 = kt.first(i);
+      const int cls = mask_class(a, kt, i, j0, q0, q1);
+      if (cls == kNone) continue;
+      const int tl = buf * kStage + 2 * kUnit * sub;
+      f32x16 s, dp;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        s[x] = 0.f;
+        dp[x] = start;
       }
-      const float p = exp2f(wave_sum(s) * a.scale_log2 - a.lse[static_cast<size_t>(hq) * a.T + t] * kLog2e);
-      const float ds = p * (wave_sum(dp) - a.row[static_cast<size_t>(hq) * a.T + t]);
+      u32x4 op[kAhead];
+      // product e: scores (keys) and dP (values) take turns, k-step e / 2
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) op[e] = row_operand(tl + kUnit * (e & 1), ad, e >> 1);
+#pragma unroll
+      for (int e = 0; e < 2 * kKS; ++e) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (e & 1) dp = mfma(op[e % kAhead], df[e >> 1], dp);
+        else s = mfma(op[e % kAhead], qf[e >> 1], s);
+        if (e + kAhead < 2 * kKS) op[e % kAhead] = row_operand(tl + kUnit * (e & 1), ad, (e + kAhead) >> 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (cls == kSome) hide(s, a, i < kt.nsk, j0, t, hf);
+      if (first) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2, -lse2));
+          dcol += p * dp[x];
+          psum += p;
+        }
+        continue;
+      }
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) op[e] = col_operand(tl, ad, e % kDB, e / kDB);
+      float ds[16];
+#pragma unroll
+      for (int x = 0; x < 16; ++x) ds[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2, -lse2)) * dp[x];
+      const u32x4 du[2] = {pack_bf16(ds), pack_bf16(ds + 8)};   // rounded as in the key-major pass
+#pragma unroll
+      for (int e = 0; e < 2 * kDB; ++e) {
+        __builtin_amdgcn_sched_barrier(0);
+        dqa[e % kDB] = mfma(op[e % kAhead], du[e / kDB], dqa[e % kDB]);
+        if (e + kAhead < 2 * kDB) op[e % kAhead] = col_operand(tl, ad, (e + kAhead) % kDB, (e + kAhead) / kDB);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  for (int v = 0; v < walk; v += 2) {
+    attend(v, std::integral_constant<int, 0>{});
+    if (v + 1 < walk) attend(v + 1, std::integral_constant<int, 1>{});
+  }
+
+  if (ok && hf == 0)
+    a.rows[static_cast<size_t>(h * a.g + qh) * a.Ts + s0 + t] = f32x2{-lse2 / a.scale_log2, -dcol};
+  const float scale = a.scale_log2 / kLog2e;
+  bool bad = not_finite(dcol);
+#pragma unroll
+  for (int x = 0; x < kDB; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      bad |= not_finite(dqa[x][i]);
+      if (a.single) dqa[x][i] = 0.f;
+    }
+  store_row<D>(a.dq + row * D, dqa, scale, hf, ok);
+  const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && ok);
+  for (uint32_t cols = static_cast<uint32_t>(lanes | lanes >> 32); cols; cols &= cols - 1) {
+    const int c = wave * 32 + __builtin_ctz(cols);
+    exact_dq_row<D>(a, s0, p0 + c / a.g, h * a.g + c % a.g);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dK / dV pass.  Workgroup = (KV head, 128 keys of one sequence); wave x owns 32
+// of them as the columns of its products, with their K and V operands in
+// registers, and walks the query tiles (32 positions) that see the block, every
+// head of the group: dV^T += dO^T P, dK^T += Q^T dS with P, dS [query, key] from
+// S = Q K^T, dP = dO V^T.
+// A sink is seen by every later query.  A block that holds sinks walks on to
+// position kFar; what lies further is shared out to workgroups of kFar
+// positions (`far` below), whose sums window_sinks_kernel adds in order.
+// ---------------------------------------------------------------------------
+constexpr int kFar = 512;
+constexpr int kKeys = 128;
+
+// First position (a multiple of 32) that the block of keys from j0 on leaves to others.
+__device__ inline int far_begin(const WindowArgs& a, int j0) {
+  const int end = j0 + ((kKeys + a.w + 31) & ~31);
+  return j0 < a.sinks ? max(end, kFar) : end;
+}
+
+// dK and dV of key j by one wave from the queries that see it.
+template <int D>
+__device__ inline void exact_key(const WindowArgs& a, int s0, int len, int j, int h) {
+  constexpr int E = D / 64;
+  const int lane = threadIdx.x & 63, Hq = a.H * a.g;
+  const size_t kr = (static_cast<size_t>(s0 + j) * a.H + h) * D + E * lane;
+  float k[E], v[E], dk[E] = {}, dv[E] = {};
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    k[e] = static_cast<float>(a.k[kr + e]);
+    v[e] = static_cast<float>(a.v[kr + e]);
+  }
+  const int end = j < a.sinks ? len : static_cast<int>(min<int64_t>(len, static_cast<int64_t>(j) + a.w));
+#pragma unroll 1
+  for (int t = j; t < end; ++t)
+#pragma unroll 1
+    for (int hq = h * a.g; hq < (h + 1) * a.g; ++hq) {
+      const size_t qr = (static_cast<size_t>(s0 + t) * Hq + hq) * D + E * lane;
+      float q[E], dO[E], s = 0.f, dp = 0.f;
+#pragma unroll
       for (int e = 0; e < E; ++e) {
-        dv[e] += p * static_cast<float>(a.dout[qr + e]);
-        dk[e] += ds * static_cast<float>(a.q[qr + e]);
+        q[e] = static_cast<float>(a.q[qr + e]);
+        dO[e] = static_cast<float>(a.dout[qr + e]);
+        s += k[e] * q[e];
+        dp += v[e] * dO[e];
+      }
+      const f32x2 r = a.rows[hq * a.Ts + s0 + t];
+      const float p = exp2f((wave_sum(s) + r[0]) * a.scale_log2), ds = p * (wave_sum(dp) + r[1]);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        dv[e] += p * dO[e];
+        dk[e] += ds * q[e];
       }
     }
+#pragma unroll
   for (int e = 0; e < E; ++e) {
-    a.dk[row * D + E * lane + e] = static_cast<__bf16>(a.single ? 0.f : dk[e] * a.scale_log2 / kLog2e);
-    a.dv[row * D + E * lane + e] = static_cast<__bf16>(dv[e]);
+    a.dk[kr + e] = static_cast<__bf16>(a.single ? 0.f : dk[e] * a.scale_log2 / kLog2e);
+    a.dv[kr + e] = static_cast<__bf16>(dv[e]);
+  }
+}
+
+// Sums of far queries: slot b of the workspace belongs to positions 512 c .. of the sequence that starts in
+// the packed tokens' (b - c)-th 512, c >= 1; a sequence's key blocks leave theirs in slot cu / 512.  Only
+// sequences longer than 512 have any, so that no two share a slot.
+__device__ inline float* part_of(const WindowArgs& a, bool blocks, int slot, int tile, int h, int D) {
+  const size_t slots = a.T / kFar + 1;
+  return a.part + (((blocks ? slots : 0) + slot) * a.sink_tiles + tile) * a.H * 64 * D + static_cast<size_t>(h) * 64 * D;
+}
+
+// The (query tile, head) steps of a workgroup: tiles first .. last, heads inside a tile.
+template <int D>
+struct QuerySteps {
+  const WindowArgs& a;
+  const char* src;        // this wave's tensor (queries or output gradients), first token of the sequence
+  const f32x2* rows;      // the first head's rows, first token of the sequence
+  int len, total, wave, lane;
+  uint32_t stride, tiles, row_lds;
+  int ld_step, ld_qh, ld_pos;
+
+  __device__ QuerySteps(const WindowArgs& a, int s0, int len, int h, int first, int count, int wave, int lane,
+                        uint32_t tiles, uint32_t row_lds)
+      : a(a), len(len), total(count * a.g), wave(wave), lane(lane), tiles(tiles), row_lds(row_lds) {
+    const int Hq = a.H * a.g;
+    stride = Hq * TileOf<D>::kRowB;
+    src = reinterpret_cast<const char*>((wave >> 1 ? a.dout : a.q) + (static_cast<size_t>(s0) * Hq + h * a.g) * D);
+    rows = a.rows + h * a.g * a.Ts + s0;
+    ld_step = wave & 1;
+    ld_qh = ld_step % a.g;
+    ld_pos = first + 32 * (ld_step / a.g);
+  }
+  // this wave copies tensor wave / 2 of step 2 st + wave % 2, and the step's row sums
+  __device__ void issue(int buf, const LaneOffsets& lo) {
+    constexpr int kUnit = TileOf<D>::kUnit;
+    if (ld_step < total) {
+      copy_tile<D>(src + static_cast<size_t>(ld_qh) * TileOf<D>::kRowB, ld_pos, len, stride, lo, lane,
+                   tiles + buf * 4 * kUnit + 2 * kUnit * (wave & 1) + kUnit * (wave >> 1), &kZeros);
+      if (wave < 2)
+        lds_copy4(rows + ld_qh * a.Ts + ld_pos, 4 * fresh(lane), row_lds + 512 * buf + 256 * (wave & 1));
+    }
+    ld_step += 2;
+    ld_qh += 2;
+    while (ld_qh >= a.g) {
+      ld_qh -= a.g;
+      ld_pos += 32;
+    }
+  }
+};
+
+// Scores and dP of the step staged at `tl`, started from its rows' -lse and -D.
+template <int D, bool DP>
+__device__ __forceinline__ void query_products(uint32_t tl, const float* rows, const LaneOffsets& lo, const u32x4* kf,
+                                               const u32x4* vf, int hf, f32x16& s, f32x16& dp) {
+  constexpr int kKS = TileOf<D>::kKS;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const f32x4 r = *reinterpret_cast<const f32x4*>(rows + 2 * (16 * (i >> 2) + 8 * hf + 2 * (i & 3)));
+    s[2 * i] = r[0];
+    dp[2 * i] = r[1];
+    s[2 * i + 1] = r[2];
+    dp[2 * i + 1] = r[3];
+  }
+#pragma unroll
+  for (int x = 0; x < kKS; ++x) s = mfma(row_operand<D>(tl, lo, x), kf[x], s);
+  if (DP) {
+#pragma unroll
+    for (int x = 0; x < kKS; ++x) dp = mfma(row_operand<D>(tl + TileOf<D>::kUnit, lo, x), vf[x], dp);
+    paced<kKS + 2, 2 * kKS, 1>();
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// One sum of products over the step's queries: acc += (tensor at `tl`)^T w, w rounded to bf16 already.
+template <int D>
+__device__ __forceinline__ void query_sums(uint32_t tl, const LaneOffsets& lo, const u32x4* w, f32x16* acc) {
+  constexpr int kDB = TileOf<D>::kDB;
+  u32x4 op[kFew];
+#pragma unroll
+  for (int e = 0; e < kFew; ++e) op[e] = col_operand<D>(tl, lo, e % kDB, e / kDB);
+#pragma unroll
+  for (int e = 0; e < 2 * kDB; ++e) {
+    __builtin_amdgcn_sched_barrier(0);
+    acc[e % kDB] = mfma(op[e % kFew], w[e / kDB], acc[e % kDB]);
+    if (e + kFew < 2 * kDB) op[e % kFew] = col_operand<D>(tl, lo, (e + kFew) % kDB, (e + kFew) / kDB);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Accumulators of one key (column) to float32 rows.
+template <int D>
+__device__ inline void store_sums(float* dst, const f32x16* o, int hf) {
+#pragma unroll
+  for (int x = 0; x < TileOf<D>::kDB; ++x)
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      *reinterpret_cast<f32x4*>(dst + 32 * x + 8 * y + 4 * hf) =
+          f32x4{o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]};
+}
+
+// Weights exp(s - lse) of a step's queries tq .. tq + 31 (register i of a lane: query tq + 16 (i / 8) + 8 hf
+// + i % 8) for the 32 keys from key0 on, 0 where a query does not see the key or is none.
+__device__ __forceinline__ void query_weights(const WindowArgs& a, f32x16& s, int tq, int key0, int len, int lane) {
+  if (tq + 31 < len && tq >= key0 + 31 && (tq + 31 < key0 + a.w || key0 + 32 <= a.sinks)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * a.scale_log2);
+    return;
+  }
+  const int ln = fresh(lane);
+  const int j = key0 + (ln & 31), t0 = tq + 8 * (ln >> 5);
+  const int first = j - t0;                                                    // first query that sees the key
+  const int end = min(len - t0, j < a.sinks ? len - t0 : first + a.w);         // first one that does not
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int c = 16 * (i >> 3) + (i & 7);
+    s[i] = c >= first && c < end ? __builtin_amdgcn_exp2f(s[i] * a.scale_log2) : 0.f;
+  }
+}
+
+// Sums of one tile of sinks over the queries of [first, last).  The two steps of a stage go to two waves
+// each: one sums dV, the other dK.
+template <int D>
+__device__ __forceinline__ void far_queries(const WindowArgs& a, char* tile_lds, const float (*row_lds)[2][64], int s0,
+                                            int len, int h, int key0, int first, int last, int slot) {
+  using Tile = TileOf<D>;
+  constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
+  const int lane = threadIdx.x & 63, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tiles = lds_addr(tile_lds);
+  QuerySteps<D> qs(a, s0, len, h, first, (last - first + 31) >> 5, wave, lane, tiles, lds_addr(row_lds));
+  LaneOffsets lo = lane_offsets<D>(lane, qs.stride);
+  qs.issue(0, lo);
+  const int j = key0 + (lane & 31);
+  const bool jok = j < len;
+  const size_t krow = (static_cast<size_t>(s0 + (jok ? j : 0)) * a.H + h) * D;
+  u32x4 kf[kKS], vf[kKS];
+#pragma unroll
+  for (int x = 0; x < kKS; ++x) {
+    kf[x] = jok ? ld16(a.k + krow + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
+    vf[x] = jok ? ld16(a.v + krow + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
+  }
+  f32x16 acc[kDB];
+#pragma unroll
+  for (int x = 0; x < kDB; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
+  const bool keys = wave >> 1;
+  const int nst = (qs.total + 1) >> 1;
+  int step = wave & 1;
+  for (int st = 0; st < nst; ++st, step += 2) {
+    wait_copies();
+    __syncthreads();
+    if (st + 1 < nst) qs.issue((st & 1) ^ 1, lo);
+    if (step >= qs.total) continue;
+    const uint32_t tl = tiles + (st & 1) * 4 * kUnit + 2 * kUnit * (wave & 1);
+    const float* rows = row_lds[st & 1][wave & 1];
+    f32x16 s, dp;
+    if (keys) query_products<D, true>(tl, rows, lo, kf, vf, hf, s, dp);
+    else query_products<D, false>(tl, rows, lo, kf, vf, hf, s, dp);
+    query_weights(a, s, first + 32 * (step / a.g), key0, len, lane);
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = keys ? s[i] * dp[i] : s[i];
+    const u32x4 w[2] = {pack_bf16(x), pack_bf16(x + 8)};
+    query_sums<D>(tl + (keys ? 0 : kUnit), lo, w, acc);
+  }
+  // even and odd steps' sums are added in LDS, whose tiles nothing reads any more
+  __syncthreads();
+  float* sum = reinterpret_cast<float*>(tile_lds) + (wave >> 1) * 32 * D + (lane & 31) * D;
+  if (wave & 1) store_sums<D>(sum, acc, hf);
+  __syncthreads();
+  if (wave & 1) return;
+#pragma unroll
+  for (int x = 0; x < kDB; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[x][i] += sum[32 * x + 8 * (i >> 2) + 4 * hf + (i & 3)];
+  store_sums<D>(part_of(a, false, slot, key0 >> 5, h, D) + (keys ? 0 : 32 * D) + (lane & 31) * D, acc, hf);
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(WindowArgs a) {
+  using Tile = TileOf<D>;
+  constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
+  __shared__ __attribute__((aligned(256))) char tile_lds[2][4 * kUnit];                  // [Q tile | dO tile] x 2
+  __shared__ __attribute__((aligned(16))) float row_lds[2][2][64];                       // [step][row][-lse, -D]
+  const int2 wg = xcd_order();
+  const int h = wg.y;
+  // four key blocks (512 keys), then the far queries of as many positions, once per tile of sinks
+  const int group = wg.x / (4 + a.sink_tiles), in_group = wg.x % (4 + a.sink_tiles);
+  if (in_group >= 4) {
+    // positions 512 c .. (c >= 1) of the last sequence that starts before this 512 of the packed tokens
+    if (group == 0) return;
+    const Block f = block_of(a, group - 1, kFar, 0);
+    const int key0 = 32 * (in_group - 4);
+    const int first = max(f.p0 + kFar, far_begin(a, key0 & ~(kKeys - 1))), last = min(f.len, f.p0 + 2 * kFar);
+    if (first >= last || key0 >= f.len) return;
+    far_queries<D>(a, tile_lds[0], row_lds, f.s0, f.len, h, key0, first, last, group);
+    return;
+  }
+  const Block blk = block_of(a, 4 * group + in_group, kKeys);
+  if (blk.p0 >= blk.len) return;
+  const int s0 = blk.s0, len = blk.len;
+  const int lane = threadIdx.x & 63, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t tiles = lds_addr(tile_lds);
+  const int last = min(len, far_begin(a, blk.p0));
+  QuerySteps<D> qs(a, s0, len, h, blk.p0, (last - blk.p0 + 31) >> 5, wave, lane, tiles, lds_addr(row_lds));
+  LaneOffsets lo = lane_offsets<D>(lane, qs.stride);
+  qs.issue(0, lo);
+
+  const int key0 = blk.p0 + 32 * wave;       // this wave's keys
+  const int j = key0 + (lane & 31);          // this lane's key
+  const bool jok = j < len;
+  const size_t krow = (static_cast<size_t>(s0 + (jok ? j : 0)) * a.H + h) * D;
+  u32x4 kf[kKS], vf[kKS];
+#pragma unroll
+  for (int x = 0; x < kKS; ++x) {
+    kf[x] = jok ? ld16(a.k + krow + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
+    vf[x] = jok ? ld16(a.v + krow + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
+  }
+  f32x16 dka[kDB], dva[kDB];
+#pragma unroll
+  for (int x = 0; x < kDB; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) dka[x][i] = dva[x][i] = 0.f;
+
+  const int nst = (qs.total + 1) >> 1;
+  int step_qh = 0, tq = blk.p0;
+  for (int st = 0; st < nst; ++st) {
+    wait_copies();
+    __syncthreads();
+    if (st + 1 < nst) qs.issue((st & 1) ^ 1, lo);
+#pragma unroll 1
+    for (int sub = 0; sub < 2; ++sub) {
+      if (2 * st + sub >= qs.total) break;
+      if (tq + 31 >= key0 && (tq < key0 + 31 + a.w || key0 < a.sinks) && key0 < len) {
+        const uint32_t tl = tiles + (st & 1) * 4 * kUnit + 2 * kUnit * sub;
+        refresh(lo);
+        f32x16 s, dp;
+        query_products<D, true>(tl, row_lds[st & 1][sub], lo, kf, vf, hf, s, dp);
+        query_weights(a, s, tq, key0, len, lane);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dp[i] *= s[i];
+        // dV^T += dO^T P, dK^T += Q^T dS with P, dS rounded to bf16
+        float p[16], ds[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          p[i] = s[i];
+          ds[i] = dp[i];
+        }
+        const u32x4 pu[2] = {pack_bf16(p), pack_bf16(p + 8)}, du[2] = {pack_bf16(ds), pack_bf16(ds + 8)};
+        // product e: dV (dO) and dK (Q) take turns, dim block (e / 2) % kDB, token half e / (2 kDB)
+        u32x4 op[kFew];
+        auto read = [&](int e) {
+          return col_operand<D>(tl + kUnit * ((e & 1) ^ 1), lo, (e >> 1) % kDB, e / (2 * kDB));
+        };
+#pragma unroll
+        for (int e = 0; e < kFew; ++e) op[e] = read(e);
+#pragma unroll
+        for (int e = 0; e < 4 * kDB; ++e) {
+          __builtin_amdgcn_sched_barrier(0);
+          const int x = (e >> 1) % kDB, y = e / (2 * kDB);
+          if (e & 1) dka[x] = mfma(op[e % kFew], du[y], dka[x]);
+          else dva[x] = mfma(op[e % kFew], pu[y], dva[x]);
+          if (e + kFew < 4 * kDB) op[e % kFew] = read(e + kFew);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (++step_qh == a.g) {
+        step_qh = 0;
+        tq += 32;
+      }
+    }
+  }
+
+  const int je = key0 + (fresh(lane) & 31);
+  if (a.sink_tiles && key0 < a.sinks && far_begin(a, blk.p0) < len) {
+    // far queries follow: keys past the last sink of this tile are complete, their other sums are zeros
+    float* dst = part_of(a, true, s0 / kFar, key0 >> 5, h, D) + (je - key0) * D;
+    store_sums<D>(dst, dka, hf);
+    store_sums<D>(dst + 32 * D, dva, hf);
+    return;
+  }
+  bool bad = false;
+#pragma unroll
+  for (int x = 0; x < kDB; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      bad |= not_finite(dka[x][i]) || not_finite(dva[x][i]);
+      if (a.single) dka[x][i] = 0.f;
+    }
+  const bool jo = je < len;
+  const size_t out = (static_cast<size_t>(s0 + (jo ? je : 0)) * a.H + h) * D;
+  store_row<D>(a.dk + out, dka, a.scale_log2 / kLog2e, hf, jo);
+  store_row<D>(a.dv + out, dva, 1.0f, hf, jo);
+  const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && jo);
+  for (uint32_t cols = static_cast<uint32_t>(lanes | lanes >> 32); cols; cols &= cols - 1)
+    exact_key<D>(a, s0, len, key0 + __builtin_ctz(cols), h);
+}
+
+// Keys of the sink tiles of one sequence with far queries, a wave each: the key blocks' sums and, in order
+// of position, those of the far queries.
+template <int D>
+__global__ __launch_bounds__(kThreads) void window_sinks_kernel(WindowArgs a) {
+  constexpr int E = D / 64;
+  const int slot = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63;
+  const Block blk = block_of(a, slot, kFar, 0);       // the sequence that starts in this 512, if it is long
+  if (blk.p0 != 0) return;
+  for (int j = blockIdx.z * (kThreads / 64) + (threadIdx.x >> 6); j < min(32 * a.sink_tiles, blk.len);
+       j += gridDim.z * (kThreads / 64)) {
+    const int begin = far_begin(a, j & ~(kKeys - 1));
+    if (begin >= blk.len) continue;                     // stored by its block
+    const size_t in = static_cast<size_t>(j & 31) * D + E * lane;
+    float dk[E], dv[E];
+    auto add = [&](const float* p) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        dk[e] += p[in + e];
+        dv[e] += p[in + 32 * D + e];
+      }
+    };
+#pragma unroll
+    for (int e = 0; e < E; ++e) dk[e] = dv[e] = 0.f;
+    add(part_of(a, true, slot, j >> 5, h, D));
+    for (int c = begin / kFar; c * kFar < blk.len; ++c) add(part_of(a, false, slot + c, j >> 5, h, D));
+    bool bad = false;
+    const size_t out = (static_cast<size_t>(blk.s0 + j) * a.H + h) * D + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      bad |= not_finite(dk[e]) || not_finite(dv[e]);
+      a.dk[out + e] = static_cast<__bf16>(dk[e] * a.scale_log2 / kLog2e);
+      a.dv[out + e] = static_cast<__bf16>(dv[e]);
+    }
+    if (__builtin_amdgcn_ballot_w64(bad)) exact_key<D>(a, blk.s0, blk.len, j, h);
   }
 }
 
@@ -434,13 +933,42 @@ WindowArgs window_args(const dms_window_config& c, const int32_t* cu, const void
   return a;
 }
 
-unsigned row_blocks(int64_t rows) { return static_cast<unsigned>((rows + kThreads / 64 - 1) / (kThreads / 64)); }
+// Row values of the queries, then the sinks' sums where a sequence can have far queries.
+struct WindowLayout {
+  size_t rows, part, bytes;
+  int64_t Ts;
+  int sink_tiles;
+};
+WindowLayout window_layout(const dms_window_config& c) {
+  WindowLayout l{};
+  l.Ts = static_cast<int64_t>(c.total_tokens) + 32;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, kAlign); return o; };
+  l.rows = take(static_cast<size_t>(c.num_kv_heads) * c.group_size * l.Ts * 8);
+  const int sinks = std::min(c.sinks, c.max_seqlen);
+  l.sink_tiles = c.max_seqlen > kFar ? (sinks + 31) / 32 : 0;
+  l.part = take(static_cast<size_t>(2) * (c.total_tokens / kFar + 1) * l.sink_tiles * c.num_kv_heads * 64 * c.head_dim * 4);
+  l.bytes = off;
+  return l;
+}
+
+// Rows of fewer than this many keys get their D_t from a walk over the keys of its own.
+constexpr int kExactKeys = 128;
+
+template <int D>
+void launch_backward(const WindowArgs& a, bool exact, hipStream_t st) {
+  const dim3 gq(a.T / a.PB + a.n, a.H);
+  if (exact) hipLaunchKernelGGL((window_dq_kernel<D, true>), gq, dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((window_dq_kernel<D, false>), gq, dim3(kThreads), 0, st, a);
+  const int groups = (a.T / kKeys + a.n + 3) / 4;
+  hipLaunchKernelGGL(window_dkv_kernel<D>, dim3(groups * (4 + a.sink_tiles), a.H), dim3(kThreads), 0, st, a);
+  if (a.sink_tiles)
+    hipLaunchKernelGGL(window_sinks_kernel<D>, dim3(a.T / kFar + 1, a.H, std::min(8 * a.sink_tiles, 64)), dim3(kThreads), 0, st, a);
+}
 
 }  // namespace
 
-size_t window_workspace_bytes(const dms_window_config& c) {
-  return align_up(static_cast<size_t>(c.total_tokens) * c.num_kv_heads * c.group_size * 4 + 4, kAlign);
-}
+size_t window_workspace_bytes(const dms_window_config& c) { return window_layout(c).bytes; }
 
 hipError_t launch_window_fwd(const dms_window_config& c, const int32_t* cu, const void* q, const void* k,
                              const void* v, void* out, float* lse, void*, hipStream_t st) {
@@ -454,23 +982,23 @@ hipError_t launch_window_fwd(const dms_window_config& c, const int32_t* cu, cons
 }
 
 hipError_t launch_window_bwd(const dms_window_config& c, const int32_t* cu, const void* q, const void* k,
-                             const void* v, const void*, const float* lse, const void* dout, void* dq,
+                             const void* v, const void* out, const float* lse, const void* dout, void* dq,
                              void* dk, void* dv, void* ws, hipStream_t st) {
   WindowArgs a = window_args(c, cu, q, k, v);
-  a.row = static_cast<float*>(ws);
+  const WindowLayout l = window_layout(c);
+  a.rows = reinterpret_cast<f32x2*>(static_cast<char*>(ws) + l.rows);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + l.part);
+  a.Ts = l.Ts;
+  a.sink_tiles = l.sink_tiles;
+  a.o = static_cast<const __bf16*>(out);
   a.lse = lse;
   a.dout = static_cast<const __bf16*>(dout);
   a.dq = static_cast<__bf16*>(dq);
   a.dk = static_cast<__bf16*>(dk);
   a.dv = static_cast<__bf16*>(dv);
-  const dim3 gq(row_blocks(static_cast<int64_t>(a.T) * a.H * a.g)), gk(row_blocks(static_cast<int64_t>(a.T) * a.H));
-  if (c.head_dim == 64) {
-    hipLaunchKernelGGL(window_dq_kernel<64>, gq, dim3(kThreads), 0, st, a);
-    hipLaunchKernelGGL(window_dkv_kernel<64>, gk, dim3(kThreads), 0, st, a);
-  } else {
-    hipLaunchKernelGGL(window_dq_kernel<128>, gq, dim3(kThreads), 0, st, a);
-    hipLaunchKernelGGL(window_dkv_kernel<128>, gk, dim3(kThreads), 0, st, a);
-  }
+  const bool exact = a.w + a.sinks < kExactKeys;
+  if (c.head_dim == 64) launch_backward<64>(a, exact, st);
+  else launch_backward<128>(a, exact, st);
   return hipGetLastError();
 }
 

@@ -90,6 +90,9 @@ CASES = [
     ([129, 127], 2, 16, 64, 7, 0), ([300], 1, 6, 128, 256, 16), ([517], 1, 2, 64, 100, 33),
     ([260, 3, 90], 2, 8, 128, 128, 64), ([400], 1, 1, 128, 1, 200), ([90], 3, 5, 64, 20, 90),
     ([40, 500], 2, 5, 128, 64, 40), ([700], 1, 3, 128, 32, 1),
+    # sinks with queries in several far shares, over more than one block of keys, among short sequences
+    ([1500, 30, 0, 700], 1, 2, 64, 40, 140), ([1100], 2, 1, 128, 300, 5), ([512, 513, 514, 7], 1, 1, 64, 3, 1),
+    ([9, 1025], 1, 3, 128, 1, 64),
 ]
 
 
@@ -126,8 +129,8 @@ def test_hidden_keys_of_any_value_change_nothing(bad, d):
     """Infinite or NaN keys and values reach the queries that see them and no others; an Inf or NaN query
     or output gradient reaches the gradients of the keys it sees and no others.  Results that they do not
     reach stay within the slack of the results without them."""
-    lens, H, g, w, sinks = [130, 90], 1, 2, 20, 2
-    x = _inputs(220, H, g, d, 9)
+    lens, H, g, w, sinks, T = [130, 700], 1, 2, 20, 2, 830
+    x = _inputs(T, H, g, d, 9)
     ref, slack = _reference(x, lens, H, g, d, w, sinks)
 
     def near(got, name, rows):
@@ -135,15 +138,15 @@ def test_hidden_keys_of_any_value_change_nothing(bad, d):
         assert (np.abs(got[name][at] - ref[name][at]) <= slack[name][at]).all(), name
 
     word = _bf16(np.array([bad]))[0]
-    at = 130 + 40                       # token 40 of the second sequence
+    at = 130 + 600                      # token 600 of the second sequence
     y = {n: b.copy() for n, b in x.items()}
     y["k"][at], y["v"][at] = word, word
     got = _gpu(y, lens, H, g, d, w, sinks)
-    miss = np.ones(220, bool)
+    miss = np.ones(T, bool)
     miss[at:at + w] = False
     for n in ("out", "lse", "dq"):
         near(got, n, miss)
-    far = np.ones(220, bool)            # keys that no query of [at, at + w) sees
+    far = np.ones(T, bool)            # keys that no query of [at, at + w) sees
     far[at - w + 1:at + w] = False
     far[130:130 + sinks] = False
     for n in ("dk", "dv"):
@@ -151,12 +154,12 @@ def test_hidden_keys_of_any_value_change_nothing(bad, d):
     y = {n: b.copy() for n, b in x.items()}
     y["q"][at], y["dout"][at] = word, word
     got = _gpu(y, lens, H, g, d, w, sinks)
-    unseen = np.ones(220, bool)
+    unseen = np.ones(T, bool)
     unseen[at - w + 1:at + 1] = False
     unseen[130:130 + sinks] = False
     for n in ("dk", "dv"):
         near(got, n, unseen)
-    others = np.arange(220) != at
+    others = np.arange(T) != at
     for n in ("out", "lse", "dq"):
         near(got, n, others)
 
