@@ -130,7 +130,8 @@ Layout make_layout(const dms_config& c) {
   lo.ws_fk_base = take(Ly * NH * 4);
   lo.ws_fk_tiles = take(Ly * (NH + 1) * 4);
   lo.ws_fk_block = take(Ly * 8);
-  lo.ws_cp_map = take(Ly * static_cast<size_t>(c.num_pages) * 4);
+  lo.cp_list_stride = static_cast<size_t>(c.num_pages) / 2 + 1 + 2 * ((static_cast<size_t>(c.num_pages) + 31) / 32);
+  lo.ws_cp_lists = take(Ly * lo.cp_list_stride * 4);
   lo.workspace_bytes = off;
   return lo;
 }

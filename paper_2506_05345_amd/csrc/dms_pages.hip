@@ -17,6 +17,7 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 constexpr int kPlanThreads = 1024;
 constexpr int kCopyThreads = 256;
 constexpr int kShare = 4;          // adjacent copies of one source that share its reads
+constexpr int kPieces = 4;         // 16-byte pieces a thread has in flight
 constexpr int kIdChunk = 1 << 18;  // page ids marked at a time in LDS
 
 __device__ inline int load_status(const int32_t* status) { return __atomic_load_n(status, __ATOMIC_RELAXED); }
@@ -202,40 +203,64 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(ForkArgs a) {
       continue;
     }
     const int i = hh / p.H, h = hh - i * p.H;
-    int copies = 1;
-    while ((i + copies) % kShare != 0 && i + copies < a.n && a.src[i + copies] == a.src[i]) ++copies;
     const size_t so = static_cast<size_t>(a.src[i]) * p.H + h;
     const int L = s.len[so];
+    // the copies of this row: their heads and first pages in the call's block
+    size_t sd[kShare];
+    const int32_t* pages[kShare];
+    bool on[kShare];
+#pragma unroll
+    for (int c = 0; c < kShare; ++c) {
+      on[c] = c == 0 || (on[c - 1] && (i + c) % kShare != 0 && i + c < a.n && a.src[i + c] == a.src[i]);
+      const int ic = on[c] ? i + c : i;
+      sd[c] = static_cast<size_t>(a.dst[ic]) * p.H + h;
+      pages[c] = s.stack + first + base[static_cast<size_t>(ic) * p.H + h];
+    }
     for (; t < min(t1, c1); ++t) {
       const int k = t - c0;   // tile of the head
-      const char* from = pool + static_cast<size_t>(s.pt[so * p.maxp + k / tpp]) * p.page_bytes +
-                         static_cast<size_t>(k % tpp) * p.tile_bytes;
+      const int pg = k / tpp;
+      const size_t in_page = static_cast<size_t>(k - pg * tpp) * p.tile_bytes;
+      const int from_page = s.pt[so * p.maxp + pg];
+      const char* from = pool + static_cast<size_t>(from_page) * p.page_bytes + in_page;
       char* to[kShare];
-      for (int c = 0; c < copies; ++c) {
-        const int page = s.stack[first + base[static_cast<size_t>(i + c) * p.H + h] + k / tpp];
-        to[c] = pool + static_cast<size_t>(page) * p.page_bytes + static_cast<size_t>(k % tpp) * p.tile_bytes;
-        const size_t sd = static_cast<size_t>(a.dst[i + c]) * p.H + h;
-        if (k % tpp == 0) {
-          if (tid == 0) s.pt[sd * p.maxp + k / tpp] = page;
-          if (p.bounds_bytes) {
-            const char* bf = s.bounds + static_cast<size_t>(s.pt[so * p.maxp + k / tpp]) * p.bounds_bytes;
-            char* bt = s.bounds + static_cast<size_t>(page) * p.bounds_bytes;
-            if (16 * tid < p.bounds_bytes) *reinterpret_cast<u32x4*>(bt + 16 * tid) = *reinterpret_cast<const u32x4*>(bf + 16 * tid);
-          }
+#pragma unroll
+      for (int c = 0; c < kShare; ++c)
+        to[c] = on[c] ? pool + static_cast<size_t>(pages[c][pg]) * p.page_bytes + in_page : nullptr;
+      for (int e0 = 0; e0 < p.tile_bytes; e0 += kPieces * 16 * kCopyThreads) {
+        u32x4 x[kPieces];
+#pragma unroll
+        for (int n = 0; n < kPieces; ++n) {
+          const int e = e0 + 16 * (n * kCopyThreads + tid);
+          if (e < p.tile_bytes) x[n] = *reinterpret_cast<const u32x4*>(from + e);
         }
-        if (tid < kTile && kTile * k + tid < L)
-          s.slot_meta[sd * p.max_slots + kTile * k + tid] = s.slot_meta[so * p.max_slots + kTile * k + tid];
-        if (k == 0) {
-          for (int e = tid; e < p.w; e += kCopyThreads) s.ring[sd * p.w + e] = s.ring[so * p.w + e];
-          if (tid == 0) {
-            s.len[sd] = L;
-            if (h == 0) s.pos[a.dst[i + c]] = s.pos[a.src[i]];
-          }
-        }
+#pragma unroll
+        for (int c = 0; c < kShare; ++c)
+          if (on[c])
+#pragma unroll
+            for (int n = 0; n < kPieces; ++n) {
+              const int e = e0 + 16 * (n * kCopyThreads + tid);
+              if (e < p.tile_bytes) *reinterpret_cast<u32x4*>(to[c] + e) = x[n];
+            }
       }
-      for (int e = 16 * tid; e < p.tile_bytes; e += 16 * kCopyThreads) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(from + e);
-        for (int c = 0; c < copies; ++c) *reinterpret_cast<u32x4*>(to[c] + e) = x;
+#pragma unroll
+      for (int c = 0; c < kShare; ++c) {
+        if (!on[c]) continue;
+        if (tid < kTile && kTile * k + tid < L)
+          s.slot_meta[sd[c] * p.max_slots + kTile * k + tid] = s.slot_meta[so * p.max_slots + kTile * k + tid];
+        if (in_page == 0) {
+          const int page = pages[c][pg];
+          if (tid == 0) s.pt[sd[c] * p.maxp + pg] = page;
+          if (16 * tid < p.bounds_bytes)
+            *reinterpret_cast<u32x4*>(s.bounds + static_cast<size_t>(page) * p.bounds_bytes + 16 * tid) =
+                *reinterpret_cast<const u32x4*>(s.bounds + static_cast<size_t>(from_page) * p.bounds_bytes + 16 * tid);
+        }
+        if (k == 0) {
+          for (int e = tid; e < p.w; e += kCopyThreads) s.ring[sd[c] * p.w + e] = s.ring[so * p.w + e];
+          if (tid == 0) {
+            s.len[sd[c]] = L;
+            if (h == 0) s.pos[sd[c] / p.H] = s.pos[a.src[i]];
+          }
+        }
       }
     }
   }
@@ -247,31 +272,54 @@ __global__ __launch_bounds__(kCopyThreads) void fork_copy_kernel(ForkArgs a) {
 
 struct CompactArgs {
   PagesArgs p;
-  int32_t* map;            // [layers of the context][num_pages]
+  int32_t* lists;          // [layers of the context][list_stride]: see CompactLists
+  size_t list_stride;
   int32_t* used_out;       // nullable, one entry per layer of the call
   int out0;                // entry of the launch's first layer
 };
 
-// map[id] = where live page id >= U goes, -1 for free ids >= U (U live pages).
-// Below U the map holds the free ids in ascending order meanwhile: there are as
-// many of them as live ids past U.
+// A layer's part of the workspace, U live pages: the free ids below U in
+// ascending order, of every 32 ids which are live and at least U, and how many
+// such ids come before them.  There are as many live ids past U as free ones
+// below it, and the r-th of these takes the r-th of those.
+struct CompactLists {
+  int32_t* holes;
+  uint32_t* live;
+  int32_t* before;
+};
+__device__ inline CompactLists lists_of(const CompactArgs& a, int y) {
+  int32_t* b = a.lists + static_cast<size_t>(a.p.layer + y) * a.list_stride;
+  const int words = (a.p.num_pages + 31) / 32;
+  return CompactLists{b, reinterpret_cast<uint32_t*>(b + a.p.num_pages / 2 + 1), b + a.p.num_pages / 2 + 1 + words};
+}
+__device__ inline int moved_to(const CompactLists& l, int id) {   // of a live id >= U
+  const uint32_t below = l.live[id >> 5] & ((1u << (id & 31)) - 1);
+  return l.holes[l.before[id >> 5] + __builtin_popcount(below)];
+}
+
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactArgs a) {
   __shared__ uint32_t freed[kIdChunk / 32];
   __shared__ int lds[34];
   const PagesArgs& p = a.p;
   if (__syncthreads_or(load_status(p.status) != 0)) return;
   const LayerPtrs s = layer_ptrs(p, blockIdx.x);
-  int32_t* map = a.map + static_cast<size_t>(p.layer + blockIdx.x) * p.num_pages;
+  const CompactLists l = lists_of(a, blockIdx.x);
   const int top = *s.top, U = p.num_pages - top;
   if (threadIdx.x == 0 && a.used_out) a.used_out[a.out0 + blockIdx.x] = U;
   int holes = 0, moved = 0;
   for (int64_t c0 = 0; c0 < p.num_pages; c0 += kIdChunk) {
     const int ids = static_cast<int>(min<int64_t>(kIdChunk, p.num_pages - c0));
-    for (int i = threadIdx.x; i < (ids + 31) / 32; i += blockDim.x) freed[i] = 0;
+    for (int i = threadIdx.x; i < (ids + 31) / 32; i += kPlanThreads) freed[i] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < top; i += blockDim.x) {
-      const int64_t id = s.stack[i] - c0;
-      if (id >= 0 && id < ids) atomicOr(&freed[id >> 5], 1u << (id & 31));
+    for (int i0 = threadIdx.x; i0 < top; i0 += 8 * kPlanThreads) {
+      int id[8];
+#pragma unroll
+      for (int n = 0; n < 8; ++n) id[n] = s.stack[min(i0 + n * kPlanThreads, top - 1)];   // past the end: the last one again
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        const int64_t x = id[n] - c0;
+        if (x >= 0 && x < ids) atomicOr(&freed[x >> 5], 1u << (x & 31));
+      }
     }
     __syncthreads();
     // 1024 words at a time, a word per thread
@@ -284,24 +332,18 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(CompactArgs 
         const uint32_t low = U - id0 >= 32 ? ~0u : U - id0 <= 0 ? 0u : (1u << (U - id0)) - 1;   // ids below U
         hole = freed[wi] & in & low;
         live = ~freed[wi] & in & ~low;
-        for (uint32_t f = freed[wi] & in & ~low; f; f &= f - 1) map[id0 + __builtin_ctz(f)] = -1;
       }
       int2 tot;
       const int2 ex = block_exclusive_scan2(make_int2(__builtin_popcount(hole), __builtin_popcount(live)), lds, &tot);
-      int r = holes + ex.x;
-      for (; hole; hole &= hole - 1) map[r++] = static_cast<int32_t>(id0 + __builtin_ctz(hole));
-      r = moved + ex.y;
-      for (; live; live &= live - 1) map[id0 + __builtin_ctz(live)] = r++;
+      if (32 * wi < ids) {
+        l.live[id0 >> 5] = live;
+        l.before[id0 >> 5] = moved + ex.y;
+      }
+      for (int r = holes + ex.x; hole; hole &= hole - 1) l.holes[r++] = static_cast<int32_t>(id0 + __builtin_ctz(hole));
       holes += tot.x;
       moved += tot.y;
     }
     __syncthreads();
-  }
-  __threadfence_block();
-  __syncthreads();
-  for (int64_t id = U + static_cast<int64_t>(threadIdx.x); id < p.num_pages; id += blockDim.x) {
-    const int r = map[id];
-    if (r >= 0) map[id] = map[r];
   }
 }
 
@@ -309,7 +351,7 @@ __global__ __launch_bounds__(kCopyThreads) void compact_move_kernel(CompactArgs 
   const PagesArgs& p = a.p;
   if (load_status(p.status) != 0) return;
   const LayerPtrs s = layer_ptrs(p, blockIdx.y);
-  const int32_t* map = a.map + static_cast<size_t>(p.layer + blockIdx.y) * p.num_pages;
+  const CompactLists l = lists_of(a, blockIdx.y);
   char* pool = p.pools[blockIdx.y];
   const int top = *s.top, U = p.num_pages - top;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -321,17 +363,28 @@ __global__ __launch_bounds__(kCopyThreads) void compact_move_kernel(CompactArgs 
     const int np = (s.len[hh] + p.P - 1) / p.P;
     for (int k = lane; k < np; k += 64) {
       const int id = s.pt[hh * p.maxp + k];
-      if (id >= U) s.pt[hh * p.maxp + k] = map[id];
+      if (id >= U) s.pt[hh * p.maxp + k] = moved_to(l, id);
     }
   }
   // pages, a workgroup each
   for (int64_t id = U + static_cast<int64_t>(blockIdx.x); id < p.num_pages; id += gridDim.x) {
-    const int to = map[id];
-    if (to < 0) continue;
+    if (!(l.live[id >> 5] >> (id & 31) & 1)) continue;
+    const int to = moved_to(l, static_cast<int>(id));
     const char* from = pool + static_cast<size_t>(id) * p.page_bytes;
     char* dst = pool + static_cast<size_t>(to) * p.page_bytes;
-    for (size_t e = 16 * tid; e < p.page_bytes; e += 16 * kCopyThreads)
-      *reinterpret_cast<u32x4*>(dst + e) = *reinterpret_cast<const u32x4*>(from + e);
+    for (size_t e0 = 0; e0 < p.page_bytes; e0 += kPieces * 16 * kCopyThreads) {
+      u32x4 x[kPieces];
+#pragma unroll
+      for (int n = 0; n < kPieces; ++n) {
+        const size_t e = e0 + 16 * (n * kCopyThreads + tid);
+        if (e < p.page_bytes) x[n] = *reinterpret_cast<const u32x4*>(from + e);
+      }
+#pragma unroll
+      for (int n = 0; n < kPieces; ++n) {
+        const size_t e = e0 + 16 * (n * kCopyThreads + tid);
+        if (e < p.page_bytes) *reinterpret_cast<u32x4*>(dst + e) = x[n];
+      }
+    }
     if (16 * tid < p.bounds_bytes)
       *reinterpret_cast<u32x4*>(s.bounds + static_cast<size_t>(to) * p.bounds_bytes + 16 * tid) =
           *reinterpret_cast<const u32x4*>(s.bounds + static_cast<size_t>(id) * p.bounds_bytes + 16 * tid);
@@ -407,7 +460,8 @@ hipError_t launch_compact(const dms_config& c, const Layout& lo, void* meta, voi
                           int layer, int32_t* used_out, hipStream_t st) {
   CompactArgs a{};
   a.p = pages_args(c, lo, meta);
-  a.map = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + lo.ws_cp_map);
+  a.lists = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + lo.ws_cp_lists);
+  a.list_stride = lo.cp_list_stride;
   a.used_out = used_out;
   return over_layers(c, a.p, pools, layer, [&](int y, int layers) {
     a.out0 = y - std::max(layer, 0);
