@@ -190,19 +190,35 @@ def lib():
 
 
 def _ptr(x):
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
     if hasattr(x, "data_ptr"):
         return x.data_ptr()
+    if isinstance(x, int):
+        return x
     raise TypeError(f"cannot pass {type(x)} as a pointer")
+
+
+torch = None     # bound by the first call that is given a tensor or no stream
+
+
+def _torch():
+    global torch, _KINDS, _RAW_STREAM
+    if torch is None:
+        import torch as module
+        _KINDS = {_BF16: module.bfloat16, _U8: module.uint8, _I32: module.int32, _F32: module.float32,
+                  _F64: module.float64}
+        # the handle of the current stream without a Stream object around it (2 us a call)
+        _RAW_STREAM = getattr(module._C, "_cuda_getCurrentRawStream",
+                              lambda device: module.cuda.current_stream(device).cuda_stream)
+        torch = module
+    return torch
 
 
 def _stream(s):
     if s is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _RAW_STREAM(_torch().cuda.current_device()) if torch is not None else \
+            _torch().cuda.current_stream().cuda_stream
     if isinstance(s, int):
         return s
     return s.cuda_stream
@@ -229,11 +245,15 @@ def _args(where, *specs):
     types of all arguments are checked first, then that each is a contiguous
     GPU tensor with enough elements.  Integers (raw device addresses) and None
     pass through; the library checks null pointers itself."""
-    if all(x is None or isinstance(x, int) for x, *_ in specs):
+    for x, _, kind, count in specs:
+        if x is None or type(x) is int:
+            continue
+        if not (isinstance(x, _torch().Tensor) and x.dtype is _KINDS[kind] and x.is_cuda and
+                x.is_contiguous() and x.numel() >= count):
+            break
+    else:
         return
-    import torch
-    kinds = {_BF16: torch.bfloat16, _U8: torch.uint8, _I32: torch.int32, _F32: torch.float32,
-             _F64: torch.float64}
+    kinds = _KINDS
     live = []
     for x, name, kind, count in specs:
         if x is None or isinstance(x, int):
@@ -259,12 +279,13 @@ def _arg(x, name, kind, count, where):
 
 def _one_device(where, *tensors):
     """Tensors of one call lie on the current device, where its kernels run."""
-    devices = {x.device for x in tensors if hasattr(x, "data_ptr")}
-    if not devices:
-        return
-    import torch
-    if len(devices) > 1 or devices.pop().index != torch.cuda.current_device():
-        raise DmsError(DMS_ERR_INVALID, f"{where}: tensors must be on the current device")
+    here = None
+    for x in tensors:
+        if x is not None and type(x) is not int:
+            if here is None:
+                here = _torch().cuda.current_device()
+            if x.get_device() != here:
+                raise DmsError(DMS_ERR_INVALID, f"{where}: tensors must be on the current device")
 
 
 def _rows_stride(x, heads, dim, stride):
@@ -690,21 +711,21 @@ def make_rope_config(num_kv_heads, group_size, head_dim, rotary_dim, sections, r
 
 def _rope_strided(where, x, name, tokens, heads, dim, kind, stride):
     """Checks a tensor of rows that may lie apart and returns the rows' stride."""
-    if x is None or isinstance(x, int):
+    if x is None or type(x) is int:
         return heads * dim if stride is None else stride
-    import torch
-    want = {_BF16: torch.bfloat16, _F32: torch.float32}.get(kind)
-    if not isinstance(x, torch.Tensor):
+    if not isinstance(x, _torch().Tensor):
         raise TypeError(f"{where}: {name} must be a tensor or a device address, got {type(x)}")
-    if want is not None and x.dtype != want:
+    if kind is not None and x.dtype is not _KINDS[kind]:
         raise DmsError(DMS_ERR_INVALID, f"{where}: {name} must be {kind}, got {x.dtype}")
     if not x.is_cuda:
         raise DmsError(DMS_ERR_INVALID, f"{where}: {name} must be a GPU tensor")
     got = _rows_stride(x, heads, dim, stride)
     if got is None:
         raise DmsError(DMS_ERR_INVALID, f"{where}: {name} must have dense rows of [{heads}, {dim}]")
-    # elements from the first to the end of the last row inside the tensor's own extent
-    have = 1 + sum((n - 1) * st for n, st in zip(x.shape, x.stride())) if x.numel() else 0
+    if x.is_contiguous():
+        have = x.numel()
+    else:   # elements from the first to the end of the last row inside the tensor's own extent
+        have = 1 + sum((n - 1) * st for n, st in zip(x.shape, x.stride())) if x.numel() else 0
     if tokens > 0 and have < (tokens - 1) * got + heads * dim:
         raise DmsError(DMS_ERR_INVALID, f"{where}: {name} holds fewer than {tokens} rows")
     return got
