@@ -157,6 +157,11 @@ __device__ inline void lds_copy4(const void* base, uint32_t off, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" : : "s"(m0), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ inline void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // vmcnt(0)
+// All but the N newest copies (fewer than 16) have landed.
+template <int N>
+__device__ inline void wait_copies_but() {
+  __builtin_amdgcn_s_waitcnt(0x0F70 | N);
+}
 
 // keeps the compiler from forming what follows from x ahead of a loop and holding it
 __device__ inline int fresh(int x) {
@@ -165,23 +170,26 @@ __device__ inline int fresh(int x) {
 }
 
 // One wave copies rows t0 .. t0 + 31 of one head (row t at base + t * stride
-// bytes) to the LDS tile `dst`.  Rows from `end` on are copied from 16 zero
+// bytes) to the LDS tile `dst`, or every second of the copies (PARTS = 2: the
+// copies m with m % 2 = part).  Rows from `end` on are copied from 16 zero
 // bytes: their weights are 0, and 0 times an Inf or NaN of some token must not
 // reach the sums.
-template <int D>
+template <int D, int PARTS = 1>
 __device__ inline void copy_tile(const char* base, int t0, int end, uint32_t stride, const LaneOffsets& o,
-                                 int lane, uint32_t dst, const void* zeros) {
+                                 int lane, uint32_t dst, const void* zeros, int part = 0) {
   constexpr int kRows = kCopyRows<D>, kPieces = D / 8, kShift = D == 128 ? 4 : 3;
   if (t0 + 32 <= end) {
-    const char* src = base + static_cast<size_t>(t0) * stride;
+    const char* src = base + static_cast<size_t>(t0 + (PARTS > 1 ? kRows * part : 0)) * stride;
 #pragma unroll
-    for (int m = 0; m < 32 / kRows; ++m)
-      lds_copy16(src + static_cast<size_t>(kRows * m) * stride, o.src ^ copy_flip<D>(m), dst + 1024 * m);
+    for (int m = 0; m < 32 / kRows; m += PARTS)
+      lds_copy16(src + static_cast<size_t>(kRows * m) * stride, o.src ^ (PARTS > 1 ? copy_flip<D>(m + part) : copy_flip<D>(m)),
+                 dst + 1024 * (PARTS > 1 ? m + part : m));
   } else {
     const int ln = fresh(lane);   // formed here, not held ahead of the loop
     const int tr = ln >> kShift, c = ln & (kPieces - 1);
 #pragma unroll
-    for (int m = 0; m < 32 / kRows; ++m) {
+    for (int m0 = 0; m0 < 32 / kRows; m0 += PARTS) {
+      const int m = PARTS > 1 ? m0 + part : m0;
       const int t = t0 + kRows * m + tr;
       const char* p = base + static_cast<size_t>(t) * stride + 16 * (c ^ (row_flip<D>(tr) + static_cast<int>(copy_flip<D>(m)) / 16));
       lds_copy16(t < end ? p : static_cast<const char*>(zeros), dst + 1024 * m);

@@ -39,6 +39,8 @@ struct WindowArgs {
   int n, T, H, g, w, sinks;
   int single;              // every row sees one key: P = 1 and dS = 0
   int PB;                  // positions of a query block: kCols / g
+  uint32_t inv_pb;         // 2^32 / PB + 1
+  uint32_t inv_g;          // 65536 / g + 1: col / g = col * inv_g >> 16 for columns below 128
   int sink_tiles;          // 32-key tiles of sinks whose far queries go to workgroups of their own (else 0)
   float scale_log2;
 };
@@ -55,62 +57,87 @@ __device__ inline float wave_sum(float x) {
   return x;
 }
 
-// Block b of a packed launch whose blocks hold PB tokens each: sequence i owns blocks
+// x / d for 0 <= x < 2^31, inv = 2^32 / d + 1: the product is at most one too large.
+__device__ inline int divide(int x, int d, uint32_t inv) {
+  const int q = static_cast<int>(__umulhi(static_cast<uint32_t>(x), inv));
+  return q * static_cast<int64_t>(d) > x ? q - 1 : q;
+}
+constexpr uint32_t inverse(int d) { return static_cast<uint32_t>((uint64_t(1) << 32) / d + 1); }
+
+// Block b of a packed launch whose blocks hold PB tokens each (inv = 2^32 / PB + 1): sequence i owns blocks
 // cu[i] / PB + i .. cu[i + 1] / PB + i, at least as many as it needs, so that a block finds its sequence
 // by a search over cu (64 candidates a round) and the host needs no prefix sums.  With per_seq = 0 the
 // blocks are cu[i] / PB + 0, 1, ... instead, which is unambiguous for sequences longer than PB.
 struct Block {
   int s0, len, p0;   // first token and length of the sequence, first position of the block (>= len: no block)
 };
-__device__ inline Block block_of(const WindowArgs& a, int b, int PB, int per_seq = 1) {
-  const int lane = threadIdx.x & 63;
+__device__ inline Block block_of(const WindowArgs& a, int b, int PB, uint32_t inv, int per_seq = 1) {
   int lo = 0, cnt = a.n;
   while (cnt > 1) {
+    const int lane = threadIdx.x & 63;
     const int step = (cnt + 63) >> 6;
     const int i = min(lo + lane * step, a.n);
-    const bool le = lane * step < cnt && min(max(a.cu[i], 0), a.T) / PB + per_seq * i <= b;
+    const bool le = lane * step < cnt && divide(min(max(a.cu[i], 0), a.T), PB, inv) + per_seq * i <= b;
     const int k = max(1, __builtin_popcountll(__builtin_amdgcn_ballot_w64(le)));
     lo += (k - 1) * step;
     cnt = min(step, cnt - (k - 1) * step);
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   const int2 r = bounds_of(a, lo);
-  return Block{r.x, r.y - r.x, max(b - (r.x / PB + per_seq * lo), 0) * PB};
+  return Block{r.x, r.y - r.x, max(b - (divide(r.x, PB, inv) + per_seq * lo), 0) * PB};
 }
 
-// Keys that queries [p0, p1) of a sequence see, as tiles of 32: `nsk` tiles of sinks from position 0
-// where a gap separates them from the window, then tiles from b0 on.
+// Keys that queries [p0, p1) of a sequence see, listed without a gap: the sinks, then the window from its
+// first key on (a window that reaches the sinks: the whole sequence up to p1).  Entry e of the list is key e
+// among the sinks and key base + e past them; tiles are 32 entries.
 struct KeyTiles {
-  int nsk, b0, nt;
-  __device__ int first(int i) const { return i < nsk ? 32 * i : b0 + 32 * (i - nsk); }
+  int base, nt;
 };
 __device__ inline KeyTiles key_tiles(const WindowArgs& a, int p0, int p1) {
-  const int b0 = max(0, p0 - a.w + 1);
-  KeyTiles t;
-  t.nsk = a.sinks >= b0 ? 0 : (a.sinks + 31) >> 5;
-  t.b0 = a.sinks >= b0 ? 0 : b0;
-  t.nt = t.nsk + ((p1 - t.b0 + 31) >> 5);
-  return t;
+  const int base = max(0, p0 - a.w + 1 - a.sinks);
+  return KeyTiles{base, (p1 - base + 31) >> 5};
 }
 
-enum { kAll, kSome, kNone };
-// What queries [q0, q1] (positions) see of tile i, whose first key is j0.
-__device__ inline int mask_class(const WindowArgs& a, const KeyTiles& kt, int i, int j0, int q0, int q1) {
-  if (i >= kt.nt || j0 > q1 || q0 > q1) return kNone;
-  if (i < kt.nsk) return j0 + 32 <= a.sinks ? kAll : kSome;
-  if (j0 + 31 <= q0 - a.w && j0 >= a.sinks) return kNone;
-  return j0 + 31 <= q0 && (j0 > q1 - a.w || j0 + 32 <= a.sinks) ? kAll : kSome;
+// Tiles of the list that the queries [q0, q1] (positions of one wave) see: some key of [some0, some1) and of
+// those with sinks, every key of [all0, all1).
+struct WaveTiles {
+  int some0, some1, all0, all1, sinks;
+};
+__device__ inline WaveTiles wave_tiles(const WindowArgs& a, const KeyTiles& t, int q0, int q1) {
+  WaveTiles w;
+  w.some0 = max(0, (q0 - a.w + 1 - t.base) >> 5);
+  w.some1 = q0 > q1 ? 0 : ((q1 - t.base) >> 5) + 1;
+  w.all0 = max(0, (q1 - a.w + 32 - t.base) >> 5);
+  w.all1 = (q0 + 1 - t.base) >> 5;
+  w.sinks = (a.sinks + 31) >> 5;
+  return w;
 }
-// Hides what position t does not see: register i of a lane is key j0 + 16 (i / 8) + 8 hf + i % 8.
-__device__ inline void hide(f32x16& s, const WindowArgs& a, bool sink_tile, int j0, int t, int hf) {
-  const int first = j0 + 8 * hf;
-  const int hi = sink_tile ? a.sinks - 1 - first : t - first;   // last key seen
-  const int lo = sink_tile ? -1 : t - a.w - first;              // last one before the window
-  const int sn = a.sinks - first;
+__device__ inline bool tile_seen(const WaveTiles& w, int i) {
+  return i < w.some1 && (i >= w.some0 || i < w.sinks);
+}
+// Hides what position t does not see of tile i: register x of a lane is entry 32 i + 16 (x / 8) + 8 hf + x % 8.
+// Most tiles at an edge have one edge only: a comparison and a select for each score.
+__device__ inline void hide(f32x16& s, const WindowArgs& a, const KeyTiles& kt, const WaveTiles& wt, int i, int t,
+                            int hf) {
+  if (i >= wt.all0 && i < wt.all1) return;
+  const int first = 32 * i + 8 * hf;
+  const int hi = t - kt.base - first;        // last entry seen
+  if (i < wt.all0) {
+    const int lo = hi - a.w;                 // last one before the window
+    if (i < wt.sinks) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int k = 16 * (i >> 3) + (i & 7);
-    s[i] = k <= hi && (k > lo || k < sn) ? s[i] : -INFINITY;
+      for (int x = 0; x < 16; ++x) {
+        const int k = 16 * (x >> 3) + (x & 7);
+        s[x] = k > lo || k < a.sinks - first ? s[x] : -INFINITY;
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[x] = 16 * (x >> 3) + (x & 7) > lo ? s[x] : -INFINITY;
+    }
+  }
+  if (i >= wt.all1) {
+#pragma unroll
+    for (int x = 0; x < 16; ++x) s[x] = 16 * (x >> 3) + (x & 7) <= hi ? s[x] : -INFINITY;
   }
 }
 
@@ -120,6 +147,8 @@ __device__ inline float max3(float a, float b, float c) {   // scores of visible
   return d;
 }
 __device__ inline bool not_finite(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
+// 0 times an Inf or a NaN is a NaN, which every later sum keeps: one sum tells whether a row met any.
+__device__ inline bool is_nan(float x) { return (__float_as_uint(x) & 0x7FFFFFFFu) > 0x7F800000u; }
 
 // Row (position t of the sequence at s0, query head hq) by one wave, lanes over the head's elements and
 // only visible keys read: rows whose sums are not finite, where a product may have met an Inf or NaN of
@@ -157,8 +186,11 @@ __device__ const u32x4 kZeros = {0u, 0u, 0u, 0u};
 
 // Accumulators of one column (rows: dims 32 x + 8 y + 4 hf + 0 .. 3 in registers 4 y .. of block x),
 // times f, to the row's bf16 elements: the two lanes of the column exchange halves and each writes 16 bytes.
+// Returns whether the column holds a NaN (in one of its lanes; also if it holds infinities of both signs).
 template <int D>
-__device__ inline void store_row(__bf16* dst, const f32x16* o, float f, int hf, bool ok) {
+__device__ inline bool store_row(__bf16* dst, const f32x16* o, float f, int hf, bool ok) {
+  const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+  float sum = 0.f;
 #pragma unroll
   for (int x = 0; x < TileOf<D>::kDB; ++x)
 #pragma unroll
@@ -169,7 +201,9 @@ __device__ inline void store_row(__bf16* dst, const f32x16* o, float f, int hf, 
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const f32x2 pr = {o[x][4 * (y + z) + 2 * e] * f, o[x][4 * (y + z) + 2 * e + 1] * f};
-          r[z][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
+          const bf16x2 pb = __builtin_convertvector(pr, bf16x2);
+          sum = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, sum, false);
+          r[z][e] = __builtin_bit_cast(uint32_t, pb);
         }
       u32x4 w;
 #pragma unroll
@@ -180,22 +214,80 @@ __device__ inline void store_row(__bf16* dst, const f32x16* o, float f, int hf, 
       }
       if (ok) *reinterpret_cast<u32x4*>(dst + 32 * x + 8 * y + 8 * hf) = w;
     }
+  return is_nan(sum);
+}
+
+// ---------------------------------------------------------------------------
+// LDS ring of 3 or 4 steps, each two 32-row tiles of 2 D bytes a row ([K | V] of
+// 32 keys, or [Q | dO] of 32 positions of one head): while one step is computed
+// the next are on their way.  A window is few steps long, so that a
+// workgroup spends as long waiting as computing unless its first copies leave
+// together.  Wave x copies half x % 2 of tile x / 2.
+// ---------------------------------------------------------------------------
+template <int D>
+constexpr int kCopies = D / 32;   // copies of a step by one wave
+
+// Wave x copies its half of tile i of the listed keys; only a tile that holds both the last sinks and the
+// window's first keys takes each row by itself.
+template <int D>
+__device__ inline void copy_keys(const WindowArgs& a, const KeyTiles& kt, const char* kv, int i, int end, uint32_t stride,
+                                 const LaneOffsets& lo, int lane, int wave, uint32_t dst) {
+  dst += TileOf<D>::kUnit * (wave >> 1);
+  const bool mixed = 32 * i < a.sinks && 32 * i + 32 > a.sinks && kt.base > 0;
+  if (!mixed) {
+    copy_tile<D, 2>(kv, 32 * i < a.sinks ? 32 * i : kt.base + 32 * i, end, stride, lo, lane, dst, &kZeros, wave & 1);
+    return;
+  }
+  // both parts at the places of their rows, each lane in one of the two copies (a wait for the newest copies
+  // counts them as one: it waits for more than it has to)
+  constexpr int kRows = kCopyRows<D>;
+  const int tr = fresh(lane) / (D / 8);
+#pragma unroll
+  for (int m0 = 0; m0 < 32 / kRows; m0 += 2) {
+    const int m = m0 + (wave & 1), e = 32 * i + kRows * m;
+    const uint32_t off = lo.src ^ copy_flip<D>(m);
+    if (e + tr < a.sinks) lds_copy16(kv + static_cast<size_t>(e) * stride, off, dst + 1024 * m);
+    else if (kt.base + e + tr < end) lds_copy16(kv + static_cast<size_t>(kt.base + e) * stride, off, dst + 1024 * m);
+    else lds_copy16(&kZeros, dst + 1024 * m);
+  }
+}
+
+// Of the steps after this one `left` are there to come and up to SLOTS - 2 of them have been issued: this
+// one has landed for every wave.
+template <int D, int SLOTS>
+__device__ inline void step_ready(int left) {
+  if (SLOTS >= 4 && left >= 2) wait_copies_but<2 * kCopies<D>>();
+  else if (left >= 1) wait_copies_but<kCopies<D>>();
+  else wait_copies();
+  __syncthreads();
+}
+
+// f(step, slot) for steps 0 .. n - 1, the slot a constant.
+template <int SLOTS, typename F>
+__device__ __forceinline__ void over_steps(int n, F f) {
+  for (int i = 0; i < n; i += SLOTS) {
+    f(i, std::integral_constant<int, 0>{});
+    if (i + 1 < n) f(i + 1, std::integral_constant<int, 1>{});
+    if (i + 2 < n) f(i + 2, std::integral_constant<int, 2>{});
+    if constexpr (SLOTS > 3)
+      if (i + 3 < n) f(i + 3, std::integral_constant<int, 3>{});
+  }
 }
 
 // ---------------------------------------------------------------------------
 // Forward.  Workgroup = (KV head, block of PB positions of one sequence);
 // columns are (position, query head) pairs, the g heads of a position
-// consecutive, 32 per wave.  The block's key tiles go through LDS two at a
-// time, the next two being copied while these are attended.
+// consecutive, 32 per wave.  The block's key tiles go through the LDS ring.
 // ---------------------------------------------------------------------------
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(WindowArgs a) {
+__global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
   using Tile = TileOf<D>;
-  constexpr int kUnit = Tile::kUnit, kStage = 4 * kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
-  __shared__ __attribute__((aligned(256))) char tile_lds[2][kStage];   // [K tile | V tile] x 2
+  constexpr int kSlots = 3;
+  constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
+  __shared__ __attribute__((aligned(256))) char tile_lds[kSlots][2 * kUnit];
   const int2 wg = xcd_order();
   const int h = wg.y;
-  const Block blk = block_of(a, wg.x, a.PB);
+  const Block blk = block_of(a, wg.x, a.PB, a.inv_pb);
   if (blk.p0 >= blk.len) return;
   const int s0 = blk.s0, p0 = blk.p0, p1 = min(blk.len, p0 + a.PB);
   const KeyTiles kt = key_tiles(a, p0, p1);
@@ -208,15 +300,13 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(WindowArgs a) {
   const LaneOffsets lo = lane_offsets<D>(lane, stride);
   const uint32_t tiles = lds_addr(tile_lds);
   const char* kv = reinterpret_cast<const char*>((wave >> 1 ? a.v : a.k) + (static_cast<size_t>(s0) * a.H + h) * D);
-  auto issue = [&](int st, int buf) {   // a second tile past the last has zero rows
-    const int i = 2 * st + (wave & 1);
-    copy_tile<D>(kv, i < kt.nt ? kt.first(i) : p1, p1, stride, lo, lane,
-                 tiles + buf * kStage + 2 * kUnit * (wave & 1) + kUnit * (wave >> 1), &kZeros);
-  };
-  issue(0, 0);
+  auto issue = [&](int i, int slot) { copy_keys<D>(a, kt, kv, i, blk.len, stride, lo, lane, wave, tiles + slot * 2 * kUnit); };
+#pragma unroll
+  for (int i = 0; i < kSlots - 1; ++i)
+    if (i < kt.nt) issue(i, i);
 
   const int col = wave * 32 + (lane & 31);
-  const int pl = col / a.g, qh = col % a.g;
+  const int pl = static_cast<int>(col * a.inv_g >> 16), qh = col - pl * a.g;
   const bool ok = pl < a.PB && p0 + pl < p1;
   const int t = ok ? p0 + pl : p0;
   const size_t row = static_cast<size_t>(s0 + t) * Hq + h * a.g + qh;
@@ -225,7 +315,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(WindowArgs a) {
   for (int x = 0; x < kKS; ++x)
     qf[x] = ok ? ld16(a.q + row * D + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
   // positions of this wave's columns
-  const int q0 = p0 + wave * 32 / a.g, q1 = min(p1 - 1, p0 + (wave * 32 + 31) / a.g);
+  const int q0 = p0 + static_cast<int>(wave * 32 * a.inv_g >> 16);
+  const WaveTiles wt = wave_tiles(a, kt, q0, min(p1 - 1, p0 + static_cast<int>((wave * 32 + 31) * a.inv_g >> 16)));
   const LaneAddresses<D> ad = lane_addresses<D>(tiles, lo);
 
   f32x16 o[kDB];
@@ -236,36 +327,33 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(WindowArgs a) {
   float m_ref = kMInit, l_run = 0.f;
   const float thr = kRescale / a.scale_log2;
 
-  const int steps = (kt.nt + 1) >> 1;
-  auto attend = [&](int st, auto buf_c) {
-    constexpr int buf = decltype(buf_c)::value;
-    wait_copies();
-    __syncthreads();
-    if (st + 1 < steps) issue(st + 1, buf ^ 1);
-    constexpr int tl = buf * kStage;
-    const int j0 = kt.first(2 * st), j1 = kt.first(2 * st + 1);
-    const int c0 = mask_class(a, kt, 2 * st, j0, q0, q1), c1 = mask_class(a, kt, 2 * st + 1, j1, q0, q1);
-    if (c0 == kNone && c1 == kNone) return;
-    f32x16 s[2];
+  over_steps<kSlots>(kt.nt, [&](int i, auto slot_c) {
+    constexpr int slot = decltype(slot_c)::value, tl = slot * 2 * kUnit;
+    step_ready<D, kSlots>(kt.nt - 1 - i);
+    if (i + kSlots - 1 < kt.nt) issue(i + kSlots - 1, (slot + kSlots - 1) % kSlots);
+    if (!tile_seen(wt, i)) return;
+    f32x16 s;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
+    for (int x = 0; x < 16; ++x) s[x] = 0.f;
     u32x4 op[kAhead];
-    // score product e: tile e % 2, k-step e / 2 (the two chains take turns)
 #pragma unroll
-    for (int e = 0; e < kAhead; ++e) op[e] = row_operand(tl + 2 * kUnit * (e & 1), ad, e >> 1);
+    for (int e = 0; e < kAhead; ++e) op[e] = row_operand(tl, ad, e);
 #pragma unroll
-    for (int e = 0; e < 2 * kKS; ++e) {
+    for (int e = 0; e < kKS; ++e) {
       __builtin_amdgcn_sched_barrier(0);
-      s[e & 1] = mfma(op[e % kAhead], qf[e >> 1], s[e & 1]);
-      if (e + kAhead < 2 * kKS) op[e % kAhead] = row_operand(tl + 2 * kUnit * (e & 1), ad, (e + kAhead) >> 1);
+      s = mfma(op[e % kAhead], qf[e], s);
+      if (e + kAhead < kKS) op[e % kAhead] = row_operand(tl, ad, e + kAhead);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (c0 != kAll) hide(s[0], a, 2 * st < kt.nsk, j0, c0 == kNone ? j0 - 1 : t, hf);
-    if (c1 != kAll) hide(s[1], a, 2 * st + 1 < kt.nsk, j1, c1 == kNone ? j1 - 1 : t, hf);
-    float mx = max3(s[0][0], s[1][0], s[0][1]);
+    hide(s, a, kt, wt, i, t, hf);
+    // value product e: token half e / kDB, dim block e % kDB
+    auto read_v = [&](int e) { return col_operand(tl + kUnit, ad, e % kDB, e / kDB); };
 #pragma unroll
-    for (int i = 1; i < 15; ++i) mx = max3(mx, s[1][i], s[0][i + 1]);
-    mx = col_max(fmaxf(mx, s[1][15]));
+    for (int e = 0; e < kAhead; ++e) op[e] = read_v(e);
+    float mx = max3(s[0], s[1], s[2]);
+#pragma unroll
+    for (int x = 3; x < 15; x += 2) mx = max3(mx, s[x], s[x + 1]);
+    mx = col_max(fmaxf(mx, s[15]));
     const bool raise = mx > m_ref + thr;
     if (__builtin_amdgcn_ballot_w64(raise)) {
       const float m_new = raise ? mx : m_ref;
@@ -278,48 +366,28 @@ __global__ __launch_bounds__(kThreads, 2) void window_fwd_kernel(WindowArgs a) {
     const float mb = m_ref * a.scale_log2;
     // the products take weights rounded to bf16 (half a step, 2^-8 of each, averaged over the row); the
     // denominator adds them unrounded, so that lse keeps float32 precision
-    u32x4 pu[2][2];
-    auto weight_pair = [&](int u, int j) {
-      const f32x2 pr = {__builtin_amdgcn_exp2f(fmaf(s[u][2 * j], a.scale_log2, -mb)),
-                        __builtin_amdgcn_exp2f(fmaf(s[u][2 * j + 1], a.scale_log2, -mb))};
+    u32x4 pu[2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const f32x2 pr = {__builtin_amdgcn_exp2f(fmaf(s[2 * j], a.scale_log2, -mb)),
+                        __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], a.scale_log2, -mb))};
       l_run += pr[0] + pr[1];
-      pu[u][j >> 2][j & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
-    };
+      pu[j >> 2][j & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
+    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) weight_pair(0, j);
-    // value product e: tile e / (2 kDB), token half (e / kDB) % 2, dim block e % kDB; the second
-    // tile's weights are formed beside the first one's products
-    auto read_v = [&](int e) {
-      return col_operand(tl + 2 * kUnit * (e / (2 * kDB)) + kUnit, ad, e % kDB, (e / kDB) % 2);
-    };
-#pragma unroll
-    for (int e = 0; e < kAhead; ++e) op[e] = read_v(e);
-#pragma unroll
-    for (int e = 0; e < 4 * kDB; ++e) {
+    for (int e = 0; e < 2 * kDB; ++e) {
       __builtin_amdgcn_sched_barrier(0);
-      o[e % kDB] = mfma(op[e % kAhead], pu[e / (2 * kDB)][(e / kDB) % 2], o[e % kDB]);
-      if (e + kAhead < 4 * kDB) op[e % kAhead] = read_v(e + kAhead);
-      if (e < 2 * kDB)
-#pragma unroll
-        for (int j = 0; j < 4 / kDB; ++j) weight_pair(1, 4 / kDB * e + j);
+      o[e % kDB] = mfma(op[e % kAhead], pu[e / kDB], o[e % kDB]);
+      if (e + kAhead < 2 * kDB) op[e % kAhead] = read_v(e + kAhead);
     }
     __builtin_amdgcn_sched_barrier(0);
-  };
-  for (int st = 0; st < steps; st += 2) {
-    attend(st, std::integral_constant<int, 0>{});
-    if (st + 1 < steps) attend(st + 1, std::integral_constant<int, 1>{});
-  }
+  });
 
   const float l = col_sum(l_run);
   const float inv = 1.0f / l;
-  store_row<D>(a.out + row * D, o, inv, hf, ok);
+  const bool bad = store_row<D>(a.out + row * D, o, inv, hf, ok) || not_finite(inv);
   if (ok && hf == 0)
     a.lse_out[static_cast<size_t>(h * a.g + qh) * a.T + s0 + t] = (m_ref * a.scale_log2 + __log2f(l)) * kLn2;
-  bool bad = not_finite(inv);
-#pragma unroll
-  for (int x = 0; x < kDB; ++x)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) bad |= not_finite(o[x][i]);
   const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && ok);
   for (uint32_t cols = static_cast<uint32_t>(lanes | lanes >> 32); cols; cols &= cols - 1) {
     const int c = wave * 32 + __builtin_ctz(cols);
@@ -382,11 +450,11 @@ __device__ inline void exact_dq_row(const WindowArgs& a, int s0, int t, int hq) 
 template <int D, bool EXACT>
 __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
   using Tile = TileOf<D>;
-  constexpr int kUnit = Tile::kUnit, kStage = 4 * kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
-  __shared__ __attribute__((aligned(256))) char tile_lds[2][kStage];
+  constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
+  __shared__ __attribute__((aligned(256))) char tile_lds[2][4 * kUnit];   // [K | V] of two tiles, twice
   const int2 wg = xcd_order();
   const int h = wg.y;
-  const Block blk = block_of(a, wg.x, a.PB);
+  const Block blk = block_of(a, wg.x, a.PB, a.inv_pb);
   if (blk.p0 >= blk.len) return;
   const int s0 = blk.s0, p0 = blk.p0, p1 = min(blk.len, p0 + a.PB);
   const KeyTiles kt = key_tiles(a, p0, p1);
@@ -399,16 +467,16 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
   const LaneOffsets lo = lane_offsets<D>(lane, stride);
   const uint32_t tiles = lds_addr(tile_lds);
   const char* kv = reinterpret_cast<const char*>((wave >> 1 ? a.v : a.k) + (static_cast<size_t>(s0) * a.H + h) * D);
-  const int steps = (kt.nt + 1) >> 1, walk = EXACT ? 2 * steps : steps;
+  const int steps = (kt.nt + 1) >> 1;
   auto issue = [&](int st, int buf) {
-    const int i = 2 * (EXACT && st >= steps ? st - steps : st) + (wave & 1);
-    copy_tile<D>(kv, i < kt.nt ? kt.first(i) : p1, p1, stride, lo, lane,
-                 tiles + buf * kStage + 2 * kUnit * (wave & 1) + kUnit * (wave >> 1), &kZeros);
+    copy_keys<D>(a, kt, kv, 2 * st, blk.len, stride, lo, lane, wave, tiles + buf * 4 * kUnit);
+    if (2 * st + 1 < kt.nt)
+      copy_keys<D>(a, kt, kv, 2 * st + 1, blk.len, stride, lo, lane, wave, tiles + buf * 4 * kUnit + 2 * kUnit);
   };
   issue(0, 0);
 
   const int col = wave * 32 + (lane & 31);
-  const int pl = col / a.g, qh = col % a.g;
+  const int pl = static_cast<int>(col * a.inv_g >> 16), qh = col - pl * a.g;
   const bool ok = pl < a.PB && p0 + pl < p1;
   const int t = ok ? p0 + pl : p0;
   const size_t row = static_cast<size_t>(s0 + t) * Hq + h * a.g + qh;
@@ -421,44 +489,32 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
     if (!EXACT && ok) {
       const u32x4 ov = ld16(a.o + row * D + 16 * x + 8 * hf);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        dcol += __uint_as_float(df[x][i] << 16) * __uint_as_float(ov[i] << 16) +
-                __uint_as_float(df[x][i] & 0xFFFF0000u) * __uint_as_float(ov[i] & 0xFFFF0000u);
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t d2 = df[x][i], o2 = ov[i];
+        dcol = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, d2), __builtin_bit_cast(bf16x2, o2), dcol, false);
+      }
     }
   }
   if (!EXACT) dcol = col_sum(dcol);
   const size_t at = static_cast<size_t>(h * a.g + qh) * a.T + s0 + t;
   const float lse2 = ok ? a.lse[at] * kLog2e : 0.f;
-  const int q0 = p0 + wave * 32 / a.g, q1 = min(p1 - 1, p0 + (wave * 32 + 31) / a.g);
+  const int q0 = p0 + static_cast<int>(wave * 32 * a.inv_g >> 16);
+  const WaveTiles wt = wave_tiles(a, kt, q0, min(p1 - 1, p0 + static_cast<int>((wave * 32 + 31) * a.inv_g >> 16)));
   const LaneAddresses<D> ad = lane_addresses<D>(tiles, lo);
 
-  f32x16 dqa[kDB];
-#pragma unroll
-  for (int x = 0; x < kDB; ++x)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) dqa[x][i] = 0.f;
-
-  auto attend = [&](int v, auto buf_c) {
+  f32x16 dqa[kDB], start;   // -D in every row starts the dP products
+  auto attend = [&](int st, auto buf_c, auto sum_c) {
     constexpr int buf = decltype(buf_c)::value;
+    constexpr bool kSum = decltype(sum_c)::value;   // only summing D
     wait_copies();
     __syncthreads();
-    if (v + 1 < walk) issue(v + 1, buf ^ 1);
-    const bool first = EXACT && v < steps;   // summing D
-    const int st = EXACT && v >= steps ? v - steps : v;
-    if (EXACT && v == steps) dcol = col_sum(dcol) / col_sum(psum);
-    const float start = first ? 0.f : -dcol;   // -D in every row starts the dP products
+    if (st + 1 < steps) issue(st + 1, buf ^ 1);
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
-      const int i = 2 * st + sub, j0 = kt.first(i);
-      const int cls = mask_class(a, kt, i, j0, q0, q1);
-      if (cls == kNone) continue;
-      const int tl = buf * kStage + 2 * kUnit * sub;
+      const int i = 2 * st + sub;
+      const int tl = buf * 4 * kUnit + 2 * kUnit * sub;
+      if (i >= kt.nt || !tile_seen(wt, i)) continue;
       f32x16 s, dp;
-#pragma unroll
-      for (int x = 0; x < 16; ++x) {
-        s[x] = 0.f;
-        dp[x] = start;
-      }
       u32x4 op[kAhead];
       // product e: scores (keys) and dP (values) take turns, k-step e / 2
 #pragma unroll
@@ -466,53 +522,60 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
 #pragma unroll
       for (int e = 0; e < 2 * kKS; ++e) {
         __builtin_amdgcn_sched_barrier(0);
-        if (e & 1) dp = mfma(op[e % kAhead], df[e >> 1], dp);
-        else s = mfma(op[e % kAhead], qf[e >> 1], s);
+        if (e & 1) dp = mfma(op[e % kAhead], df[e >> 1], e > 1 ? dp : kSum ? f32x16{} : start);
+        else s = mfma(op[e % kAhead], qf[e >> 1], e ? s : f32x16{});
         if (e + kAhead < 2 * kKS) op[e % kAhead] = row_operand(tl + kUnit * (e & 1), ad, (e + kAhead) >> 1);
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (cls == kSome) hide(s, a, i < kt.nsk, j0, t, hf);
-      if (first) {
+      hide(s, a, kt, wt, i, t, hf);
+      if constexpr (kSum) {
 #pragma unroll
         for (int x = 0; x < 16; ++x) {
           const float p = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2, -lse2));
           dcol += p * dp[x];
           psum += p;
         }
-        continue;
-      }
+      } else {
 #pragma unroll
-      for (int e = 0; e < kAhead; ++e) op[e] = col_operand(tl, ad, e % kDB, e / kDB);
-      float ds[16];
+        for (int e = 0; e < kAhead; ++e) op[e] = col_operand(tl, ad, e % kDB, e / kDB);
+        float ds[16];
 #pragma unroll
-      for (int x = 0; x < 16; ++x) ds[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2, -lse2)) * dp[x];
-      const u32x4 du[2] = {pack_bf16(ds), pack_bf16(ds + 8)};   // rounded as in the key-major pass
+        for (int x = 0; x < 16; ++x) ds[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2, -lse2)) * dp[x];
+        const u32x4 du[2] = {pack_bf16(ds), pack_bf16(ds + 8)};   // rounded as in the key-major pass
 #pragma unroll
-      for (int e = 0; e < 2 * kDB; ++e) {
+        for (int e = 0; e < 2 * kDB; ++e) {
+          __builtin_amdgcn_sched_barrier(0);
+          dqa[e % kDB] = mfma(op[e % kAhead], du[e / kDB], dqa[e % kDB]);
+          if (e + kAhead < 2 * kDB) op[e % kAhead] = col_operand(tl, ad, (e + kAhead) % kDB, (e + kAhead) / kDB);
+        }
         __builtin_amdgcn_sched_barrier(0);
-        dqa[e % kDB] = mfma(op[e % kAhead], du[e / kDB], dqa[e % kDB]);
-        if (e + kAhead < 2 * kDB) op[e % kAhead] = col_operand(tl, ad, (e + kAhead) % kDB, (e + kAhead) / kDB);
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
   };
-  for (int v = 0; v < walk; v += 2) {
-    attend(v, std::integral_constant<int, 0>{});
-    if (v + 1 < walk) attend(v + 1, std::integral_constant<int, 1>{});
+  auto walk = [&](auto sum_c) {
+    for (int st = 0; st < steps; st += 2) {
+      attend(st, std::integral_constant<int, 0>{}, sum_c);
+      if (st + 1 < steps) attend(st + 1, std::integral_constant<int, 1>{}, sum_c);
+    }
+  };
+  if constexpr (EXACT) {
+    walk(std::true_type{});
+    dcol = col_sum(dcol) / col_sum(psum);
+    __syncthreads();   // every wave is done with the tiles
+    issue(0, 0);
   }
-
-  if (ok && hf == 0)
-    a.rows[static_cast<size_t>(h * a.g + qh) * a.Ts + s0 + t] = f32x2{-lse2 / a.scale_log2, -dcol};
-  const float scale = a.scale_log2 / kLog2e;
-  bool bad = not_finite(dcol);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) start[i] = -dcol;
 #pragma unroll
   for (int x = 0; x < kDB; ++x)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      bad |= not_finite(dqa[x][i]);
-      if (a.single) dqa[x][i] = 0.f;
-    }
-  store_row<D>(a.dq + row * D, dqa, scale, hf, ok);
+    for (int i = 0; i < 16; ++i) dqa[x][i] = 0.f;
+  walk(std::false_type{});
+
+  if (ok && hf == 0)
+    a.rows[static_cast<size_t>(h * a.g + qh) * a.Ts + s0 + t] = f32x2{-lse2 / a.scale_log2, -dcol};
+  const float scale = a.single ? 0.f : a.scale_log2 / kLog2e;
+  const bool bad = store_row<D>(a.dq + row * D, dqa, scale, hf, ok) || not_finite(dcol);
   const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && ok);
   for (uint32_t cols = static_cast<uint32_t>(lanes | lanes >> 32); cols; cols &= cols - 1) {
     const int c = wave * 32 + __builtin_ctz(cols);
@@ -769,14 +832,14 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(WindowArgs a) {
   if (in_group >= 4) {
     // positions 512 c .. (c >= 1) of the last sequence that starts before this 512 of the packed tokens
     if (group == 0) return;
-    const Block f = block_of(a, group - 1, kFar, 0);
+    const Block f = block_of(a, group - 1, kFar, inverse(kFar), 0);
     const int key0 = 32 * (in_group - 4);
     const int first = max(f.p0 + kFar, far_begin(a, key0 & ~(kKeys - 1))), last = min(f.len, f.p0 + 2 * kFar);
     if (first >= last || key0 >= f.len) return;
     far_queries<D>(a, tile_lds[0], row_lds, f.s0, f.len, h, key0, first, last, group);
     return;
   }
-  const Block blk = block_of(a, 4 * group + in_group, kKeys);
+  const Block blk = block_of(a, 4 * group + in_group, kKeys, inverse(kKeys));
   if (blk.p0 >= blk.len) return;
   const int s0 = blk.s0, len = blk.len;
   const int lane = threadIdx.x & 63, hf = lane >> 5;
@@ -860,18 +923,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(WindowArgs a) {
     store_sums<D>(dst + 32 * D, dva, hf);
     return;
   }
-  bool bad = false;
-#pragma unroll
-  for (int x = 0; x < kDB; ++x)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      bad |= not_finite(dka[x][i]) || not_finite(dva[x][i]);
-      if (a.single) dka[x][i] = 0.f;
-    }
   const bool jo = je < len;
   const size_t out = (static_cast<size_t>(s0 + (jo ? je : 0)) * a.H + h) * D;
-  store_row<D>(a.dk + out, dka, a.scale_log2 / kLog2e, hf, jo);
-  store_row<D>(a.dv + out, dva, 1.0f, hf, jo);
+  bool bad = store_row<D>(a.dk + out, dka, a.single ? 0.f : a.scale_log2 / kLog2e, hf, jo);
+  bad |= store_row<D>(a.dv + out, dva, 1.0f, hf, jo);
   const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && jo);
   for (uint32_t cols = static_cast<uint32_t>(lanes | lanes >> 32); cols; cols &= cols - 1)
     exact_key<D>(a, s0, len, key0 + __builtin_ctz(cols), h);
@@ -883,7 +938,7 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void window_sinks_kernel(WindowArgs a) {
   constexpr int E = D / 64;
   const int slot = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63;
-  const Block blk = block_of(a, slot, kFar, 0);       // the sequence that starts in this 512, if it is long
+  const Block blk = block_of(a, slot, kFar, inverse(kFar), 0);       // the sequence that starts in this 512, if it is long
   if (blk.p0 != 0) return;
   for (int j = blockIdx.z * (kThreads / 64) + (threadIdx.x >> 6); j < min(32 * a.sink_tiles, blk.len);
        j += gridDim.z * (kThreads / 64)) {
@@ -927,6 +982,8 @@ WindowArgs window_args(const dms_window_config& c, const int32_t* cu, const void
   a.w = std::min(c.window, std::max(1, c.max_seqlen));   // no query is further from a key
   a.sinks = std::min(c.sinks, c.max_seqlen);
   a.PB = kCols / a.g;
+  a.inv_pb = inverse(a.PB);
+  a.inv_g = 65536 / a.g + 1;
   a.single = a.w == 1 && (a.sinks == 0 || c.max_seqlen == 1);
   const float scale = c.softmax_scale > 0.f ? c.softmax_scale : 1.0f / sqrtf(static_cast<float>(c.head_dim));
   a.scale_log2 = scale * kLog2e;
