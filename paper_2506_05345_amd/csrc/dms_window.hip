@@ -218,6 +218,88 @@ __device__ inline bool store_row(__bf16* dst, const f32x16* o, float f, int hf, 
 }
 
 // ---------------------------------------------------------------------------
+// Rows of a wave's 32 columns between memory and MFMA operands.  Column c of
+// the block is row pl (Hq - g) + c past the block's first one (pl its position).
+// Memory is read and written in whole 128-byte lines, 8 rows an instruction
+// (lane l: row 8 m + l / 8, 16-byte piece l % 8 of a 64-element half), and the
+// halves are turned in 4 KB of LDS of the wave's own, pieces permuted by row as
+// in the tiles.  Read straight into operands (32 rows of 32 bytes an
+// instruction) and written so, rows took 60 of the forward's 165 us.
+// ---------------------------------------------------------------------------
+constexpr int kTurn = 4096;   // LDS bytes of a wave's half rows
+struct Rows {
+  uint32_t off[4];   // bytes from the block's first row
+  bool ok[4];
+  uint32_t wr, rd;   // LDS offsets: this lane's piece of rows 8 m .. (m odd: ^ 32), of its column's row (k-step s: ^ 32 s)
+};
+template <int D>
+__device__ inline Rows wave_rows(const WindowArgs& a, int wave, int lane, int positions) {
+  Rows r;
+  const int r8 = lane >> 3, c8 = lane & 7, col = lane & 31;
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    const int c = wave * 32 + 8 * m + r8;
+    const int pl = static_cast<int>(c * a.inv_g >> 16);
+    r.ok[m] = pl < positions;
+    r.off[m] = (r.ok[m] ? static_cast<uint32_t>(pl * (a.H - 1) * a.g + c) * TileOf<D>::kRowB : 0u) + 16 * c8;
+  }
+  r.wr = r8 * 128 + 16 * (c8 ^ row_flip<64>(r8));
+  r.rd = col * 128 + 16 * ((lane >> 5) ^ piece_flip<64>(col));
+  return r;
+}
+// Loads (not waited for) of the rows at `base`: piece set h * 4 + m is half h of rows 8 m ..
+template <int D>
+__device__ inline void load_rows(u32x4* x, const __bf16* base, const Rows& r) {
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+    for (int m = 0; m < 4; ++m) x[4 * h + m] = ld16(reinterpret_cast<const char*>(base) + r.off[m] + 128 * h);
+}
+// Loaded rows to column operands, in place.
+template <int D>
+__device__ inline void to_operands(u32x4* x, const Rows& r, uint32_t turn) {
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+      *reinterpret_cast<DMS_LDS u32x4*>(turn + 1024 * m + (r.wr ^ (32 * (m & 1)))) = x[4 * h + m];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) x[4 * h + s] = *reinterpret_cast<DMS_LDS const u32x4*>(turn + (r.rd ^ (32 * s)));
+  }
+}
+// Accumulators of the columns, times f (per column), to their bf16 rows.  Returns whether this lane's part of
+// its column holds a NaN (also if it holds infinities of both signs).
+template <int D>
+__device__ inline bool store_rows(__bf16* base, const f32x16* o, float f, const Rows& r, uint32_t turn, int hf) {
+  const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+  float sum = 0.f;
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        u32x2 w;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const f32x2 pr = {o[2 * h + x][4 * y + 2 * e] * f, o[2 * h + x][4 * y + 2 * e + 1] * f};
+          const bf16x2 pb = __builtin_convertvector(pr, bf16x2);
+          sum = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, sum, false);
+          w[e] = __builtin_bit_cast(uint32_t, pb);
+        }
+        // piece 4 x + y of the half; the lane's 8 bytes of it (rd holds piece hf)
+        *reinterpret_cast<DMS_LDS u32x2*>(turn + ((r.rd ^ (16 * hf)) ^ (16 * (4 * x + y))) + 8 * hf) = w;
+      }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const u32x4 v = *reinterpret_cast<DMS_LDS const u32x4*>(turn + 1024 * m + (r.wr ^ (32 * (m & 1))));
+      if (r.ok[m]) *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(base) + r.off[m] + 128 * h) = v;
+    }
+  }
+  return is_nan(sum);
+}
+
+// ---------------------------------------------------------------------------
 // LDS ring of 3 or 4 steps, each two 32-row tiles of 2 D bytes a row ([K | V] of
 // 32 keys, or [Q | dO] of 32 positions of one head): while one step is computed
 // the next are on their way.  A window is few steps long, so that a
@@ -284,7 +366,9 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
   using Tile = TileOf<D>;
   constexpr int kSlots = 3;
   constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
-  __shared__ __attribute__((aligned(256))) char tile_lds[kSlots][2 * kUnit];
+  // the last slot, idle until the first step, and its end (D = 64) also turn the waves' rows
+  constexpr int kTurnAt = (kSlots - 1) * 2 * kUnit;
+  __shared__ __attribute__((aligned(256))) char tile_lds[kTurnAt + (D == 128 ? 2 * kUnit : 4 * kTurn)];
   const int2 wg = xcd_order();
   const int h = wg.y;
   const Block blk = block_of(a, wg.x, a.PB, a.inv_pb);
@@ -309,11 +393,10 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
   const int pl = static_cast<int>(col * a.inv_g >> 16), qh = col - pl * a.g;
   const bool ok = pl < a.PB && p0 + pl < p1;
   const int t = ok ? p0 + pl : p0;
-  const size_t row = static_cast<size_t>(s0 + t) * Hq + h * a.g + qh;
+  const size_t first_row = static_cast<size_t>(s0 + p0) * Hq + h * a.g;
+  const Rows rows = wave_rows<D>(a, wave, lane, p1 - p0);
   u32x4 qf[kKS];
-#pragma unroll
-  for (int x = 0; x < kKS; ++x)
-    qf[x] = ok ? ld16(a.q + row * D + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
+  load_rows<D>(qf, a.q + first_row * D, rows);
   // positions of this wave's columns
   const int q0 = p0 + static_cast<int>(wave * 32 * a.inv_g >> 16);
   const WaveTiles wt = wave_tiles(a, kt, q0, min(p1 - 1, p0 + static_cast<int>((wave * 32 + 31) * a.inv_g >> 16)));
@@ -324,6 +407,7 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
   for (int x = 0; x < kDB; ++x)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[x][i] = 0.f;
+  to_operands<D>(qf, rows, tiles + kTurnAt + wave * kTurn);
   float m_ref = kMInit, l_run = 0.f;
   const float thr = kRescale / a.scale_log2;
 
@@ -385,7 +469,8 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
 
   const float l = col_sum(l_run);
   const float inv = 1.0f / l;
-  const bool bad = store_row<D>(a.out + row * D, o, inv, hf, ok) || not_finite(inv);
+  __syncthreads();   // every wave is done with the tiles
+  const bool bad = store_rows<D>(a.out + first_row * D, o, inv, rows, tiles + wave * kTurn, hf) || not_finite(inv);
   if (ok && hf == 0)
     a.lse_out[static_cast<size_t>(h * a.g + qh) * a.T + s0 + t] = (m_ref * a.scale_log2 + __log2f(l)) * kLn2;
   const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && ok);
@@ -451,7 +536,9 @@ template <int D, bool EXACT>
 __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
   using Tile = TileOf<D>;
   constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
-  __shared__ __attribute__((aligned(256))) char tile_lds[2][4 * kUnit];   // [K | V] of two tiles, twice
+  // [K | V] of two tiles, twice; the second pair of tiles, idle until the first step, also turns the waves' rows
+  __shared__ __attribute__((aligned(256))) char tile_lds[2][4 * kUnit];
+  __shared__ float dsum_lds[kCols];
   const int2 wg = xcd_order();
   const int h = wg.y;
   const Block blk = block_of(a, wg.x, a.PB, a.inv_pb);
@@ -479,23 +566,34 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
   const int pl = static_cast<int>(col * a.inv_g >> 16), qh = col - pl * a.g;
   const bool ok = pl < a.PB && p0 + pl < p1;
   const int t = ok ? p0 + pl : p0;
-  const size_t row = static_cast<size_t>(s0 + t) * Hq + h * a.g + qh;
+  const size_t first_row = static_cast<size_t>(s0 + p0) * Hq + h * a.g;
+  const Rows rows = wave_rows<D>(a, wave, lane, p1 - p0);
+  const uint32_t turn = tiles + 4 * kUnit + wave * kTurn;
   u32x4 qf[kKS], df[kKS];
+  load_rows<D>(qf, a.q + first_row * D, rows);
+  load_rows<D>(df, a.dout + first_row * D, rows);
   float dcol = 0.f, psum = 0.f;
+  if (!EXACT) {
+    u32x4 ov[kKS];
+    load_rows<D>(ov, a.o + first_row * D, rows);
 #pragma unroll
-  for (int x = 0; x < kKS; ++x) {
-    qf[x] = ok ? ld16(a.q + row * D + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
-    df[x] = ok ? ld16(a.dout + row * D + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
-    if (!EXACT && ok) {
-      const u32x4 ov = ld16(a.o + row * D + 16 * x + 8 * hf);
+    for (int m = 0; m < 4; ++m) {   // row 8 m + lane / 8: its pieces lie with 8 lanes
+      float d = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t d2 = df[x][i], o2 = ov[i];
-        dcol = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, d2), __builtin_bit_cast(bf16x2, o2), dcol, false);
-      }
+      for (int x = 0; x < D / 64; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t d2 = df[4 * x + m][i], o2 = ov[4 * x + m][i];
+          d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, d2), __builtin_bit_cast(bf16x2, o2), d, false);
+        }
+#pragma unroll
+      for (int off = 1; off < 8; off <<= 1) d += __shfl_xor(d, off, 64);
+      if ((lane & 7) == 0) dsum_lds[wave * 32 + 8 * m + (lane >> 3)] = d;
     }
+    dcol = dsum_lds[col];   // written by this wave
   }
-  if (!EXACT) dcol = col_sum(dcol);
+  to_operands<D>(qf, rows, turn);
+  to_operands<D>(df, rows, turn);
   const size_t at = static_cast<size_t>(h * a.g + qh) * a.T + s0 + t;
   const float lse2 = ok ? a.lse[at] * kLog2e : 0.f;
   const int q0 = p0 + static_cast<int>(wave * 32 * a.inv_g >> 16);
@@ -575,7 +673,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
   if (ok && hf == 0)
     a.rows[static_cast<size_t>(h * a.g + qh) * a.Ts + s0 + t] = f32x2{-lse2 / a.scale_log2, -dcol};
   const float scale = a.single ? 0.f : a.scale_log2 / kLog2e;
-  const bool bad = store_row<D>(a.dq + row * D, dqa, scale, hf, ok) || not_finite(dcol);
+  __syncthreads();   // every wave is done with the tiles
+  const bool bad = store_rows<D>(a.dq + first_row * D, dqa, scale, rows, tiles + wave * kTurn, hf) || not_finite(dcol);
   const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && ok);
   for (uint32_t cols = static_cast<uint32_t>(lanes | lanes >> 32); cols; cols &= cols - 1) {
     const int c = wave * 32 + __builtin_ctz(cols);
