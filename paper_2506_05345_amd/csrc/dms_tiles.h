@@ -157,10 +157,10 @@ __device__ inline void lds_copy4(const void* base, uint32_t off, uint32_t m0) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" : : "s"(m0), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ inline void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // vmcnt(0)
-// All but the N newest copies (fewer than 16) have landed.
+// All but the N newest copies (fewer than 64) have landed.
 template <int N>
 __device__ inline void wait_copies_but() {
-  __builtin_amdgcn_s_waitcnt(0x0F70 | N);
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
 }
 
 // keeps the compiler from forming what follows from x ahead of a loop and holding it

@@ -20,7 +20,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kCols = 128;            // (position, query head) columns of a query block, 32 per wave
 constexpr int kAhead = 4;              // operands are read this many MFMAs ahead, in pinned order
-constexpr int kFew = 2;                // the same for the key-major pass, whose registers are short
 constexpr float kRescale = 8.0f;      // lazy rescale threshold, log2 units
 constexpr float kMInit = -1.0e30f;    // running max before the first visible key
 constexpr float kLog2e = 1.4426950408889634f;
@@ -32,16 +31,21 @@ struct WindowArgs {
   const float* lse;
   __bf16 *out, *dq, *dk, *dv;
   float* lse_out;
-  f32x2* rows;             // [Hq][Ts]: -lse / scale (raw score units) and -D of each query (workspace)
-  float* part;             // sinks' sums: [slots][tiles][H] of (dk, dv) [32][D] of the far queries, then
-                           // [slots] of the same from the key blocks (workspace)
-  int64_t Ts;              // rows of a head in `rows`: T + 32, whole tiles are read past a sequence
+  float* nlse;             // [Hq][Ts] -lse / scale (raw score units) of each query (workspace)
+  float* nsum;             // [Hq][Ts] -D of each query (workspace)
+  float* part;             // [splits][T][H][2 D]: sums of a key block's shares of steps (splits > 1; workspace)
+  float* far_part;         // [T / far + 1][sink tiles][H][2][32][D]: (dk, dv) of sinks' far queries, and, without
+                           // splits, as much again of the sinks from their key blocks (workspace)
+  int64_t Ts;              // rows of a head in nlse, nsum: T + 128, whole copies are read past a sequence
   int n, T, H, g, w, sinks;
   int single;              // every row sees one key: P = 1 and dS = 0
   int PB;                  // positions of a query block: kCols / g
   uint32_t inv_pb;         // 2^32 / PB + 1
   uint32_t inv_g;          // 65536 / g + 1: col / g = col * inv_g >> 16 for columns below 128
-  int sink_tiles;          // 32-key tiles of sinks whose far queries go to workgroups of their own (else 0)
+  int far;                 // a sink's queries from this position on go to workgroups of `far` positions
+  uint32_t inv_far;
+  int sink_tiles;          // 32-key tiles of sinks with such queries
+  int splits;              // workgroups that share a key block's steps
   float scale_log2;
 };
 
@@ -59,6 +63,7 @@ __device__ inline float wave_sum(float x) {
 
 // x / d for 0 <= x < 2^31, inv = 2^32 / d + 1: the product is at most one too large.
 __device__ inline int divide(int x, int d, uint32_t inv) {
+  if (d == 1) return x;
   const int q = static_cast<int>(__umulhi(static_cast<uint32_t>(x), inv));
   return q * static_cast<int64_t>(d) > x ? q - 1 : q;
 }
@@ -344,6 +349,15 @@ __device__ inline void step_ready(int left) {
   __syncthreads();
 }
 
+// f(0), .. f(N - 1), each a constant.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each(F f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    each<N, I + 1>(f);
+  }
+}
+
 // f(step, slot) for steps 0 .. n - 1, the slot a constant.
 template <int SLOTS, typename F>
 __device__ __forceinline__ void over_steps(int n, F f) {
@@ -529,7 +543,10 @@ __device__ inline void exact_dq_row(const WindowArgs& a, int s0, int t, int hq) 
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) a.dq[row + e] = static_cast<__bf16>(a.single ? 0.f : dq[e] * a.scale_log2 / kLog2e);
-  if (lane == 0) a.rows[hq * a.Ts + s0 + t] = f32x2{-lse2 / a.scale_log2, -d};
+  if (lane == 0) {
+    a.nlse[hq * a.Ts + s0 + t] = -lse2 / a.scale_log2;
+    a.nsum[hq * a.Ts + s0 + t] = -d;
+  }
 }
 
 template <int D, bool EXACT>
@@ -670,8 +687,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
     for (int i = 0; i < 16; ++i) dqa[x][i] = 0.f;
   walk(std::false_type{});
 
-  if (ok && hf == 0)
-    a.rows[static_cast<size_t>(h * a.g + qh) * a.Ts + s0 + t] = f32x2{-lse2 / a.scale_log2, -dcol};
+  if (ok) (hf ? a.nsum : a.nlse)[static_cast<size_t>(h * a.g + qh) * a.Ts + s0 + t] = hf ? -dcol : -lse2 / a.scale_log2;
   const float scale = a.single ? 0.f : a.scale_log2 / kLog2e;
   __syncthreads();   // every wave is done with the tiles
   const bool bad = store_rows<D>(a.dq + first_row * D, dqa, scale, rows, tiles + wave * kTurn, hf) || not_finite(dcol);
@@ -683,22 +699,34 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// dK / dV pass.  Workgroup = (KV head, 128 keys of one sequence); wave x owns 32
-// of them as the columns of its products, with their K and V operands in
-// registers, and walks the query tiles (32 positions) that see the block, every
-// head of the group: dV^T += dO^T P, dK^T += Q^T dS with P, dS [query, key] from
-// S = Q K^T, dP = dO V^T.
+// dK / dV pass.  Workgroup = (KV head, 128 keys of one sequence, share of the
+// steps); wave x owns 32 of the keys as the columns of its products, with their
+// K and V operands in registers, and walks the query tiles (32 positions) that
+// see the block, every head of the group: dV^T += dO^T P, dK^T += Q^T dS with
+// P, dS [query, key] from S = Q K^T, dP = dO V^T.
+// Two steps (tile, head) go through the matrix core together: the weights of
+// one are formed beside the other's products, and operands are read kDeep
+// products ahead.  That takes the registers of one wave per SIMD at d = 128.
+// With two waves of 256 registers, each step by itself and operands two ahead,
+// the pass ran 330 us against NEW us (16384 tokens of 8 x 5 heads, w = 256, 4
+// sinks).
 // A sink is seen by every later query.  A block that holds sinks walks on to
-// position kFar; what lies further is shared out to workgroups of kFar
-// positions (`far` below), whose sums window_sinks_kernel adds in order.
+// position `far`; what lies further is shared out to workgroups of `far`
+// positions, whose waves take the steps in turn.
+// When the call has too few blocks to fill the chip, each block's steps are
+// split over `splits` workgroups.  Sums that several workgroups hold are added,
+// in order, by window_sum_kernel.
 // ---------------------------------------------------------------------------
-constexpr int kFar = 512;
 constexpr int kKeys = 128;
+constexpr int kSplitTarget = 256;   // key blocks below which their steps are split
+constexpr int kMaxSplits = 8;
+constexpr int kStages = 4;     // pairs of steps in LDS
+constexpr int kDeep = 6;       // operands are read this many products ahead
 
 // First position (a multiple of 32) that the block of keys from j0 on leaves to others.
 __device__ inline int far_begin(const WindowArgs& a, int j0) {
   const int end = j0 + ((kKeys + a.w + 31) & ~31);
-  return j0 < a.sinks ? max(end, kFar) : end;
+  return j0 < a.sinks ? max(end, a.far) : end;
 }
 
 // dK and dV of key j by one wave from the queries that see it.
@@ -727,8 +755,8 @@ __device__ inline void exact_key(const WindowArgs& a, int s0, int len, int j, in
         s += k[e] * q[e];
         dp += v[e] * dO[e];
       }
-      const f32x2 r = a.rows[hq * a.Ts + s0 + t];
-      const float p = exp2f((wave_sum(s) + r[0]) * a.scale_log2), ds = p * (wave_sum(dp) + r[1]);
+      const size_t at = hq * a.Ts + s0 + t;
+      const float p = exp2f((wave_sum(s) + a.nlse[at]) * a.scale_log2), ds = p * (wave_sum(dp) + a.nsum[at]);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         dv[e] += p * dO[e];
@@ -742,89 +770,181 @@ __device__ inline void exact_key(const WindowArgs& a, int s0, int len, int j, in
   }
 }
 
-// Sums of far queries: slot b of the workspace belongs to positions 512 c .. of the sequence that starts in
-// the packed tokens' (b - c)-th 512, c >= 1; a sequence's key blocks leave theirs in slot cu / 512.  Only
-// sequences longer than 512 have any, so that no two share a slot.
-__device__ inline float* part_of(const WindowArgs& a, bool blocks, int slot, int tile, int h, int D) {
-  const size_t slots = a.T / kFar + 1;
-  return a.part + (((blocks ? slots : 0) + slot) * a.sink_tiles + tile) * a.H * 64 * D + static_cast<size_t>(h) * 64 * D;
+// Sums of the far queries of slot b: positions far c .. of the sequence that starts in the packed tokens'
+// (b - c)-th `far`, c >= 1.  Only sequences longer than that have any, so that no two share a slot.
+__device__ inline float* far_sums(const WindowArgs& a, int slot, int tile, int h, int D) {
+  return a.far_part + ((static_cast<size_t>(slot) * a.sink_tiles + tile) * a.H + h) * 64 * D;
+}
+// Sums of a tile of sinks from its key block, where nothing else is shared: of the sequence that starts in the
+// packed tokens' slot-th `far`.
+__device__ inline float* near_sums(const WindowArgs& a, int slot, int tile, int h, int D) {
+  return far_sums(a, divide(a.T, a.far, a.inv_far) + 1 + slot, tile, h, D);
+}
+// Sums of one share of a key block: row of packed token t.
+__device__ inline float* share_sums(const WindowArgs& a, int split, int t, int h, int D) {
+  return a.part + ((static_cast<size_t>(split) * a.T + t) * a.H + h) * 2 * D;
 }
 
-// The (query tile, head) steps of a workgroup: tiles first .. last, heads inside a tile.
+// The list of (query tile, head) steps of a workgroup: `tiles` tiles of positions from pos0 on, beginning with
+// tile `start` and around to the one before it, heads inside a tile.  Key blocks begin with the tile whose
+// number is a multiple of the tiles that a block sees: blocks of one sequence that run together then read the
+// same tile at about the same time, and each XCD's L2 serves most of them (each block beginning with its own
+// first tile, copies took 1.1 GB past the L2s and 180 us).
+struct StepList {
+  int pos0, tiles, start, g;
+  int qh, tile;           // current step
+  __device__ void seek(int step) {
+    qh = step % g;
+    tile = start + step / g;
+    while (tile >= tiles) tile -= tiles;
+  }
+  __device__ void skip(int n) {
+    qh += n;
+    while (qh >= g) {
+      qh -= g;
+      if (++tile >= tiles) tile -= tiles;
+    }
+  }
+  __device__ int pos() const { return pos0 + 32 * tile; }
+};
+
+// Copies the steps, two at a time, through a ring of stages: [Q | dO] of both steps, then their rows' -lse and -D.
 template <int D>
 struct QuerySteps {
-  const WindowArgs& a;
-  const char* src;        // this wave's tensor (queries or output gradients), first token of the sequence
-  const f32x2* rows;      // the first head's rows, first token of the sequence
-  int len, total, wave, lane;
+  static constexpr int kUnit = TileOf<D>::kUnit;
+  static constexpr int kBytes = 4 * kUnit;             // tiles of a stage
+  static constexpr int kCopies = TileOf<D>::kUnit / 1024 + 1;   // copies of a stage by one wave
+  const char* src;        // this wave's tensor (queries or output gradients): first head, first token
+  const float* rows;      // this wave's row values
+  int64_t head_step;
+  int len, wave, lane;
   uint32_t stride, tiles, row_lds;
-  int ld_step, ld_qh, ld_pos;
+  StepList ld;            // this wave's next step
 
-  __device__ QuerySteps(const WindowArgs& a, int s0, int len, int h, int first, int count, int wave, int lane,
-                        uint32_t tiles, uint32_t row_lds)
-      : a(a), len(len), total(count * a.g), wave(wave), lane(lane), tiles(tiles), row_lds(row_lds) {
+  __device__ QuerySteps(const WindowArgs& a, int s0, int len_, int h, const StepList& list, int first, int wave_,
+                        int lane_, uint32_t tiles_, uint32_t row_lds_)
+      : len(len_), wave(wave_), lane(lane_), tiles(tiles_), row_lds(row_lds_), ld(list) {
     const int Hq = a.H * a.g;
     stride = Hq * TileOf<D>::kRowB;
+    // wave x copies tensor x / 2 and row values x / 2 of step 2 st + x % 2
     src = reinterpret_cast<const char*>((wave >> 1 ? a.dout : a.q) + (static_cast<size_t>(s0) * Hq + h * a.g) * D);
-    rows = a.rows + h * a.g * a.Ts + s0;
-    ld_step = wave & 1;
-    ld_qh = ld_step % a.g;
-    ld_pos = first + 32 * (ld_step / a.g);
+    rows = (wave >> 1 ? a.nsum : a.nlse) + h * a.g * a.Ts + s0;
+    head_step = a.Ts;
+    ld.seek(first + (wave & 1));
   }
-  // this wave copies tensor wave / 2 of step 2 st + wave % 2, and the step's row sums
-  __device__ void issue(int buf, const LaneOffsets& lo) {
-    constexpr int kUnit = TileOf<D>::kUnit;
-    if (ld_step < total) {
-      copy_tile<D>(src + static_cast<size_t>(ld_qh) * TileOf<D>::kRowB, ld_pos, len, stride, lo, lane,
-                   tiles + buf * 4 * kUnit + 2 * kUnit * (wave & 1) + kUnit * (wave >> 1), &kZeros);
-      if (wave < 2)
-        lds_copy4(rows + ld_qh * a.Ts + ld_pos, 4 * fresh(lane), row_lds + 512 * buf + 256 * (wave & 1));
-    }
-    ld_step += 2;
-    ld_qh += 2;
-    while (ld_qh >= a.g) {
-      ld_qh -= a.g;
-      ld_pos += 32;
-    }
+  __device__ void issue(int stage, const LaneOffsets& lo) {
+    // (a step past the last is copied like the others, so that waits can count copies, and read by nobody)
+    copy_tile<D>(src + static_cast<size_t>(ld.qh) * TileOf<D>::kRowB, ld.pos(), len, stride, lo, lane,
+                 tiles + stage * kBytes + 2 * kUnit * (wave & 1) + kUnit * (wave >> 1), &kZeros);
+    lds_copy4(rows + ld.qh * head_step + ld.pos(), 4 * fresh(lane), row_lds + 1024 * stage + 512 * (wave & 1) + 256 * (wave >> 1));
+    ld.skip(2);
+  }
+  // stages 0 .. 2 are issued ahead; `left` stages follow this one
+  __device__ static void ready(int left) {
+    if (left >= 2) wait_copies_but<2 * kCopies>();
+    else if (left == 1) wait_copies_but<kCopies>();
+    else wait_copies();
+    __syncthreads();
   }
 };
 
-// Scores and dP of the step staged at `tl`, started from its rows' -lse and -D.
-template <int D, bool DP>
-__device__ __forceinline__ void query_products(uint32_t tl, const float* rows, const LaneOffsets& lo, const u32x4* kf,
-                                               const u32x4* vf, int hf, f32x16& s, f32x16& dp) {
-  constexpr int kKS = TileOf<D>::kKS;
+// N = 1 or 2 steps, the first `live` of which count, for one wave's 32 keys from key0 on: their tiles by `ad`,
+// their row values from LDS address `rows` on, step u's queries from position tq[u] on.
+template <int D, int N>
+__device__ __forceinline__ void key_steps(const WindowArgs& a, const LaneAddresses<D>& ad, uint32_t rows,
+                                          const int (&tq)[2], int live, int key0, int len, int lane,
+                                          const u32x4* kf, const u32x4* vf, f32x16* dka, f32x16* dva) {
+  constexpr int kUnit = TileOf<D>::kUnit, kKS = TileOf<D>::kKS, kDB = TileOf<D>::kDB;
+  constexpr int kProd = 2 * kKS, kSum = 4 * kDB, kPart = N * kProd, kAll = N * (kProd + kSum);
+  static_assert(kProd == kSum, "a step's products and sums take as many operands");
+  const int hf = lane >> 5;
+  f32x16 s[N], dp[N];
+  // -lse and -D of the rows start the products: register i of a lane is query tq + 16 (i / 8) + 8 hf + i % 8
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const f32x4 r = *reinterpret_cast<const f32x4*>(rows + 2 * (16 * (i >> 2) + 8 * hf + 2 * (i & 3)));
-    s[2 * i] = r[0];
-    dp[2 * i] = r[1];
-    s[2 * i + 1] = r[2];
-    dp[2 * i + 1] = r[3];
+  for (int u = 0; u < N; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t r = rows + 32 * hf + 512 * u + 4 * (16 * (i >> 1) + 4 * (i & 1));
+      const f32x4 l = *reinterpret_cast<DMS_LDS const f32x4*>(r), d = *reinterpret_cast<DMS_LDS const f32x4*>(r + 256);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[u][4 * i + e] = l[e];
+        dp[u][4 * i + e] = d[e];
+      }
+    }
+  // operand e: products of step 0, of step 1, sums of step 0, of step 1.  In a step's products scores (Q rows)
+  // and dP (dO rows) take turns, in its sums dV (dO columns) and dK (Q columns).
+  auto read = [&](auto ec) {
+    constexpr int e = ec, u = e < kPart ? e / kProd : (e - kPart) / kSum, x = e < kPart ? e % kProd : (e - kPart) % kSum;
+    if constexpr (e < kPart) return row_operand(kUnit * (2 * u + (x & 1)), ad, x >> 1);
+    else return col_operand(kUnit * (2 * u + ((x & 1) ^ 1)), ad, (x >> 1) % kDB, x / (2 * kDB));
+  };
+  // bit c of a lane's mask: query tq + 8 hf + c sees its key.  Hidden weights are cleared in their packed words,
+  // whatever they are (rows of no sequence have any values): a branch around the steps that hide something took
+  // 70 of 385 us, as it parts the products from the weights beside them.
+  uint32_t seen[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int j = key0 + (lane & 31), t0 = tq[u] + 8 * hf;
+    const int end = u < live ? min(len - t0, j < a.sinks ? len - t0 : j - t0 + a.w) : 0;
+    seen[u] = ((1u << min(max(end, 0), 24)) - 1) & ~((1u << min(max(j - t0, 0), 24)) - 1);
   }
-#pragma unroll
-  for (int x = 0; x < kKS; ++x) s = mfma(row_operand<D>(tl, lo, x), kf[x], s);
-  if (DP) {
-#pragma unroll
-    for (int x = 0; x < kKS; ++x) dp = mfma(row_operand<D>(tl + TileOf<D>::kUnit, lo, x), vf[x], dp);
-    paced<kKS + 2, 2 * kKS, 1>();
-  }
-  __builtin_amdgcn_sched_barrier(0);
-}
-
-// One sum of products over the step's queries: acc += (tensor at `tl`)^T w, w rounded to bf16 already.
-template <int D>
-__device__ __forceinline__ void query_sums(uint32_t tl, const LaneOffsets& lo, const u32x4* w, f32x16* acc) {
-  constexpr int kDB = TileOf<D>::kDB;
-  u32x4 op[kFew];
-#pragma unroll
-  for (int e = 0; e < kFew; ++e) op[e] = col_operand<D>(tl, lo, e % kDB, e / kDB);
-#pragma unroll
-  for (int e = 0; e < 2 * kDB; ++e) {
+  // Weights P = exp(s - lse) and dS = P dP of step u, rounded to bf16, an element a slot: slot i scales element i,
+  // raises element i - 1 and multiplies element i - 2, which leaves each result a slot's time.  A slot's results
+  // are pinned to it: left alone the compiler forms all weights at once, ahead of the products or after them.
+  u32x4 pu[N][2], du[N][2];
+  float x[N][16], p[N][16], d[N][16];
+  auto weight_slot = [&](auto uc, auto ic) {
+    constexpr int u = uc, i = ic;
+    if constexpr (i < 16) x[u][i] = s[u][i] * a.scale_log2;
+    if constexpr (i >= 1 && i < 17) p[u][i - 1] = __builtin_amdgcn_exp2f(x[u][i - 1]);
+    if constexpr (i >= 2 && i < 18) d[u][i - 2] = p[u][i - 2] * dp[u][i - 2];
+    if constexpr (i < 16) asm volatile("" : "+v"(x[u][i]));
+    if constexpr (i >= 1 && i < 17) asm volatile("" : "+v"(p[u][i - 1]));
+    if constexpr (i >= 2 && i < 18) asm volatile("" : "+v"(d[u][i - 2]));
+    if constexpr (i >= 3 && (i & 1) && i < 18) {
+      constexpr int e = (i - 3) / 2;
+      const f32x2 pp = {p[u][2 * e], p[u][2 * e + 1]}, dd = {d[u][2 * e], d[u][2 * e + 1]};
+      uint32_t pw = __builtin_bit_cast(uint32_t, __builtin_convertvector(pp, bf16x2));
+      uint32_t dw = __builtin_bit_cast(uint32_t, __builtin_convertvector(dd, bf16x2));
+      constexpr int c = 16 * (e >> 2) + 2 * (e & 3);
+      const uint32_t lo = __builtin_amdgcn_sbfe(seen[u], c, 1), hi = __builtin_amdgcn_sbfe(seen[u], c + 1, 1);
+      const uint32_t m = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
+      pw &= m;
+      dw &= m;
+      asm volatile("" : "+v"(pw), "+v"(dw));
+      pu[u][e >> 2][e & 3] = pw;
+      du[u][e >> 2][e & 3] = dw;
+    }
+  };
+  u32x4 op[kDeep];
+  each<kDeep>([&](auto ec) { op[ec] = read(ec); });
+  each<kAll>([&](auto ec) {
+    constexpr int e = ec;
     __builtin_amdgcn_sched_barrier(0);
-    acc[e % kDB] = mfma(op[e % kFew], w[e / kDB], acc[e % kDB]);
-    if (e + kFew < 2 * kDB) op[e % kFew] = col_operand<D>(tl, lo, (e + kFew) % kDB, (e + kFew) / kDB);
-  }
+    if constexpr (N == 1 && e == kPart) {
+      each<18>([&](auto ic) { weight_slot(std::integral_constant<int, 0>{}, ic); });
+    }
+    if constexpr (e < kPart) {
+      constexpr int u = e / kProd, x = e % kProd;
+      if constexpr (x & 1) dp[u] = mfma(op[e % kDeep], vf[x >> 1], dp[u]);
+      else s[u] = mfma(op[e % kDeep], kf[x >> 1], s[u]);
+    } else {
+      constexpr int u = (e - kPart) / kSum, x = (e - kPart) % kSum, b = (x >> 1) % kDB, half = x / (2 * kDB);
+      if constexpr (x & 1) dka[b] = mfma(op[e % kDeep], du[u][half], dka[b]);
+      else dva[b] = mfma(op[e % kDeep], pu[u][half], dva[b]);
+    }
+    if constexpr (e + kDeep < kAll) op[e % kDeep] = read(std::integral_constant<int, e + kDeep>{});
+    // step 0's weights beside step 1's products, step 1's beside step 0's sums; the last slots of each come with
+    // the first products of the next part, which need the first elements only
+    if constexpr (N == 2 && e >= kProd) {
+      constexpr int part = e / kProd - 1, n = e % kProd, kEach = 16 / kProd;   // slots beside a product
+      if constexpr (part < 2)
+        each<kEach>([&](auto c) { weight_slot(std::integral_constant<int, part>{}, std::integral_constant<int, kEach * n + c>{}); });
+      if constexpr (part > 0 && part < 3 && n < 2)
+        weight_slot(std::integral_constant<int, part - 1>{}, std::integral_constant<int, 16 + n>{});
+    }
+  });
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -839,117 +959,63 @@ __device__ inline void store_sums(float* dst, const f32x16* o, int hf) {
           f32x4{o[x][4 * y], o[x][4 * y + 1], o[x][4 * y + 2], o[x][4 * y + 3]};
 }
 
-// Weights exp(s - lse) of a step's queries tq .. tq + 31 (register i of a lane: query tq + 16 (i / 8) + 8 hf
-// + i % 8) for the 32 keys from key0 on, 0 where a query does not see the key or is none.
-__device__ __forceinline__ void query_weights(const WindowArgs& a, f32x16& s, int tq, int key0, int len, int lane) {
-  if (tq + 31 < len && tq >= key0 + 31 && (tq + 31 < key0 + a.w || key0 + 32 <= a.sinks)) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * a.scale_log2);
-    return;
-  }
-  const int ln = fresh(lane);
-  const int j = key0 + (ln & 31), t0 = tq + 8 * (ln >> 5);
-  const int first = j - t0;                                                    // first query that sees the key
-  const int end = min(len - t0, j < a.sinks ? len - t0 : first + a.w);         // first one that does not
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int c = 16 * (i >> 3) + (i & 7);
-    s[i] = c >= first && c < end ? __builtin_amdgcn_exp2f(s[i] * a.scale_log2) : 0.f;
-  }
-}
-
-// Sums of one tile of sinks over the queries of [first, last).  The two steps of a stage go to two waves
-// each: one sums dV, the other dK.
 template <int D>
-__device__ __forceinline__ void far_queries(const WindowArgs& a, char* tile_lds, const float (*row_lds)[2][64], int s0,
-                                            int len, int h, int key0, int first, int last, int slot) {
+__global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void window_dkv_kernel(WindowArgs a) {
   using Tile = TileOf<D>;
+  using Steps = QuerySteps<D>;
   constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
-  const int lane = threadIdx.x & 63, hf = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t tiles = lds_addr(tile_lds);
-  QuerySteps<D> qs(a, s0, len, h, first, (last - first + 31) >> 5, wave, lane, tiles, lds_addr(row_lds));
-  LaneOffsets lo = lane_offsets<D>(lane, qs.stride);
-  qs.issue(0, lo);
-  const int j = key0 + (lane & 31);
-  const bool jok = j < len;
-  const size_t krow = (static_cast<size_t>(s0 + (jok ? j : 0)) * a.H + h) * D;
-  u32x4 kf[kKS], vf[kKS];
-#pragma unroll
-  for (int x = 0; x < kKS; ++x) {
-    kf[x] = jok ? ld16(a.k + krow + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
-    vf[x] = jok ? ld16(a.v + krow + 16 * x + 8 * hf) : u32x4{0u, 0u, 0u, 0u};
-  }
-  f32x16 acc[kDB];
-#pragma unroll
-  for (int x = 0; x < kDB; ++x)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[x][i] = 0.f;
-  const bool keys = wave >> 1;
-  const int nst = (qs.total + 1) >> 1;
-  int step = wave & 1;
-  for (int st = 0; st < nst; ++st, step += 2) {
-    wait_copies();
-    __syncthreads();
-    if (st + 1 < nst) qs.issue((st & 1) ^ 1, lo);
-    if (step >= qs.total) continue;
-    const uint32_t tl = tiles + (st & 1) * 4 * kUnit + 2 * kUnit * (wave & 1);
-    const float* rows = row_lds[st & 1][wave & 1];
-    f32x16 s, dp;
-    if (keys) query_products<D, true>(tl, rows, lo, kf, vf, hf, s, dp);
-    else query_products<D, false>(tl, rows, lo, kf, vf, hf, s, dp);
-    query_weights(a, s, first + 32 * (step / a.g), key0, len, lane);
-    float x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = keys ? s[i] * dp[i] : s[i];
-    const u32x4 w[2] = {pack_bf16(x), pack_bf16(x + 8)};
-    query_sums<D>(tl + (keys ? 0 : kUnit), lo, w, acc);
-  }
-  // even and odd steps' sums are added in LDS, whose tiles nothing reads any more
-  __syncthreads();
-  float* sum = reinterpret_cast<float*>(tile_lds) + (wave >> 1) * 32 * D + (lane & 31) * D;
-  if (wave & 1) store_sums<D>(sum, acc, hf);
-  __syncthreads();
-  if (wave & 1) return;
-#pragma unroll
-  for (int x = 0; x < kDB; ++x)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[x][i] += sum[32 * x + 8 * (i >> 2) + 4 * hf + (i & 3)];
-  store_sums<D>(part_of(a, false, slot, key0 >> 5, h, D) + (keys ? 0 : 32 * D) + (lane & 31) * D, acc, hf);
-}
-
-template <int D>
-__global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(WindowArgs a) {
-  using Tile = TileOf<D>;
-  constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
-  __shared__ __attribute__((aligned(256))) char tile_lds[2][4 * kUnit];                  // [Q tile | dO tile] x 2
-  __shared__ __attribute__((aligned(16))) float row_lds[2][2][64];                       // [step][row][-lse, -D]
+  __shared__ __attribute__((aligned(256))) char tile_lds[kStages * Steps::kBytes];
+  __shared__ __attribute__((aligned(16))) float row_lds[kStages][2][2][64];               // [step][-lse, -D][row]
   const int2 wg = xcd_order();
   const int h = wg.y;
-  // four key blocks (512 keys), then the far queries of as many positions, once per tile of sinks
-  const int group = wg.x / (4 + a.sink_tiles), in_group = wg.x % (4 + a.sink_tiles);
-  if (in_group >= 4) {
-    // positions 512 c .. (c >= 1) of the last sequence that starts before this 512 of the packed tokens
-    if (group == 0) return;
-    const Block f = block_of(a, group - 1, kFar, inverse(kFar), 0);
-    const int key0 = 32 * (in_group - 4);
-    const int first = max(f.p0 + kFar, far_begin(a, key0 & ~(kKeys - 1))), last = min(f.len, f.p0 + 2 * kFar);
-    if (first >= last || key0 >= f.len) return;
-    far_queries<D>(a, tile_lds[0], row_lds, f.s0, f.len, h, key0, first, last, group);
-    return;
-  }
-  const Block blk = block_of(a, 4 * group + in_group, kKeys, inverse(kKeys));
-  if (blk.p0 >= blk.len) return;
-  const int s0 = blk.s0, len = blk.len;
   const int lane = threadIdx.x & 63, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t tiles = lds_addr(tile_lds);
-  const int last = min(len, far_begin(a, blk.p0));
-  QuerySteps<D> qs(a, s0, len, h, blk.p0, (last - blk.p0 + 31) >> 5, wave, lane, tiles, lds_addr(row_lds));
-  LaneOffsets lo = lane_offsets<D>(lane, qs.stride);
-  qs.issue(0, lo);
+  const uint32_t tiles = lds_addr(tile_lds), rows = lds_addr(row_lds);
+  // the key blocks of `far` tokens, each in its shares, then the far queries of as many positions, once per
+  // tile of sinks
+  const int near = a.far / kKeys * a.splits;
+  const int group = wg.x / (near + a.sink_tiles), in_group = wg.x % (near + a.sink_tiles);
+  const bool far = in_group >= near;
+  int s0, len, key0, pos0, first = 0, total;   // sequence, this wave's keys, the steps' first position, this share of them
+  StepList list;
+  list.g = a.g;
+  list.start = 0;
+  if (far) {
+    // positions far c .. (c >= 1) of the last sequence that starts before this `far` of the packed tokens
+    if (group == 0) return;
+    const Block f = block_of(a, group - 1, a.far, a.inv_far, 0);
+    s0 = f.s0;
+    len = f.len;
+    key0 = 32 * (in_group - near);
+    pos0 = max(f.p0 + a.far, far_begin(a, key0 & ~(kKeys - 1)));
+    const int last = min(len, f.p0 + 2 * a.far);
+    if (pos0 >= last || key0 >= len) return;
+    list.tiles = (last - pos0 + 31) / 32;
+    total = list.tiles * a.g;
+  } else {
+    const Block b = block_of(a, a.far / kKeys * group + in_group / a.splits, kKeys, inverse(kKeys));
+    if (b.p0 >= b.len) return;
+    s0 = b.s0;
+    len = b.len;
+    key0 = b.p0 + 32 * wave;
+    pos0 = b.p0;
+    list.tiles = (min(len, far_begin(a, pos0)) - pos0 + 31) / 32;
+    const int see = (kKeys + a.w + 31) >> 5;   // tiles of a block inside the sequence
+    list.start = (see - (pos0 >> 5) % see) % see;
+    if (list.start >= list.tiles) list.start = 0;
+    const int64_t all = static_cast<int64_t>(list.tiles) * a.g;
+    const int split = in_group % a.splits;
+    first = static_cast<int>(all * split / a.splits);
+    total = static_cast<int>(all * (split + 1) / a.splits) - first;
+  }
+  list.pos0 = pos0;
+  Steps qs(a, s0, len, h, list, first, wave, lane, tiles, rows);
+  const LaneOffsets lo = lane_offsets<D>(lane, qs.stride);
+  const int stages = (total + 1) >> 1;
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i)
+    if (i < stages) qs.issue(i, lo);
 
-  const int key0 = blk.p0 + 32 * wave;       // this wave's keys
   const int j = key0 + (lane & 31);          // this lane's key
   const bool jok = j < len;
   const size_t krow = (static_cast<size_t>(s0 + (jok ? j : 0)) * a.H + h) * D;
@@ -964,60 +1030,92 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(WindowArgs a) {
   for (int x = 0; x < kDB; ++x)
 #pragma unroll
     for (int i = 0; i < 16; ++i) dka[x][i] = dva[x][i] = 0.f;
+  LaneAddresses<D> ad = lane_addresses<D>(tiles, lo);
+  auto move_to = [&](uint32_t by) {   // addresses of another stage, by bytes from this one
+#pragma unroll
+    for (int x = 0; x < kKS; ++x) ad.row[x] += by;
+#pragma unroll
+    for (int x = 0; x < kDB; ++x) {
+      ad.col[x][0] += by;
+      ad.col[x][1] += by;
+    }
+  };
 
-  const int nst = (qs.total + 1) >> 1;
-  int step_qh = 0, tq = blk.p0;
-  for (int st = 0; st < nst; ++st) {
+  StepList at = list, next = list;   // steps 2 st and 2 st + 1
+  at.seek(first);
+  next.seek(first + 1);
+  for (int st = 0; st < stages && !far; ++st) {
+    const int slot = st & (kStages - 1);
+    Steps::ready(min(stages - 1 - st, kStages - 2));
+    if (st + kStages - 1 < stages) qs.issue((slot + kStages - 1) & (kStages - 1), lo);
+    const int tq = at.pos(), tq1 = next.pos();
+    const bool seen = key0 < len;
+    const bool on0 = seen && tq + 31 >= key0 && (tq < key0 + 31 + a.w || key0 < a.sinks);
+    const bool on1 = seen && 2 * st + 1 < total && tq1 + 31 >= key0 && (tq1 < key0 + 31 + a.w || key0 < a.sinks);
+    if (on0 || on1)
+      key_steps<D, 2>(a, ad, rows + 1024 * slot, {tq, tq1}, min(2, total - 2 * st), key0, len, lane, kf, vf, dka, dva);
+    move_to(slot == kStages - 1 ? -(kStages - 1) * Steps::kBytes : Steps::kBytes);
+    at.skip(2);
+    next.skip(2);
+  }
+  // far: two stages at a time, a step for each wave
+  for (int st = 0; st < stages && far; st += 2) {
     wait_copies();
     __syncthreads();
-    if (st + 1 < nst) qs.issue((st & 1) ^ 1, lo);
-#pragma unroll 1
-    for (int sub = 0; sub < 2; ++sub) {
-      if (2 * st + sub >= qs.total) break;
-      if (tq + 31 >= key0 && (tq < key0 + 31 + a.w || key0 < a.sinks) && key0 < len) {
-        const uint32_t tl = tiles + (st & 1) * 4 * kUnit + 2 * kUnit * sub;
-        refresh(lo);
-        f32x16 s, dp;
-        query_products<D, true>(tl, row_lds[st & 1][sub], lo, kf, vf, hf, s, dp);
-        query_weights(a, s, tq, key0, len, lane);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) dp[i] *= s[i];
-        // dV^T += dO^T P, dK^T += Q^T dS with P, dS rounded to bf16
-        float p[16], ds[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          p[i] = s[i];
-          ds[i] = dp[i];
-        }
-        const u32x4 pu[2] = {pack_bf16(p), pack_bf16(p + 8)}, du[2] = {pack_bf16(ds), pack_bf16(ds + 8)};
-        // product e: dV (dO) and dK (Q) take turns, dim block (e / 2) % kDB, token half e / (2 kDB)
-        u32x4 op[kFew];
-        auto read = [&](int e) {
-          return col_operand<D>(tl + kUnit * ((e & 1) ^ 1), lo, (e >> 1) % kDB, e / (2 * kDB));
-        };
-#pragma unroll
-        for (int e = 0; e < kFew; ++e) op[e] = read(e);
-#pragma unroll
-        for (int e = 0; e < 4 * kDB; ++e) {
-          __builtin_amdgcn_sched_barrier(0);
-          const int x = (e >> 1) % kDB, y = e / (2 * kDB);
-          if (e & 1) dka[x] = mfma(op[e % kFew], du[y], dka[x]);
-          else dva[x] = mfma(op[e % kFew], pu[y], dva[x]);
-          if (e + kFew < 4 * kDB) op[e % kFew] = read(e + kFew);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if (++step_qh == a.g) {
-        step_qh = 0;
-        tq += 32;
-      }
+    if (st + 3 < stages) qs.issue((st + 3) & (kStages - 1), lo);
+    const int step = 2 * st + wave, slot = (st + (wave >> 1)) & (kStages - 1);
+    if (step < total) {
+      const int q = pos0 + 32 * (step / a.g);
+      move_to(slot * Steps::kBytes + 2 * kUnit * (wave & 1));
+      key_steps<D, 1>(a, ad, rows + 1024 * slot + 512 * (wave & 1), {q, q}, 1, key0, len, lane, kf, vf, dka, dva);
+      move_to(-(slot * Steps::kBytes + 2 * kUnit * (wave & 1)));
+    }
+    if (st + 4 < stages) {
+      __syncthreads();             // slot st is read by nobody any more
+      qs.issue((st + 4) & (kStages - 1), lo);
     }
   }
 
   const int je = key0 + (fresh(lane) & 31);
-  if (a.sink_tiles && key0 < a.sinks && far_begin(a, blk.p0) < len) {
-    // far queries follow: keys past the last sink of this tile are complete, their other sums are zeros
-    float* dst = part_of(a, true, s0 / kFar, key0 >> 5, h, D) + (je - key0) * D;
+  if (far) {
+    // the waves' sums are added in LDS, whose tiles nothing reads any more, two waves at a time
+    float* sum = reinterpret_cast<float*>(tile_lds) + (wave & 1) * 64 * D + (je - key0) * D;
+#pragma unroll 1
+    for (int round = 0; round < 2; ++round) {   // 3 -> 1 and 2 -> 0, then 1 -> 0
+      __syncthreads();
+      const bool give = round ? wave == 1 : wave >= 2, take = round ? wave == 0 : wave < 2;
+      if (give) {
+        float* to = round ? sum - 64 * D : sum;
+        store_sums<D>(to, dka, hf);
+        store_sums<D>(to + 32 * D, dva, hf);
+      }
+      __syncthreads();
+      if (take)
+#pragma unroll
+        for (int x = 0; x < kDB; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int e = 32 * x + 8 * (i >> 2) + 4 * hf + (i & 3);
+            dka[x][i] += sum[e];
+            dva[x][i] += sum[32 * D + e];
+          }
+    }
+    if (wave) return;
+    float* dst = far_sums(a, group, key0 >> 5, h, D) + (je - key0) * D;
+    store_sums<D>(dst, dka, hf);
+    store_sums<D>(dst + 32 * D, dva, hf);
+    return;
+  }
+  if (a.splits > 1) {   // others hold sums of these keys, too
+    if (je < len) {
+      float* dst = share_sums(a, in_group % a.splits, s0 + je, h, D);
+      store_sums<D>(dst, dka, hf);
+      store_sums<D>(dst + D, dva, hf);
+    }
+    return;
+  }
+  if (a.sink_tiles && key0 < a.sinks && far_begin(a, pos0) < len) {
+    float* dst = near_sums(a, divide(s0, a.far, a.inv_far), key0 >> 5, h, D) + (je - key0) * D;
     store_sums<D>(dst, dka, hf);
     store_sums<D>(dst + 32 * D, dva, hf);
     return;
@@ -1031,41 +1129,60 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(WindowArgs a) {
     exact_key<D>(a, s0, len, key0 + __builtin_ctz(cols), h);
 }
 
-// Keys of the sink tiles of one sequence with far queries, a wave each: the key blocks' sums and, in order
-// of position, those of the far queries.
+// Keys whose sums lie with several workgroups, a wave each: the shares of their block in order, then, for a
+// sink, the far queries in order of position.  Workgroup (x, head): keys 4 x .. of the packed tokens (splits > 1),
+// or of the sinks of the sequence that starts in a `far` of them.
 template <int D>
-__global__ __launch_bounds__(kThreads) void window_sinks_kernel(WindowArgs a) {
+__global__ __launch_bounds__(kThreads) void window_sum_kernel(WindowArgs a) {
   constexpr int E = D / 64;
-  const int slot = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 63;
-  const Block blk = block_of(a, slot, kFar, inverse(kFar), 0);       // the sequence that starts in this 512, if it is long
-  if (blk.p0 != 0) return;
-  for (int j = blockIdx.z * (kThreads / 64) + (threadIdx.x >> 6); j < min(32 * a.sink_tiles, blk.len);
-       j += gridDim.z * (kThreads / 64)) {
-    const int begin = far_begin(a, j & ~(kKeys - 1));
-    if (begin >= blk.len) continue;                     // stored by its block
-    const size_t in = static_cast<size_t>(j & 31) * D + E * lane;
-    float dk[E], dv[E];
-    auto add = [&](const float* p) {
+  const int h = blockIdx.y, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Block blk;
+  int j;                    // the wave's key
+  if (a.splits > 1) {
+    const int t = blockIdx.x * (kThreads / 64) + wave;
+    if (t >= a.T) return;
+    blk = block_of(a, t, 1, 0, 0);
+    j = t - blk.s0;
+  } else {
+    const int per = 8 * a.sink_tiles;   // workgroups of a sequence's sinks
+    blk = block_of(a, blockIdx.x / per, a.far, a.inv_far, 0);
+    if (blk.p0 != 0) return;
+    j = blockIdx.x % per * (kThreads / 64) + wave;
+  }
+  if (j < 0 || j >= blk.len) return;
+  const int begin = far_begin(a, j & ~(kKeys - 1));
+  const bool far = a.sink_tiles && (j & ~31) < a.sinks && begin < blk.len;   // the tile has far queries
+  if (a.splits == 1 && !far) return;                                         // stored by its block
+  float dk[E], dv[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        dk[e] += p[in + e];
-        dv[e] += p[in + 32 * D + e];
-      }
-    };
-#pragma unroll
-    for (int e = 0; e < E; ++e) dk[e] = dv[e] = 0.f;
-    add(part_of(a, true, slot, j >> 5, h, D));
-    for (int c = begin / kFar; c * kFar < blk.len; ++c) add(part_of(a, false, slot + c, j >> 5, h, D));
-    bool bad = false;
-    const size_t out = (static_cast<size_t>(blk.s0 + j) * a.H + h) * D + E * lane;
+  for (int e = 0; e < E; ++e) dk[e] = dv[e] = 0.f;
+  auto add = [&](const float* p, int to_v) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      bad |= not_finite(dk[e]) || not_finite(dv[e]);
-      a.dk[out + e] = static_cast<__bf16>(dk[e] * a.scale_log2 / kLog2e);
-      a.dv[out + e] = static_cast<__bf16>(dv[e]);
+      dk[e] += p[E * lane + e];
+      dv[e] += p[to_v + E * lane + e];
     }
-    if (__builtin_amdgcn_ballot_w64(bad)) exact_key<D>(a, blk.s0, blk.len, j, h);
+  };
+  const int slot = divide(blk.s0, a.far, a.inv_far);
+  if (a.splits == 1) add(near_sums(a, slot, j >> 5, h, D) + (j & 31) * D, 32 * D);
+  else
+#pragma unroll 4
+    for (int sp = 0; sp < a.splits; ++sp) add(share_sums(a, sp, blk.s0 + j, h, D), D);
+  if (far) {
+    const int end = divide(blk.len + a.far - 1, a.far, a.inv_far);
+#pragma unroll 4
+    for (int c = divide(begin, a.far, a.inv_far); c < end; ++c) add(far_sums(a, slot + c, j >> 5, h, D) + (j & 31) * D, 32 * D);
   }
+  bool bad = false;
+  const size_t out = (static_cast<size_t>(blk.s0 + j) * a.H + h) * D + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    bad |= not_finite(dk[e]) || not_finite(dv[e]);
+    a.dk[out + e] = static_cast<__bf16>(a.single ? 0.f : dk[e] * a.scale_log2 / kLog2e);
+    a.dv[out + e] = static_cast<__bf16>(dv[e]);
+  }
+  if (__builtin_amdgcn_ballot_w64(bad)) exact_key<D>(a, blk.s0, blk.len, j, h);
 }
 
 WindowArgs window_args(const dms_window_config& c, const int32_t* cu, const void* q, const void* k, const void* v) {
@@ -1089,21 +1206,29 @@ WindowArgs window_args(const dms_window_config& c, const int32_t* cu, const void
   return a;
 }
 
-// Row values of the queries, then the sinks' sums where a sequence can have far queries.
+// Row values of the queries, then sums that workgroups leave to others: shares of key blocks' steps and far
+// queries of sinks.
 struct WindowLayout {
-  size_t rows, part, bytes;
+  size_t nlse, nsum, part, far_part, bytes;
   int64_t Ts;
-  int sink_tiles;
+  int far, sink_tiles, splits;
 };
 WindowLayout window_layout(const dms_window_config& c) {
   WindowLayout l{};
-  l.Ts = static_cast<int64_t>(c.total_tokens) + 32;
+  const size_t T = c.total_tokens, H = c.num_kv_heads, D = c.head_dim;
+  l.Ts = static_cast<int64_t>(T) + 128;
+  const int64_t blocks = (static_cast<int64_t>(T) + kKeys - 1) / kKeys * c.num_kv_heads;
+  // fewer blocks than a quarter of the CUs' workgroups: shares of their steps, and shorter lists of far queries
+  l.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, kSplitTarget / std::max<int64_t>(1, blocks))));
+  l.far = blocks < kSplitTarget ? kKeys : 4 * kKeys;
+  const int sinks = std::min(c.sinks, c.max_seqlen);
+  l.sink_tiles = c.max_seqlen > l.far ? (sinks + 31) / 32 : 0;
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, kAlign); return o; };
-  l.rows = take(static_cast<size_t>(c.num_kv_heads) * c.group_size * l.Ts * 8);
-  const int sinks = std::min(c.sinks, c.max_seqlen);
-  l.sink_tiles = c.max_seqlen > kFar ? (sinks + 31) / 32 : 0;
-  l.part = take(static_cast<size_t>(2) * (c.total_tokens / kFar + 1) * l.sink_tiles * c.num_kv_heads * 64 * c.head_dim * 4);
+  l.nlse = take(H * c.group_size * l.Ts * 4);
+  l.nsum = take(H * c.group_size * l.Ts * 4);
+  l.part = take(l.splits > 1 ? l.splits * T * H * 2 * D * 4 : 0);
+  l.far_part = take((l.splits > 1 ? 1 : 2) * (T / l.far + 1) * l.sink_tiles * H * 64 * D * 4);
   l.bytes = off;
   return l;
 }
@@ -1116,10 +1241,13 @@ void launch_backward(const WindowArgs& a, bool exact, hipStream_t st) {
   const dim3 gq(a.T / a.PB + a.n, a.H);
   if (exact) hipLaunchKernelGGL((window_dq_kernel<D, true>), gq, dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL((window_dq_kernel<D, false>), gq, dim3(kThreads), 0, st, a);
-  const int groups = (a.T / kKeys + a.n + 3) / 4;
-  hipLaunchKernelGGL(window_dkv_kernel<D>, dim3(groups * (4 + a.sink_tiles), a.H), dim3(kThreads), 0, st, a);
-  if (a.sink_tiles)
-    hipLaunchKernelGGL(window_sinks_kernel<D>, dim3(a.T / kFar + 1, a.H, std::min(8 * a.sink_tiles, 64)), dim3(kThreads), 0, st, a);
+  const int per = a.far / kKeys;
+  const int groups = (a.T / kKeys + a.n + per - 1) / per;
+  hipLaunchKernelGGL(window_dkv_kernel<D>, dim3(groups * (per * a.splits + a.sink_tiles), a.H), dim3(kThreads), 0, st, a);
+  if (a.splits > 1)
+    hipLaunchKernelGGL(window_sum_kernel<D>, dim3((a.T + 3) / 4, a.H), dim3(kThreads), 0, st, a);
+  else if (a.sink_tiles)
+    hipLaunchKernelGGL(window_sum_kernel<D>, dim3((a.T / a.far + 1) * 8 * a.sink_tiles, a.H), dim3(kThreads), 0, st, a);
 }
 
 }  // namespace
@@ -1142,10 +1270,16 @@ hipError_t launch_window_bwd(const dms_window_config& c, const int32_t* cu, cons
                              void* dk, void* dv, void* ws, hipStream_t st) {
   WindowArgs a = window_args(c, cu, q, k, v);
   const WindowLayout l = window_layout(c);
-  a.rows = reinterpret_cast<f32x2*>(static_cast<char*>(ws) + l.rows);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + l.part);
+  char* w = static_cast<char*>(ws);
+  a.nlse = reinterpret_cast<float*>(w + l.nlse);
+  a.nsum = reinterpret_cast<float*>(w + l.nsum);
+  a.part = reinterpret_cast<float*>(w + l.part);
+  a.far_part = reinterpret_cast<float*>(w + l.far_part);
   a.Ts = l.Ts;
+  a.far = l.far;
+  a.inv_far = inverse(l.far);
   a.sink_tiles = l.sink_tiles;
+  a.splits = l.splits;
   a.o = static_cast<const __bf16*>(out);
   a.lse = lse;
   a.dout = static_cast<const __bf16*>(dout);
