@@ -349,15 +349,6 @@ __device__ inline void step_ready(int left) {
   __syncthreads();
 }
 
-// f(0), .. f(N - 1), each a constant.
-template <int N, int I = 0, typename F>
-__device__ __forceinline__ void each(F f) {
-  if constexpr (I < N) {
-    f(std::integral_constant<int, I>{});
-    each<N, I + 1>(f);
-  }
-}
-
 // f(step, slot) for steps 0 .. n - 1, the slot a constant.
 template <int SLOTS, typename F>
 __device__ __forceinline__ void over_steps(int n, F f) {
@@ -704,12 +695,12 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
 // K and V operands in registers, and walks the query tiles (32 positions) that
 // see the block, every head of the group: dV^T += dO^T P, dK^T += Q^T dS with
 // P, dS [query, key] from S = Q K^T, dP = dO V^T.
-// Two steps (tile, head) go through the matrix core together: the weights of
-// one are formed beside the other's products, and operands are read kDeep
-// products ahead.  That takes the registers of one wave per SIMD at d = 128.
-// With two waves of 256 registers, each step by itself and operands two ahead,
-// the pass ran 330 us against NEW us (16384 tokens of 8 x 5 heads, w = 256, 4
-// sinks).
+// At d = 128 sums, operands and one step's scores fill the 256 registers of two
+// waves per SIMD, so that a wave takes one step at a time, with operands read two
+// ahead: while one wave forms weights the other has the matrix core.  One wave of
+// 512 registers that takes two steps together, operands read six ahead, ran
+// 400 us against 300 (16384 tokens of 8 x 5 heads, w = 256, 4 sinks); three and
+// four ahead spill in this form (+80 us).
 // A sink is seen by every later query.  A block that holds sinks walks on to
 // position `far`; what lies further is shared out to workgroups of `far`
 // positions, whose waves take the steps in turn.
@@ -720,8 +711,8 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
 constexpr int kKeys = 128;
 constexpr int kSplitTarget = 256;   // key blocks below which their steps are split
 constexpr int kMaxSplits = 8;
-constexpr int kStages = 4;     // pairs of steps in LDS
-constexpr int kDeep = 6;       // operands are read this many products ahead
+constexpr int kStages = 2;     // pairs of steps in LDS
+constexpr int kDeep = 2;        // operands are read this many products ahead
 
 // First position (a multiple of 32) that the block of keys from j0 on leaves to others.
 __device__ inline int far_begin(const WindowArgs& a, int j0) {
@@ -813,7 +804,6 @@ template <int D>
 struct QuerySteps {
   static constexpr int kUnit = TileOf<D>::kUnit;
   static constexpr int kBytes = 4 * kUnit;             // tiles of a stage
-  static constexpr int kCopies = TileOf<D>::kUnit / 1024 + 1;   // copies of a stage by one wave
   const char* src;        // this wave's tensor (queries or output gradients): first head, first token
   const float* rows;      // this wave's row values
   int64_t head_step;
@@ -839,112 +829,81 @@ struct QuerySteps {
     lds_copy4(rows + ld.qh * head_step + ld.pos(), 4 * fresh(lane), row_lds + 1024 * stage + 512 * (wave & 1) + 256 * (wave >> 1));
     ld.skip(2);
   }
-  // stages 0 .. 2 are issued ahead; `left` stages follow this one
-  __device__ static void ready(int left) {
-    if (left >= 2) wait_copies_but<2 * kCopies>();
-    else if (left == 1) wait_copies_but<kCopies>();
-    else wait_copies();
-    __syncthreads();
-  }
 };
 
-// N = 1 or 2 steps, the first `live` of which count, for one wave's 32 keys from key0 on: their tiles by `ad`,
-// their row values from LDS address `rows` on, step u's queries from position tq[u] on.
-template <int D, int N>
-__device__ __forceinline__ void key_steps(const WindowArgs& a, const LaneAddresses<D>& ad, uint32_t rows,
-                                          const int (&tq)[2], int live, int key0, int len, int lane,
-                                          const u32x4* kf, const u32x4* vf, f32x16* dka, f32x16* dva) {
+// One step for one wave's 32 keys from key0 on: its tiles from LDS address `tl` on, its rows' values from `rows`
+// on, its queries from position tq on.
+template <int D>
+__device__ __forceinline__ void key_step(const WindowArgs& a, LaneOffsets lo, uint32_t tl, uint32_t rows, int tq,
+                                         int key0, int len, int lane, const u32x4* kf, const u32x4* vf, f32x16* dka,
+                                         f32x16* dva) {
   constexpr int kUnit = TileOf<D>::kUnit, kKS = TileOf<D>::kKS, kDB = TileOf<D>::kDB;
-  constexpr int kProd = 2 * kKS, kSum = 4 * kDB, kPart = N * kProd, kAll = N * (kProd + kSum);
-  static_assert(kProd == kSum, "a step's products and sums take as many operands");
   const int hf = lane >> 5;
-  f32x16 s[N], dp[N];
+  f32x16 s, dp;
   // -lse and -D of the rows start the products: register i of a lane is query tq + 16 (i / 8) + 8 hf + i % 8
 #pragma unroll
-  for (int u = 0; u < N; ++u)
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t r = rows + 32 * hf + 4 * (16 * (i >> 1) + 4 * (i & 1));
+    const f32x4 l = *reinterpret_cast<DMS_LDS const f32x4*>(r), d = *reinterpret_cast<DMS_LDS const f32x4*>(r + 256);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t r = rows + 32 * hf + 512 * u + 4 * (16 * (i >> 1) + 4 * (i & 1));
-      const f32x4 l = *reinterpret_cast<DMS_LDS const f32x4*>(r), d = *reinterpret_cast<DMS_LDS const f32x4*>(r + 256);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[u][4 * i + e] = l[e];
-        dp[u][4 * i + e] = d[e];
-      }
+    for (int e = 0; e < 4; ++e) {
+      s[4 * i + e] = l[e];
+      dp[4 * i + e] = d[e];
     }
-  // operand e: products of step 0, of step 1, sums of step 0, of step 1.  In a step's products scores (Q rows)
-  // and dP (dO rows) take turns, in its sums dV (dO columns) and dK (Q columns).
-  auto read = [&](auto ec) {
-    constexpr int e = ec, u = e < kPart ? e / kProd : (e - kPart) / kSum, x = e < kPart ? e % kProd : (e - kPart) % kSum;
-    if constexpr (e < kPart) return row_operand(kUnit * (2 * u + (x & 1)), ad, x >> 1);
-    else return col_operand(kUnit * (2 * u + ((x & 1) ^ 1)), ad, (x >> 1) % kDB, x / (2 * kDB));
-  };
-  // bit c of a lane's mask: query tq + 8 hf + c sees its key.  Hidden weights are cleared in their packed words,
-  // whatever they are (rows of no sequence have any values): a branch around the steps that hide something took
-  // 70 of 385 us, as it parts the products from the weights beside them.
-  uint32_t seen[N];
-#pragma unroll
-  for (int u = 0; u < N; ++u) {
-    const int j = key0 + (lane & 31), t0 = tq[u] + 8 * hf;
-    const int end = u < live ? min(len - t0, j < a.sinks ? len - t0 : j - t0 + a.w) : 0;
-    seen[u] = ((1u << min(max(end, 0), 24)) - 1) & ~((1u << min(max(j - t0, 0), 24)) - 1);
   }
-  // Weights P = exp(s - lse) and dS = P dP of step u, rounded to bf16, an element a slot: slot i scales element i,
-  // raises element i - 1 and multiplies element i - 2, which leaves each result a slot's time.  A slot's results
-  // are pinned to it: left alone the compiler forms all weights at once, ahead of the products or after them.
-  u32x4 pu[N][2], du[N][2];
-  float x[N][16], p[N][16], d[N][16];
-  auto weight_slot = [&](auto uc, auto ic) {
-    constexpr int u = uc, i = ic;
-    if constexpr (i < 16) x[u][i] = s[u][i] * a.scale_log2;
-    if constexpr (i >= 1 && i < 17) p[u][i - 1] = __builtin_amdgcn_exp2f(x[u][i - 1]);
-    if constexpr (i >= 2 && i < 18) d[u][i - 2] = p[u][i - 2] * dp[u][i - 2];
-    if constexpr (i < 16) asm volatile("" : "+v"(x[u][i]));
-    if constexpr (i >= 1 && i < 17) asm volatile("" : "+v"(p[u][i - 1]));
-    if constexpr (i >= 2 && i < 18) asm volatile("" : "+v"(d[u][i - 2]));
-    if constexpr (i >= 3 && (i & 1) && i < 18) {
-      constexpr int e = (i - 3) / 2;
-      const f32x2 pp = {p[u][2 * e], p[u][2 * e + 1]}, dd = {d[u][2 * e], d[u][2 * e + 1]};
-      uint32_t pw = __builtin_bit_cast(uint32_t, __builtin_convertvector(pp, bf16x2));
-      uint32_t dw = __builtin_bit_cast(uint32_t, __builtin_convertvector(dd, bf16x2));
-      constexpr int c = 16 * (e >> 2) + 2 * (e & 3);
-      const uint32_t lo = __builtin_amdgcn_sbfe(seen[u], c, 1), hi = __builtin_amdgcn_sbfe(seen[u], c + 1, 1);
-      const uint32_t m = (lo & 0xFFFFu) | (hi & 0xFFFF0000u);
-      pw &= m;
-      dw &= m;
-      asm volatile("" : "+v"(pw), "+v"(dw));
-      pu[u][e >> 2][e & 3] = pw;
-      du[u][e >> 2][e & 3] = dw;
-    }
+  // addresses are formed here, by an exclusive or each: held ahead of the loop they do not fit the registers
+  refresh(lo);
+  const uint32_t row0 = tl + lo.row, col0 = tl + lo.col;
+  // product e: scores (Q rows) and dP (dO rows) take turns
+  auto read_row = [&](int e) {
+    return *reinterpret_cast<DMS_LDS const u32x4*>((row0 ^ (32 * (e >> 1))) + (e & 1) * kUnit);
   };
+  constexpr int kProd = 2 * kKS, kSum = 4 * kDB;
   u32x4 op[kDeep];
-  each<kDeep>([&](auto ec) { op[ec] = read(ec); });
-  each<kAll>([&](auto ec) {
-    constexpr int e = ec;
+#pragma unroll
+  for (int e = 0; e < kDeep; ++e) op[e] = read_row(e);
+#pragma unroll
+  for (int e = 0; e < kProd; ++e) {
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (N == 1 && e == kPart) {
-      each<18>([&](auto ic) { weight_slot(std::integral_constant<int, 0>{}, ic); });
-    }
-    if constexpr (e < kPart) {
-      constexpr int u = e / kProd, x = e % kProd;
-      if constexpr (x & 1) dp[u] = mfma(op[e % kDeep], vf[x >> 1], dp[u]);
-      else s[u] = mfma(op[e % kDeep], kf[x >> 1], s[u]);
-    } else {
-      constexpr int u = (e - kPart) / kSum, x = (e - kPart) % kSum, b = (x >> 1) % kDB, half = x / (2 * kDB);
-      if constexpr (x & 1) dka[b] = mfma(op[e % kDeep], du[u][half], dka[b]);
-      else dva[b] = mfma(op[e % kDeep], pu[u][half], dva[b]);
-    }
-    if constexpr (e + kDeep < kAll) op[e % kDeep] = read(std::integral_constant<int, e + kDeep>{});
-    // step 0's weights beside step 1's products, step 1's beside step 0's sums; the last slots of each come with
-    // the first products of the next part, which need the first elements only
-    if constexpr (N == 2 && e >= kProd) {
-      constexpr int part = e / kProd - 1, n = e % kProd, kEach = 16 / kProd;   // slots beside a product
-      if constexpr (part < 2)
-        each<kEach>([&](auto c) { weight_slot(std::integral_constant<int, part>{}, std::integral_constant<int, kEach * n + c>{}); });
-      if constexpr (part > 0 && part < 3 && n < 2)
-        weight_slot(std::integral_constant<int, part - 1>{}, std::integral_constant<int, 16 + n>{});
-    }
-  });
+    if (e & 1) dp = mfma(op[e % kDeep], vf[e >> 1], dp);
+    else s = mfma(op[e % kDeep], kf[e >> 1], s);
+    if (e + kDeep < kProd) op[e % kDeep] = read_row(e + kDeep);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  // sum e: dV (dO columns) and dK (Q columns) take turns
+  auto read_col = [&](int e) {
+    const int x = e >> 1;   // dim block x % kDB, query half x / kDB
+    const uint32_t at = (col0 ^ (64 * (x % kDB))) + (e & 1 ? 0 : kUnit) + 16 * (x / kDB) * TileOf<D>::kRowB;
+    const uint32_t at4 = (col0 ^ (64 * (x % kDB)) ^ 16) + (e & 1 ? 0 : kUnit) + (16 * (x / kDB) + 4) * TileOf<D>::kRowB;
+    const u32x2 l = tr_read16(at), h = tr_read16(at4);
+    return u32x4{l[0], l[1], h[0], h[1]};
+  };
+#pragma unroll
+  for (int e = 0; e < kDeep; ++e) op[e] = read_col(e);
+  // bit c of a lane's mask: query tq + 8 hf + c sees its key.  Hidden weights are cleared in their packed words,
+  // whatever they are (rows of no sequence have any values).
+  const int j = key0 + (lane & 31), t0 = tq + 8 * hf;
+  const int end = min(len - t0, j < a.sinks ? len - t0 : j - t0 + a.w);
+  const uint32_t seen = ((1u << min(max(end, 0), 24)) - 1) & ~((1u << min(max(j - t0, 0), 24)) - 1);
+  u32x4 pu[2], du[2];   // P = exp(s - lse) and dS = P dP, rounded to bf16
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const f32x2 p = {__builtin_amdgcn_exp2f(s[2 * e] * a.scale_log2), __builtin_amdgcn_exp2f(s[2 * e + 1] * a.scale_log2)};
+    const int c = 16 * (e >> 2) + 2 * (e & 3);
+    const uint32_t lo_m = __builtin_amdgcn_sbfe(seen, c, 1), hi_m = __builtin_amdgcn_sbfe(seen, c + 1, 1);
+    const uint32_t m = (lo_m & 0xFFFFu) | (hi_m & 0xFFFF0000u);
+    pu[e >> 2][e & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2)) & m;
+    const f32x2 d = {p[0] * dp[2 * e], p[1] * dp[2 * e + 1]};
+    du[e >> 2][e & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(d, bf16x2)) & m;
+  }
+#pragma unroll
+  for (int e = 0; e < kSum; ++e) {
+    __builtin_amdgcn_sched_barrier(0);
+    const int x = e >> 1, b = x % kDB, half = x / kDB;
+    if (e & 1) dka[b] = mfma(op[e % kDeep], du[half], dka[b]);
+    else dva[b] = mfma(op[e % kDeep], pu[half], dva[b]);
+    if (e + kDeep < kSum) op[e % kDeep] = read_col(e + kDeep);
+  }
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -960,7 +919,7 @@ __device__ inline void store_sums(float* dst, const f32x16* o, int hf) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void window_dkv_kernel(WindowArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(WindowArgs a) {
   using Tile = TileOf<D>;
   using Steps = QuerySteps<D>;
   constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
@@ -1012,9 +971,7 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void window_dkv_kernel(
   Steps qs(a, s0, len, h, list, first, wave, lane, tiles, rows);
   const LaneOffsets lo = lane_offsets<D>(lane, qs.stride);
   const int stages = (total + 1) >> 1;
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i)
-    if (i < stages) qs.issue(i, lo);
+  qs.issue(0, lo);
 
   const int j = key0 + (lane & 31);          // this lane's key
   const bool jok = j < len;
@@ -1030,80 +987,39 @@ __global__ __launch_bounds__(kThreads, D == 128 ? 1 : 2) void window_dkv_kernel(
   for (int x = 0; x < kDB; ++x)
 #pragma unroll
     for (int i = 0; i < 16; ++i) dka[x][i] = dva[x][i] = 0.f;
-  LaneAddresses<D> ad = lane_addresses<D>(tiles, lo);
-  auto move_to = [&](uint32_t by) {   // addresses of another stage, by bytes from this one
-#pragma unroll
-    for (int x = 0; x < kKS; ++x) ad.row[x] += by;
-#pragma unroll
-    for (int x = 0; x < kDB; ++x) {
-      ad.col[x][0] += by;
-      ad.col[x][1] += by;
-    }
-  };
-
-  StepList at = list, next = list;   // steps 2 st and 2 st + 1
+  StepList at = list;       // steps 2 st and 2 st + 1, one after the other
   at.seek(first);
-  next.seek(first + 1);
-  for (int st = 0; st < stages && !far; ++st) {
-    const int slot = st & (kStages - 1);
-    Steps::ready(min(stages - 1 - st, kStages - 2));
-    if (st + kStages - 1 < stages) qs.issue((slot + kStages - 1) & (kStages - 1), lo);
-    const int tq = at.pos(), tq1 = next.pos();
-    const bool seen = key0 < len;
-    const bool on0 = seen && tq + 31 >= key0 && (tq < key0 + 31 + a.w || key0 < a.sinks);
-    const bool on1 = seen && 2 * st + 1 < total && tq1 + 31 >= key0 && (tq1 < key0 + 31 + a.w || key0 < a.sinks);
-    if (on0 || on1)
-      key_steps<D, 2>(a, ad, rows + 1024 * slot, {tq, tq1}, min(2, total - 2 * st), key0, len, lane, kf, vf, dka, dva);
-    move_to(slot == kStages - 1 ? -(kStages - 1) * Steps::kBytes : Steps::kBytes);
-    at.skip(2);
-    next.skip(2);
-  }
-  // far: two stages at a time, a step for each wave
-  for (int st = 0; st < stages && far; st += 2) {
+  for (int st = 0; st < stages; ++st) {
     wait_copies();
     __syncthreads();
-    if (st + 3 < stages) qs.issue((st + 3) & (kStages - 1), lo);
-    const int step = 2 * st + wave, slot = (st + (wave >> 1)) & (kStages - 1);
-    if (step < total) {
-      const int q = pos0 + 32 * (step / a.g);
-      move_to(slot * Steps::kBytes + 2 * kUnit * (wave & 1));
-      key_steps<D, 1>(a, ad, rows + 1024 * slot + 512 * (wave & 1), {q, q}, 1, key0, len, lane, kf, vf, dka, dva);
-      move_to(-(slot * Steps::kBytes + 2 * kUnit * (wave & 1)));
-    }
-    if (st + 4 < stages) {
-      __syncthreads();             // slot st is read by nobody any more
-      qs.issue((st + 4) & (kStages - 1), lo);
+    if (st + 1 < stages) qs.issue((st & 1) ^ 1, lo);
+#pragma unroll 1
+    for (int sub = 0; sub < 2; ++sub) {
+      const int tq = at.pos();
+      const uint32_t t = tiles + (st & 1) * Steps::kBytes + 2 * kUnit * sub, r = rows + 1024 * (st & 1) + 512 * sub;
+      const bool seen = tq + 31 >= key0 && (tq < key0 + 31 + a.w || key0 < a.sinks) && key0 < len && 2 * st + sub < total;
+      if (seen && (!far || wave == ((2 * st + sub) & 3)))
+        key_step<D>(a, lo, t, r, tq, key0, len, lane, kf, vf, dka, dva);
+      at.skip(1);
     }
   }
 
   const int je = key0 + (fresh(lane) & 31);
   if (far) {
-    // the waves' sums are added in LDS, whose tiles nothing reads any more, two waves at a time
-    float* sum = reinterpret_cast<float*>(tile_lds) + (wave & 1) * 64 * D + (je - key0) * D;
-#pragma unroll 1
-    for (int round = 0; round < 2; ++round) {   // 3 -> 1 and 2 -> 0, then 1 -> 0
+    // the waves took a step in four each: the four sums of a value meet in LDS, whose tiles nothing reads any more
+    float* sum = reinterpret_cast<float*>(tile_lds);
+    float* dst = far_sums(a, group, key0 >> 5, h, D);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
       __syncthreads();
-      const bool give = round ? wave == 1 : wave >= 2, take = round ? wave == 0 : wave < 2;
-      if (give) {
-        float* to = round ? sum - 64 * D : sum;
-        store_sums<D>(to, dka, hf);
-        store_sums<D>(to + 32 * D, dva, hf);
+      store_sums<D>(sum + (32 * wave + je - key0) * D, x ? dva : dka, hf);
+      __syncthreads();
+      for (int i = 4 * threadIdx.x; i < 32 * D; i += 4 * kThreads) {
+        f32x4 all = *reinterpret_cast<const f32x4*>(sum + i);
+        for (int n = 1; n < kThreads / 64; ++n) all += *reinterpret_cast<const f32x4*>(sum + 32 * D * n + i);
+        *reinterpret_cast<f32x4*>(dst + 32 * D * x + i) = all;
       }
-      __syncthreads();
-      if (take)
-#pragma unroll
-        for (int x = 0; x < kDB; ++x)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int e = 32 * x + 8 * (i >> 2) + 4 * hf + (i & 3);
-            dka[x][i] += sum[e];
-            dva[x][i] += sum[32 * D + e];
-          }
     }
-    if (wave) return;
-    float* dst = far_sums(a, group, key0 >> 5, h, D) + (je - key0) * D;
-    store_sums<D>(dst, dka, hf);
-    store_sums<D>(dst + 32 * D, dva, hf);
     return;
   }
   if (a.splits > 1) {   // others hold sums of these keys, too
