@@ -102,6 +102,44 @@ def test_forward_and_backward(lens, H, g, d, w, sinks):
     _check(x, lens, H, g, d, w, sinks, _gpu(x, lens, H, g, d, w, sinks))
 
 
+@pytest.mark.parametrize("lens, H, g, d, w, sinks", [
+    ([1100], 29, 1, 64, 20, 3), ([700, 1, 0, 430], 29, 1, 128, 300, 37), ([1300], 26, 2, 64, 1200, 140),
+    ([640, 600], 28, 1, 128, 1, 5),
+])
+def test_blocks_enough_to_fill_the_chip(lens, H, g, d, w, sinks):
+    """256 blocks of 128 keys over the heads and more: no block's steps are shared out, sinks' far queries lie in
+    longer pieces, and the near sums of sinks wait for them."""
+    assert -(-sum(lens) // 128) * H >= 256
+    x = _inputs(sum(lens), H, g, d, 12, 2.0)
+    _check(x, lens, H, g, d, w, sinks, _gpu(x, lens, H, g, d, w, sinks))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_hidden_values_with_blocks_enough_to_fill_the_chip(bad):
+    lens, H, g, d, w, sinks, T = [1100], 29, 1, 64, 20, 3, 1100
+    x = _inputs(T, H, g, d, 13)
+    ref, slack = _reference(x, lens, H, g, d, w, sinks)
+    word, at = _bf16(np.array([bad]))[0], 800
+    y = {n: b.copy() for n, b in x.items()}
+    y["k"][at], y["v"][at] = word, word
+    got = _gpu(y, lens, H, g, d, w, sinks)
+    rows = np.ones(T, bool)             # queries that do not see key `at`
+    rows[at:at + w] = False
+    keys = np.ones(T, bool)             # keys that none of the others' gradients come from
+    keys[at - w + 1:at + w] = False
+    keys[:sinks] = False
+    for n, where in (("out", rows), ("dq", rows), ("dk", keys), ("dv", keys)):
+        assert (np.abs(got[n][where] - ref[n][where]) <= slack[n][where]).all(), n
+    y = {n: b.copy() for n, b in x.items()}
+    y["q"][at], y["dout"][at] = word, word
+    got = _gpu(y, lens, H, g, d, w, sinks)
+    keys = np.ones(T, bool)
+    keys[at - w + 1:at + 1] = False
+    keys[:sinks] = False
+    for n in ("dk", "dv"):
+        assert (np.abs(got[n][keys] - ref[n][keys]) <= slack[n][keys]).all(), n
+
+
 def test_rows_past_the_last_sequence_and_a_longer_bound():
     """cu[n] below the tensors' rows, max_seqlen above the longest sequence."""
     x = _inputs(230, 2, 3, 128, 5)
