@@ -540,7 +540,7 @@ typedef struct dms_rope_config {
   float factor;           /* <= 0 selects 1 */
 } dms_rope_config;
 
-/* Rotate `tokens` tokens.  q_dev [tokens][Hq][d] and k_dev [tokens][Hkv][d] (in_type)
+/* Rotate `tokens` tokens (fewer than 2^26, and 2^38 elements).  q_dev [tokens][Hq][d] and k_dev [tokens][Hkv][d] (in_type)
  * have q_stride / k_stride elements from a token to the next (>= Hq d / Hkv d: they
  * may be parts of the rows of one projection); q_out_dev, k_out_dev (out_type) are
  * dense.  Either of q and k may be NULL together with its output.
@@ -589,13 +589,14 @@ int dms_rope_bwd(const dms_rope_config* cfg, int tokens, const void* dq_dev, con
  */
 typedef struct dms_window_config {
   int32_t num_seqs;       /* n >= 1, at most 65535 */
-  int32_t total_tokens;   /* rows of the tensors, >= 0 */
+  int32_t total_tokens;   /* rows of the tensors, >= 0; total_tokens Hq < 2^31 */
   int32_t max_seqlen;     /* longest sequence, 0 .. total_tokens */
-  int32_t num_kv_heads;   /* Hkv >= 1 */
+  int32_t num_kv_heads;   /* Hkv: 1 .. 4096 */
   int32_t group_size;     /* g = Hq / Hkv, 1 .. 16 */
   int32_t head_dim;       /* d: 64 or 128 */
   int32_t window;         /* w >= 1 */
-  int32_t sinks;          /* first tokens that stay visible, >= 0 */
+  int32_t sinks;          /* first tokens that stay visible, >= 0 (past max_seqlen: full attention);
+                             total_tokens / 512 * min(sinks, max_seqlen) / 4 < 2^24 */
   float softmax_scale;    /* <= 0 selects 1 / sqrt(head_dim) */
 } dms_window_config;
 

@@ -822,8 +822,8 @@ static int check_rope_call(const dms_rope_config* c, int tokens, const dms::Rope
   if (tokens < 0) return DMS_ERR_INVALID;
   const int64_t kv = static_cast<int64_t>(c->num_kv_heads) * c->head_dim, qr = kv * c->group_size;
   if (t.q_stride < qr || t.k_stride < kv || t.q_out_stride < qr || t.k_out_stride < kv) return DMS_ERR_INVALID;
-  // one thread per pair and a grid of fewer than 2^31 workgroups
-  if (tokens * (qr + kv) >= int64_t(1) << 38) return DMS_ERR_UNSUPPORTED;
+  // a wave per token and a grid of fewer than 2^32 threads
+  if (tokens >= 1 << 26 || tokens * (qr + kv) >= int64_t(1) << 38) return DMS_ERR_UNSUPPORTED;
   if (tokens == 0) return DMS_OK;
   if (!t.q != !t.q_out || !t.k != !t.k_out || (!t.q && !t.k) || !positions || !inv_freq) return DMS_ERR_INVALID;
   return DMS_OK;
@@ -874,6 +874,7 @@ static int validate_window_config(const dms_window_config* c) {
   // rows of the query tensors; a grid row per KV head; a token's bytes in 32 bits
   const int64_t heads = static_cast<int64_t>(c->num_kv_heads) * c->group_size;
   if (c->num_kv_heads > 4096 || heads * c->total_tokens >= int64_t(1) << 31) return DMS_ERR_UNSUPPORTED;
+  if (!dms::window_grids_fit(*c)) return DMS_ERR_UNSUPPORTED;
   return DMS_OK;
 }
 

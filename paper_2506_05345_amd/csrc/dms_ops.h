@@ -26,6 +26,7 @@ hipError_t launch_rope(const dms_rope_config& c, int tokens, const RopeTensors& 
                        const float* dlogits, hipStream_t st);
 
 size_t window_workspace_bytes(const dms_window_config& c);
+bool window_grids_fit(const dms_window_config& c);   // of a configuration that is otherwise valid
 hipError_t launch_window_fwd(const dms_window_config& c, const int32_t* cu, const void* q, const void* k,
                              const void* v, void* out, float* lse, void* ws, hipStream_t st);
 hipError_t launch_window_bwd(const dms_window_config& c, const int32_t* cu, const void* q, const void* k,

@@ -75,38 +75,43 @@ __device__ inline float neuron_gradient(const RopeArgs& a, int t, int h) {
   return a.dlogits ? a.dlogits[static_cast<size_t>(t) * a.H + h] : 0.f;
 }
 
-// Any shape, stride and alignment: a thread per pair or copied element of a head.
+// Any shape, stride and alignment: a thread per pair or copied element of a head, and the next kMaxBlocks blocks
+// further on again (a grid holds fewer than 2^32 threads).
+constexpr int kMaxBlocks = 65536;
+
 template <typename TI, typename TO>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
   const int units = a.rot / 2 + a.d - a.rot;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
   const int row = (a.t.q ? a.Hq : 0) + (a.t.k ? a.H : 0);
-  if (i >= static_cast<int64_t>(a.T) * row * units) return;
-  const int u = static_cast<int>(i % units);
-  const int64_t th = i / units;
-  const int t = static_cast<int>(th / row);
-  int h = static_cast<int>(th % row);
-  const bool isq = a.t.q && h < a.Hq;
-  if (!isq && a.t.q) h -= a.Hq;
-  const TI* x = static_cast<const TI*>(isq ? a.t.q : a.t.k) + t * (isq ? a.t.q_stride : a.t.k_stride) + static_cast<int64_t>(h) * a.d;
-  TO* y = static_cast<TO*>(isq ? a.t.q_out : a.t.k_out) + t * (isq ? a.t.q_out_stride : a.t.k_out_stride) + static_cast<int64_t>(h) * a.d;
-  const bool first = a.borrow && isq && h % a.g == 0;   // element 0 is the neuron
-  if (u >= a.rot / 2) {
-    int e = u - a.rot / 2;
-    if (e >= a.off) e += a.rot;
-    float v = load1(x + e);
-    if (first && e == 0) v = a.back ? neuron_gradient(a, t, h / a.g) : borrow_neuron(a, t, h / a.g, v);
-    store1(y + e, v);
-    return;
+  const int64_t total = static_cast<int64_t>(a.T) * row * units;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i < total;
+       i += static_cast<int64_t>(gridDim.x) * kThreads) {
+    const int u = static_cast<int>(i % units);
+    const int64_t th = i / units;
+    const int t = static_cast<int>(th / row);
+    int h = static_cast<int>(th % row);
+    const bool isq = a.t.q && h < a.Hq;
+    if (!isq && a.t.q) h -= a.Hq;
+    const TI* x = static_cast<const TI*>(isq ? a.t.q : a.t.k) + t * (isq ? a.t.q_stride : a.t.k_stride) + static_cast<int64_t>(h) * a.d;
+    TO* y = static_cast<TO*>(isq ? a.t.q_out : a.t.k_out) + t * (isq ? a.t.q_out_stride : a.t.k_out_stride) + static_cast<int64_t>(h) * a.d;
+    const bool first = a.borrow && isq && h % a.g == 0;   // element 0 is the neuron
+    if (u >= a.rot / 2) {
+      int e = u - a.rot / 2;
+      if (e >= a.off) e += a.rot;
+      float v = load1(x + e);
+      if (first && e == 0) v = a.back ? neuron_gradient(a, t, h / a.g) : borrow_neuron(a, t, h / a.g, v);
+      store1(y + e, v);
+      continue;
+    }
+    const int e1 = a.off + (a.adjacent ? 2 * u : u), e2 = e1 + (a.adjacent ? 1 : a.rot / 2);
+    float x1 = load1(x + e1);
+    const float x2 = load1(x + e2);
+    if (first && e1 == 0 && !a.back) x1 = borrow_neuron(a, t, h / a.g, x1);
+    f32x2 r = rotate(x1, x2, turn(a, t, u));
+    if (first && e1 == 0 && a.back) r[0] = neuron_gradient(a, t, h / a.g);
+    store1(y + e1, r[0]);
+    store1(y + e2, r[1]);
   }
-  const int e1 = a.off + (a.adjacent ? 2 * u : u), e2 = e1 + (a.adjacent ? 1 : a.rot / 2);
-  float x1 = load1(x + e1);
-  const float x2 = load1(x + e2);
-  if (first && e1 == 0 && !a.back) x1 = borrow_neuron(a, t, h / a.g, x1);
-  f32x2 r = rotate(x1, x2, turn(a, t, u));
-  if (first && e1 == 0 && a.back) r[0] = neuron_gradient(a, t, h / a.g);
-  store1(y + e1, r[0]);
-  store1(y + e2, r[1]);
 }
 
 // ---------------------------------------------------------------------------
@@ -268,7 +273,7 @@ hipError_t run_rope(const RopeArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   const int64_t units = static_cast<int64_t>(a.T) * heads * (a.d - a.rot / 2);
-  const int64_t blocks = (units + kThreads - 1) / kThreads;
+  const int64_t blocks = std::min<int64_t>(kMaxBlocks, (units + kThreads - 1) / kThreads);
   hipLaunchKernelGGL((rope_kernel<TI, TO>), dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }

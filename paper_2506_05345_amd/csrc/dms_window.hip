@@ -1152,30 +1152,44 @@ WindowLayout window_layout(const dms_window_config& c) {
 // Rows of fewer than this many keys get their D_t from a walk over the keys of its own.
 constexpr int kExactKeys = 128;
 
+// Workgroups of a KV head in each launch.
+struct WindowGrids {
+  int64_t rows, keys, sums;   // query blocks; key blocks' shares and far queries; sums (0: no launch)
+};
+WindowGrids window_grids(const dms_window_config& c, const WindowLayout& l) {
+  const int64_t T = c.total_tokens, n = c.num_seqs, per = l.far / kKeys;
+  WindowGrids w{};
+  w.rows = T / (kCols / c.group_size) + n;
+  w.keys = (T / kKeys + n + per - 1) / per * (per * l.splits + l.sink_tiles);
+  w.sums = l.splits > 1 ? (T + 3) / 4 : l.sink_tiles ? (T / l.far + 1) * 8 * l.sink_tiles : 0;
+  return w;
+}
+
 template <int D>
-void launch_backward(const WindowArgs& a, bool exact, hipStream_t st) {
-  const dim3 gq(a.T / a.PB + a.n, a.H);
-  if (exact) hipLaunchKernelGGL((window_dq_kernel<D, true>), gq, dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((window_dq_kernel<D, false>), gq, dim3(kThreads), 0, st, a);
-  const int per = a.far / kKeys;
-  const int groups = (a.T / kKeys + a.n + per - 1) / per;
-  hipLaunchKernelGGL(window_dkv_kernel<D>, dim3(groups * (per * a.splits + a.sink_tiles), a.H), dim3(kThreads), 0, st, a);
-  if (a.splits > 1)
-    hipLaunchKernelGGL(window_sum_kernel<D>, dim3((a.T + 3) / 4, a.H), dim3(kThreads), 0, st, a);
-  else if (a.sink_tiles)
-    hipLaunchKernelGGL(window_sum_kernel<D>, dim3((a.T / a.far + 1) * 8 * a.sink_tiles, a.H), dim3(kThreads), 0, st, a);
+void launch_backward(const WindowArgs& a, const WindowGrids& w, bool exact, hipStream_t st) {
+  auto grid = [&](int64_t x) { return dim3(static_cast<unsigned>(x), a.H); };
+  if (exact) hipLaunchKernelGGL((window_dq_kernel<D, true>), grid(w.rows), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((window_dq_kernel<D, false>), grid(w.rows), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL(window_dkv_kernel<D>, grid(w.keys), dim3(kThreads), 0, st, a);
+  if (w.sums) hipLaunchKernelGGL(window_sum_kernel<D>, grid(w.sums), dim3(kThreads), 0, st, a);
 }
 
 }  // namespace
 
 size_t window_workspace_bytes(const dms_window_config& c) { return window_layout(c).bytes; }
 
+// A grid holds fewer than 2^32 threads (more than that many rows, or sinks of hundreds of thousands of tokens).
+bool window_grids_fit(const dms_window_config& c) {
+  const WindowGrids w = window_grids(c, window_layout(c));
+  return std::max({w.rows, w.keys, w.sums}) < (int64_t(1) << 32) / kThreads;
+}
+
 hipError_t launch_window_fwd(const dms_window_config& c, const int32_t* cu, const void* q, const void* k,
                              const void* v, void* out, float* lse, void*, hipStream_t st) {
   WindowArgs a = window_args(c, cu, q, k, v);
   a.out = static_cast<__bf16*>(out);
   a.lse_out = lse;
-  const dim3 grid(a.T / a.PB + a.n, a.H);
+  const dim3 grid(static_cast<unsigned>(window_grids(c, window_layout(c)).rows), a.H);
   if (c.head_dim == 64) hipLaunchKernelGGL(window_fwd_kernel<64>, grid, dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL(window_fwd_kernel<128>, grid, dim3(kThreads), 0, st, a);
   return hipGetLastError();
@@ -1203,8 +1217,9 @@ hipError_t launch_window_bwd(const dms_window_config& c, const int32_t* cu, cons
   a.dk = static_cast<__bf16*>(dk);
   a.dv = static_cast<__bf16*>(dv);
   const bool exact = a.w + a.sinks < kExactKeys;
-  if (c.head_dim == 64) launch_backward<64>(a, exact, st);
-  else launch_backward<128>(a, exact, st);
+  const WindowGrids grids = window_grids(c, l);
+  if (c.head_dim == 64) launch_backward<64>(a, grids, exact, st);
+  else launch_backward<128>(a, grids, exact, st);
   return hipGetLastError();
 }
 

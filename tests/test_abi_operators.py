@@ -52,6 +52,7 @@ def test_rope_arguments_refused():
     assert dms.lib().dms_rope_fwd(None, 4, SOME, 384, SOME, 128, *[SOME] * 4, None, None, None) == dms.DMS_ERR_INVALID
     big = _rope(num_kv_heads=1 << 10, group_size=16)
     assert _rope_fwd(big, tokens=1 << 20, qs=1 << 40, ks=1 << 40) == dms.DMS_ERR_UNSUPPORTED
+    assert _rope_fwd(cfg, tokens=1 << 26) == dms.DMS_ERR_UNSUPPORTED
     assert _rope_fwd(cfg, tokens=0, q=None, k=None, qo=None, ko=None, pos=None, inv=None) == dms.DMS_OK
     bwd = lambda c, dl=None, qo=SOME, qs=384: dms.lib().dms_rope_bwd(B(c), 4, SOME, SOME, SOME, SOME, dl, qo, qs, SOME, 128, None)
     assert bwd(_rope(borrow=0), dl=SOME) == dms.DMS_ERR_INVALID
@@ -75,6 +76,10 @@ def _win(**kw):
     (dict(sinks=-1), dms.DMS_ERR_INVALID), (dict(softmax_scale=float("nan")), dms.DMS_ERR_INVALID),
     (dict(softmax_scale=float("inf")), dms.DMS_ERR_INVALID), (dict(num_kv_heads=5000), dms.DMS_ERR_UNSUPPORTED),
     (dict(total_tokens=1 << 30, max_seqlen=5), dms.DMS_ERR_UNSUPPORTED),
+    # grids of 2^32 threads and more
+    (dict(total_tokens=2**31 - 1, num_kv_heads=1, group_size=1), dms.DMS_ERR_UNSUPPORTED),
+    (dict(total_tokens=1 << 20, max_seqlen=1 << 20, sinks=1 << 20), dms.DMS_ERR_UNSUPPORTED),
+    (dict(total_tokens=2**31 // 6 - 1, max_seqlen=600, sinks=600), dms.DMS_ERR_UNSUPPORTED),
 ])
 def test_window_configurations_refused(kw, code):
     cfg = _win(**kw)
@@ -85,6 +90,10 @@ def test_window_configurations_refused(kw, code):
 
 def test_window_arguments_refused():
     cfg = _win()
+    # sinks' sums: (T / 512 + 1) 8 (sinks / 32) workgroups of 256 threads, 2049 x 8192 >= 2^24 and 1025 x 8192 < 2^24
+    far = lambda T: _win(total_tokens=T, max_seqlen=1 << 15, sinks=2**31 - 1, window=2**31 - 1)
+    assert dms.lib().dms_window_workspace(B(far(1 << 20)), None) == dms.DMS_ERR_UNSUPPORTED
+    assert dms.dms_window_workspace(far(1 << 19)) > 0
     assert dms.dms_window_workspace(cfg) > 0
     for call, n in ((dms.lib().dms_window_attention_fwd, 7), (dms.lib().dms_window_attention_bwd, 11)):
         for i in range(n):

@@ -34,6 +34,7 @@ CASES = [
     _case(17, 1, 2, 6, 2, [1], off=3, adjacent=True),            # odd sizes: one element at a time
     _case(19, 2, 2, 36, 20, [3, 7], off=8, tout="f32"),
     _case(700, 2, 6, 128, 128, [64], fused=False, borrow=False),
+    _case(33000, 4, 4, 36, 20, [3, 7], off=8),                   # more elements than a grid has threads
     _case(12, 2, 2, 1024, 512, [256], off=256),
     _case(2100, 1, 2, 64, 64, [12, 10, 10], interleaved=True, adjacent=True),
 ]
