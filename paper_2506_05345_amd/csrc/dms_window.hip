@@ -229,7 +229,8 @@ __device__ inline bool store_row(__bf16* dst, const f32x16* o, float f, int hf, 
 // (lane l: row 8 m + l / 8, 16-byte piece l % 8 of a 64-element half), and the
 // halves are turned in 4 KB of LDS of the wave's own, pieces permuted by row as
 // in the tiles.  Read straight into operands (32 rows of 32 bytes an
-// instruction) and written so, rows took 60 of the forward's 165 us.
+// instruction) and written so, rows took 60 of the forward's 165 us (16384
+// tokens of 8 x 5 heads, w = 256, 4 sinks).
 // ---------------------------------------------------------------------------
 constexpr int kTurn = 4096;   // LDS bytes of a wave's half rows
 struct Rows {
@@ -305,12 +306,14 @@ __device__ inline bool store_rows(__bf16* base, const f32x16* o, float f, const 
 }
 
 // ---------------------------------------------------------------------------
-// LDS ring of 3 or 4 steps, each two 32-row tiles of 2 D bytes a row ([K | V] of
-// 32 keys, or [Q | dO] of 32 positions of one head): while one step is computed
-// the next are on their way.  A window is few steps long, so that a
-// workgroup spends as long waiting as computing unless its first copies leave
-// together.  Wave x copies half x % 2 of tile x / 2.
+// LDS ring of steps, each two 32-row tiles of 2 D bytes a row ([K | V] of 32
+// keys): while one step is computed the next are on their way.  A window is few
+// steps long, so that a workgroup spends as long waiting as computing unless its
+// first copies leave together.  Wave x copies half x % 2 of tile x / 2.  Three
+// slots (48 KB at d = 128) leave room for three workgroups per CU: 16384 tokens
+// of 8 x 5 heads, w = 256, take 151 us, with four slots and two workgroups 165.
 // ---------------------------------------------------------------------------
+constexpr int kSlots = 3;
 template <int D>
 constexpr int kCopies = D / 32;   // copies of a step by one wave
 
@@ -339,25 +342,22 @@ __device__ inline void copy_keys(const WindowArgs& a, const KeyTiles& kt, const 
   }
 }
 
-// Of the steps after this one `left` are there to come and up to SLOTS - 2 of them have been issued: this
-// one has landed for every wave.
-template <int D, int SLOTS>
+// Of the steps after this one `left` are there to come and the first has been issued: this one has landed for
+// every wave.
+template <int D>
 __device__ inline void step_ready(int left) {
-  if (SLOTS >= 4 && left >= 2) wait_copies_but<2 * kCopies<D>>();
-  else if (left >= 1) wait_copies_but<kCopies<D>>();
+  if (left >= 1) wait_copies_but<kCopies<D>>();
   else wait_copies();
   __syncthreads();
 }
 
 // f(step, slot) for steps 0 .. n - 1, the slot a constant.
-template <int SLOTS, typename F>
+template <typename F>
 __device__ __forceinline__ void over_steps(int n, F f) {
-  for (int i = 0; i < n; i += SLOTS) {
+  for (int i = 0; i < n; i += kSlots) {
     f(i, std::integral_constant<int, 0>{});
     if (i + 1 < n) f(i + 1, std::integral_constant<int, 1>{});
     if (i + 2 < n) f(i + 2, std::integral_constant<int, 2>{});
-    if constexpr (SLOTS > 3)
-      if (i + 3 < n) f(i + 3, std::integral_constant<int, 3>{});
   }
 }
 
@@ -369,7 +369,6 @@ __device__ __forceinline__ void over_steps(int n, F f) {
 template <int D>
 __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
   using Tile = TileOf<D>;
-  constexpr int kSlots = 3;
   constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
   // the last slot, idle until the first step, and its end (D = 64) also turn the waves' rows
   constexpr int kTurnAt = (kSlots - 1) * 2 * kUnit;
@@ -416,9 +415,9 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
   float m_ref = kMInit, l_run = 0.f;
   const float thr = kRescale / a.scale_log2;
 
-  over_steps<kSlots>(kt.nt, [&](int i, auto slot_c) {
+  over_steps(kt.nt, [&](int i, auto slot_c) {
     constexpr int slot = decltype(slot_c)::value, tl = slot * 2 * kUnit;
-    step_ready<D, kSlots>(kt.nt - 1 - i);
+    step_ready<D>(kt.nt - 1 - i);
     if (i + kSlots - 1 < kt.nt) issue(i + kSlots - 1, (slot + kSlots - 1) % kSlots);
     if (!tile_seen(wt, i)) return;
     f32x16 s;
@@ -1134,7 +1133,9 @@ WindowLayout window_layout(const dms_window_config& c) {
   const size_t T = c.total_tokens, H = c.num_kv_heads, D = c.head_dim;
   l.Ts = static_cast<int64_t>(T) + 128;
   const int64_t blocks = (static_cast<int64_t>(T) + kKeys - 1) / kKeys * c.num_kv_heads;
-  // fewer blocks than a quarter of the CUs' workgroups: shares of their steps, and shorter lists of far queries
+  // fewer blocks than CUs: shares of their steps, and shorter lists of far queries.  28 blocks (1777 tokens of 2
+  // x 6 heads, w = 256): forward and backward take 63 us, without shares 110, with far lists of 512 positions
+  // 111; enough blocks (16384 tokens of 8 x 5 heads) take 633 us, with far lists of 128 positions 712.
   l.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, kSplitTarget / std::max<int64_t>(1, blocks))));
   l.far = blocks < kSplitTarget ? kKeys : 4 * kKeys;
   const int sinks = std::min(c.sinks, c.max_seqlen);
@@ -1149,7 +1150,10 @@ WindowLayout window_layout(const dms_window_config& c) {
   return l;
 }
 
-// Rows of fewer than this many keys get their D_t from a walk over the keys of its own.
+// Rows of fewer than this many keys get their D_t from a walk over the keys of its own: `out`'s rounding weighs
+// on their small sums.  The walk costs less than the reading of `out` below some 50 keys (16384 tokens of 8 x 5
+// heads: 402 us of a whole step against 407 at w = 16, 427 each at 64), 516 against 484 at w = 120 and 709
+// against 633 at w = 256.
 constexpr int kExactKeys = 128;
 
 // Workgroups of a KV head in each launch.
