@@ -489,7 +489,12 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
 // S^T = K Q^T and dP^T = V dO^T over rows, dQ^T += K^T dS^T over columns.  It
 // also leaves -lse and -D of every row to the key-major pass.  EXACT: D_t is
 // summed from P and dP in a first walk over the tiles (two more products and no
-// reading of `out`), else formed from dO and the rounded `out`.
+// reading of `out`), else formed from dO and the rounded `out`.  The latter puts
+// 0.0011 of error on dQ and dK (of their 2-norm, w = 256), where dS and the
+// output rounded to bf16 put 0.0017 each.  So that they stay near 0.002, dQ's
+// product takes dS in two bf16 parts (a second product; 636 to 667 us forward
+// and backward, 16384 tokens of 8 x 5 heads), and the key-major pass gets D with
+// sum_j dS_j added, which would be 0 for the true one (sum_j P_j = 1).
 // ---------------------------------------------------------------------------
 // A dQ row as exact_row above.
 template <int D>
@@ -579,7 +584,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
   u32x4 qf[kKS], df[kKS];
   load_rows<D>(qf, a.q + first_row * D, rows);
   load_rows<D>(df, a.dout + first_row * D, rows);
-  float dcol = 0.f, psum = 0.f;
+  float dcol = 0.f, psum = 0.f, rest = 0.f;
   if (!EXACT) {
     u32x4 ov[kKS];
     load_rows<D>(ov, a.o + first_row * D, rows);
@@ -645,12 +650,27 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
         for (int e = 0; e < kAhead; ++e) op[e] = col_operand(tl, ad, e % kDB, e / kDB);
         float ds[16];
 #pragma unroll
-        for (int x = 0; x < 16; ++x) ds[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2, -lse2)) * dp[x];
-        const u32x4 du[2] = {pack_bf16(ds), pack_bf16(ds + 8)};   // rounded as in the key-major pass
+        for (int x = 0; x < 16; ++x) {
+          ds[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2, -lse2)) * dp[x];
+          if (!EXACT) rest += ds[x];
+        }
+        const u32x4 du[2] = {pack_bf16(ds), pack_bf16(ds + 8)};
+        u32x4 dl[2];   // what du's rounding left
+        if constexpr (!EXACT) {
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const uint32_t two = du[x >> 2][x & 3];
+            ds[2 * x] -= __uint_as_float(two << 16);
+            ds[2 * x + 1] -= __uint_as_float(two & 0xFFFF0000u);
+          }
+          dl[0] = pack_bf16(ds);
+          dl[1] = pack_bf16(ds + 8);
+        }
 #pragma unroll
         for (int e = 0; e < 2 * kDB; ++e) {
           __builtin_amdgcn_sched_barrier(0);
           dqa[e % kDB] = mfma(op[e % kAhead], du[e / kDB], dqa[e % kDB]);
+          if constexpr (!EXACT) dqa[e % kDB] = mfma(op[e % kAhead], dl[e / kDB], dqa[e % kDB]);
           if (e + kAhead < 2 * kDB) op[e % kAhead] = col_operand(tl, ad, (e + kAhead) % kDB, (e + kAhead) / kDB);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -676,6 +696,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) dqa[x][i] = 0.f;
   walk(std::false_type{});
+  if (!EXACT) dcol += col_sum(rest);
 
   if (ok) (hf ? a.nsum : a.nlse)[static_cast<size_t>(h * a.g + qh) * a.Ts + s0 + t] = hf ? -dcol : -lse2 / a.scale_log2;
   const float scale = a.single ? 0.f : a.scale_log2 / kLog2e;
@@ -1134,8 +1155,8 @@ WindowLayout window_layout(const dms_window_config& c) {
   l.Ts = static_cast<int64_t>(T) + 128;
   const int64_t blocks = (static_cast<int64_t>(T) + kKeys - 1) / kKeys * c.num_kv_heads;
   // fewer blocks than CUs: shares of their steps, and shorter lists of far queries.  28 blocks (1777 tokens of 2
-  // x 6 heads, w = 256): forward and backward take 63 us, without shares 110, with far lists of 512 positions
-  // 111; enough blocks (16384 tokens of 8 x 5 heads) take 633 us, with far lists of 128 positions 712.
+  // x 6 heads, w = 256): forward and backward take 65 us, without shares 47 more, with far lists of 512 positions
+  // 48; 1024 blocks (16384 tokens of 8 x 5 heads): 667 us, with far lists of 128 positions 79 more.
   l.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, kSplitTarget / std::max<int64_t>(1, blocks))));
   l.far = blocks < kSplitTarget ? kKeys : 4 * kKeys;
   const int sinks = std::min(c.sinks, c.max_seqlen);
@@ -1151,9 +1172,8 @@ WindowLayout window_layout(const dms_window_config& c) {
 }
 
 // Rows of fewer than this many keys get their D_t from a walk over the keys of its own: `out`'s rounding weighs
-// on their small sums.  The walk costs less than the reading of `out` below some 50 keys (16384 tokens of 8 x 5
-// heads: 402 us of a whole step against 407 at w = 16, 427 each at 64), 516 against 484 at w = 120 and 709
-// against 633 at w = 256.
+// on their small sums.  A whole step with the walk and without, 16384 tokens of 8 x 5 heads: 403 us against 408
+// at w = 16, 439 against 438 at 64, 535 against 505 at 120, 723 against 676 at 256.
 constexpr int kExactKeys = 128;
 
 // Workgroups of a KV head in each launch.
