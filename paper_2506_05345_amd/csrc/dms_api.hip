@@ -126,13 +126,7 @@ Layout make_layout(const dms_config& c) {
   lo.ws_q_sel = take(NH * static_cast<size_t>(c.quest_page_budget) * 4);
   lo.ws_q_page = take(NH * static_cast<size_t>(c.quest_page_budget) * 4);
   lo.ws_q_len = take(NH * 4);
-  const size_t Ly = c.num_layers;
-  lo.ws_fk_base = take(Ly * NH * 4);
-  lo.ws_fk_tiles = take(Ly * (NH + 1) * 4);
-  lo.ws_fk_block = take(Ly * 8);
-  lo.cp_list_stride = static_cast<size_t>(c.num_pages) / 2 + 1 + 2 * ((static_cast<size_t>(c.num_pages) + 31) / 32);
-  lo.ws_cp_lists = take(Ly * lo.cp_list_stride * 4);
-  lo.workspace_bytes = off;
+  lo.workspace_bytes = off + pages_layout(c, NH, off).bytes;
   return lo;
 }
 

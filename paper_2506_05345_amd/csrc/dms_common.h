@@ -41,10 +41,6 @@ struct Layout {
       ws_pf_order;
   size_t ws_q_sel, ws_q_page, ws_q_len;   // quest: selection [NH][B] (page-table
                                           // indices, physical pages), attended lengths [NH]
-  size_t ws_fk_base, ws_fk_tiles, ws_fk_block;   // forks, per layer: page and tile prefix sums per
-                                                 // (pair, head), the call's block of free pages
-  size_t ws_cp_lists;      // compaction: free ids below the live count and which pages move, per layer
-  size_t cp_list_stride;   // int32 entries of one layer
   int pf_tiles_per_head;   // tiles of one (region, KV head) in ws_pf_tiles
   size_t workspace_bytes;
   int max_heads, max_partials, max_slots;

@@ -33,6 +33,15 @@ hipError_t launch_window_bwd(const dms_window_config& c, const int32_t* cu, cons
                              const void* v, const void* out, const float* lse, const void* dout, void* dq,
                              void* dk, void* dv, void* ws, hipStream_t st);
 
+// Forks' and compactions' part of a context's workspace, its last bytes.
+struct PagesLayout {
+  size_t fk_base, fk_tiles, fk_block;   // per layer: page and tile prefix sums per (pair, head), the call's block of pages
+  size_t cp_lists;                      // per layer: free ids below the live count and which pages move
+  size_t cp_list_stride;                // int32 entries of one layer
+  size_t bytes;                         // of this part
+};
+PagesLayout pages_layout(const dms_config& c, size_t max_heads, size_t at);
+
 // layer -1: every layer.  pools: one pointer per layer of the context.
 hipError_t launch_seq_fork(const dms_config& c, const Layout& lo, void* meta, void* ws, void* const* pools,
                            int layer, int n, const int32_t* src, const int32_t* dst, hipStream_t st);

@@ -445,7 +445,26 @@ hipError_t over_layers(const dms_config& c, PagesArgs& p, void* const* pools, in
   return hipSuccess;
 }
 
+PagesLayout layout_of(const dms_config& c, const Layout& lo) {
+  const size_t heads = lo.max_heads;
+  return pages_layout(c, heads, lo.workspace_bytes - pages_layout(c, heads, 0).bytes);
+}
+
 }  // namespace
+
+PagesLayout pages_layout(const dms_config& c, size_t max_heads, size_t at) {
+  PagesLayout l{};
+  const size_t layers = c.num_layers, words = (static_cast<size_t>(c.num_pages) + 31) / 32;
+  size_t off = at;
+  auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, kAlign); return o; };
+  l.fk_base = take(layers * max_heads * 4);
+  l.fk_tiles = take(layers * (max_heads + 1) * 4);
+  l.fk_block = take(layers * 8);
+  l.cp_list_stride = static_cast<size_t>(c.num_pages) / 2 + 1 + 2 * words;
+  l.cp_lists = take(layers * l.cp_list_stride * 4);
+  l.bytes = off - at;
+  return l;
+}
 
 hipError_t launch_seq_fork(const dms_config& c, const Layout& lo, void* meta, void* ws, void* const* pools,
                            int layer, int n, const int32_t* src, const int32_t* dst, hipStream_t st) {
@@ -456,9 +475,10 @@ hipError_t launch_seq_fork(const dms_config& c, const Layout& lo, void* meta, vo
   a.dst = dst;
   a.n = n;
   a.nh_max = static_cast<size_t>(lo.max_heads);
-  a.base = reinterpret_cast<int32_t*>(w + lo.ws_fk_base);
-  a.tiles = reinterpret_cast<int32_t*>(w + lo.ws_fk_tiles);
-  a.block = reinterpret_cast<int32_t*>(w + lo.ws_fk_block);
+  const PagesLayout l = layout_of(c, lo);
+  a.base = reinterpret_cast<int32_t*>(w + l.fk_base);
+  a.tiles = reinterpret_cast<int32_t*>(w + l.fk_tiles);
+  a.block = reinterpret_cast<int32_t*>(w + l.fk_block);
   hipError_t e = over_layers(c, a.p, pools, layer, [&](int, int layers) {
     hipLaunchKernelGGL(fork_plan_kernel, dim3(layers), dim3(kPlanThreads), 0, st, a);
   });
@@ -476,8 +496,9 @@ hipError_t launch_compact(const dms_config& c, const Layout& lo, void* meta, voi
                           int layer, int32_t* used_out, hipStream_t st) {
   CompactArgs a{};
   a.p = pages_args(c, lo, meta);
-  a.lists = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + lo.ws_cp_lists);
-  a.list_stride = lo.cp_list_stride;
+  const PagesLayout l = layout_of(c, lo);
+  a.lists = reinterpret_cast<int32_t*>(static_cast<char*>(ws) + l.cp_lists);
+  a.list_stride = l.cp_list_stride;
   a.used_out = used_out;
   return over_layers(c, a.p, pools, layer, [&](int y, int layers) {
     a.out0 = y - std::max(layer, 0);
