@@ -4,6 +4,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <initializer_list>
 #include <mutex>
 #include <vector>
@@ -869,6 +870,9 @@ static int validate_window_config(const dms_window_config* c) {
   const int64_t heads = static_cast<int64_t>(c->num_kv_heads) * c->group_size;
   if (c->num_kv_heads > 4096 || heads * c->total_tokens >= int64_t(1) << 31) return DMS_ERR_UNSUPPORTED;
   if (!dms::window_grids_fit(*c)) return DMS_ERR_UNSUPPORTED;
+  // positions and window ends in int32
+  if (static_cast<int64_t>(c->max_seqlen) + std::min(c->window, c->max_seqlen) >= (int64_t(1) << 31) - 1024)
+    return DMS_ERR_UNSUPPORTED;
   return DMS_OK;
 }
 

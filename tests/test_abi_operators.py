@@ -80,6 +80,9 @@ def _win(**kw):
     (dict(total_tokens=2**31 - 1, num_kv_heads=1, group_size=1), dms.DMS_ERR_UNSUPPORTED),
     (dict(total_tokens=1 << 20, max_seqlen=1 << 20, sinks=1 << 20), dms.DMS_ERR_UNSUPPORTED),
     (dict(total_tokens=2**31 // 6 - 1, max_seqlen=600, sinks=600), dms.DMS_ERR_UNSUPPORTED),
+    # the end of a key's window past int32
+    (dict(total_tokens=1 << 30, max_seqlen=1 << 30, num_kv_heads=1, group_size=1, window=1 << 30, sinks=0),
+     dms.DMS_ERR_UNSUPPORTED),
 ])
 def test_window_configurations_refused(kw, code):
     cfg = _win(**kw)
