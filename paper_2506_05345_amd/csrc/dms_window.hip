@@ -157,7 +157,8 @@ __device__ inline bool is_nan(float x) { return (__float_as_uint(x) & 0x7FFFFFFF
 
 // Row (position t of the sequence at s0, query head hq) by one wave, lanes over the head's elements and
 // only visible keys read: rows whose sums are not finite, where a product may have met an Inf or NaN of
-// a hidden key.
+// a hidden key.  A score that is NaN itself makes all of the row NaN: the walk ends there, so that a step on
+// NaN inputs takes no longer than others.
 template <int D>
 __device__ inline void exact_row(const WindowArgs& a, int s0, int t, int hq) {
   constexpr int E = D / 64;
@@ -175,6 +176,10 @@ __device__ inline void exact_row(const WindowArgs& a, int s0, int t, int hq) {
 #pragma unroll
     for (int e = 0; e < E; ++e) s += q[e] * static_cast<float>(a.k[kr + e]);
     s = wave_sum(s) * a.scale_log2;
+    if (is_nan(s)) {
+      l = s;
+      break;
+    }
     const float mn = fmaxf(m, s), c = exp2f(m - mn), p = exp2f(s - mn);
     l = l * c + p;
 #pragma unroll
@@ -525,6 +530,13 @@ __device__ inline void exact_dq_row(const WindowArgs& a, int s0, int t, int hq) 
       }
       const float p = exp2f(wave_sum(s) * a.scale_log2 - lse2);
       dp = wave_sum(dp);
+      if (is_nan(p) || is_nan(dp)) {
+        d = NAN;
+#pragma unroll
+        for (int e = 0; e < E; ++e) dq[e] = NAN;
+        pass = 1;
+        break;
+      }
       if (pass) {
 #pragma unroll
         for (int e = 0; e < E; ++e) dq[e] += p * (dp - d) * k[e];
@@ -768,6 +780,12 @@ __device__ inline void exact_key(const WindowArgs& a, int s0, int len, int j, in
       }
       const size_t at = hq * a.Ts + s0 + t;
       const float p = exp2f((wave_sum(s) + a.nlse[at]) * a.scale_log2), ds = p * (wave_sum(dp) + a.nsum[at]);
+      if (is_nan(p)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) dk[e] = dv[e] = NAN;
+        t = end;
+        break;
+      }
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         dv[e] += p * dO[e];

@@ -229,6 +229,17 @@ def test_hidden_keys_of_any_value_change_nothing(bad, d):
         near(got, n, others)
 
 
+@pytest.mark.parametrize("H, d, w", [(1, 64, 1500), (32, 128, 1500), (2, 128, 30)])
+@pytest.mark.parametrize("name", ["q", "k"])
+def test_nan_scores_make_nan(name, H, d, w):
+    """Queries, or keys, that are all NaN (a step that has diverged): every result that a score reaches is NaN."""
+    T, g, sinks = 2500, 2, 3
+    x = _inputs(T, H, g, d, 16)
+    x[name][:] = _bf16(np.array([float("nan")]))[0]
+    got = _gpu(x, [T], H, g, d, w, sinks)
+    assert all(np.isnan(y).all() for y in got.values())
+
+
 def test_results_do_not_depend_on_the_packing():
     """A sequence alone and between others gives the same bits (head dims 64 and 128)."""
     for d in (64, 128):
