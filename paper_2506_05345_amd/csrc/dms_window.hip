@@ -370,6 +370,10 @@ __device__ __forceinline__ void over_steps(int n, F f) {
 // Forward.  Workgroup = (KV head, block of PB positions of one sequence);
 // columns are (position, query head) pairs, the g heads of a position
 // consecutive, 32 per wave.  The block's key tiles go through the LDS ring.
+// 16384 tokens of 8 x 5 heads, d = 128, w = 256, 4 sinks (405 MB, 86 GFLOP) take
+// 131 to 150 us.  Issue bounds it: a tile's 16 products take 512 cycles of a
+// SIMD's matrix core, its 117 other instructions, 16 of them exponentials at a
+// quarter of the rate, about 660.
 // ---------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
@@ -499,7 +503,9 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
 // output rounded to bf16 put 0.0017 each.  So that they stay near 0.002, dQ's
 // product takes dS in two bf16 parts (a second product; 636 to 667 us forward
 // and backward, 16384 tokens of 8 x 5 heads), and the key-major pass gets D with
-// sum_j dS_j added, which would be 0 for the true one (sum_j P_j = 1).
+// sum_j dS_j added, which would be 0 for the true one (sum_j P_j = 1).  The pass
+// takes 245 to 270 us of the step (two waves of 252 registers per SIMD, matrix
+// core 42 % busy).
 // ---------------------------------------------------------------------------
 // A dQ row as exact_row above.
 template <int D>
