@@ -540,7 +540,7 @@ typedef struct dms_rope_config {
   float factor;           /* <= 0 selects 1 */
 } dms_rope_config;
 
-/* Rotate `tokens` tokens (fewer than 2^26, and 2^38 elements).  q_dev [tokens][Hq][d] and k_dev [tokens][Hkv][d] (in_type)
+/* Rotate `tokens` tokens (at most 2^26 - 4, and fewer than 2^38 elements).  q_dev [tokens][Hq][d] and k_dev [tokens][Hkv][d] (in_type)
  * have q_stride / k_stride elements from a token to the next (>= Hq d / Hkv d: they
  * may be parts of the rows of one projection); q_out_dev, k_out_dev (out_type) are
  * dense.  Either of q and k may be NULL together with its output.

@@ -817,8 +817,8 @@ static int check_rope_call(const dms_rope_config* c, int tokens, const dms::Rope
   if (tokens < 0) return DMS_ERR_INVALID;
   const int64_t kv = static_cast<int64_t>(c->num_kv_heads) * c->head_dim, qr = kv * c->group_size;
   if (t.q_stride < qr || t.k_stride < kv || t.q_out_stride < qr || t.k_out_stride < kv) return DMS_ERR_INVALID;
-  // a wave per token and a grid of fewer than 2^32 threads
-  if (tokens >= 1 << 26 || tokens * (qr + kv) >= int64_t(1) << 38) return DMS_ERR_UNSUPPORTED;
+  // a wave per token, four to a workgroup, and a grid of fewer than 2^32 threads
+  if (tokens > (1 << 26) - 4 || tokens * (qr + kv) >= int64_t(1) << 38) return DMS_ERR_UNSUPPORTED;
   if (tokens == 0) return DMS_OK;
   if (!t.q != !t.q_out || !t.k != !t.k_out || (!t.q && !t.k) || !positions || !inv_freq) return DMS_ERR_INVALID;
   return DMS_OK;
