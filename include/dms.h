@@ -590,14 +590,14 @@ int dms_rope_bwd(const dms_rope_config* cfg, int tokens, const void* dq_dev, con
 typedef struct dms_window_config {
   int32_t num_seqs;       /* n >= 1, at most 65535 */
   int32_t total_tokens;   /* rows of the tensors, >= 0; total_tokens Hq < 2^31 */
-  int32_t max_seqlen;     /* longest sequence, 0 .. total_tokens */
+  int32_t max_seqlen;     /* longest sequence, 1 .. total_tokens (0 where there are no tokens) */
   int32_t num_kv_heads;   /* Hkv: 1 .. 4096 */
   int32_t group_size;     /* g = Hq / Hkv, 1 .. 16 */
   int32_t head_dim;       /* d: 64 or 128 */
   int32_t window;         /* w >= 1 */
   int32_t sinks;          /* first tokens that stay visible, >= 0 (past max_seqlen: full attention);
                              total_tokens / 512 * min(sinks, max_seqlen) / 4 < 2^24 */
-  float softmax_scale;    /* <= 0 selects 1 / sqrt(head_dim) */
+  float softmax_scale;    /* <= 0 selects 1 / sqrt(head_dim); at least 2^-100 */
 } dms_window_config;
 
 int dms_window_workspace(const dms_window_config* cfg, size_t* workspace_bytes);

@@ -866,6 +866,8 @@ static int validate_window_config(const dms_window_config* c) {
   if (c->group_size > dms::kMaxGroup) return DMS_ERR_UNSUPPORTED;
   if (c->head_dim != 64 && c->head_dim != 128) return DMS_ERR_UNSUPPORTED;
   if (isnan(c->softmax_scale) || (c->softmax_scale > 0.0f && !isfinite(c->softmax_scale))) return DMS_ERR_INVALID;
+  // -lse / scale of a row stays inside float32
+  if (c->softmax_scale > 0.0f && c->softmax_scale < 0x1p-100f) return DMS_ERR_INVALID;
   // rows of the query tensors; a grid row per KV head; a token's bytes in 32 bits
   const int64_t heads = static_cast<int64_t>(c->num_kv_heads) * c->group_size;
   if (c->num_kv_heads > 4096 || heads * c->total_tokens >= int64_t(1) << 31) return DMS_ERR_UNSUPPORTED;

@@ -19,3 +19,18 @@ def test_rope_grids_stay_below_two_to_the_32_threads(tokens):
                                   None) == dms.DMS_ERR_UNSUPPORTED
     assert dms.lib().dms_rope_bwd(B(cfg), tokens, SOME, None, SOME, SOME, None, SOME, 64, None, 64,
                                   None) == dms.DMS_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("scale", [1e-45, 1e-38, 2.0 ** -101])
+def test_scales_whose_row_values_leave_float32_are_refused(scale):
+    """The key-major gradients start from -lse / scale of each row: at scale 1e-38 the log of a few thousand equal
+    weights, about 8, is already past float32, and every weight would be 0."""
+    import numpy as np
+    with np.errstate(over="ignore"):
+        assert np.isinf(np.float32(8.0) / np.float32(1e-38))
+    cfg = dms.make_window_config(1, 100, 100, 2, 3, 128, 16, 4, scale)
+    assert dms.lib().dms_window_workspace(B(cfg), None) == dms.DMS_ERR_INVALID
+    assert dms.lib().dms_window_attention_fwd(B(cfg), *[SOME] * 7, None) == dms.DMS_ERR_INVALID
+    assert dms.lib().dms_window_attention_bwd(B(cfg), *[SOME] * 11, None) == dms.DMS_ERR_INVALID
+    for fine in (2.0 ** -100, 0.0, -1.0):
+        assert dms.dms_window_workspace(dms.make_window_config(1, 100, 100, 2, 3, 128, 16, 4, fine)) > 0
