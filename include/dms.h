@@ -607,7 +607,9 @@ int dms_window_attention_fwd(const dms_window_config* cfg, const int32_t* cu_seq
                              const void* q_dev, const void* k_dev, const void* v_dev,
                              void* out_dev, float* lse_dev, void* workspace_dev, void* stream);
 
-/* Backward: dq, dk, dv from the forward's inputs, out, lse and dout. */
+/* Backward: dq, dk, dv from the forward's inputs, out, lse and dout.  (The row term
+ * dO . out is summed again in float32, so that the rounding of `out` enters no
+ * gradient: out_dev has to be there and is not read.) */
 int dms_window_attention_bwd(const dms_window_config* cfg, const int32_t* cu_seqlens_dev,
                              const void* q_dev, const void* k_dev, const void* v_dev,
                              const void* out_dev, const float* lse_dev, const void* dout_dev,

@@ -8,7 +8,10 @@ Beside every result goes `slack`, how far a computation may lie from it whose
 products take bf16 operands: probabilities P and score gradients dS rounded to
 bf16 (half a step each, 2^-8 of the value), outputs rounded to bf16, the row
 term D = dO . out formed from the rounded outputs, and score errors up to
-`delta` relative in exp(s) from float32 sums.
+`delta` relative in exp(s) from float32 sums.  With `summed_d` the row term is
+sum_j P_j dP_j / sum_j P_j in float32 instead, and no rounding of `out` is allowed
+for: weights off by delta, relative, move the mean D of dP by at most 2 delta
+sum_j |dS_j|, and the float32 sums of n terms by n half steps of their magnitudes.
 """
 from __future__ import annotations
 
@@ -60,7 +63,7 @@ def window_attention(q, k, v, w, sinks, group, scale=None):
     return out, slack, lse, lslack
 
 
-def window_attention_grads(q, k, v, dout, w, sinks, group, scale=None):
+def window_attention_grads(q, k, v, dout, w, sinks, group, scale=None, summed_d=False):
     """Gradients of sum(out * dout): {"dq", "dk", "dv"} and their slacks, one sequence."""
     q, k, v, dout = (np.asarray(x, np.float64) for x in (q, k, v, dout))
     T, Hq, d = q.shape
@@ -77,8 +80,13 @@ def window_attention_grads(q, k, v, dout, w, sinks, group, scale=None):
         row = (do * out[:, hq]).sum(1, keepdims=True)
         ds = p * (dp - row)
         near = (d + 4) * 2.0 ** -24 * (np.abs(do) @ np.abs(v[:, h]).T + (np.abs(do) * np.abs(out[:, hq])).sum(1, keepdims=True))
-        ds_off = HALF * np.abs(ds) + 1.01 * p * ((np.abs(do) * oslack[:, hq]).sum(1, keepdims=True) + near) + \
-            3 * dl * np.abs(ds)
+        if summed_d:
+            n = mask.sum(1, keepdims=True)
+            row_off = 2 * dl * np.abs(ds).sum(1, keepdims=True) + (n + 8) * 2.0 ** -24 * \
+                ((p * np.abs(dp)).sum(1, keepdims=True) + np.abs(row)) + (p * near).sum(1, keepdims=True)
+        else:
+            row_off = (np.abs(do) * oslack[:, hq]).sum(1, keepdims=True)
+        ds_off = HALF * np.abs(ds) + 1.01 * p * (row_off + near) + 3 * dl * np.abs(ds)
         g["dv"][:, h] += p.T @ do
         sl["dv"][:, h] += (HALF + 3 * dl) * (p.T @ np.abs(do))
         g["dq"][:, hq] = scale * (ds @ k[:, h])

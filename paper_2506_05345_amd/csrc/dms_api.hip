@@ -915,8 +915,8 @@ int dms_window_attention_bwd(const dms_window_config* cfg, const int32_t* cu_seq
   if (!cu_seqlens_dev || !lse_dev || !workspace_dev || reinterpret_cast<uintptr_t>(workspace_dev) % dms::kAlign)
     return DMS_ERR_INVALID;
   if ((rc = check_aligned({q_dev, k_dev, v_dev, out_dev, dout_dev, dq_dev, dk_dev, dv_dev}))) return rc;
-  return hip_rc(dms::launch_window_bwd(*cfg, cu_seqlens_dev, q_dev, k_dev, v_dev, out_dev, lse_dev, dout_dev, dq_dev,
-                                       dk_dev, dv_dev, workspace_dev, as_stream(stream)));
+  return hip_rc(dms::launch_window_bwd(*cfg, cu_seqlens_dev, q_dev, k_dev, v_dev, lse_dev, dout_dev, dq_dev, dk_dev,
+                                       dv_dev, workspace_dev, as_stream(stream)));
 }
 
 }  // extern "C"

@@ -30,7 +30,7 @@ bool window_grids_fit(const dms_window_config& c);   // of a configuration that 
 hipError_t launch_window_fwd(const dms_window_config& c, const int32_t* cu, const void* q, const void* k,
                              const void* v, void* out, float* lse, void* ws, hipStream_t st);
 hipError_t launch_window_bwd(const dms_window_config& c, const int32_t* cu, const void* q, const void* k,
-                             const void* v, const void* out, const float* lse, const void* dout, void* dq,
+                             const void* v, const float* lse, const void* dout, void* dq,
                              void* dk, void* dv, void* ws, hipStream_t st);
 
 // Forks' and compactions' part of a context's workspace, its last bytes.

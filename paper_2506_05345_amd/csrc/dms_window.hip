@@ -5,8 +5,9 @@
 //   bwd: P = exp(s - lse), dP = dO V^T, D_t = dO.out, dS = P (dP - D),
 //        dQ = scale dS K, dK = scale dS^T Q, dV = P^T dO.
 // D_t is formed as sum_j P_j dP_j / sum_j P_j: from the rounded `out` it would be
-// off by 2^-9 of |dO||out|, which dS = P (dP - D) of a row with few keys does not
-// forgive (where one key takes nearly all the weight dP - D is nearly 0).
+// off by up to 2^-8 of |dO||out|, which dS = P (dP - D) of a row with few keys or
+// peaked weights does not forgive (where one key takes nearly all the weight
+// dP - D is nearly 0).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -27,7 +28,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 struct WindowArgs {
   const int32_t* cu;
-  const __bf16 *q, *k, *v, *o, *dout;
+  const __bf16 *q, *k, *v, *dout;
   const float* lse;
   __bf16 *out, *dq, *dk, *dv;
   float* lse_out;
@@ -494,18 +495,15 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// dQ pass.  Workgroups, columns and tiles as in the forward.  Per key tile:
-// S^T = K Q^T and dP^T = V dO^T over rows, dQ^T += K^T dS^T over columns.  It
-// also leaves -lse and -D of every row to the key-major pass.  EXACT: D_t is
-// summed from P and dP in a first walk over the tiles (two more products and no
-// reading of `out`), else formed from dO and the rounded `out`.  The latter puts
-// 0.0011 of error on dQ and dK (of their 2-norm, w = 256), where dS and the
-// output rounded to bf16 put 0.0017 each.  So that they stay near 0.002, dQ's
-// product takes dS in two bf16 parts (a second product; 636 to 667 us forward
-// and backward, 16384 tokens of 8 x 5 heads), and the key-major pass gets D with
-// sum_j dS_j added, which would be 0 for the true one (sum_j P_j = 1).  The pass
-// takes 245 to 270 us of the step (two waves of 252 registers per SIMD, matrix
-// core 42 % busy).
+// dQ pass.  Workgroups, columns and tiles as in the forward.  Two walks over
+// the key tiles, each S^T = K Q^T and dP^T = V dO^T over rows: the first sums
+// D_t from P and dP, the second adds dQ^T += K^T dS^T over columns.  The pass
+// also leaves -lse and -D of every row to the key-major pass.
+// D_t from dO and the rounded `out` costs no walk, but errors of up to 5 times a
+// row's own dQ where its weights are peaked (queries of scale 8, w = 256), with
+// dS in two bf16 parts in the last product already.  The walk makes a backward
+// of 16384 tokens of 8 x 5 heads take 573 us instead of 531 at w = 256, 1499
+// instead of 1328 at w = 1024.
 // ---------------------------------------------------------------------------
 // A dQ row as exact_row above.
 template <int D>
@@ -562,13 +560,12 @@ __device__ inline void exact_dq_row(const WindowArgs& a, int s0, int t, int hq) 
   }
 }
 
-template <int D, bool EXACT>
+template <int D>
 __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
   using Tile = TileOf<D>;
   constexpr int kUnit = Tile::kUnit, kKS = Tile::kKS, kDB = Tile::kDB;
   // [K | V] of two tiles, twice; the second pair of tiles, idle until the first step, also turns the waves' rows
   __shared__ __attribute__((aligned(256))) char tile_lds[2][4 * kUnit];
-  __shared__ float dsum_lds[kCols];
   const int2 wg = xcd_order();
   const int h = wg.y;
   const Block blk = block_of(a, wg.x, a.PB, a.inv_pb);
@@ -602,26 +599,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
   u32x4 qf[kKS], df[kKS];
   load_rows<D>(qf, a.q + first_row * D, rows);
   load_rows<D>(df, a.dout + first_row * D, rows);
-  float dcol = 0.f, psum = 0.f, rest = 0.f;
-  if (!EXACT) {
-    u32x4 ov[kKS];
-    load_rows<D>(ov, a.o + first_row * D, rows);
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {   // row 8 m + lane / 8: its pieces lie with 8 lanes
-      float d = 0.f;
-#pragma unroll
-      for (int x = 0; x < D / 64; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t d2 = df[4 * x + m][i], o2 = ov[4 * x + m][i];
-          d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, d2), __builtin_bit_cast(bf16x2, o2), d, false);
-        }
-#pragma unroll
-      for (int off = 1; off < 8; off <<= 1) d += __shfl_xor(d, off, 64);
-      if ((lane & 7) == 0) dsum_lds[wave * 32 + 8 * m + (lane >> 3)] = d;
-    }
-    dcol = dsum_lds[col];   // written by this wave
-  }
+  float dcol = 0.f, psum = 0.f;
   to_operands<D>(qf, rows, turn);
   to_operands<D>(df, rows, turn);
   const size_t at = static_cast<size_t>(h * a.g + qh) * a.T + s0 + t;
@@ -668,27 +646,12 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
         for (int e = 0; e < kAhead; ++e) op[e] = col_operand(tl, ad, e % kDB, e / kDB);
         float ds[16];
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          ds[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2, -lse2)) * dp[x];
-          if (!EXACT) rest += ds[x];
-        }
-        const u32x4 du[2] = {pack_bf16(ds), pack_bf16(ds + 8)};
-        u32x4 dl[2];   // what du's rounding left
-        if constexpr (!EXACT) {
-#pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            const uint32_t two = du[x >> 2][x & 3];
-            ds[2 * x] -= __uint_as_float(two << 16);
-            ds[2 * x + 1] -= __uint_as_float(two & 0xFFFF0000u);
-          }
-          dl[0] = pack_bf16(ds);
-          dl[1] = pack_bf16(ds + 8);
-        }
+        for (int x = 0; x < 16; ++x) ds[x] = __builtin_amdgcn_exp2f(fmaf(s[x], a.scale_log2, -lse2)) * dp[x];
+        const u32x4 du[2] = {pack_bf16(ds), pack_bf16(ds + 8)};   // half a step, 2^-8 of each, averaged over the row
 #pragma unroll
         for (int e = 0; e < 2 * kDB; ++e) {
           __builtin_amdgcn_sched_barrier(0);
           dqa[e % kDB] = mfma(op[e % kAhead], du[e / kDB], dqa[e % kDB]);
-          if constexpr (!EXACT) dqa[e % kDB] = mfma(op[e % kAhead], dl[e / kDB], dqa[e % kDB]);
           if (e + kAhead < 2 * kDB) op[e % kAhead] = col_operand(tl, ad, (e + kAhead) % kDB, (e + kAhead) / kDB);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -701,12 +664,10 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
       if (st + 1 < steps) attend(st + 1, std::integral_constant<int, 1>{}, sum_c);
     }
   };
-  if constexpr (EXACT) {
-    walk(std::true_type{});
-    dcol = col_sum(dcol) / col_sum(psum);
-    __syncthreads();   // every wave is done with the tiles
-    issue(0, 0);
-  }
+  walk(std::true_type{});
+  dcol = col_sum(dcol) / col_sum(psum);
+  __syncthreads();   // every wave is done with the tiles
+  issue(0, 0);
 #pragma unroll
   for (int i = 0; i < 16; ++i) start[i] = -dcol;
 #pragma unroll
@@ -714,7 +675,6 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) dqa[x][i] = 0.f;
   walk(std::false_type{});
-  if (!EXACT) dcol += col_sum(rest);
 
   if (ok) (hf ? a.nsum : a.nlse)[static_cast<size_t>(h * a.g + qh) * a.Ts + s0 + t] = hf ? -dcol : -lse2 / a.scale_log2;
   const float scale = a.single ? 0.f : a.scale_log2 / kLog2e;
@@ -1195,11 +1155,6 @@ WindowLayout window_layout(const dms_window_config& c) {
   return l;
 }
 
-// Rows of fewer than this many keys get their D_t from a walk over the keys of its own: `out`'s rounding weighs
-// on their small sums.  A whole step with the walk and without, 16384 tokens of 8 x 5 heads: 403 us against 408
-// at w = 16, 439 against 438 at 64, 535 against 505 at 120, 723 against 676 at 256.
-constexpr int kExactKeys = 128;
-
 // Workgroups of a KV head in each launch.
 struct WindowGrids {
   int64_t rows, keys, sums;   // query blocks; key blocks' shares and far queries; sums (0: no launch)
@@ -1214,10 +1169,9 @@ WindowGrids window_grids(const dms_window_config& c, const WindowLayout& l) {
 }
 
 template <int D>
-void launch_backward(const WindowArgs& a, const WindowGrids& w, bool exact, hipStream_t st) {
+void launch_backward(const WindowArgs& a, const WindowGrids& w, hipStream_t st) {
   auto grid = [&](int64_t x) { return dim3(static_cast<unsigned>(x), a.H); };
-  if (exact) hipLaunchKernelGGL((window_dq_kernel<D, true>), grid(w.rows), dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((window_dq_kernel<D, false>), grid(w.rows), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL(window_dq_kernel<D>, grid(w.rows), dim3(kThreads), 0, st, a);
   hipLaunchKernelGGL(window_dkv_kernel<D>, grid(w.keys), dim3(kThreads), 0, st, a);
   if (w.sums) hipLaunchKernelGGL(window_sum_kernel<D>, grid(w.sums), dim3(kThreads), 0, st, a);
 }
@@ -1244,7 +1198,7 @@ hipError_t launch_window_fwd(const dms_window_config& c, const int32_t* cu, cons
 }
 
 hipError_t launch_window_bwd(const dms_window_config& c, const int32_t* cu, const void* q, const void* k,
-                             const void* v, const void* out, const float* lse, const void* dout, void* dq,
+                             const void* v, const float* lse, const void* dout, void* dq,
                              void* dk, void* dv, void* ws, hipStream_t st) {
   WindowArgs a = window_args(c, cu, q, k, v);
   const WindowLayout l = window_layout(c);
@@ -1258,16 +1212,14 @@ hipError_t launch_window_bwd(const dms_window_config& c, const int32_t* cu, cons
   a.inv_far = inverse(l.far);
   a.sink_tiles = l.sink_tiles;
   a.splits = l.splits;
-  a.o = static_cast<const __bf16*>(out);
   a.lse = lse;
   a.dout = static_cast<const __bf16*>(dout);
   a.dq = static_cast<__bf16*>(dq);
   a.dk = static_cast<__bf16*>(dk);
   a.dv = static_cast<__bf16*>(dv);
-  const bool exact = a.w + a.sinks < kExactKeys;
   const WindowGrids grids = window_grids(c, l);
-  if (c.head_dim == 64) launch_backward<64>(a, grids, exact, st);
-  else launch_backward<128>(a, grids, exact, st);
+  if (c.head_dim == 64) launch_backward<64>(a, grids, st);
+  else launch_backward<128>(a, grids, st);
   return hipGetLastError();
 }
 
