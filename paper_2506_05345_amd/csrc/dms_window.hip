@@ -156,40 +156,96 @@ __device__ inline bool not_finite(float x) { return (__float_as_uint(x) & 0x7F80
 // 0 times an Inf or a NaN is a NaN, which every later sum keeps: one sum tells whether a row met any.
 __device__ inline bool is_nan(float x) { return (__float_as_uint(x) & 0x7FFFFFFFu) > 0x7F800000u; }
 
-// Row (position t of the sequence at s0, query head hq) by one wave, lanes over the head's elements and
-// only visible keys read: rows whose sums are not finite, where a product may have met an Inf or NaN of
-// a hidden key.  A score that is NaN itself makes all of the row NaN: the walk ends there, so that a step on
-// NaN inputs takes no longer than others.
+// The exact walks: a result whose sums may have met an Inf or NaN of a hidden key or query (0 times it is a
+// NaN) is formed again by one wave from what is visible alone.  A lane takes the weight of one of 64 keys or
+// rows, then all lanes add the 64, a pair of the head's elements each.  Only elements that were stored as NaN
+// are open; a walk ends, and leaves the stored ones, once all of these are NaN again, and it looks first at the
+// one key that every query sees, its own.  16384 tokens of 8 x 5 heads, w = 256, 4 sinks, forward and backward:
+// 139 and 595 us; all values NaN 264 and 732, all output gradients NaN 137 and 776, one token's values NaN 950
+// and 8700 (one key or row at a time and to the end, 29 ms and 124 ms, 142 us and 124 ms, 4 and 90 ms).  What
+// has to be walked to its end stays slow: all values +Inf 8 and 3 ms, all output gradients +Inf 0.1 and 47 ms.
+__device__ inline float low(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ inline float high(uint32_t pair) { return __uint_as_float(pair & 0xFFFF0000u); }
+// This lane's pair of a row's D elements (D = 64: two lanes to a pair).
+template <int D>
+__device__ inline uint32_t pair_of(const __bf16* row) {
+  return reinterpret_cast<const uint32_t*>(row)[threadIdx.x & (D / 2 - 1)];
+}
+template <int D>
+__device__ inline void store_pair(__bf16* row, float x, float y) {
+  const f32x2 pr = {x, y};
+  reinterpret_cast<uint32_t*>(row)[threadIdx.x & (D / 2 - 1)] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
+}
+// This lane's row times the row whose pairs lie over the lanes.
+template <int D>
+__device__ inline float row_dot(const __bf16* row, uint32_t pairs) {
+  float s = 0.f;
+#pragma unroll 2
+  for (int c = 0; c < D / 8; ++c) {
+    const u32x4 r = ld16(row + 8 * c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t two = r[i], other = __builtin_amdgcn_readlane(pairs, 4 * c + i);
+      s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), __builtin_bit_cast(bf16x2, other), s, false);
+    }
+  }
+  return s;
+}
+__device__ inline float lane_value(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane));
+}
+__device__ inline bool any_lane(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0; }
+constexpr int kAdd = 8;   // rows read together
+
+// What the wave has stored lies before what it reads next (other lanes' elements, through another type).
+__device__ inline void after_stores() { __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "workgroup"); }
+
+// Entry e of the keys that position t sees, listed without a gap from `base` on (as in KeyTiles).
+__device__ inline int seen_key(const WindowArgs& a, int base, int e) { return e < a.sinks ? e : base + e; }
+
+// Row (position t of the sequence at s0, query head hq) of the output, whose scores hold no NaN.
 template <int D>
 __device__ inline void exact_row(const WindowArgs& a, int s0, int t, int hq) {
-  constexpr int E = D / 64;
   const int lane = threadIdx.x & 63, Hq = a.H * a.g, h = hq / a.g;
-  const size_t row = (static_cast<size_t>(s0 + t) * Hq + hq) * D + E * lane;
-  float q[E], o[E] = {}, m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) q[e] = static_cast<float>(a.q[row + e]);
-  const int band = max(0, t - a.w + 1);
-  int j = a.sinks > 0 ? 0 : band;
+  auto key_row = [&](int j) { return (static_cast<size_t>(s0 + j) * a.H + h) * D; };
+  const size_t row = (static_cast<size_t>(s0 + t) * Hq + hq) * D;
+  after_stores();
+  const uint32_t was = pair_of<D>(a.out + row), own = pair_of<D>(a.v + key_row(t)), q = pair_of<D>(a.q + row);
+  const bool open0 = is_nan(low(was)), open1 = is_nan(high(was));
+  if (!any_lane((open0 && !is_nan(low(own))) || (open1 && !is_nan(high(own))))) return;
+  float o0 = 0.f, o1 = 0.f, m = -INFINITY, l = 0.f;
+  const int base = max(0, t - a.w + 1 - a.sinks), keys = t + 1 - base;
 #pragma unroll 1
-  while (j <= t) {
-    const size_t kr = (static_cast<size_t>(s0 + j) * a.H + h) * D + E * lane;
-    float s = 0.f;
+  for (int k0 = 0; k0 < keys; k0 += 64) {
+    const bool in = k0 + lane < keys;
+    const float x = row_dot<D>(a.k + key_row(seen_key(a, base, min(k0 + lane, keys - 1))), q) * a.scale_log2;
+    const float s = in ? x : -INFINITY;
+    if (any_lane(is_nan(s) || s == INFINITY)) return;   // all of the row is NaN, as it was stored
+    float mn = fmaxf(m, s);
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += q[e] * static_cast<float>(a.k[kr + e]);
-    s = wave_sum(s) * a.scale_log2;
-    if (is_nan(s)) {
-      l = s;
-      break;
-    }
-    const float mn = fmaxf(m, s), c = exp2f(m - mn), p = exp2f(s - mn);
-    l = l * c + p;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * c + p * static_cast<float>(a.v[kr + e]);
+    for (int off = 32; off; off >>= 1) mn = fmaxf(mn, __shfl_xor(mn, off, 64));
+    const float ref = mn == -INFINITY ? 0.f : mn;   // no weight so far: exp2(-Inf - 0) = 0
+    const float c = exp2f(m - ref), p = exp2f(s - ref);
+    l = l * c + wave_sum(p);
+    o0 *= c;
+    o1 *= c;
     m = mn;
-    j = j + 1 >= a.sinks ? max(j + 1, band) : j + 1;
-  }
+    const int n = min(64, keys - k0);
+#pragma unroll 1
+    for (int i = 0; i < n; i += kAdd) {
+      uint32_t v[kAdd];
 #pragma unroll
-  for (int e = 0; e < E; ++e) a.out[row + e] = static_cast<__bf16>(o[e] / l);
+      for (int u = 0; u < kAdd; ++u) v[u] = i + u < n ? pair_of<D>(a.v + key_row(seen_key(a, base, k0 + i + u))) : 0u;
+#pragma unroll
+      for (int u = 0; u < kAdd; ++u) {
+        const float pu = lane_value(p, i + u);
+        o0 += pu * low(v[u]);
+        o1 += pu * high(v[u]);
+      }
+      if (!any_lane((open0 && !is_nan(o0)) || (open1 && !is_nan(o1)))) return;
+    }
+  }
+  store_pair<D>(a.out + row, o0 / l, o1 / l);
   if (lane == 0) a.lse_out[static_cast<size_t>(hq) * a.T + s0 + t] = (m + log2f(l)) * kLn2;
 }
 
@@ -484,7 +540,8 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
   const float l = col_sum(l_run);
   const float inv = 1.0f / l;
   __syncthreads();   // every wave is done with the tiles
-  const bool bad = store_rows<D>(a.out + first_row * D, o, inv, rows, tiles + wave * kTurn, hf) || not_finite(inv);
+  // (weights that add to a NaN are those of visible scores: all of the row is NaN)
+  const bool bad = (store_rows<D>(a.out + first_row * D, o, inv, rows, tiles + wave * kTurn, hf) || not_finite(inv)) && !is_nan(l);
   if (ok && hf == 0)
     a.lse_out[static_cast<size_t>(h * a.g + qh) * a.T + s0 + t] = (m_ref * a.scale_log2 + __log2f(l)) * kLn2;
   const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && ok);
@@ -505,59 +562,60 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
 // of 16384 tokens of 8 x 5 heads take 573 us instead of 531 at w = 256, 1499
 // instead of 1328 at w = 1024.
 // ---------------------------------------------------------------------------
-// A dQ row as exact_row above.
+// A dQ row as exact_row above, whose lse is no NaN; the row's values for the key-major pass go with it.
 template <int D>
 __device__ inline void exact_dq_row(const WindowArgs& a, int s0, int t, int hq) {
-  constexpr int E = D / 64;
   const int lane = threadIdx.x & 63, Hq = a.H * a.g, h = hq / a.g;
-  const size_t row = (static_cast<size_t>(s0 + t) * Hq + hq) * D + E * lane;
-  float q[E], dO[E], dq[E] = {}, d = 0.f, sum = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    q[e] = static_cast<float>(a.q[row + e]);
-    dO[e] = static_cast<float>(a.dout[row + e]);
-  }
+  auto key_row = [&](int j) { return (static_cast<size_t>(s0 + j) * a.H + h) * D; };
+  const size_t row = (static_cast<size_t>(s0 + t) * Hq + hq) * D;
+  after_stores();
+  const uint32_t was = pair_of<D>(a.dq + row), own = pair_of<D>(a.v + key_row(t));
+  const uint32_t q = pair_of<D>(a.q + row), dO = pair_of<D>(a.dout + row);
+  const bool open0 = is_nan(low(was)), open1 = is_nan(high(was));
+  // a NaN D makes all of the row NaN, as it was stored
+  if (any_lane(is_nan(low(own)) || is_nan(high(own)) || is_nan(low(dO)) || is_nan(high(dO)))) return;
   const float lse2 = a.lse[static_cast<size_t>(hq) * a.T + s0 + t] * kLog2e;
-  const int band = max(0, t - a.w + 1);
+  float dq0 = 0.f, dq1 = 0.f, d = 0.f, sum = 0.f;
+  const int base = max(0, t - a.w + 1 - a.sinks), keys = t + 1 - base;
 #pragma unroll 1
   for (int pass = 0; pass < 2; ++pass) {
-    int j = a.sinks > 0 ? 0 : band;
 #pragma unroll 1
-    while (j <= t) {
-      const size_t kr = (static_cast<size_t>(s0 + j) * a.H + h) * D + E * lane;
-      float k[E], s = 0.f, dp = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        k[e] = static_cast<float>(a.k[kr + e]);
-        s += q[e] * k[e];
-        dp += dO[e] * static_cast<float>(a.v[kr + e]);
+    for (int k0 = 0; k0 < keys; k0 += 64) {
+      const bool in = k0 + lane < keys;
+      const size_t kr = key_row(seen_key(a, base, min(k0 + lane, keys - 1)));
+      const float x = exp2f(row_dot<D>(a.k + kr, q) * a.scale_log2 - lse2), dp = row_dot<D>(a.v + kr, dO);
+      if (!pass) {
+        d += wave_sum(in ? x * dp : 0.f);
+        sum += wave_sum(in ? x : 0.f);
+        if (is_nan(d)) return;
+        continue;
       }
-      const float p = exp2f(wave_sum(s) * a.scale_log2 - lse2);
-      dp = wave_sum(dp);
-      if (is_nan(p) || is_nan(dp)) {
-        d = NAN;
+      const float ds = x * (dp - d);
+      const int n = min(64, keys - k0);
+#pragma unroll 1
+      for (int i = 0; i < n; i += kAdd) {
+        uint32_t k[kAdd];
 #pragma unroll
-        for (int e = 0; e < E; ++e) dq[e] = NAN;
-        pass = 1;
-        break;
-      }
-      if (pass) {
+        for (int u = 0; u < kAdd; ++u) k[u] = i + u < n ? pair_of<D>(a.k + key_row(seen_key(a, base, k0 + i + u))) : 0u;
 #pragma unroll
-        for (int e = 0; e < E; ++e) dq[e] += p * (dp - d) * k[e];
-      } else {
-        d += p * dp;
-        sum += p;
+        for (int u = 0; u < kAdd; ++u) {
+          const float du = i + u < n ? lane_value(ds, i + u) : 0.f;
+          dq0 += du * low(k[u]);
+          dq1 += du * high(k[u]);
+        }
+        if (!any_lane((open0 && !is_nan(dq0)) || (open1 && !is_nan(dq1)))) return;
       }
-      j = j + 1 >= a.sinks ? max(j + 1, band) : j + 1;
     }
-    if (!pass) d /= sum;
+    if (!pass) {
+      d /= sum;
+      if (lane == 0) {
+        a.nlse[hq * a.Ts + s0 + t] = -lse2 / a.scale_log2;
+        a.nsum[hq * a.Ts + s0 + t] = -d;
+      }
+    }
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e) a.dq[row + e] = static_cast<__bf16>(a.single ? 0.f : dq[e] * a.scale_log2 / kLog2e);
-  if (lane == 0) {
-    a.nlse[hq * a.Ts + s0 + t] = -lse2 / a.scale_log2;
-    a.nsum[hq * a.Ts + s0 + t] = -d;
-  }
+  const float scale = a.scale_log2 / kLog2e;
+  store_pair<D>(a.dq + row, a.single ? 0.f : dq0 * scale, a.single ? 0.f : dq1 * scale);
 }
 
 template <int D>
@@ -679,7 +737,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
   if (ok) (hf ? a.nsum : a.nlse)[static_cast<size_t>(h * a.g + qh) * a.Ts + s0 + t] = hf ? -dcol : -lse2 / a.scale_log2;
   const float scale = a.single ? 0.f : a.scale_log2 / kLog2e;
   __syncthreads();   // every wave is done with the tiles
-  const bool bad = store_rows<D>(a.dq + first_row * D, dqa, scale, rows, tiles + wave * kTurn, hf) || not_finite(dcol);
+  const bool bad = (store_rows<D>(a.dq + first_row * D, dqa, scale, rows, tiles + wave * kTurn, hf) || not_finite(dcol)) && !is_nan(lse2);
   const uint64_t lanes = __builtin_amdgcn_ballot_w64(bad && ok);
   for (uint32_t cols = static_cast<uint32_t>(lanes | lanes >> 32); cols; cols &= cols - 1) {
     const int c = wave * 32 + __builtin_ctz(cols);
@@ -718,51 +776,69 @@ __device__ inline int far_begin(const WindowArgs& a, int j0) {
   return j0 < a.sinks ? max(end, a.far) : end;
 }
 
-// dK and dV of key j by one wave from the queries that see it.
+// dK and dV of key j as exact_row above, from the queries that see it.
 template <int D>
 __device__ inline void exact_key(const WindowArgs& a, int s0, int len, int j, int h) {
-  constexpr int E = D / 64;
   const int lane = threadIdx.x & 63, Hq = a.H * a.g;
-  const size_t kr = (static_cast<size_t>(s0 + j) * a.H + h) * D + E * lane;
-  float k[E], v[E], dk[E] = {}, dv[E] = {};
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    k[e] = static_cast<float>(a.k[kr + e]);
-    v[e] = static_cast<float>(a.v[kr + e]);
-  }
-  const int end = j < a.sinks ? len : static_cast<int>(min<int64_t>(len, static_cast<int64_t>(j) + a.w));
+  // row r: query j + r / g, head r % g of the group
+  auto query_row = [&](int r) { return (static_cast<size_t>(s0 + j + r / a.g) * Hq + h * a.g + r % a.g) * D; };
+  auto value_at = [&](int r) { return (h * a.g + r % a.g) * a.Ts + s0 + j + r / a.g; };
+  const size_t kr = (static_cast<size_t>(s0 + j) * a.H + h) * D;
+  after_stores();
+  const uint32_t was_k = pair_of<D>(a.dk + kr), was_v = pair_of<D>(a.dv + kr), own = pair_of<D>(a.dout + query_row(0));
+  const bool no_p = is_nan(a.nlse[value_at(0)]), no_ds = no_p || is_nan(a.nsum[value_at(0)]);
+  const bool open_k0 = is_nan(low(was_k)) && !no_ds, open_k1 = is_nan(high(was_k)) && !no_ds;
+  const bool open_v0 = is_nan(low(was_v)) && !no_p && !is_nan(low(own)), open_v1 = is_nan(high(was_v)) && !no_p && !is_nan(high(own));
+  if (!any_lane(open_k0 || open_k1 || open_v0 || open_v1)) return;
+  if (j < a.sinks) {
+    // The only queries that its sums met unseen are those before it in its tile of 32: where these are finite
+    // every NaN comes from a visible one (its walk would take all of a long sequence to tell).
+    bool met = false;
+    const int before = (j & 31) * a.g;
 #pragma unroll 1
-  for (int t = j; t < end; ++t)
-#pragma unroll 1
-    for (int hq = h * a.g; hq < (h + 1) * a.g; ++hq) {
-      const size_t qr = (static_cast<size_t>(s0 + t) * Hq + hq) * D + E * lane;
-      float q[E], dO[E], s = 0.f, dp = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        q[e] = static_cast<float>(a.q[qr + e]);
-        dO[e] = static_cast<float>(a.dout[qr + e]);
-        s += k[e] * q[e];
-        dp += v[e] * dO[e];
-      }
-      const size_t at = hq * a.Ts + s0 + t;
-      const float p = exp2f((wave_sum(s) + a.nlse[at]) * a.scale_log2), ds = p * (wave_sum(dp) + a.nsum[at]);
-      if (is_nan(p)) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) dk[e] = dv[e] = NAN;
-        t = end;
-        break;
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        dv[e] += p * dO[e];
-        dk[e] += ds * q[e];
-      }
+    for (int r = 0; r < before; ++r) {
+      const size_t qr = (static_cast<size_t>(s0 + (j & ~31) + r / a.g) * Hq + h * a.g + r % a.g) * D;
+      const uint32_t q = pair_of<D>(a.q + qr), dO = pair_of<D>(a.dout + qr);
+      met |= not_finite(low(q)) || not_finite(high(q)) || not_finite(low(dO)) || not_finite(high(dO));
     }
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    a.dk[kr + e] = static_cast<__bf16>(a.single ? 0.f : dk[e] * a.scale_log2 / kLog2e);
-    a.dv[kr + e] = static_cast<__bf16>(dv[e]);
+    if (!any_lane(met)) return;
   }
+  const uint32_t k = pair_of<D>(a.k + kr), v = pair_of<D>(a.v + kr);
+  float dk0 = 0.f, dk1 = 0.f, dv0 = 0.f, dv1 = 0.f;
+  const int end = j < a.sinks ? len : static_cast<int>(min<int64_t>(len, static_cast<int64_t>(j) + a.w));
+  const int rows = (end - j) * a.g;
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += 64) {
+    const int mine = min(r0 + lane, rows - 1);
+    const size_t qr = query_row(mine), at = value_at(mine);
+    const float p = exp2f((row_dot<D>(a.q + qr, k) + a.nlse[at]) * a.scale_log2);
+    const float ds = p * (row_dot<D>(a.dout + qr, v) + a.nsum[at]);
+    const int n = min(64, rows - r0);
+#pragma unroll 1
+    for (int i = 0; i < n; i += kAdd) {
+      uint32_t q[kAdd], dO[kAdd];
+#pragma unroll
+      for (int u = 0; u < kAdd; ++u) {
+        const size_t x = query_row(min(r0 + i + u, rows - 1));
+        q[u] = i + u < n ? pair_of<D>(a.q + x) : 0u;
+        dO[u] = i + u < n ? pair_of<D>(a.dout + x) : 0u;
+      }
+#pragma unroll
+      for (int u = 0; u < kAdd; ++u) {
+        const float pu = i + u < n ? lane_value(p, i + u) : 0.f, du = i + u < n ? lane_value(ds, i + u) : 0.f;
+        dv0 += pu * low(dO[u]);
+        dv1 += pu * high(dO[u]);
+        dk0 += du * low(q[u]);
+        dk1 += du * high(q[u]);
+      }
+      if (!any_lane((open_k0 && !is_nan(dk0)) || (open_k1 && !is_nan(dk1)) || (open_v0 && !is_nan(dv0)) ||
+                    (open_v1 && !is_nan(dv1))))
+        return;
+    }
+  }
+  const float scale = a.scale_log2 / kLog2e;
+  store_pair<D>(a.dk + kr, a.single ? 0.f : dk0 * scale, a.single ? 0.f : dk1 * scale);
+  store_pair<D>(a.dv + kr, dv0, dv1);
 }
 
 // Sums of the far queries of slot b: positions far c .. of the sequence that starts in the packed tokens'
