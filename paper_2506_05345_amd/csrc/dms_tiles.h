@@ -144,17 +144,18 @@ __device__ inline uint32_t lds_addr(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((DMS_LDS const char*)p));
 }
 // 64 lanes x 16 bytes (4 bytes) from base + off (per lane), or src (per lane), to LDS m0 + 16 (4) lane.  The LDS
-// destination goes in M0, written by the same statement; nothing else in this
-// file reads M0.  The compiler does not count these loads: the kernels wait
+// destination goes in M0, written by the same statement from a numbered scalar
+// register (not from VCC, so that every M0 write looks alike); nothing else in
+// this file reads M0.  The compiler does not count these loads: the kernels wait
 // for them (vmcnt) before the barrier that publishes a stage.
 __device__ inline void lds_copy16(const void* base, uint32_t off, uint32_t m0) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(m0), "v"(off), "s"(base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(m0), "v"(off), "s"(base) : "memory", "m0", "vcc");
 }
 __device__ inline void lds_copy16(const void* src, uint32_t m0) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(m0), "v"(src) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(m0), "v"(src) : "memory", "m0", "vcc");
 }
 __device__ inline void lds_copy4(const void* base, uint32_t off, uint32_t m0) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" : : "s"(m0), "v"(off), "s"(base) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" : : "s"(m0), "v"(off), "s"(base) : "memory", "m0", "vcc");
 }
 __device__ inline void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0F70); }   // vmcnt(0)
 // All but the N newest copies (fewer than 64) have landed.
