@@ -585,7 +585,10 @@ int dms_rope_bwd(const dms_rope_config* cfg, int tokens, const void* dq_dev, con
  * writes inside its tensors whatever cu_seqlens_dev holds; values that break its
  * rules make the rows of the sequences concerned undefined.  One workspace
  * (dms_window_workspace bytes, 256-byte aligned, contents of no meaning between
- * calls) serves one stream at a time.
+ * calls) serves one stream at a time.  Its size grows with total_tokens: row
+ * values of 8 bytes per query head, and with few tokens (fewer than 16384 / Hkv)
+ * or many sinks float32 sums of dk and dv, up to 64 d bytes of each per token and
+ * KV head.  The forward touches none of it: any aligned address will do there.
  */
 typedef struct dms_window_config {
   int32_t num_seqs;       /* n >= 1, at most 65535 */

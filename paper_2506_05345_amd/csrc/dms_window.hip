@@ -43,7 +43,7 @@ struct WindowArgs {
   int PB;                  // positions of a query block: kCols / g
   uint32_t inv_pb;         // 2^32 / PB + 1
   uint32_t inv_g;          // 65536 / g + 1: col / g = col * inv_g >> 16 for columns below 128
-  int far;                 // a sink's queries from this position on go to workgroups of `far` positions
+  int far;                 // a sink's queries from this position on go to workgroups of `far` positions (a multiple of 128)
   uint32_t inv_far;
   int sink_tiles;          // 32-key tiles of sinks with such queries
   int splits;              // workgroups that share a key block's steps
@@ -1027,7 +1027,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dkv_kernel(WindowArgs a) {
     len = f.len;
     key0 = 32 * (in_group - near);
     pos0 = max(f.p0 + a.far, far_begin(a, key0 & ~(kKeys - 1)));
-    const int last = min(len, f.p0 + 2 * a.far);
+    const int last = static_cast<int>(min<int64_t>(len, f.p0 + 2 * static_cast<int64_t>(a.far)));
     if (pos0 >= last || key0 >= len) return;
     list.tiles = (last - pos0 + 31) / 32;
     total = list.tiles * a.g;
@@ -1166,7 +1166,7 @@ __global__ __launch_bounds__(kThreads) void window_sum_kernel(WindowArgs a) {
 #pragma unroll 4
     for (int sp = 0; sp < a.splits; ++sp) add(share_sums(a, sp, blk.s0 + j, h, D), D);
   if (far) {
-    const int end = divide(blk.len + a.far - 1, a.far, a.inv_far);
+    const int end = divide(blk.len - 1, a.far, a.inv_far) + 1;
 #pragma unroll 4
     for (int c = divide(begin, a.far, a.inv_far); c < end; ++c) add(far_sums(a, slot + c, j >> 5, h, D) + (j & 31) * D, 32 * D);
   }
@@ -1218,8 +1218,13 @@ WindowLayout window_layout(const dms_window_config& c) {
   // x 6 heads, w = 256): forward and backward take 65 us, without shares 47 more, with far lists of 512 positions
   // 48; 1024 blocks (16384 tokens of 8 x 5 heads): 667 us, with far lists of 128 positions 79 more.
   l.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, kSplitTarget / std::max<int64_t>(1, blocks))));
-  l.far = blocks < kSplitTarget ? kKeys : 4 * kKeys;
   const int sinks = std::min(c.sinks, c.max_seqlen);
+  // Far lists as long as the sinks (a fourth of them where blocks are few) at least: their sums, T / far lists for
+  // each 32 sinks, then take no more than 32 D bytes of each token and KV head, and where all tokens are sinks
+  // (full attention) there are none.  16384 tokens of 8 x 5 heads, w = 256, 4096 sinks: 0.3 GB of workspace, backward
+  // 6.7 ms (lists of 512: 2.2 GB, 7.3 ms); all sinks: 5 MB, 13.0 ms (8.9 GB, 16.9 ms).
+  const bool few = blocks < kSplitTarget;
+  l.far = std::max(few ? kKeys : 4 * kKeys, static_cast<int>(align_up(few ? sinks / 4 : sinks, kKeys)));
   l.sink_tiles = c.max_seqlen > l.far ? (sinks + 31) / 32 : 0;
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, kAlign); return o; };
@@ -1256,10 +1261,11 @@ void launch_backward(const WindowArgs& a, const WindowGrids& w, hipStream_t st) 
 
 size_t window_workspace_bytes(const dms_window_config& c) { return window_layout(c).bytes; }
 
-// A grid holds fewer than 2^32 threads (more than that many rows, or sinks of hundreds of thousands of tokens).
+// A grid holds fewer than 2^32 threads.  Tokens times sinks have the limit that lists of 512 queries set.
 bool window_grids_fit(const dms_window_config& c) {
   const WindowGrids w = window_grids(c, window_layout(c));
-  return std::max({w.rows, w.keys, w.sums}) < (int64_t(1) << 32) / kThreads;
+  const int64_t sinks = c.max_seqlen > 512 ? (static_cast<int64_t>(std::min(c.sinks, c.max_seqlen)) + 31) / 32 : 0;
+  return std::max({w.rows, w.keys, w.sums, (c.total_tokens / 512 + int64_t(1)) * 8 * sinks}) < (int64_t(1) << 32) / kThreads;
 }
 
 hipError_t launch_window_fwd(const dms_window_config& c, const int32_t* cu, const void* q, const void* k,

@@ -795,7 +795,8 @@ def _check_window_args(cfg, where, workspace, cu_seqlens, **t):
         n = rows.get(name, T * H * cfg.group_size)
         specs.append((x, name, _F32, n) if name == "lse" else (x, name, _BF16, n * D))
     if workspace is not None and not isinstance(workspace, int):
-        specs.append((workspace, "workspace", _U8, dms_window_workspace(cfg)))
+        # the forward touches none of it
+        specs.append((workspace, "workspace", _U8, dms_window_workspace(cfg) if "dq" in t else 1))
     _args(where, *specs)
     _one_device(where, workspace, cu_seqlens, *t.values())
 

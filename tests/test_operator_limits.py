@@ -34,3 +34,14 @@ def test_scales_whose_row_values_leave_float32_are_refused(scale):
     assert dms.lib().dms_window_attention_bwd(B(cfg), *[SOME] * 11, None) == dms.DMS_ERR_INVALID
     for fine in (2.0 ** -100, 0.0, -1.0):
         assert dms.dms_window_workspace(dms.make_window_config(1, 100, 100, 2, 3, 128, 16, 4, fine)) > 0
+
+
+@pytest.mark.parametrize("tokens", [1777, 6000, 16384, 131072])
+@pytest.mark.parametrize("H,g,d", [(2, 6, 128), (8, 5, 128), (2, 2, 64)])
+def test_window_workspace_grows_with_the_tokens_alone(tokens, H, g, d):
+    """Row values of each query head and at most 64 d bytes of dk's and of dv's sums per token and KV head, however
+    many tokens are sinks."""
+    for sinks in (0, 64, 200, 513, 1024, 4096, tokens // 2, tokens):
+        cfg = dms.make_window_config(1, tokens, tokens, H, g, d, 256, sinks)
+        rows = 2 * H * g * (tokens + 128) * 4
+        assert dms.dms_window_workspace(cfg) <= rows + 2 * 64 * d * H * tokens + 65536, sinks
