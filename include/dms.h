@@ -290,7 +290,8 @@ int dms_seq_fork(dms_ctx* ctx, int layer, int n, const int32_t* src_ids_dev,
  * (popped U, U+1, ...).  Attention is unchanged.  The first U pages are then all
  * that a snapshot or an offload of the pool has to hold.
  * pages_used_out_dev: int32 [num_layers] (layer = -1) or [1], may be NULL:
- * receives U per layer. */
+ * receives U per layer.  With an error in the sticky status nothing moves and
+ * pages_used_out_dev stays as it was. */
 int dms_compact(dms_ctx* ctx, int layer, int32_t* pages_used_out_dev, void* stream);
 
 /* Append one token per listed sequence to one layer (Sec. 3.2 cache

@@ -6,12 +6,12 @@
 // retained lengths, so a one-workgroup plan per layer leaves prefix sums in the
 // workspace and the copy kernel's workgroups take equal shares of them.
 //
-// Measured, one layer of 8 heads, d = 128: 8 prompts of 32K tokens into 120
-// chains (2.0 GB), 8192 workgroups writing past the caches 370 us (5.5 TB/s);
-// 2048 of them 420 us, cached writes 570 us (4096 of these 525, 1024 665);
-// 16384, or 8 copies to a read, 390.  85 live of 128 chains compacted (1.5 GB):
-// 305 us with 24K workgroups, 330 with 8192, 350 with 2048.  A plain copy of 2
-// GiB reaches 5.1 TB/s, a fill 6.8.
+// Measured, one layer of 8 heads, d = 128, two pools in turn: 8 prompts of 32K
+// tokens into 120 chains (2.0 GB), 8192 workgroups writing past the caches 396 us
+// (5.1 TB/s; 357 at the shortest, 385 on one pool); 2048 of them 446, 16384 412,
+// 8 copies to a read 405, cached writes 461.  85 live of 128 chains compacted
+// (1.5 GB): 293 us with 24K workgroups, 311 with 8192, 329 with 2048.  A plain
+// copy of 2 GiB reaches 5.1 TB/s, a fill 6.8.
 #include <algorithm>
 
 #include "dms_ops.h"

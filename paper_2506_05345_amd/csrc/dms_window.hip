@@ -428,9 +428,14 @@ __device__ __forceinline__ void over_steps(int n, F f) {
 // columns are (position, query head) pairs, the g heads of a position
 // consecutive, 32 per wave.  The block's key tiles go through the LDS ring.
 // 16384 tokens of 8 x 5 heads, d = 128, w = 256, 4 sinks (405 MB, 86 GFLOP) take
-// 131 to 150 us.  Issue bounds it: a tile's 16 products take 512 cycles of a
-// SIMD's matrix core, its 117 other instructions, 16 of them exponentials at a
-// quarter of the rate, about 660.
+// 136 to 146 us among other calls (25 launches in a row from an idle clock 135 to
+// 201, 169 on average), d = 64 77 to 80.  A steady tile's 16 products take 512
+// cycles of a SIMD's matrix core beside 58 vector instructions and 16
+// exponentials at a quarter of the rate, 488 cycles, and long walks run at the
+// matrix core's rate (w = 4096: 1.0 ms, 1.2 PFLOP/s).  At w = 256 a walk is 9
+// tiles, and what lies around its steady tiles (the sequence search, the rows'
+// turns, edge masks, the first rescale) brings it to 162 vector instructions a
+// tile and leaves the matrix core 38 % busy.
 // ---------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
@@ -560,7 +565,8 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
 // row's own dQ where its weights are peaked (queries of scale 8, w = 256), with
 // dS in two bf16 parts in the last product already.  The walk makes a backward
 // of 16384 tokens of 8 x 5 heads take 573 us instead of 531 at w = 256, 1499
-// instead of 1328 at w = 1024.
+// instead of 1328 at w = 1024.  The pass takes 296 to 326 us of the former (two
+// waves of 237 registers per SIMD, matrix core 44 % busy).
 // ---------------------------------------------------------------------------
 // A dQ row as exact_row above, whose lse is no NaN; the row's values for the key-major pass go with it.
 template <int D>
@@ -753,10 +759,13 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
 // P, dS [query, key] from S = Q K^T, dP = dO V^T.
 // At d = 128 sums, operands and one step's scores fill the 256 registers of two
 // waves per SIMD, so that a wave takes one step at a time, with operands read two
-// ahead: while one wave forms weights the other has the matrix core.  One wave of
-// 512 registers that takes two steps together, operands read six ahead, ran
-// 400 us against 300 (16384 tokens of 8 x 5 heads, w = 256, 4 sinks); three and
-// four ahead spill in this form (+80 us).
+// ahead: while one wave forms weights the other has the matrix core.  16384 tokens
+// of 8 x 5 heads, w = 256, 4 sinks: 298 us at the shortest, 334 on average of 25
+// launches in a row, matrix core 39 % busy.  One wave of 512 registers that takes
+// two steps together, operands read six ahead, ran 400 us against 300; three and
+// four ahead spill in this form (+80 us).  Every step clears hidden weights, 48 of
+// its 126 vector instructions, and a wave waits through 3 of the 12 query tiles
+// that its block walks.
 // A sink is seen by every later query.  A block that holds sinks walks on to
 // position `far`; what lies further is shared out to workgroups of `far`
 // positions, whose waves take the steps in turn.
@@ -1215,8 +1224,8 @@ WindowLayout window_layout(const dms_window_config& c) {
   l.Ts = static_cast<int64_t>(T) + 128;
   const int64_t blocks = (static_cast<int64_t>(T) + kKeys - 1) / kKeys * c.num_kv_heads;
   // fewer blocks than CUs: shares of their steps, and shorter lists of far queries.  28 blocks (1777 tokens of 2
-  // x 6 heads, w = 256): forward and backward take 65 us, without shares 47 more, with far lists of 512 positions
-  // 48; 1024 blocks (16384 tokens of 8 x 5 heads): 667 us, with far lists of 128 positions 79 more.
+  // x 6 heads, w = 256, 16 sinks): forward and backward take 68 us, without shares 48 more, with far lists of 512
+  // positions 49; 1024 blocks (16384 tokens of 8 x 5 heads, 4 sinks): 726 us, with far lists of 128 positions 82 more.
   l.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, kSplitTarget / std::max<int64_t>(1, blocks))));
   const int sinks = std::min(c.sinks, c.max_seqlen);
   // Far lists as long as the sinks (a fourth of them where blocks are few) at least: their sums, T / far lists for
