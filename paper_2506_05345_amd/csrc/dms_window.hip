@@ -428,8 +428,8 @@ __device__ __forceinline__ void over_steps(int n, F f) {
 // columns are (position, query head) pairs, the g heads of a position
 // consecutive, 32 per wave.  The block's key tiles go through the LDS ring.
 // 16384 tokens of 8 x 5 heads, d = 128, w = 256, 4 sinks (405 MB, 86 GFLOP) take
-// 136 to 146 us among other calls (25 launches in a row from an idle clock 135 to
-// 201, 169 on average), d = 64 77 to 80.  A steady tile's 16 products take 512
+// 136 to 146 us among other calls (25 launches in a row from an idle clock 130 to
+// 205, 160 to 170 on average), d = 64 77 to 80.  A steady tile's 16 products take 512
 // cycles of a SIMD's matrix core beside 58 vector instructions and 16
 // exponentials at a quarter of the rate, 488 cycles, and long walks run at the
 // matrix core's rate (w = 4096: 1.0 ms, 1.2 PFLOP/s).  At w = 256 a walk is 9
@@ -565,7 +565,7 @@ __global__ __launch_bounds__(kThreads, 3) void window_fwd_kernel(WindowArgs a) {
 // row's own dQ where its weights are peaked (queries of scale 8, w = 256), with
 // dS in two bf16 parts in the last product already.  The walk makes a backward
 // of 16384 tokens of 8 x 5 heads take 573 us instead of 531 at w = 256, 1499
-// instead of 1328 at w = 1024.  The pass takes 296 to 326 us of the former (two
+// instead of 1328 at w = 1024.  The pass takes 290 to 330 us of the former (two
 // waves of 237 registers per SIMD, matrix core 44 % busy).
 // ---------------------------------------------------------------------------
 // A dQ row as exact_row above, whose lse is no NaN; the row's values for the key-major pass go with it.
@@ -760,7 +760,7 @@ __global__ __launch_bounds__(kThreads, 2) void window_dq_kernel(WindowArgs a) {
 // At d = 128 sums, operands and one step's scores fill the 256 registers of two
 // waves per SIMD, so that a wave takes one step at a time, with operands read two
 // ahead: while one wave forms weights the other has the matrix core.  16384 tokens
-// of 8 x 5 heads, w = 256, 4 sinks: 298 us at the shortest, 334 on average of 25
+// of 8 x 5 heads, w = 256, 4 sinks: 290 to 300 us at the shortest, 333 on average of 25
 // launches in a row, matrix core 39 % busy.  One wave of 512 registers that takes
 // two steps together, operands read six ahead, ran 400 us against 300; three and
 // four ahead spill in this form (+80 us).  Every step clears hidden weights, 48 of
