@@ -259,7 +259,7 @@ def _prepare_cache(case, seed):
     s["flags"] = (torch.rand((Ly, total, H), generator=gen, device=DEV) < case["evict"]).to(torch.uint8)
     if case["kind"] == "tree":
         s["q"] = _normal(gen, (total, H * g, d), bf, 2.0)
-        s["out"] = torch.empty((total, H * g, d), device=DEV)
+        s["out"] = torch.empty((total, H * g, d), dtype=bf, device=DEV)
     else:
         # accepted paths: from the root to a node of the tree
         path, lens = np.full(total, -1), []
@@ -400,7 +400,7 @@ def _run_tree(s):
     p = (p - p.amax(-1, keepdim=True)).exp_() * see
     out = (p @ v) / p.sum(-1, keepdim=True)
     out = out.view(n, H, M, g, d).permute(0, 2, 1, 3, 4).reshape(n, M, H * g, d)
-    s["out"][row[there]] = out[there]
+    s["out"][row[there]] = out[there].to(torch.bfloat16)
     return {"out": s["out"]}
 
 
@@ -484,7 +484,7 @@ def _work_tree(case):
     row = TILE_BYTES[case["kv"]](d) / 32 + 4
     nodes, kept = _nodes(case), _kept(case)
     mean = nodes / case["seqs"]
-    return {"bytes": H * kept * row + nodes * H * (4 * d + 1) + nodes * H * g * d * 6 + 4 * nodes,
+    return {"bytes": H * kept * row + nodes * H * (4 * d + 1) + nodes * H * g * d * 4 + 4 * nodes,
             "flops": 4 * d * g * H * (kept * mean + nodes * min(mean, 4))}
 
 
