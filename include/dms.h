@@ -620,6 +620,127 @@ int dms_window_attention_bwd(const dms_window_config* cfg, const int32_t* cu_seq
                              void* dq_dev, void* dk_dev, void* dv_dev, void* workspace_dev,
                              void* stream);
 
+/*
+ * Trees of drafted tokens (speculative decoding over the cache)
+ * -------------------------------------------------------------
+ * A draft proposes several continuations of each sequence, as a tree of tokens;
+ * one pass of the model attends them all, and the path of drafted tokens that
+ * agrees with what the model chooses is appended.  Sequence i of a call owns
+ * nodes cu_nodes[i] .. cu_nodes[i+1]-1 (int32 [n + 1] on the device, cu[0] = 0,
+ * non-decreasing, cu[n] = total_nodes, no tree larger than max_nodes <= 256;
+ * trees may be empty).  parents_dev: int32 [total_nodes], a node's parent by its
+ * index inside the tree, less than the node's own, or -1 for a root.  With pos
+ * tokens appended so far, a node of depth z (roots: 0) stands at position
+ * pos + z.  A root is commonly the last chosen token, not yet in the cache.
+ *
+ * A call reads its sizes on the host (total_nodes, max_nodes) and checks the
+ * device arrays against them: ones that break the rules set DMS_ERR_INVALID
+ * (ids: DMS_ERR_BAD_SEQ) in the sticky status, and nothing else changes.
+ * One workspace (dms_tree_workspace bytes for the context's configuration and a
+ * call's sizes, 256-byte aligned, contents of no meaning between calls) serves
+ * one stream at a time.
+ */
+int dms_tree_workspace(const dms_config* cfg, int n, int total_nodes, int max_nodes,
+                       size_t* workspace_bytes);
+
+/* Attention of every node over the cache of one layer and over its tree; the
+ * cache is left as it is.  A node at position t sees the retained tokens and the
+ * nodes on the path from its root to itself, each if it is not flagged or
+ * younger than w: key j is visible iff flag_j = 0 or j > t - w.  With a single
+ * path this is what dms_decode_step calls over the same tokens attend.
+ * q_dev: bf16 [total_nodes, Hq, d], k_dev, v_dev: bf16 [total_nodes, Hkv, d],
+ * flags_dev: uint8 [total_nodes, Hkv], out_dev: bf16 [total_nodes, Hq, d]; bf16
+ * tensors 16-byte aligned.  Weights are rounded to bf16 for their product with
+ * the values, softmax statistics and sums are float32.  8-bit pages: every key
+ * and value in its stored form, the drafted ones too.  With page retrieval
+ * (quest_page_budget > 0) all retained slots are attended, as in prefill.
+ * Delayed eviction only, and no latent rows (DMS_ERR_UNSUPPORTED).
+ * DMS_DECIDE_QUERY: use dms_tree_attention_q. */
+int dms_tree_attention(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev,
+                       const int32_t* cu_nodes_dev, int total_nodes, int max_nodes,
+                       const int32_t* parents_dev, const void* q_dev, const void* k_dev,
+                       const void* v_dev, const uint8_t* flags_dev, void* out_dev,
+                       void* workspace_dev, void* stream);
+
+/* dms_tree_attention with decisions read from the queries (DMS_DECIDE_QUERY
+ * only); the decisions taken are also written to decisions_out_dev (uint8
+ * [total_nodes, Hkv], may be NULL): the flags of the commit. */
+int dms_tree_attention_q(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev,
+                         const int32_t* cu_nodes_dev, int total_nodes, int max_nodes,
+                         const int32_t* parents_dev, const void* q_dev, const void* k_dev,
+                         const void* v_dev, uint8_t* decisions_out_dev, void* out_dev,
+                         void* workspace_dev, void* stream);
+
+/* The accepted path of every tree.  tokens_dev: int32 [total_nodes], the drafted
+ * tokens; targets_dev: int32 [total_nodes], the token that the model chose after
+ * each node (dms_sample over the nodes' logits).  The walk starts before the
+ * roots, wanting first_dev[i] (int32 [n]; NULL: it takes the first root as it
+ * is, and an empty tree's next token is -1), and goes on to the lowest child
+ * whose token is the wanted one; that child's target is wanted next.
+ * path_out_dev: int32 [total_nodes], sequence i's path as node indices inside
+ * its tree from cu_nodes[i] on, -1 for the rest of its tree; path_len_out_dev:
+ * int32 [n]; next_out_dev: int32 [n], the token wanted at the end, the next of
+ * the sequence.  No context and no status: values of cu_nodes_dev that break the
+ * rules are clamped to the tensors, parents that do are no node's children. */
+int dms_tree_accept(int n, const int32_t* cu_nodes_dev, int total_nodes, int max_nodes,
+                    const int32_t* parents_dev, const int32_t* tokens_dev,
+                    const int32_t* targets_dev, const int32_t* first_dev, int32_t* path_out_dev,
+                    int32_t* path_len_out_dev, int32_t* next_out_dev, void* stream);
+
+/* Append the nodes of one path per sequence to one layer: what dms_append_chunk
+ * does with the rows k[cu_nodes[i] + path[cu_nodes[i] + c]], c < path_len[i], in
+ * any page format and eviction mode, with counts that only the device knows.
+ * path_dev int32 [total_nodes] and path_len_dev int32 [n] as dms_tree_accept
+ * writes them (any path of nodes of the tree is taken); k_dev, v_dev, flags_dev:
+ * of all nodes, 16-byte aligned (latent rows: v_dev is ignored). */
+int dms_tree_commit(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev,
+                    const int32_t* cu_nodes_dev, int total_nodes, int max_nodes,
+                    const int32_t* path_dev, const int32_t* path_len_dev, const void* k_dev,
+                    const void* v_dev, const uint8_t* flags_dev, void* workspace_dev,
+                    void* stream);
+
+/*
+ * Sampling
+ * --------
+ * One token per row of logits, from given random numbers.  With x the row and
+ * T its temperature, the weight of token j is
+ *   w_j = round(2^43 exp((x_j - max x) / T)),
+ * an integer, formed in float64, so that every sum is exact.  Tokens sorted by
+ * logit (equal ones by index) are cut
+ *   to the first top_k (0, negative or past the vocabulary: all),
+ *   to the shortest prefix with at least top_p of what top-k left (1 and more,
+ *     or NaN: all; at least one token stays),
+ *   to those with w_j >= min_p 2^43, min_p at most 1 (0, negative or NaN: all);
+ * with S the weight of the rest, the token is the first by index at which the
+ * running weight exceeds u S.  T <= 0 or NaN is greedy: the largest logit, the
+ * lowest index of equal ones.  NaN logits count as -inf (never taken), +inf as
+ * the largest finite value; a row without any other logit gives token -1 and a
+ * NaN log-probability.  u is read as in [0, 1): below and NaN as 0, above as the
+ * largest float32 below 1.
+ */
+typedef struct dms_sample_config {
+  int32_t vocab;        /* logits of a row, 1 .. 2^20 */
+  int32_t logits_type;  /* DMS_TYPE_* */
+  float temperature;    /* settings of rows that have none of their own */
+  int32_t top_k;
+  float top_p;
+  float min_p;
+} dms_sample_config;
+
+/* Bytes of the workspace of a call of `rows` rows (256-byte aligned, contents of
+ * no meaning between calls, one stream at a time). */
+int dms_sample_workspace(const dms_sample_config* cfg, int rows, size_t* workspace_bytes);
+
+/* logits_dev [rows][vocab] with row_stride elements from a row to the next
+ * (>= vocab).  temperature_dev, top_p_dev, min_p_dev (float32 [rows]) and
+ * top_k_dev (int32 [rows]) may each be NULL: cfg's for every row.  u_dev: float32
+ * [rows].  tokens_out_dev: int32 [rows]; logprobs_out_dev: float32 [rows], the
+ * natural log of the token's probability after the cuts, may be NULL. */
+int dms_sample(const dms_sample_config* cfg, int rows, const void* logits_dev, int64_t row_stride,
+               const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev,
+               const float* min_p_dev, const float* u_dev, int32_t* tokens_out_dev,
+               float* logprobs_out_dev, void* workspace_dev, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

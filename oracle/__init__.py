@@ -11,3 +11,5 @@ from .kv_fp8 import *  # noqa: F401,F403
 from .quest import *  # noqa: F401,F403
 from .window_oracle import *  # noqa: F401,F403
 from .rope_oracle import *  # noqa: F401,F403
+from .tree_oracle import *  # noqa: F401,F403
+from .sample_oracle import *  # noqa: F401,F403

@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libdms.so")
 SOURCES = ["dms_api.hip", "dms_cache.hip", "dms_decode.hip", "dms_mla.hip", "dms_pages.hip",
-           "dms_prefill.hip", "dms_quest.hip", "dms_rope.hip", "dms_train.hip", "dms_window.hip"]
+           "dms_prefill.hip", "dms_quest.hip", "dms_rope.hip", "dms_sample.hip", "dms_train.hip",
+           "dms_tree.hip", "dms_window.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 instructions are kept out of every kernel.

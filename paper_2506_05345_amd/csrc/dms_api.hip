@@ -919,4 +919,141 @@ int dms_window_attention_bwd(const dms_window_config* cfg, const int32_t* cu_seq
                                        dv_dev, workspace_dev, as_stream(stream)));
 }
 
+// ---------------------------------------------------------------------------
+// Trees of drafted tokens
+// ---------------------------------------------------------------------------
+
+// Sizes of a tree call, host values.
+static int check_tree_sizes(const dms_config& c, int n, int total, int max_nodes) {
+  if (n < 1 || n > c.max_seqs || total < 0 || max_nodes < 0 || max_nodes > total) return DMS_ERR_INVALID;
+  if (total > 0 && max_nodes == 0) return DMS_ERR_INVALID;
+  if (max_nodes > dms::kTreeMaxNodes) return DMS_ERR_UNSUPPORTED;
+  if (total > static_cast<int64_t>(n) * max_nodes) return DMS_ERR_INVALID;
+  // rows of the query tensor in int32; grids of fewer than 2^32 threads: a
+  // workgroup of 256 per (head, 32 nodes), and per sequence
+  const int64_t heads = static_cast<int64_t>(n) * c.num_kv_heads, words = (max_nodes + 31) / 32;
+  if (static_cast<int64_t>(c.num_kv_heads) * c.group_size * total >= int64_t(1) << 31) return DMS_ERR_UNSUPPORTED;
+  if (1 + n + heads * std::max<int64_t>(words, 1) >= int64_t(1) << 24) return DMS_ERR_UNSUPPORTED;
+  return DMS_OK;
+}
+
+int dms_tree_workspace(const dms_config* cfg, int n, int total_nodes, int max_nodes, size_t* workspace_bytes) {
+  if (!cfg) return DMS_ERR_INVALID;
+  int rc = dms::validate_config(*cfg);
+  if (rc) return rc;
+  if ((rc = check_tree_sizes(*cfg, n, total_nodes, max_nodes))) return rc;
+  if (workspace_bytes) *workspace_bytes = dms::tree_workspace_bytes(*cfg, n, total_nodes, max_nodes);
+  return DMS_OK;
+}
+
+static int check_tree_call(const dms_ctx* ctx, int layer, int n, const void* seq_ids, const void* cu, int total,
+                           int max_nodes) {
+  int rc = check_call(ctx, layer, n, seq_ids);
+  if (rc) return rc;
+  if (!cu) return DMS_ERR_INVALID;
+  return check_tree_sizes(ctx->c.cfg, n, total, max_nodes);
+}
+
+static bool off_workspace(const void* ws) { return !ws || reinterpret_cast<uintptr_t>(ws) % dms::kAlign; }
+
+static int tree_attention(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev, const int32_t* cu_nodes_dev,
+                          int total_nodes, int max_nodes, const int32_t* parents_dev, const void* q_dev,
+                          const void* k_dev, const void* v_dev, const uint8_t* flags_dev, uint8_t* decisions_out_dev,
+                          bool from_q, void* out_dev, void* workspace_dev, void* stream) {
+  int rc = check_tree_call(ctx, layer, n, seq_ids_dev, cu_nodes_dev, total_nodes, max_nodes);
+  if (rc) return rc;
+  const dms::Ctx& c = ctx->c;
+  if (mla(ctx) || c.cfg.eviction != DMS_EVICT_DELAYED) return DMS_ERR_UNSUPPORTED;
+  if ((c.cfg.decision_source == DMS_DECIDE_QUERY) != from_q) return DMS_ERR_INVALID;
+  if (total_nodes == 0) return DMS_OK;
+  if (!parents_dev || (!from_q && !flags_dev) || off_workspace(workspace_dev)) return DMS_ERR_INVALID;
+  if ((rc = check_aligned({q_dev, k_dev, v_dev, out_dev}))) return rc;
+  return hip_rc(dms::launch_tree_attention(c.cfg, c.lo, c.meta, c.pools[layer], layer, n, seq_ids_dev, cu_nodes_dev,
+                                           total_nodes, max_nodes, parents_dev, q_dev, k_dev, v_dev, flags_dev,
+                                           decisions_out_dev, out_dev, workspace_dev, as_stream(stream)));
+}
+
+int dms_tree_attention(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev, const int32_t* cu_nodes_dev,
+                       int total_nodes, int max_nodes, const int32_t* parents_dev, const void* q_dev,
+                       const void* k_dev, const void* v_dev, const uint8_t* flags_dev, void* out_dev,
+                       void* workspace_dev, void* stream) {
+  return tree_attention(ctx, layer, n, seq_ids_dev, cu_nodes_dev, total_nodes, max_nodes, parents_dev, q_dev, k_dev,
+                        v_dev, flags_dev, nullptr, false, out_dev, workspace_dev, stream);
+}
+
+int dms_tree_attention_q(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev, const int32_t* cu_nodes_dev,
+                         int total_nodes, int max_nodes, const int32_t* parents_dev, const void* q_dev,
+                         const void* k_dev, const void* v_dev, uint8_t* decisions_out_dev, void* out_dev,
+                         void* workspace_dev, void* stream) {
+  return tree_attention(ctx, layer, n, seq_ids_dev, cu_nodes_dev, total_nodes, max_nodes, parents_dev, q_dev, k_dev,
+                        v_dev, nullptr, decisions_out_dev, true, out_dev, workspace_dev, stream);
+}
+
+int dms_tree_accept(int n, const int32_t* cu_nodes_dev, int total_nodes, int max_nodes, const int32_t* parents_dev,
+                    const int32_t* tokens_dev, const int32_t* targets_dev, const int32_t* first_dev,
+                    int32_t* path_out_dev, int32_t* path_len_out_dev, int32_t* next_out_dev, void* stream) {
+  if (n < 1 || n > dms::kMaxSeqs || total_nodes < 0 || max_nodes < 0 || max_nodes > total_nodes) return DMS_ERR_INVALID;
+  if (total_nodes > 0 && max_nodes == 0) return DMS_ERR_INVALID;
+  if (max_nodes > dms::kTreeMaxNodes) return DMS_ERR_UNSUPPORTED;
+  if (total_nodes > static_cast<int64_t>(n) * max_nodes) return DMS_ERR_INVALID;
+  if (!cu_nodes_dev || !path_len_out_dev || !next_out_dev) return DMS_ERR_INVALID;
+  if (total_nodes > 0 && (!parents_dev || !tokens_dev || !targets_dev || !path_out_dev)) return DMS_ERR_INVALID;
+  return hip_rc(dms::launch_tree_accept(n, cu_nodes_dev, total_nodes, max_nodes, parents_dev, tokens_dev, targets_dev,
+                                        first_dev, path_out_dev, path_len_out_dev, next_out_dev, as_stream(stream)));
+}
+
+int dms_tree_commit(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev, const int32_t* cu_nodes_dev,
+                    int total_nodes, int max_nodes, const int32_t* path_dev, const int32_t* path_len_dev,
+                    const void* k_dev, const void* v_dev, const uint8_t* flags_dev, void* workspace_dev, void* stream) {
+  int rc = check_tree_call(ctx, layer, n, seq_ids_dev, cu_nodes_dev, total_nodes, max_nodes);
+  if (rc) return rc;
+  if (total_nodes == 0) return DMS_OK;
+  if (!path_dev || !path_len_dev || !flags_dev || off_workspace(workspace_dev)) return DMS_ERR_INVALID;
+  const dms::Ctx& c = ctx->c;
+  if ((rc = check_aligned({k_dev, mla(ctx) ? k_dev : v_dev}))) return rc;
+  hipError_t e = dms::launch_tree_commit(c.cfg, c.lo, c.meta, c.pools[layer], layer, n, seq_ids_dev, cu_nodes_dev,
+                                         total_nodes, max_nodes, path_dev, path_len_dev, k_dev, v_dev, flags_dev,
+                                         workspace_dev, as_stream(stream));
+  // page retrieval: a path may write into any page of a head (reused slots)
+  if (e == hipSuccess && c.cfg.quest_page_budget > 0)
+    e = dms::launch_quest_bounds(c.cfg, c.lo, c.meta, c.ws, c.pools[layer], layer, n, true, seq_ids_dev,
+                                 as_stream(stream));
+  return hip_rc(e);
+}
+
+// ---------------------------------------------------------------------------
+// Sampling
+// ---------------------------------------------------------------------------
+
+static int validate_sample_config(const dms_sample_config* c, int rows) {
+  if (!c || c->vocab < 1 || rows < 0) return DMS_ERR_INVALID;
+  if (c->logits_type != DMS_TYPE_BF16 && c->logits_type != DMS_TYPE_F32) return DMS_ERR_INVALID;
+  if (c->vocab > dms::kSampleMaxVocab) return DMS_ERR_UNSUPPORTED;
+  // grids of fewer than 2^32 threads
+  if (rows >= 1 << 20) return DMS_ERR_UNSUPPORTED;
+  return DMS_OK;
+}
+
+int dms_sample_workspace(const dms_sample_config* cfg, int rows, size_t* workspace_bytes) {
+  const int rc = validate_sample_config(cfg, rows);
+  if (rc) return rc;
+  if (workspace_bytes) *workspace_bytes = dms::sample_workspace_bytes(*cfg, rows);
+  return DMS_OK;
+}
+
+int dms_sample(const dms_sample_config* cfg, int rows, const void* logits_dev, int64_t row_stride,
+               const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev,
+               const float* u_dev, int32_t* tokens_out_dev, float* logprobs_out_dev, void* workspace_dev,
+               void* stream) {
+  const int rc = validate_sample_config(cfg, rows);
+  if (rc) return rc;
+  // (offsets in bytes stay inside int64)
+  if (row_stride < cfg->vocab || row_stride >= int64_t(1) << 40) return DMS_ERR_INVALID;
+  if (rows == 0) return DMS_OK;
+  if (!logits_dev || !u_dev || !tokens_out_dev || off_workspace(workspace_dev)) return DMS_ERR_INVALID;
+  if (reinterpret_cast<uintptr_t>(logits_dev) % (cfg->logits_type == DMS_TYPE_BF16 ? 2 : 4)) return DMS_ERR_INVALID;
+  return hip_rc(dms::launch_sample(*cfg, rows, logits_dev, row_stride, temperature_dev, top_k_dev, top_p_dev, min_p_dev,
+                                   u_dev, tokens_out_dev, logprobs_out_dev, workspace_dev, as_stream(stream)));
+}
+
 }  // extern "C"

@@ -1,0 +1,1265 @@
+// Trees of drafted tokens over the cache, gfx950: attention of every node over
+// the retained slots and its own ancestors, the accepted path of a tree, and
+// the append of that path.
+//
+// Node x of a sequence at position pos (tokens appended so far) stands at
+// t = pos + depth(x), and sees
+//   a live slot of its KV head iff its token is not flagged or younger than w:
+//     flag = 0 or p > t - w (the delayed eviction that the tokens between would
+//     have done);
+//   the nodes on the path from the root to itself, by the same rule with their
+//   own flags.
+// Nothing is appended: a commit later appends the rows of one path.
+//
+// Attention is a split-K flash decode whose columns are the (node, query head)
+// pairs of a KV head.  Every launch of a call is small and fixed by the host;
+// what only the device knows (lengths) goes through the flat list of tiles:
+//   tree_prep_kernel    ancestors of every node as bits, depths, the drafted
+//                       rows as tiles in the pool's layout (8-bit pages: in
+//                       their stored form), prefix sums of the heads' tiles;
+//   tree_attn_kernel    workgroup w takes the w-th equal part of the flat list;
+//   tree_merge_kernel   joins the heads that several workgroups attended.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "dms_common.h"
+#include "dms_fp8.h"
+#include "dms_ops.h"
+#include "dms_tiles.h"
+
+namespace dms {
+namespace {
+
+#define DMS_CONST __attribute__((address_space(4)))
+
+constexpr float kRescale = 8.0f;       // lazy rescale threshold, log2 units
+constexpr float kMInit = -1.0e30f;     // running max before the first visible key
+constexpr int kPrepThreads = 256;
+
+__device__ inline int load_status(const int32_t* status) { return __atomic_load_n(status, __ATOMIC_RELAXED); }
+
+// One (sequence, KV head) of a call.
+struct __attribute__((aligned(32))) TreeRow {
+  int sh, L, tok0, m, p0, tile0, seq, pad;   // state head, live slots, first node, nodes, position, first tile of the tree
+};
+
+struct TreeArgs {
+  int32_t* status;
+  const int32_t* seq_ids;
+  const int32_t* cu;
+  const int32_t* parents;
+  const uint16_t* q;       // [total, Hq, D]
+  const uint16_t* k;       // [total, H, D]
+  const uint16_t* v;
+  const uint8_t* flags;    // [total, H]; with decisions from q: written by the preparation
+  uint8_t* flags_out;      // the same, or null
+  const char* pool;
+  const int32_t* page_table;
+  const int32_t* slot_meta;
+  const int32_t* len;
+  const int32_t* pos;
+  uint16_t* out;           // [total, Hq, D] bf16
+  TreeRow* rows;           // [n * H]
+  int32_t* cum;            // [n * H + 1] flat tiles before each head
+  uint32_t* anc;           // [total][words] ancestors and itself, bit a: node a of its tree
+  int32_t* depth;          // [total]
+  int32_t* node_seq;       // [total]
+  int32_t* deepest;        // [n]
+  char* tiles;             // [H][tph] tiles of the drafted rows
+  float* part_o;           // [2 G][UC][D]
+  float2* part_ml;         // [2 G][UC]
+  size_t page_bytes;
+  int n, H, g, w, P, log2P, maxp, max_slots, max_seqs, total, max_nodes, words, tph;
+  int G, UC, min_tiles;    // workgroups, columns of a unit, flat tiles a workgroup takes at least
+  int zero_neuron;
+  float bias, scale_log2;
+};
+
+__host__ __device__ inline int units_of(int cols, int UC) { return (cols + UC - 1) / UC; }
+__device__ inline int tiles_of(int L, int m) { return ((L + 31) >> 5) + ((m + 31) >> 5); }
+// Workgroups that share `total` flat tiles, and where part w begins.
+__device__ inline int parts_of(int total, int min_tiles, int G) { return max(1, min(G, total / min_tiles)); }
+__device__ inline int part_begin(int w, int total, int parts) {
+  return static_cast<int>(static_cast<int64_t>(w) * total / parts);
+}
+__device__ inline int part_holding(int tile, int total, int parts) {
+  return static_cast<int>((static_cast<int64_t>(tile + 1) * parts - 1) / total);
+}
+
+// ---------------------------------------------------------------------------
+// Preparation
+// ---------------------------------------------------------------------------
+
+// Block 0: the call's ids and sizes are checked, the heads described and their
+// flat tiles summed.
+__device__ void tree_plan(const TreeArgs& a) {
+  __shared__ uint32_t seen[kMaxSeqs / 32];
+  __shared__ int lds[17];
+  for (int i = threadIdx.x; i < (a.max_seqs + 31) / 32; i += blockDim.x) seen[i] = 0;
+  __syncthreads();
+  int bad_id = 0, bad = 0;
+  for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
+    const int s = a.seq_ids[i], c0 = a.cu[i], c1 = a.cu[i + 1];
+    if (s < 0 || s >= a.max_seqs) bad_id = 1;
+    else if (atomicOr(&seen[s >> 5], 1u << (s & 31)) & (1u << (s & 31))) bad_id = 1;
+    bad |= c0 < 0 || c1 < c0 || c1 > a.total || c1 - c0 > a.max_nodes;
+    bad |= (i == 0 && c0 != 0) || (i == a.n - 1 && c1 != a.total);
+  }
+  bad_id = __syncthreads_or(bad_id);
+  bad = __syncthreads_or(bad);
+  if (bad_id || bad) {
+    if (threadIdx.x == 0) set_status(a.status, bad_id ? DMS_ERR_BAD_SEQ : DMS_ERR_INVALID);
+    return;
+  }
+  const int NH = a.n * a.H;
+  int run = 0;
+  for (int base = 0; base < NH; base += blockDim.x) {
+    const int hh = base + threadIdx.x;
+    int tiles = 0;
+    if (hh < NH) {
+      const int i = hh / a.H, s = a.seq_ids[i], c0 = a.cu[i];
+      TreeRow r;
+      r.sh = s * a.H + hh % a.H;
+      r.L = a.len[r.sh];
+      r.tok0 = c0;
+      r.m = a.cu[i + 1] - c0;
+      r.p0 = a.pos[s];
+      r.tile0 = (hh % a.H) * a.tph + c0 / 32 + i;
+      r.seq = i;
+      r.pad = 0;
+      a.rows[hh] = r;
+      tiles = r.m ? tiles_of(r.L, r.m) * units_of(r.m * a.g, a.UC) : 0;
+    }
+    int tot;
+    const int ex = block_exclusive_scan(tiles, lds, &tot);
+    if (hh < NH) a.cum[hh] = run + ex;
+    run += tot;
+  }
+  if (threadIdx.x == 0) a.cum[NH] = run;
+}
+
+// The next n blocks: ancestors of a sequence's nodes.  Bits and jumps double
+// until every node's jump has left the tree (at most 8 rounds of 256 nodes, where
+// a walk up a chain would take as many dependent reads as nodes).
+__device__ void tree_ancestors(const TreeArgs& a, int i) {
+  __shared__ uint32_t bits[kTreeMaxNodes][kTreeWords + 1];   // (odd stride: rows spread over the banks)
+  __shared__ int jump[kTreeMaxNodes];
+  __shared__ int deepest;
+  const int tok0 = max(0, min(a.cu[i], a.total)), end = max(tok0, min(a.cu[i + 1], a.total));
+  const int m = min(end - tok0, a.max_nodes);
+  const int x = threadIdx.x;
+  if (x == 0) deepest = 0;
+  int mine = -1;
+  if (x < m) {
+    mine = a.parents[tok0 + x];
+    if (mine < -1 || mine >= x) {
+      set_status(a.status, DMS_ERR_INVALID);
+      mine = -1;
+    }
+    for (int u = 0; u < a.words; ++u) bits[x][u] = 0;
+    bits[x][x >> 5] = 1u << (x & 31);
+    jump[x] = mine;
+  }
+  __syncthreads();
+  for (int span = 1; span < m; span *= 2) {
+    uint32_t add[kTreeWords];
+    int next = -1;
+    const int j = x < m ? jump[x] : -1;
+    if (j >= 0) {
+      next = jump[j];
+#pragma unroll
+      for (int u = 0; u < kTreeWords; ++u) add[u] = u < a.words ? bits[j][u] : 0u;
+    }
+    __syncthreads();
+    if (j >= 0) {
+#pragma unroll
+      for (int u = 0; u < kTreeWords; ++u)
+        if (u < a.words) bits[x][u] |= add[u];
+      jump[x] = next;
+    }
+    __syncthreads();
+  }
+  if (x < m) {
+    int d = -1;
+    for (int u = 0; u < a.words; ++u) {
+      const uint32_t b = bits[x][u];
+      d += __popc(b);
+      a.anc[static_cast<size_t>(tok0 + x) * a.words + u] = b;
+    }
+    a.depth[tok0 + x] = d;
+    a.node_seq[tok0 + x] = i;
+    atomicMax(&deepest, d);
+  }
+  __syncthreads();
+  if (x == 0) a.deepest[i] = deepest;
+}
+
+// The other blocks: 32 drafted rows of one KV head as a tile; rows past the tree
+// are 0.
+template <int D, bool FP8>
+__device__ void tree_tile(const TreeArgs& a, int hh, int k) {
+  __shared__ uint16_t vrows[32][D + 2];
+  const int i = hh / a.H, h = hh % a.H, tid = threadIdx.x;
+  const int tok0 = a.cu[i], m = a.cu[i + 1] - tok0;
+  if (tok0 < 0 || m < 0 || m > a.max_nodes || tok0 + m > a.total || 32 * k >= m) return;
+  if (a.flags_out != nullptr && tid < 32 && 32 * k + tid < m) {
+    const size_t node = static_cast<size_t>(tok0) + 32 * k + tid;
+    const uint32_t bits = a.q[(node * a.H + h) * a.g * D];
+    a.flags_out[node * a.H + h] = (__uint_as_float(bits << 16) + a.bias) > 0.f;
+  }
+  constexpr int kPieces = 32 * D / 8;
+  const int tile0 = h * a.tph + tok0 / 32 + i + k;
+  char* tile = a.tiles + static_cast<size_t>(tile0) * (FP8 ? fp8_tile_bytes(D) : tile_bytes(D));
+  for (int pc = tid; pc < kPieces; pc += kPrepThreads) {
+    const int j = pc / (D / 8), part = pc % (D / 8), e0 = 8 * part;
+    uint4 kx = make_uint4(0u, 0u, 0u, 0u), vx = make_uint4(0u, 0u, 0u, 0u);
+    if (32 * k + j < m) {
+      const size_t row = ((static_cast<size_t>(tok0) + 32 * k + j) * a.H + h) * D + e0;
+      kx = *reinterpret_cast<const uint4*>(a.k + row);
+      vx = *reinterpret_cast<const uint4*>(a.v + row);
+    }
+    if constexpr (FP8) {
+      fp8_store_token(tile, j, D, part, kx, vx);
+    } else {
+      *reinterpret_cast<uint4*>(tile + k_elem_off(j, e0)) = kx;
+      const uint32_t vw[4] = {vx.x, vx.y, vx.z, vx.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) vrows[j][e0 + e] = static_cast<uint16_t>(vw[e >> 1] >> (16 * (e & 1)));
+    }
+  }
+  if constexpr (!FP8) {
+    __syncthreads();
+    // value piece x: dim x / 4, rows 8 (x % 4) .. + 7
+    for (int x = tid; x < kPieces; x += kPrepThreads) {
+      const int e = x >> 2, j0 = 8 * (x & 3);
+      u32x4 p;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        p[t] = static_cast<uint32_t>(vrows[j0 + 2 * t][e]) | (static_cast<uint32_t>(vrows[j0 + 2 * t + 1][e]) << 16);
+      *reinterpret_cast<u32x4*>(tile + v_elem_off(j0, e, D)) = p;
+    }
+  }
+}
+
+template <int D, bool FP8>
+__global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a) {
+  if (load_status(a.status) != 0) return;
+  const unsigned b = blockIdx.x;
+  if (b == 0) {
+    tree_plan(a);
+  } else if (b <= static_cast<unsigned>(a.n)) {
+    tree_ancestors(a, b - 1);
+  } else {
+    const unsigned x = b - 1 - a.n;
+    tree_tile<D, FP8>(a, x / a.words, x % a.words);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Attention
+// ---------------------------------------------------------------------------
+
+// The operands of one 32-row tile as a wave's 32x32x16 products take them:
+//   keys: lane l of k-step s holds dims 16 s + 8 (l / 32) .. + 7 of row
+//     row_token(l % 32);
+//   values: lane l of (32-dim block b, half y) holds rows 16 y + 8 (l / 32) .. + 7
+//     of dim 32 b + l % 32;
+// and the lane's row (position | flag << 31 of row l % 32).
+template <int D>
+struct TileRegs {
+  u32x4 k[D / 16], v[D / 32][2];
+  uint32_t meta;
+};
+// 8-bit tile: codes as stored, the key scale of the lane's key row, the value
+// scales of its 16 rows.
+template <int D>
+struct TileRegsF8 {
+  u32x4 k[D / 32];      // [p][y]: dims 64 p + 16 y + 8 (l / 32) .., then the same + 32
+  u32x2 v[D / 32][2];
+  u32x4 vs[2][2];
+  float ks;
+  uint32_t meta;
+};
+
+// NT: the tile is read by this wave alone
+template <bool NT>
+__device__ inline u32x4 ldt16(const char* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return *reinterpret_cast<const u32x4*>(p);
+}
+template <bool NT>
+__device__ inline u32x2 ldt8(const char* p) {
+  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+  return *reinterpret_cast<const u32x2*>(p);
+}
+
+struct LaneAt {
+  int k, v;     // byte offsets of the lane's first key and value piece in a tile
+  int ks, vs;   // and of its scales (8-bit pages)
+};
+
+template <bool NT, int D>
+__device__ inline void load_tile(TileRegs<D>& r, const char* tile, const LaneAt& at) {
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) r.k[s] = ldt16<NT>(tile + at.k + (s >> 1) * 2048 + (s & 1) * 512);
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) r.v[b][y] = ldt16<NT>(tile + at.v + b * 2048 + y * 512);
+}
+template <bool NT, int D>
+__device__ inline void load_tile(TileRegsF8<D>& r, const char* tile, const LaneAt& at) {
+#pragma unroll
+  for (int x = 0; x < D / 32; ++x) r.k[x] = ldt16<NT>(tile + at.k + (x >> 1) * 2048 + (x & 1) * 512);
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) r.v[b][y] = ldt8<NT>(tile + at.v + b * 1024 + y * 512);
+  r.ks = *reinterpret_cast<const float*>(tile + at.ks);
+#pragma unroll
+  for (int y = 0; y < 2; ++y)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) r.vs[y][x] = ld16(tile + at.vs + y * 128 + x * 16);
+}
+
+// 8 E4M3 codes to bf16 times a power of two (exact)
+__device__ inline u32x4 f8_bf16x8(uint32_t w0, uint32_t w1, float scale) {
+  u32x4 o;
+  o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, false));
+  o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, scale, true));
+  o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, false));
+  o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true));
+  return o;
+}
+template <int D>
+__device__ inline void operands(const TileRegs<D>& r, u32x4 (&k)[D / 16], u32x4 (&v)[D / 32][2]) {
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) k[s] = r.k[s];
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b) v[b][0] = r.v[b][0], v[b][1] = r.v[b][1];
+}
+template <int D>
+__device__ inline void operands(const TileRegsF8<D>& r, u32x4 (&k)[D / 16], u32x4 (&v)[D / 32][2]) {
+  // piece (p, y) holds k-steps 4 p + y and 4 p + 2 + y
+#pragma unroll
+  for (int x = 0; x < D / 32; ++x) {
+    k[4 * (x >> 1) + (x & 1)] = f8_bf16x8(r.k[x][0], r.k[x][1], r.ks);
+    k[4 * (x >> 1) + 2 + (x & 1)] = f8_bf16x8(r.k[x][2], r.k[x][3], r.ks);
+  }
+#pragma unroll
+  for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) v[b][y] = f8_bf16x8(r.v[b][y][0], r.v[b][y][1], 1.0f);
+}
+// value scale of the lane's row 8 (i / 8) + i % 8 of 16 (1 for bf16 pages)
+template <int D>
+__device__ inline float value_scale(const TileRegs<D>&, int) { return 1.0f; }
+template <int D>
+__device__ inline float value_scale(const TileRegsF8<D>& r, int i) {
+  return __uint_as_float(r.vs[i >> 3][(i >> 2) & 1][i & 3]);
+}
+// value (row j, dim e) of a stored tile; an 8-bit one without its scale
+template <int D, bool FP8>
+__device__ inline float stored_value(const char* tile, int j, int e) {
+  if constexpr (FP8)
+    return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(*reinterpret_cast<const uint8_t*>(tile + fp8_v_off(j, e, D))), 0);
+  else
+    return __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(tile + v_elem_off(j, e, D))) << 16);
+}
+
+// A segment of the flat list: tiles t0 .. t1 - 1 of unit `unit` of head hh.
+struct Segment {
+  TreeRow r;
+  int hh, unit, t0, t1, T, nc, deep;
+};
+
+// The state of a wave's NC blocks of 32 columns; lane l: column l % 32.
+template <int D, int NC>
+struct Columns {
+  u32x4 q[NC][D / 16];
+  f32x16 o[NC][D / 32];
+  float m[NC], l[NC];
+  int t[NC];              // position of the column's node
+  const uint32_t* anc[NC];   // its ancestors, one word per tile of the tree
+};
+
+template <int D, bool FP8, int NC, class Regs>
+__device__ __forceinline__ void attend_tile(const TreeArgs& a, const Segment& sg, Columns<D, NC>& c, const Regs& r,
+                                            const char* tile, int t, int blocks, int lane) {
+  constexpr int KS = D / 16, OB = D / 32;
+  const int hf = lane >> 5;
+  const float sl2 = a.scale_log2, thr = kRescale / sl2;
+  const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
+  u32x4 kf[KS], vf[OB][2];
+  operands(r, kf, vf);
+  // rows that some column does not see: none there, flagged and old enough for the
+  // deepest node, or any row of the tree
+  const bool tree = t >= sg.nc;
+  const int rows = tree ? sg.r.m - 32 * (t - sg.nc) : sg.r.L - 32 * t;
+  const uint32_t alive = rows >= 32 ? ~0u : (1u << rows) - 1u;
+  const bool soon = (r.meta & kFlagBit) != 0 && sg.deep - static_cast<int>(r.meta & ~kFlagBit) >= a.w;
+  const uint32_t old = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(soon)) & alive;
+  const bool masked = tree || old != 0 || alive != ~0u;
+  uint32_t odd = 0;       // rows whose values are not finite and which some column may not see
+  if (masked) {
+    // A hidden row takes part with weight 0, and 0 times an infinity or NaN is NaN:
+    // values of rows past the end are zeroed; those of rows that are not
+    // finite too, and are added by hand to the columns that see them.
+    uint32_t mine = 0;
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int b = 0; b < OB; ++b) {
+          const uint32_t x = (vf[b][y][e >> 1] >> (16 * (e & 1))) & 0x7F80u;
+          any |= x == 0x7F80u;
+        }
+        mine |= any << (16 * y + e);
+      }
+    mine <<= 8 * hf;
+#pragma unroll
+    for (int off = 32; off; off >>= 1) mine |= __shfl_xor(mine, off, 64);
+    odd = __builtin_amdgcn_readfirstlane(mine) & alive;
+    const uint32_t keep = (alive & ~odd) >> (8 * hf);
+    if ((alive & ~odd) != ~0u) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t bit = keep >> (16 * y + 2 * e);
+          const uint32_t and_ = ((bit & 1) ? 0x0000FFFFu : 0u) | ((bit & 2) ? 0xFFFF0000u : 0u);
+#pragma unroll
+          for (int b = 0; b < OB; ++b) vf[b][y][e] &= and_;
+        }
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < NC; ++x) {
+    if (x >= blocks) break;
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int e = 0; e < KS; ++e) s = mfma(kf[e], c.q[x][e], s);
+    uint32_t vis = ~0u;
+    if (masked) {
+      vis = alive;
+      if (tree) vis &= c.anc[x][t - sg.nc];
+      for (uint32_t left = old; left; left &= left - 1) {
+        const int j = __builtin_ctz(left);
+        const int kp = static_cast<int>(__builtin_amdgcn_readlane(static_cast<int>(r.meta), j) & ~kFlagBit);
+        if (c.t[x] - kp >= a.w) vis &= ~(1u << j);
+      }
+      const uint32_t mine = vis >> (8 * hf);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = (mine >> (16 * (i >> 3) + (i & 7))) & 1 ? s[i] : -INFINITY;
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    mx = col_max(mx);
+    const bool raise = mx > c.m[x] + thr;   // false while the column has seen no key
+    if (__builtin_amdgcn_ballot_w64(raise)) {
+      const float m_new = raise ? mx : c.m[x];
+      const float alpha = __builtin_amdgcn_exp2f((c.m[x] - m_new) * sl2);
+      c.l[x] *= alpha;
+#pragma unroll
+      for (int b = 0; b < OB; ++b) c.o[x][b] *= alpha;
+      c.m[x] = m_new;
+    }
+    // weights 2^((s - m) scale), rounded to bf16 for the products; the
+    // denominator adds the rounded values, so that one dominant key returns its
+    // value row exactly.  8-bit pages: the weight of the product carries the
+    // value scale, a power of two
+    const float mb = c.m[x] * sl2;
+    u32x4 pu[2];
+    float w[16];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const f32x2 pr = {__builtin_amdgcn_exp2f(fmaf(s[2 * j], sl2, -mb)),
+                        __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], sl2, -mb))};
+      const bf16x2 pb = __builtin_convertvector(pr, bf16x2);
+      c.l[x] = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, c.l[x], false);
+      w[2 * j] = static_cast<float>(pb[0]);
+      w[2 * j + 1] = static_cast<float>(pb[1]);
+      if constexpr (FP8) {
+        w[2 * j] *= value_scale(r, 2 * j);
+        w[2 * j + 1] *= value_scale(r, 2 * j + 1);
+        const f32x2 ws = {w[2 * j], w[2 * j + 1]};
+        pu[j >> 2][j & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(ws, bf16x2));
+      } else {
+        pu[j >> 2][j & 3] = __builtin_bit_cast(uint32_t, pb);
+      }
+    }
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int b = 0; b < OB; ++b) c.o[x][b] = mfma(vf[b][y], pu[y], c.o[x][b]);
+    for (uint32_t left = odd; left; left &= left - 1) {
+      const int j = __builtin_ctz(left);
+      float pj = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (i == 8 * (j >> 4) + (j & 7)) pj = w[i];
+      pj = __shfl(pj, (lane & 31) + 32 * ((j >> 3) & 1), 64);
+      const bool seen = (vis >> j) & 1;
+#pragma unroll
+      for (int b = 0; b < OB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float val = stored_value<D, FP8>(tile, j, 32 * b + 8 * (i >> 2) + 4 * hf + (i & 3));
+          c.o[x][b][i] = seen ? fmaf(pj, val, c.o[x][b][i]) : c.o[x][b][i];
+        }
+    }
+  }
+}
+
+// Workgroup: 4 waves, CW of them side by side over the columns of a unit (NC
+// blocks of 32 each), 4 / CW over its tiles.  A wave streams its tiles straight
+// into operand registers, the next one's loads in flight while it attends the
+// present one; waves meet only to fold their results at a segment's end.
+template <int D, bool FP8, int NC, int CW>
+__global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
+  constexpr int KW = 4 / CW, KS = D / 16, OB = D / 32, UC = 32 * NC * CW;
+  constexpr size_t TB = FP8 ? static_cast<size_t>(D) * 64 + 256 : static_cast<size_t>(D) * 128;
+  using Regs = typename std::conditional<FP8, TileRegsF8<D>, TileRegs<D>>::type;
+  __shared__ __attribute__((aligned(16))) float fold[4][32][D + 4];
+  __shared__ float2 ml_lds[4][32 * NC];
+  __shared__ int first[4];
+  if (load_status(a.status) != 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cw = wave % CW, kw = wave / CW;
+  const int NH = a.n * a.H, Hq = a.H * a.g;
+  const int total = *(const DMS_CONST int32_t*)(a.cum + NH);
+  const int parts = parts_of(total, a.min_tiles, a.G);
+  if (static_cast<int>(blockIdx.x) >= parts || total == 0) return;
+  const int tb = part_begin(blockIdx.x, total, parts), te = part_begin(blockIdx.x + 1, total, parts);
+  // the last head whose first flat tile is not past tb
+  {
+    int cnt = 0;
+    for (int x = tid; x < NH; x += 256) cnt += a.cum[x] <= tb;
+    for (int off = 32; off; off >>= 1) cnt += __shfl_xor(cnt, off, 64);
+    if (lane == 0) first[wave] = cnt;
+  }
+  __syncthreads();
+  int hh = first[0] + first[1] + first[2] + first[3] - 1;
+  hh = __builtin_amdgcn_readfirstlane(hh);
+  LaneAt at;
+  {
+    const int kt = row_token(lane & 31), h = (kt >> 2) & 1, r = 4 * (kt >> 3) + (kt & 3);
+    if (FP8) {
+      at.k = h * 1024 + hf * 256 + r * 16;
+      at.v = D * 32 + hf * 256 + (lane & 15) * 16 + 8 * ((lane >> 4) & 1);
+      at.ks = D * 64 + (kt >> 3) * 64 + (kt & 7) * 4;
+      at.vs = D * 64 + hf * 64 + 32;
+    } else {
+      at.k = h * 1024 + hf * 256 + r * 16;
+      at.v = D * 64 + ((lane >> 4) & 1) * 1024 + hf * 256 + (lane & 15) * 16;
+      at.ks = at.vs = 0;
+    }
+  }
+  for (int f = tb; f < te;) {
+    while (((const DMS_CONST int32_t*)a.cum)[hh + 1] <= f) ++hh;   // heads without nodes have no tiles
+    Segment sg;
+    {
+      typedef int __attribute__((ext_vector_type(8))) i32x8;
+      const i32x8 rd = *((const DMS_CONST i32x8*)(a.rows + hh));
+      sg.r.sh = rd[0];
+      sg.r.L = rd[1];
+      sg.r.tok0 = rd[2];
+      sg.r.m = rd[3];
+      sg.r.p0 = rd[4];
+      sg.r.tile0 = rd[5];
+      sg.r.seq = rd[6];
+    }
+    const int at0 = f - ((const DMS_CONST int32_t*)a.cum)[hh];
+    sg.hh = hh;
+    sg.T = tiles_of(sg.r.L, sg.r.m);
+    sg.unit = at0 / sg.T;
+    sg.t0 = at0 - sg.unit * sg.T;
+    sg.t1 = min(sg.T, sg.t0 + te - f);
+    sg.nc = (sg.r.L + 31) >> 5;
+    sg.deep = sg.r.p0 + ((const DMS_CONST int32_t*)a.deepest)[sg.r.seq];
+    const int h = hh % a.H, cols = sg.r.m * a.g;
+    // ---- this wave's columns
+    const int col0 = sg.unit * UC + cw * 32 * NC;
+    const int blocks = max(0, min(NC, (cols - col0 + 31) / 32));
+    Columns<D, NC> c;
+#pragma unroll
+    for (int x = 0; x < NC; ++x) {
+      const int col = col0 + 32 * x + (lane & 31);
+      const bool ok = col < cols;
+      const int node = ok ? col / a.g : 0, qh = ok ? col % a.g : 0;
+      const size_t tok = static_cast<size_t>(sg.r.tok0) + node;
+      const uint16_t* q = a.q + (tok * Hq + h * a.g + qh) * D + 8 * hf;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+        c.q[x][s] = ok ? *reinterpret_cast<const u32x4*>(q + 16 * s) : u32x4{0u, 0u, 0u, 0u};
+      // the borrowed decision neuron takes no part in attention (App. C)
+      if (a.zero_neuron && qh == 0 && hf == 0) c.q[x][0][0] &= 0xFFFF0000u;
+      c.t[x] = sg.r.p0 + a.depth[tok];
+      c.anc[x] = a.anc + tok * a.words;
+      c.m[x] = kMInit;
+      c.l[x] = 0.f;
+#pragma unroll
+      for (int b = 0; b < OB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c.o[x][b][i] = 0.f;
+    }
+    // ---- its tiles
+    auto source = [&](int t) -> const char* {
+      if (t >= sg.nc) return a.tiles + (static_cast<size_t>(sg.r.tile0) + (t - sg.nc)) * TB;
+      const int page = ((const DMS_CONST int32_t*)(a.page_table + static_cast<size_t>(sg.r.sh) * a.maxp))[(32 * t) >> a.log2P];
+      return a.pool + static_cast<size_t>(page) * a.page_bytes + static_cast<size_t>(((32 * t) & (a.P - 1)) >> 5) * TB;
+    };
+    auto load = [&](Regs& r, int t) -> const char* {
+      const char* tile = source(t);
+      load_tile<CW == 1>(r, tile, at);
+      if (t < sg.nc) {
+        r.meta = static_cast<uint32_t>(a.slot_meta[static_cast<size_t>(sg.r.sh) * a.max_slots + 32 * t + (lane & 31)]);
+      } else {
+        const int x = min(32 * (t - sg.nc) + (lane & 31), sg.r.m - 1);
+        const size_t node = static_cast<size_t>(sg.r.tok0) + x;
+        r.meta = static_cast<uint32_t>(sg.r.p0 + a.depth[node]) | (a.flags[node * a.H + h] ? kFlagBit : 0u);
+      }
+      return tile;
+    };
+    if (blocks > 0 && sg.t0 + kw < sg.t1) {
+      Regs ra, rb;
+      int t = sg.t0 + kw;
+      const int last = t + (sg.t1 - 1 - t) / KW * KW;
+      const char* ta = load(ra, t);
+      while (true) {
+        const char* tb2 = load(rb, min(t + KW, last));
+        attend_tile<D, FP8, NC>(a, sg, c, ra, ta, t, blocks, lane);
+        t += KW;
+        if (t > last) break;
+        ta = load(ra, min(t + KW, last));
+        attend_tile<D, FP8, NC>(a, sg, c, rb, tb2, t, blocks, lane);
+        t += KW;
+        if (t > last) break;
+      }
+    }
+    // ---- fold the waves of a column block and write it: the outputs of a whole
+    // unit, else a partial (slot 2 w: a unit that began before this workgroup's
+    // part; 2 w + 1: one that ends after it)
+    const bool whole = sg.t0 == 0 && sg.t1 == sg.T;
+    const int slot = 2 * blockIdx.x + (sg.t0 == 0);
+#pragma unroll
+    for (int x = 0; x < NC; ++x) {
+      const float l = col_sum(c.l[x]);
+      if (lane < 32) ml_lds[wave][32 * x + lane] = make_float2(c.m[x], l);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < NC; ++x) {
+      float M = kMInit;
+#pragma unroll
+      for (int y = 0; y < KW; ++y) M = fmaxf(M, ml_lds[y * CW + cw][32 * x + (lane & 31)].x);
+      const float scale = __builtin_amdgcn_exp2f((c.m[x] - M) * a.scale_log2);
+#pragma unroll
+      for (int b = 0; b < OB; ++b)
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          *reinterpret_cast<f32x4*>(&fold[wave][lane & 31][32 * b + 8 * y + 4 * hf]) =
+              f32x4{c.o[x][b][4 * y], c.o[x][b][4 * y + 1], c.o[x][b][4 * y + 2], c.o[x][b][4 * y + 3]} * scale;
+      __syncthreads();
+      // CW blocks of 32 columns, D / 4 pieces each
+      for (int e = tid; e < CW * 32 * (D / 4); e += 256) {
+        const int piece = e % (D / 4), cc = e / (D / 4) % 32, cx = e / (D / 4) / 32;
+        const int uc = (cx * NC + x) * 32 + cc, col = sg.unit * UC + uc;
+        if (col >= cols) continue;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        float Mc = kMInit, L = 0.f;
+#pragma unroll
+        for (int y = 0; y < KW; ++y) Mc = fmaxf(Mc, ml_lds[y * CW + cx][32 * x + cc].x);
+#pragma unroll
+        for (int y = 0; y < KW; ++y) {
+          const float2 ml = ml_lds[y * CW + cx][32 * x + cc];
+          L += ml.y * __builtin_amdgcn_exp2f((ml.x - Mc) * a.scale_log2);
+          sum += *reinterpret_cast<const f32x4*>(&fold[y * CW + cx][cc][4 * piece]);
+        }
+        if (whole) {
+          const int node = col / a.g, qh = col % a.g;
+          const float inv = 1.0f / L;
+          const f32x2 lo = {sum[0] * inv, sum[1] * inv}, hi = {sum[2] * inv, sum[3] * inv};
+          const u32x2 ob = {__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
+                            __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
+          *reinterpret_cast<u32x2*>(a.out + ((static_cast<size_t>(sg.r.tok0) + node) * Hq + h * a.g + qh) * D + 4 * piece) = ob;
+        } else {
+          const size_t pc = static_cast<size_t>(slot) * UC + uc;
+          *reinterpret_cast<f32x4*>(a.part_o + pc * D + 4 * piece) = sum;
+          if (piece == 0) a.part_ml[pc] = make_float2(Mc, L);
+        }
+      }
+      __syncthreads();
+    }
+    f += sg.t1 - sg.t0;
+  }
+}
+
+// Joins the units that several workgroups attended, a wave per output row.
+template <int D>
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
+  if (load_status(a.status) != 0) return;
+  const int lane = threadIdx.x & 63, NH = a.n * a.H, Hq = a.H * a.g;
+  const int64_t rows = static_cast<int64_t>(a.total) * Hq;
+  const int total = a.cum[NH], parts = parts_of(total, a.min_tiles, a.G);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + wave; row < rows; row += static_cast<int64_t>(gridDim.x) * 4) {
+    const int node = static_cast<int>(row / Hq), hq = static_cast<int>(row % Hq);
+    const int i = a.node_seq[node], h = hq / a.g, hh = i * a.H + h;
+    const TreeRow r = a.rows[hh];
+    const int T = tiles_of(r.L, r.m), col = (node - r.tok0) * a.g + hq % a.g, unit = col / a.UC, uc = col % a.UC;
+    const int u0 = a.cum[hh] + unit * T;
+    const int w0 = part_holding(u0, total, parts), w1 = part_holding(u0 + T - 1, total, parts);
+    if (w0 == w1) continue;   // one workgroup wrote it
+    auto slot = [&](int w) { return static_cast<size_t>(2 * w + (w == w0)) * a.UC + uc; };
+    float M = kMInit;
+    for (int w = w0 + lane; w <= w1; w += 64) M = fmaxf(M, a.part_ml[slot(w)].x);
+    for (int off = 32; off; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+    float L = 0.f;
+    constexpr int E = D / 64;
+    float acc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    constexpr int kBatch = 8;
+    for (int w = w0; w <= w1; w += kBatch) {
+      float x[kBatch][E];
+      float2 ml[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const size_t pc = slot(min(w + u, w1));
+        ml[u] = a.part_ml[pc];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[u][e] = a.part_o[pc * D + E * lane + e];
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        if (w + u > w1) continue;
+        const float f = __builtin_amdgcn_exp2f((ml[u].x - M) * a.scale_log2);
+        L += ml[u].y * f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(x[u][e], f, acc[e]);
+      }
+    }
+    const float inv = 1.0f / L;
+    uint16_t* dst = a.out + row * D + E * lane;
+    if constexpr (E == 2) {
+      const f32x2 pr = {acc[0] * inv, acc[1] * inv};
+      *reinterpret_cast<uint32_t*>(dst) = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
+    } else {
+      const f32x2 pr = {acc[0] * inv, 0.f};
+      *dst = static_cast<uint16_t>(__builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2)));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Accepted paths
+// ---------------------------------------------------------------------------
+
+// A wave per sequence; lane l holds nodes l, l + 64, ..  Each step finds the
+// lowest child of the present node whose token is the wanted one; a child's
+// index is past its parent's, so the walk ends.
+__global__ __launch_bounds__(256) void tree_accept_kernel(const int32_t* cu, const int32_t* parents, const int32_t* tokens,
+                                                          const int32_t* targets, const int32_t* first, int n, int total,
+                                                          int max_nodes, int32_t* path, int32_t* path_len, int32_t* next) {
+  constexpr int kPer = kTreeMaxNodes / 64;
+  const int lane = threadIdx.x & 63;
+  const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (i >= n) return;
+  const int tok0 = max(0, min(cu[i], total)), m = min(max(tok0, min(cu[i + 1], total)) - tok0, max_nodes);
+  int par[kPer], tok[kPer], tgt[kPer];
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const int x = lane + 64 * u;
+    par[u] = x < m ? parents[tok0 + x] : -2;
+    tok[u] = x < m ? tokens[tok0 + x] : 0;
+    tgt[u] = x < m ? targets[tok0 + x] : 0;
+  }
+  int at = -1, want = first != nullptr ? first[i] : -1, count = 0;
+  bool any = first == nullptr;   // the root is accepted as it is
+  while (count < m) {
+    int found = -1;
+#pragma unroll
+    for (int u = kPer - 1; u >= 0; --u) {
+      const int x = lane + 64 * u;
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(x > at && par[u] == at && (any || tok[u] == want));
+      if (hit) found = 64 * u + __builtin_ctzll(hit);
+    }
+    if (found < 0) break;
+    any = false;
+#pragma unroll
+    for (int u = 0; u < kPer; ++u)
+      if (found >> 6 == u) want = __builtin_amdgcn_readlane(tgt[u], found & 63);
+    if (lane == 0) path[tok0 + count] = found;
+    ++count;
+    at = found;
+  }
+  for (int x = count + lane; x < m; x += 64) path[tok0 + x] = -1;
+  if (lane == 0) {
+    path_len[i] = count;
+    next[i] = want;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Commit of accepted paths: rule R1 for every token of a path, in order
+// ---------------------------------------------------------------------------
+
+struct CommitArgs {
+  LayerState st;
+  int32_t* status;
+  const int32_t* seq_ids;
+  const int32_t* cu;
+  const int32_t* path;
+  const int32_t* path_len;
+  const uint8_t* flags;   // [total, H]
+  const uint16_t* k;      // [total, H, D]
+  const uint16_t* v;
+  char* pool;
+  size_t page_bytes;
+  int32_t* need;          // [n H] pages to pop, or the error that refuses the call
+  int32_t* fresh;         // [n H] tokens that take fresh slots
+  int32_t* base;          // [n H] first pop of each head (calls of more than kScanHeads heads)
+  int32_t* before;        // [n] positions, [n H] lengths, then stack height, ids' error, verdict, pops
+  int n, H, w, P, log2P, D, maxp, max_slots, max_seqs, total, max_nodes;
+  int immediate, fp8, mla;
+};
+constexpr int kScanHeads = 2048;   // up to here every workgroup sums the pops itself
+
+__device__ inline int32_t* commit_pos(const CommitArgs& a) { return a.before; }
+__device__ inline int32_t* commit_len(const CommitArgs& a) { return a.before + a.n; }
+__device__ inline int32_t* commit_word(const CommitArgs& a, int x) { return a.before + a.n + static_cast<size_t>(a.n) * a.H + x; }
+
+// Path of sequence i, or false if the call may not use it.
+__device__ inline bool commit_path(const CommitArgs& a, int i, int& tok0, int& len) {
+  tok0 = a.cu[i];
+  const int end = a.cu[i + 1];
+  len = a.path_len[i];
+  return tok0 >= 0 && end >= tok0 && end <= a.total && end - tok0 <= a.max_nodes && len >= 0 && len <= end - tok0 &&
+         (i > 0 || tok0 == 0) && (i < a.n - 1 || end == a.total);
+}
+
+// Whether path token c (at pos + c) takes the slot of the token w before it.
+__device__ inline bool commit_reuse(const CommitArgs& a, const int* nodes, int sh, int h, int tok0, int pos, int c) {
+  if (static_cast<int64_t>(pos) + c < a.w) return false;
+  const int j = a.immediate ? c : c - a.w;
+  if (j >= 0) return a.flags[(static_cast<size_t>(tok0) + nodes[j]) * a.H + h] != 0;
+  return (static_cast<uint32_t>(a.st.ring[static_cast<size_t>(sh) * a.w + (pos + c) % a.w]) & kFlagBit) != 0;
+}
+
+// Pass 1, a wave per head and one more for the ids: fresh tokens and pages of
+// every head, and the state that pass 2 overwrites.
+__global__ __launch_bounds__(256) void commit_scan_kernel(CommitArgs a) {
+  __shared__ uint32_t seen[kMaxSeqs / 32];
+  __shared__ int nodes_lds[4][kTreeMaxNodes];
+  if (load_status(a.status) != 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (blockIdx.x == 0) {
+    for (int x = threadIdx.x; x < (a.max_seqs + 31) / 32; x += blockDim.x) seen[x] = 0;
+    __syncthreads();
+    int bad = 0;
+    for (int x = threadIdx.x; x < a.n; x += blockDim.x) {
+      const int s = a.seq_ids[x];
+      if (s < 0 || s >= a.max_seqs) bad = 1;
+      else if (atomicOr(&seen[s >> 5], 1u << (s & 31)) & (1u << (s & 31))) bad = 1;
+    }
+    bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0) {
+      *commit_word(a, 0) = *a.st.top;
+      *commit_word(a, 1) = bad ? DMS_ERR_BAD_SEQ : DMS_OK;
+    }
+    return;
+  }
+  const int64_t hh64 = (static_cast<int64_t>(blockIdx.x) - 1) * 4 + wave;
+  if (hh64 >= static_cast<int64_t>(a.n) * a.H) return;
+  const int hh = static_cast<int>(hh64);
+  const int i = hh / a.H, h = hh % a.H, s = a.seq_ids[i];
+  int* nodes = nodes_lds[wave];
+  int tok0, len;
+  bool bad = s < 0 || s >= a.max_seqs || !commit_path(a, i, tok0, len);
+  int m = 0, pos = 0, L0 = 0, sh = 0, fresh = 0;
+  if (!bad) {
+    m = a.cu[i + 1] - tok0;
+    sh = s * a.H + h;
+    pos = a.st.pos[s];
+    L0 = a.st.len[sh];
+    int off = 0;
+    for (int c = lane; c < len; c += 64) {
+      int x = a.path[tok0 + c];
+      if (x < 0 || x >= m) {
+        off = 1;
+        x = 0;
+      }
+      nodes[c] = x;
+    }
+    bad = __builtin_amdgcn_ballot_w64(off != 0) != 0;
+    // (the wave's own LDS writes are visible to it)
+    __builtin_amdgcn_wave_barrier();
+    for (int c0 = 0; c0 < len; c0 += 64) {
+      const int c = c0 + lane;
+      const bool f = c < len && !commit_reuse(a, nodes, sh, h, tok0, pos, c);
+      fresh += __builtin_popcountll(__builtin_amdgcn_ballot_w64(f));
+    }
+  }
+  if (lane == 0) {
+    const int64_t L1 = static_cast<int64_t>(L0) + fresh;
+    a.need[hh] = bad ? DMS_ERR_INVALID : L1 > a.max_slots ? DMS_ERR_CAPACITY
+                     : static_cast<int>((L1 + a.P - 1) / a.P - (L0 + a.P - 1) / a.P);
+    a.fresh[hh] = fresh;
+    commit_len(a)[hh] = L0;
+    if (h == 0) commit_pos(a)[i] = pos;
+  }
+}
+
+// What the call's heads pop in all and whether one refuses it, as a workgroup
+// sums it; before: pops of the heads ahead of hh.
+__device__ inline int commit_verdict(const CommitArgs& a, int hh, int* lds, int& before, int& pops) {
+  const int64_t NH = static_cast<int64_t>(a.n) * a.H;
+  int all = 0, mine = 0, err = 0;
+  for (int64_t x = threadIdx.x; x < NH; x += blockDim.x) {
+    const int nd = a.need[x];
+    err |= nd == DMS_ERR_INVALID ? 1 : nd == DMS_ERR_CAPACITY ? 2 : 0;
+    all += max(nd, 0);
+    if (x < hh) mine += max(nd, 0);
+  }
+  for (int off = 32; off; off >>= 1) {
+    all += __shfl_xor(all, off, 64);
+    mine += __shfl_xor(mine, off, 64);
+    err |= __shfl_xor(err, off, 64);
+  }
+  const int wave = threadIdx.x >> 6, nw = blockDim.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    lds[3 * wave] = all;
+    lds[3 * wave + 1] = mine;
+    lds[3 * wave + 2] = err;
+  }
+  __syncthreads();
+  all = mine = err = 0;
+  for (int x = 0; x < nw; ++x) {
+    all += lds[3 * x];
+    mine += lds[3 * x + 1];
+    err |= lds[3 * x + 2];
+  }
+  before = mine;
+  pops = all;
+  const int ids = *commit_word(a, 1), top = *commit_word(a, 0);
+  return ids != DMS_OK ? ids : err & 1 ? DMS_ERR_INVALID : err & 2 ? DMS_ERR_CAPACITY : all > top ? DMS_ERR_OUT_OF_PAGES : DMS_OK;
+}
+
+// Calls of many heads: the pops summed once, by one workgroup.
+__global__ __launch_bounds__(1024) void commit_pages_kernel(CommitArgs a) {
+  __shared__ int lds[51];
+  if (load_status(a.status) != 0) return;
+  int before, pops;
+  const int err = commit_verdict(a, 0, lds, before, pops);
+  if (threadIdx.x == 0) {
+    *commit_word(a, 2) = err;
+    *commit_word(a, 3) = pops;
+  }
+  if (err != DMS_OK) return;
+  const int64_t NH = static_cast<int64_t>(a.n) * a.H;
+  int run = 0;
+  for (int64_t b = 0; b < NH; b += blockDim.x) {
+    const int64_t hh = b + threadIdx.x;
+    int tot;
+    __syncthreads();
+    const int off = block_exclusive_scan(hh < NH ? a.need[hh] : 0, lds, &tot);
+    if (hh < NH) a.base[hh] = run + off;
+    run += tot;
+  }
+}
+
+// Pass 2, a workgroup per head: slots, ring, slot owners, pages and the rows of
+// the tokens that keep their slot.
+template <bool SUMMED>
+__global__ __launch_bounds__(256) void commit_write_kernel(CommitArgs a) {
+  __shared__ int lds[12];
+  __shared__ int nodes[kTreeMaxNodes], slots[kTreeMaxNodes], keeps[kTreeMaxNodes];
+  if (load_status(a.status) != 0) return;
+  const int hh = blockIdx.x, i = hh / a.H, h = hh % a.H, tid = threadIdx.x;
+  int before, pops, err;
+  if (SUMMED) {
+    err = *commit_word(a, 2);
+    pops = *commit_word(a, 3);
+    before = err == DMS_OK ? a.base[hh] : 0;
+  } else {
+    err = commit_verdict(a, hh, lds, before, pops);
+  }
+  const int64_t last = static_cast<int64_t>(a.n) * a.H - 1;
+  if (err != DMS_OK) {
+    // the other workgroups of this launch read no status past their first line
+    if (hh == last && tid == 0) set_status(a.status, err);
+    return;
+  }
+  const int top0 = *commit_word(a, 0);
+  if (hh == last && tid == 0) *a.st.top = top0 - pops;
+  const int s = a.seq_ids[i], sh = s * a.H + h, tok0 = a.cu[i], len = a.path_len[i];
+  const int pos = commit_pos(a)[i], L0 = commit_len(a)[hh], fresh = a.fresh[hh];
+  if (len == 0) return;
+  if (tid == 0) {
+    a.st.len[sh] = L0 + fresh;
+    if (h == 0) a.st.pos[s] = pos + len;
+  }
+  const int32_t* popped = a.st.stack + top0 - 1 - before;     // k-th new page at -k
+  const size_t pt = static_cast<size_t>(sh) * a.maxp;
+  const int new0 = (L0 + a.P - 1) >> a.log2P;
+  for (int x = tid; x < a.need[hh]; x += blockDim.x) a.st.page_table[pt + new0 + x] = popped[-x];
+  for (int c = tid; c < len; c += blockDim.x) nodes[c] = a.path[tok0 + c];
+  __syncthreads();
+  // slots: fresh tokens in order; a reusing one has that of the token w before
+  // it, in the path or in the ring (kTreeMaxNodes threads, one token each)
+  const int c = tid;
+  const bool on = c < len;
+  const bool reuse = on && commit_reuse(a, nodes, sh, h, tok0, pos, c);
+  {
+    const uint64_t bal = __builtin_amdgcn_ballot_w64(on && !reuse);
+    if ((tid & 63) == 0) lds[tid >> 6] = __builtin_popcountll(bal);
+    __syncthreads();
+    int rank = __builtin_popcountll(bal & ((1ull << (tid & 63)) - 1ull));
+    for (int x = 0; x < (tid >> 6); ++x) rank += lds[x];
+    if (on) {
+      slots[c] = !reuse ? L0 + rank
+                 : c < a.w ? static_cast<int>(static_cast<uint32_t>(a.st.ring[static_cast<size_t>(sh) * a.w + (pos + c) % a.w]) & ~kFlagBit)
+                           : -1;
+      // a token keeps its slot unless the token w later takes it
+      keeps[c] = len - c <= a.w || !commit_reuse(a, nodes, sh, h, tok0, pos, c + a.w);
+    }
+  }
+  __syncthreads();
+  for (int c0 = a.w; c0 < len; c0 += a.w) {     // one window of the path at a time
+    for (int x = c0 + tid; x < min(len, c0 + a.w); x += blockDim.x)
+      if (slots[x] < 0) slots[x] = slots[x - a.w];
+    __syncthreads();
+  }
+  if (on) {
+    const uint32_t fb = a.flags[(static_cast<size_t>(tok0) + nodes[c]) * a.H + h] ? kFlagBit : 0u;
+    if (len - c <= a.w)
+      a.st.ring[static_cast<size_t>(sh) * a.w + (pos + c) % a.w] = static_cast<int32_t>(static_cast<uint32_t>(slots[c]) | fb);
+    if (keeps[c])
+      a.st.slot_meta[static_cast<size_t>(sh) * a.max_slots + slots[c]] = static_cast<int32_t>(static_cast<uint32_t>(pos + c) | fb);
+  }
+  // rows: D / 8 consecutive lanes each (an aligned lane group for the 8-bit
+  // quantizer: it takes every branch together)
+  const int kq = a.D / 8;
+  for (int x = tid; x < len * kq; x += blockDim.x) {
+    const int y = x / kq, part = x - y * kq;
+    if (!keeps[y]) continue;
+    const int slot = slots[y], row = slot & (a.P - 1), j = row & 31, pi = slot >> a.log2P;
+    const int page = pi >= new0 ? popped[new0 - pi] : a.st.page_table[pt + pi];
+    const size_t src = ((static_cast<size_t>(tok0) + nodes[y]) * a.H + h) * a.D;
+    const uint4 kx = reinterpret_cast<const uint4*>(a.k + src)[part];
+    char* pg = a.pool + static_cast<size_t>(page) * a.page_bytes;
+    if (a.mla) {
+      *reinterpret_cast<uint4*>(pg + (row >> 5) * mla_tile_bytes(a.D) + k_elem_off(j, 8 * part)) = kx;
+      continue;
+    }
+    const uint4 vx = reinterpret_cast<const uint4*>(a.v + src)[part];
+    if (a.fp8) {
+      fp8_store_token(pg + (row >> 5) * fp8_tile_bytes(a.D), j, a.D, part, kx, vx);
+      continue;
+    }
+    char* tile = pg + (row >> 5) * tile_bytes(a.D);
+    *reinterpret_cast<uint4*>(tile + k_elem_off(j, 8 * part)) = kx;
+    const uint32_t vw[4] = {vx.x, vx.y, vx.z, vx.w};
+#pragma unroll
+    for (int d = 0; d < 8; ++d)
+      *reinterpret_cast<uint16_t*>(tile + v_elem_off(j, part * 8 + d, a.D)) = static_cast<uint16_t>(vw[d >> 1] >> (16 * (d & 1)));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Launches
+// ---------------------------------------------------------------------------
+
+// compute units of the current device, at most what a workspace holds partials for
+int tree_workgroups() {
+  int dev = 0, v = 0;
+  if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v < 1)
+    return kTreeWorkgroups;
+  return std::min(v, kTreeWorkgroups);
+}
+
+// Column blocks of a wave and waves side by side for the largest tree of a call.
+struct TreeShape {
+  int nc, cw;
+};
+TreeShape tree_shape(int cols) { return cols <= 32 ? TreeShape{1, 1} : cols <= 64 ? TreeShape{2, 1} : cols <= 128 ? TreeShape{2, 2} : TreeShape{2, 4}; }
+
+struct TreeLayout {
+  size_t rows, cum, anc, depth, node_seq, deepest, flags, tiles, part_o, part_ml, need, fresh, base, before, bytes;
+  int words, tph, UC;
+};
+TreeLayout tree_layout(const dms_config& c, int n, int total, int max_nodes) {
+  TreeLayout lo{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, kAlign); return o; };
+  const size_t H = c.num_kv_heads, NH = static_cast<size_t>(n) * H, T = total, D = c.head_dim;
+  lo.need = take(NH * 4);
+  lo.fresh = take(NH * 4);
+  lo.base = take(NH * 4);
+  lo.before = take((n + NH + 4) * 4);
+  if (c.kv_format != DMS_KV_MLA) {
+    const TreeShape sh = tree_shape(max_nodes * c.group_size);
+    lo.words = std::max(1, (max_nodes + 31) / 32);
+    lo.tph = total / 32 + n + 1;
+    lo.UC = 32 * sh.nc * sh.cw;
+    lo.rows = take(NH * sizeof(TreeRow));
+    lo.cum = take((NH + 1) * 4);
+    lo.anc = take(T * lo.words * 4);
+    lo.depth = take(T * 4);
+    lo.node_seq = take(T * 4);
+    lo.deepest = take(static_cast<size_t>(n) * 4);
+    lo.flags = take(T * H);
+    lo.tiles = take(H * static_cast<size_t>(lo.tph) * (c.kv_format == DMS_KV_FP8 ? fp8_tile_bytes(c.head_dim) : tile_bytes(c.head_dim)));
+    lo.part_o = take(size_t(2) * kTreeWorkgroups * lo.UC * D * 4);
+    lo.part_ml = take(size_t(2) * kTreeWorkgroups * lo.UC * 8);
+  }
+  lo.bytes = off;
+  return lo;
+}
+
+template <int D, bool FP8>
+hipError_t launch_attention(const TreeArgs& a, const TreeShape& sh, hipStream_t st) {
+  const unsigned prep = 1u + a.n + static_cast<unsigned>(a.n) * a.H * a.words;
+  hipLaunchKernelGGL((tree_prep_kernel<D, FP8>), dim3(prep), dim3(kPrepThreads), 0, st, a);
+  if (sh.nc == 1) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 1, 1>), dim3(a.G), dim3(256), 0, st, a);
+  else if (sh.cw == 1) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 2, 1>), dim3(a.G), dim3(256), 0, st, a);
+  else if (sh.cw == 2) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 2, 2>), dim3(a.G), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 2, 4>), dim3(a.G), dim3(256), 0, st, a);
+  const int64_t rows = static_cast<int64_t>(a.total) * a.H * a.g;
+  const unsigned merge = static_cast<unsigned>(std::min<int64_t>((rows + 3) / 4, 1 << 20));
+  hipLaunchKernelGGL((tree_merge_kernel<D>), dim3(merge), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t tree_workspace_bytes(const dms_config& c, int n, int total, int max_nodes) {
+  return tree_layout(c, n, total, max_nodes).bytes;
+}
+
+hipError_t launch_tree_attention(const dms_config& c, const Layout& lo, void* meta, void* pool, int layer, int n,
+                                 const int32_t* seq_ids, const int32_t* cu, int total, int max_nodes,
+                                 const int32_t* parents, const void* q, const void* k, const void* v,
+                                 const uint8_t* flags, uint8_t* decisions_out, void* out, void* ws, hipStream_t st) {
+  const TreeLayout tl = tree_layout(c, n, total, max_nodes);
+  const TreeShape sh = tree_shape(max_nodes * c.group_size);
+  char* w = static_cast<char*>(ws);
+  const LayerState s = layer_state(lo, meta, layer);
+  TreeArgs a{};
+  a.status = reinterpret_cast<int32_t*>(static_cast<char*>(meta) + lo.status);
+  a.seq_ids = seq_ids;
+  a.cu = cu;
+  a.parents = parents;
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.flags = flags;
+  if (flags == nullptr) {
+    a.flags_out = decisions_out != nullptr ? decisions_out : reinterpret_cast<uint8_t*>(w + tl.flags);
+    a.flags = a.flags_out;
+  }
+  a.pool = static_cast<const char*>(pool);
+  a.page_table = s.page_table;
+  a.slot_meta = s.slot_meta;
+  a.len = s.len;
+  a.pos = s.pos;
+  a.out = static_cast<uint16_t*>(out);
+  a.rows = reinterpret_cast<TreeRow*>(w + tl.rows);
+  a.cum = reinterpret_cast<int32_t*>(w + tl.cum);
+  a.anc = reinterpret_cast<uint32_t*>(w + tl.anc);
+  a.depth = reinterpret_cast<int32_t*>(w + tl.depth);
+  a.node_seq = reinterpret_cast<int32_t*>(w + tl.node_seq);
+  a.deepest = reinterpret_cast<int32_t*>(w + tl.deepest);
+  a.tiles = w + tl.tiles;
+  a.part_o = reinterpret_cast<float*>(w + tl.part_o);
+  a.part_ml = reinterpret_cast<float2*>(w + tl.part_ml);
+  a.page_bytes = lo.page_bytes;
+  a.n = n;
+  a.H = c.num_kv_heads;
+  a.g = c.group_size;
+  a.w = c.window;
+  a.P = c.page_size;
+  a.log2P = 31 - __builtin_clz(c.page_size);
+  a.maxp = c.max_pages_per_head;
+  a.max_slots = lo.max_slots;
+  a.max_seqs = c.max_seqs;
+  a.total = total;
+  a.max_nodes = max_nodes;
+  a.words = tl.words;
+  a.tph = tl.tph;
+  a.G = tree_workgroups();
+  a.UC = tl.UC;
+  a.min_tiles = 2 * (4 / sh.cw);
+  a.zero_neuron = c.decision_source == DMS_DECIDE_QUERY;
+  a.bias = c.decision_bias;
+  a.scale_log2 = c.softmax_scale * 1.4426950408889634f;
+  const bool fp8 = c.kv_format == DMS_KV_FP8;
+  if (c.head_dim == 64) return fp8 ? launch_attention<64, true>(a, sh, st) : launch_attention<64, false>(a, sh, st);
+  return fp8 ? launch_attention<128, true>(a, sh, st) : launch_attention<128, false>(a, sh, st);
+}
+
+hipError_t launch_tree_accept(int n, const int32_t* cu, int total, int max_nodes, const int32_t* parents,
+                              const int32_t* tokens, const int32_t* targets, const int32_t* first, int32_t* path,
+                              int32_t* path_len, int32_t* next, hipStream_t st) {
+  hipLaunchKernelGGL(tree_accept_kernel, dim3((n + 3) / 4), dim3(256), 0, st, cu, parents, tokens, targets, first, n, total,
+                     max_nodes, path, path_len, next);
+  return hipGetLastError();
+}
+
+hipError_t launch_tree_commit(const dms_config& c, const Layout& lo, void* meta, void* pool, int layer, int n,
+                              const int32_t* seq_ids, const int32_t* cu, int total, int max_nodes, const int32_t* path,
+                              const int32_t* path_len, const void* k, const void* v, const uint8_t* flags, void* ws,
+                              hipStream_t st) {
+  const TreeLayout tl = tree_layout(c, n, total, max_nodes);
+  char* w = static_cast<char*>(ws);
+  CommitArgs a{};
+  a.st = layer_state(lo, meta, layer);
+  a.status = reinterpret_cast<int32_t*>(static_cast<char*>(meta) + lo.status);
+  a.seq_ids = seq_ids;
+  a.cu = cu;
+  a.path = path;
+  a.path_len = path_len;
+  a.flags = flags;
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.pool = static_cast<char*>(pool);
+  a.page_bytes = lo.page_bytes;
+  a.need = reinterpret_cast<int32_t*>(w + tl.need);
+  a.fresh = reinterpret_cast<int32_t*>(w + tl.fresh);
+  a.base = reinterpret_cast<int32_t*>(w + tl.base);
+  a.before = reinterpret_cast<int32_t*>(w + tl.before);
+  a.n = n;
+  a.H = c.num_kv_heads;
+  a.w = c.window;
+  a.P = c.page_size;
+  a.log2P = 31 - __builtin_clz(c.page_size);
+  a.D = c.head_dim;
+  a.maxp = c.max_pages_per_head;
+  a.max_slots = lo.max_slots;
+  a.max_seqs = c.max_seqs;
+  a.total = total;
+  a.max_nodes = max_nodes;
+  a.immediate = c.eviction == DMS_EVICT_IMMEDIATE;
+  a.fp8 = c.kv_format == DMS_KV_FP8;
+  a.mla = c.kv_format == DMS_KV_MLA;
+  const unsigned NH = static_cast<unsigned>(n) * c.num_kv_heads;
+  hipLaunchKernelGGL(commit_scan_kernel, dim3(1 + (NH + 3) / 4), dim3(256), 0, st, a);
+  if (NH > kScanHeads) {
+    hipLaunchKernelGGL(commit_pages_kernel, dim3(1), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL(commit_write_kernel<true>, dim3(NH), dim3(256), 0, st, a);
+  } else {
+    hipLaunchKernelGGL(commit_write_kernel<false>, dim3(NH), dim3(256), 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace dms

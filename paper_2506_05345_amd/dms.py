@@ -106,6 +106,17 @@ class DmsWindowConfig(ctypes.Structure):
     ]
 
 
+class DmsSampleConfig(ctypes.Structure):
+    _fields_ = [
+        ("vocab", ctypes.c_int32),
+        ("logits_type", ctypes.c_int32),
+        ("temperature", ctypes.c_float),
+        ("top_k", ctypes.c_int32),
+        ("top_p", ctypes.c_float),
+        ("min_p", ctypes.c_float),
+    ]
+
+
 DMS_TYPE_BF16 = 0
 DMS_TYPE_F32 = 1
 DMS_ROPE_SECTIONS = 0
@@ -171,6 +182,13 @@ _SIGS = {
     "dms_window_workspace": (_I, [ctypes.POINTER(DmsWindowConfig), ctypes.POINTER(_SZ)]),
     "dms_window_attention_fwd": (_I, [ctypes.POINTER(DmsWindowConfig)] + [_VP] * 8),
     "dms_window_attention_bwd": (_I, [ctypes.POINTER(DmsWindowConfig)] + [_VP] * 12),
+    "dms_tree_workspace": (_I, [ctypes.POINTER(DmsConfig), _I, _I, _I, ctypes.POINTER(_SZ)]),
+    "dms_tree_attention": (_I, [_VP, _I, _I, _VP, _VP, _I, _I] + [_VP] * 8),
+    "dms_tree_attention_q": (_I, [_VP, _I, _I, _VP, _VP, _I, _I] + [_VP] * 8),
+    "dms_tree_accept": (_I, [_I, _VP, _I, _I] + [_VP] * 8),
+    "dms_tree_commit": (_I, [_VP, _I, _I, _VP, _VP, _I, _I] + [_VP] * 7),
+    "dms_sample_workspace": (_I, [ctypes.POINTER(DmsSampleConfig), _I, ctypes.POINTER(_SZ)]),
+    "dms_sample": (_I, [ctypes.POINTER(DmsSampleConfig), _I, _VP, _I64] + [_VP] * 9),
 }
 
 
@@ -817,3 +835,127 @@ def dms_window_attention_bwd(cfg, cu_seqlens, q, k, v, out, lse, dout, dq, dk, d
                                           _ptr(v), _ptr(out), _ptr(lse), _ptr(dout), _ptr(dq),
                                           _ptr(dk), _ptr(dv), _ptr(workspace), _stream(stream)),
            "dms_window_attention_bwd")
+
+
+# ---------------------------------------------------------------------------
+# Trees of drafted tokens
+# ---------------------------------------------------------------------------
+
+def dms_tree_workspace(cfg: DmsConfig, n, total_nodes, max_nodes) -> int:
+    size = _SZ()
+    _check(lib().dms_tree_workspace(ctypes.byref(cfg), n, total_nodes, max_nodes, ctypes.byref(size)),
+           "dms_tree_workspace")
+    return size.value
+
+
+def _check_tree_args(ctx, where, workspace, n, total, max_nodes, seq_ids, cu_nodes, **t):
+    specs = [(seq_ids, "seq_ids", _I32, n), (cu_nodes, "cu_nodes", _I32, n + 1)]
+    cfg, dims = _CTX_CFG.get(ctx), _dims(ctx)
+    if dims is not None:
+        H, Hq, D, _ = dims
+        of = {"q": (_BF16, total * Hq * D), "out": (_BF16, total * Hq * D), "k": (_BF16, total * H * D),
+              "v": (_BF16, total * H * D), "flags": (_U8, total * H), "decisions_out": (_U8, total * H),
+              "parents": (_I32, total), "path": (_I32, total), "path_len": (_I32, n)}
+        specs += [(x, name, *of[name]) for name, x in t.items()]
+        if workspace is not None and type(workspace) is not int:
+            # the size is only known for sizes that the library takes (else it refuses them)
+            size = _SZ()
+            ok = lib().dms_tree_workspace(ctypes.byref(cfg), n, total, max_nodes, ctypes.byref(size)) == DMS_OK
+            specs.append((workspace, "workspace", _U8, size.value if ok else 0))
+    _args(where, *specs)
+    _one_device(where, workspace, seq_ids, cu_nodes, *t.values())
+
+
+def dms_tree_attention(ctx, layer, n, seq_ids, cu_nodes, total_nodes, max_nodes, parents, q, k, v, flags, out,
+                       workspace, stream=None):
+    w = "dms_tree_attention"
+    _check_tree_args(ctx, w, workspace, n, total_nodes, max_nodes, seq_ids, cu_nodes, parents=parents, q=q, k=k, v=v,
+                     flags=flags, out=out)
+    _check(lib().dms_tree_attention(ctx, layer, n, _ptr(seq_ids), _ptr(cu_nodes), total_nodes, max_nodes,
+                                    _ptr(parents), _ptr(q), _ptr(k), _ptr(v), _ptr(flags), _ptr(out),
+                                    _ptr(workspace), _stream(stream)), w)
+
+
+def dms_tree_attention_q(ctx, layer, n, seq_ids, cu_nodes, total_nodes, max_nodes, parents, q, k, v, decisions_out,
+                         out, workspace, stream=None):
+    w = "dms_tree_attention_q"
+    _check_tree_args(ctx, w, workspace, n, total_nodes, max_nodes, seq_ids, cu_nodes, parents=parents, q=q, k=k, v=v,
+                     decisions_out=decisions_out, out=out)
+    _check(lib().dms_tree_attention_q(ctx, layer, n, _ptr(seq_ids), _ptr(cu_nodes), total_nodes, max_nodes,
+                                      _ptr(parents), _ptr(q), _ptr(k), _ptr(v), _ptr(decisions_out), _ptr(out),
+                                      _ptr(workspace), _stream(stream)), w)
+
+
+def dms_tree_accept(n, cu_nodes, total_nodes, max_nodes, parents, tokens, targets, first, path_out, path_len_out,
+                    next_out, stream=None):
+    w = "dms_tree_accept"
+    _args(w, (cu_nodes, "cu_nodes", _I32, n + 1), (parents, "parents", _I32, total_nodes),
+          (tokens, "tokens", _I32, total_nodes), (targets, "targets", _I32, total_nodes), (first, "first", _I32, n),
+          (path_out, "path_out", _I32, total_nodes), (path_len_out, "path_len_out", _I32, n),
+          (next_out, "next_out", _I32, n))
+    _one_device(w, cu_nodes, parents, tokens, targets, first, path_out, path_len_out, next_out)
+    _check(lib().dms_tree_accept(n, _ptr(cu_nodes), total_nodes, max_nodes, _ptr(parents), _ptr(tokens),
+                                 _ptr(targets), _ptr(first), _ptr(path_out), _ptr(path_len_out), _ptr(next_out),
+                                 _stream(stream)), w)
+
+
+def dms_tree_commit(ctx, layer, n, seq_ids, cu_nodes, total_nodes, max_nodes, path, path_len, k, v, flags, workspace,
+                    stream=None):
+    w = "dms_tree_commit"
+    _check_tree_args(ctx, w, workspace, n, total_nodes, max_nodes, seq_ids, cu_nodes, path=path, path_len=path_len,
+                     k=k, v=v, flags=flags)
+    _check(lib().dms_tree_commit(ctx, layer, n, _ptr(seq_ids), _ptr(cu_nodes), total_nodes, max_nodes, _ptr(path),
+                                 _ptr(path_len), _ptr(k), _ptr(v), _ptr(flags), _ptr(workspace), _stream(stream)), w)
+
+
+# ---------------------------------------------------------------------------
+# Sampling
+# ---------------------------------------------------------------------------
+
+def make_sample_config(vocab, logits_type=DMS_TYPE_F32, temperature=1.0, top_k=0, top_p=1.0,
+                       min_p=0.0) -> DmsSampleConfig:
+    return DmsSampleConfig(vocab, logits_type, temperature, top_k, top_p, min_p)
+
+
+def dms_sample_workspace(cfg: DmsSampleConfig, rows) -> int:
+    size = _SZ()
+    _check(lib().dms_sample_workspace(ctypes.byref(cfg), rows, ctypes.byref(size)), "dms_sample_workspace")
+    return size.value
+
+
+def dms_sample(cfg, rows, logits, temperature, top_k, top_p, min_p, u, tokens_out, logprobs_out, workspace,
+               row_stride=None, stream=None):
+    """logits [rows, vocab] may be part of wider rows: the stride is its own, or given (device
+    addresses)."""
+    w = "dms_sample"
+    kind = _TYPE_KIND.get(cfg.logits_type)
+    if logits is None or type(logits) is int:
+        stride = cfg.vocab if row_stride is None else row_stride
+    else:
+        if not isinstance(logits, _torch().Tensor):
+            raise TypeError(f"{w}: logits must be a tensor or a device address, got {type(logits)}")
+        if kind is not None and logits.dtype is not _KINDS[kind]:
+            raise DmsError(DMS_ERR_INVALID, f"{w}: logits must be {kind}, got {logits.dtype}")
+        if not logits.is_cuda:
+            raise DmsError(DMS_ERR_INVALID, f"{w}: logits must be a GPU tensor")
+        if logits.is_contiguous():
+            stride, have = cfg.vocab if row_stride is None else row_stride, logits.numel()
+        elif logits.dim() == 2 and logits.shape[1] == cfg.vocab and (cfg.vocab == 1 or logits.stride(1) == 1):
+            stride = row_stride if row_stride is not None else logits.stride(0) if logits.shape[0] > 1 else cfg.vocab
+            have = (logits.shape[0] - 1) * logits.stride(0) + cfg.vocab if logits.shape[0] else 0
+        else:
+            raise DmsError(DMS_ERR_INVALID, f"{w}: logits must have dense rows of {cfg.vocab}")
+        if rows > 0 and have < (rows - 1) * stride + cfg.vocab:
+            raise DmsError(DMS_ERR_INVALID, f"{w}: logits holds fewer than {rows} rows")
+    specs = [(temperature, "temperature", _F32, rows), (top_k, "top_k", _I32, rows), (top_p, "top_p", _F32, rows),
+             (min_p, "min_p", _F32, rows), (u, "u", _F32, rows), (tokens_out, "tokens_out", _I32, rows),
+             (logprobs_out, "logprobs_out", _F32, rows)]
+    if workspace is not None and type(workspace) is not int:
+        size = _SZ()
+        ok = lib().dms_sample_workspace(ctypes.byref(cfg), rows, ctypes.byref(size)) == DMS_OK
+        specs.append((workspace, "workspace", _U8, size.value if ok else 0))
+    _args(w, *specs)
+    _one_device(w, logits, temperature, top_k, top_p, min_p, u, tokens_out, logprobs_out, workspace)
+    _check(lib().dms_sample(ctypes.byref(cfg), rows, _ptr(logits), stride, _ptr(temperature), _ptr(top_k),
+                            _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(tokens_out), _ptr(logprobs_out),
+                            _ptr(workspace), _stream(stream)), w)

@@ -1,0 +1,191 @@
+"""Token sampling on the GPU against its definition: tokens equal, log-probabilities
+to the last bits of float32."""
+import math
+
+import numpy as np
+import pytest
+
+import oracle
+
+pytestmark = pytest.mark.gpu
+
+
+def run(x, dtype="f32", temperature=None, top_k=None, top_p=None, min_p=None, u=None, cfg=None, stride=None, offset=0,
+        logprobs=True):
+    import torch
+    from paper_2506_05345_amd import dms
+    rows, vocab = x.shape
+    kind = torch.float32 if dtype == "f32" else torch.bfloat16
+    wide = torch.full((rows, (stride or vocab) + offset), 50.0, dtype=kind, device="cuda")
+    wide[:, offset:offset + vocab] = torch.from_numpy(x).cuda().to(kind)
+    logits = wide[:, offset:offset + vocab]
+    c = dms.make_sample_config(vocab, dms.DMS_TYPE_F32 if dtype == "f32" else dms.DMS_TYPE_BF16, **(cfg or {}))
+    of = lambda v, t: None if v is None else torch.as_tensor(np.asarray(v), dtype=t, device="cuda")
+    f32 = torch.float32
+    tokens = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+    logp = torch.full((rows,), -7.0, device="cuda") if logprobs else None
+    ws = torch.full((dms.dms_sample_workspace(c, rows),), 0xA5, dtype=torch.uint8, device="cuda")
+    dms.dms_sample(c, rows, logits, of(temperature, f32), of(top_k, torch.int32), of(top_p, f32), of(min_p, f32),
+                   of(u, f32), tokens, logp, ws)
+    return logits.float().cpu().numpy(), tokens.cpu().numpy(), logp.cpu().numpy() if logprobs else None
+
+
+def check(x, u, got, temperature, top_k, top_p, min_p):
+    """Log-probabilities: z and the log of the sum are float64 and their difference is rounded once, half a step of 2^-24
+    relative; an error of the sum, at most 2^-40 with weights of 2^-43, and of float64's last bits are far below it."""
+    _, tokens, logp = got
+    for r in range(len(x)):
+        tok, lp = oracle.sample_token(x[r], temperature[r], int(top_k[r]), top_p[r], min_p[r], u[r])
+        assert tokens[r] == tok, (r, tokens[r], tok, temperature[r], top_k[r], top_p[r], min_p[r], u[r])
+        if logp is not None:
+            assert math.isnan(lp) == math.isnan(logp[r])
+            if not math.isnan(lp):
+                assert abs(logp[r] - lp) <= 2.0 ** -24 * abs(lp) + 1e-10, (r, logp[r], lp)
+
+
+def mixed(rng, rows):
+    pick = lambda *v: rng.choice(np.array(v), rows)
+    return (pick(0.0, 0.3, 0.7, 1.0, 2.0, -1.0), pick(0, 0, 1, 3, 40, 5000, -3), pick(1.0, 1.0, 0.95, 0.5, 0.1, 0.0, 2.0),
+            pick(0.0, 0.0, 0.05, 0.5, 1.0, 3.0))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [1, 2, 63, 64, 65, 1000, 1025, 4099, 32001])
+def test_rows_with_settings_of_their_own(vocab, dtype):
+    rng = np.random.default_rng(vocab)
+    rows = 60 if vocab < 5000 else 24
+    x = (rng.normal(size=(rows, vocab)) * rng.choice([0.3, 2.0, 6.0], (rows, 1))).astype(np.float32)
+    T, k, p, m = mixed(rng, rows)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, dtype, T, k, p, m, u)
+    check(got[0], u, got, T, k, p, m)
+
+
+@pytest.mark.parametrize("what", ["k", "p", "min", "kp", "none"])
+def test_settings_of_the_configuration(what):
+    rng = np.random.default_rng(1)
+    rows, vocab = 20, 5003
+    x = (rng.normal(size=(rows, vocab)) * 2).astype(np.float32)
+    cfg = dict(temperature=0.8, top_k=37 if "k" in what else 0, top_p=0.9 if "p" in what else 1.0,
+               min_p=0.02 if what == "min" else 0.0)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, cfg=cfg, u=u)
+    full = lambda v: np.full(rows, v)
+    check(got[0], u, got, full(0.8), full(cfg["top_k"]), full(cfg["top_p"]), full(cfg["min_p"]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("stride,offset", [(1003, 0), (1008, 1), (1004, 2), (1000, 3), (4096, 8)])
+def test_rows_of_wider_tensors(stride, offset, dtype):
+    """Rows that begin anywhere: no alignment but an element's; what lies between rows is not read as logits."""
+    rng = np.random.default_rng(stride)
+    rows, vocab = 12, 1000
+    x = rng.normal(size=(rows, vocab)).astype(np.float32)
+    T, k, p, m = mixed(rng, rows)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, dtype, T, k, p, m, u, stride=stride, offset=offset)
+    check(got[0], u, got, T, k, p, m)
+
+
+@pytest.mark.parametrize("vocab", [7, 5000, 40000])
+def test_equal_logits_are_cut_by_index(vocab):
+    rng = np.random.default_rng(3)
+    rows = 16
+    x = np.zeros((rows, vocab), np.float32)
+    x[1::2] = rng.integers(0, 3, (rows // 2, vocab))           # three values, many equal
+    x[::2, ::2] = -0.0                                         # equals 0
+    T = np.full(rows, 1.0)
+    k = rng.choice([0, 3, vocab // 2, vocab - 1], rows)
+    p = rng.choice([1.0, 0.5, 0.25, 0.9], rows)
+    m = rng.choice([0.0, 0.1, 0.2], rows)
+    for u in (np.zeros(rows), rng.random(rows), np.full(rows, 1 - 2.0 ** -24)):
+        u = u.astype(np.float32)
+        got = run(x, "f32", T, k, p, m, u)
+        check(got[0], u, got, T, k, p, m)
+
+
+def test_special_values():
+    """-inf (masked), NaN, +inf, the type's lowest value, rows without a token, and numbers outside [0, 1)."""
+    rng = np.random.default_rng(4)
+    low = np.finfo(np.float32).min
+    x = rng.normal(size=(14, 300)).astype(np.float32)
+    x[0] = -np.inf
+    x[1] = np.nan
+    x[2, :] = -np.inf
+    x[2, 177] = 3
+    x[3, ::2] = -np.inf
+    x[4, ::3] = np.nan
+    x[5, 10] = np.inf
+    x[6, [20, 30]] = np.inf
+    x[7] = low
+    x[8, 1:] = low
+    x[9, 5:] = -np.inf
+    x[10] = np.finfo(np.float32).max
+    x[11] = np.float32(1e-45)
+    T = np.full(14, 0.9)
+    k, p, m = np.zeros(14, int), np.ones(14), np.zeros(14)
+    p[[3, 4, 9]] = 0.8
+    k[[4, 5, 12]] = 9
+    u = rng.random(14).astype(np.float32)
+    u[12], u[13] = 5.0, -1.0
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
+    assert got[1][0] == -1 and got[1][1] == -1 and got[1][2] == 177
+    nan = np.full(14, np.nan)
+    got = run(x, "f32", nan, None, nan, nan, nan)               # greedy, no cuts
+    check(x, np.zeros(14), got, nan, k * 0, nan, nan)
+
+
+def test_extreme_temperatures():
+    rng = np.random.default_rng(5)
+    x = rng.normal(size=(8, 2000)).astype(np.float32)
+    T = np.array([1e-38, 1e-45, 1e-6, 100.0, 1e30, 3e38, 1.0, 0.01])
+    u = rng.random(8).astype(np.float32)
+    k, p, m = np.array([0, 0, 5, 0, 0, 7, 0, 0]), np.array([1, 1, 1, 0.9, 0.5, 1, 0.3, 1.0]), np.zeros(8)
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
+
+
+def test_large_vocabularies_and_numbers_at_the_borders():
+    rng = np.random.default_rng(6)
+    vocab = 1 << 20
+    x = (rng.normal(size=(3, vocab)) * 3).astype(np.float32)
+    T, k, p, m = np.array([1.0, 0.7, 2.5]), np.array([0, 3000, 0]), np.array([1.0, 0.99, 0.95]), np.zeros(3)
+    u = np.array([0.5, 1 - 2.0 ** -24, 0.0], np.float32)
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
+
+
+def test_distribution():
+    """4000 draws of one row: frequencies within 5 standard deviations of the definition's probabilities."""
+    rng = np.random.default_rng(7)
+    x = np.tile((rng.normal(size=(1, 50))).astype(np.float32), (4000, 1))
+    u = rng.random(4000).astype(np.float32)
+    _, tokens, logp = run(x, cfg=dict(temperature=0.8, top_k=20), u=u)
+    z = x[0].astype(np.float64) / np.float32(0.8)
+    keep = np.argsort(-z)[:20]
+    prob = np.zeros(50)
+    prob[keep] = np.exp(z[keep]) / np.exp(z[keep]).sum()
+    freq = np.bincount(tokens, minlength=50)
+    assert (np.abs(freq - 4000 * prob) <= 5 * np.sqrt(4000 * prob * (1 - prob)) + 1e-9).all()
+    assert np.abs(np.exp(logp.astype(np.float64)) - prob[tokens]).max() <= 1e-6
+
+
+def test_log_probabilities_may_be_left_out_and_streams_differ():
+    import torch
+    from paper_2506_05345_amd import dms
+    rng = np.random.default_rng(8)
+    x = rng.normal(size=(5, 3001)).astype(np.float32)
+    u = rng.random(5).astype(np.float32)
+    a = run(x, u=u, cfg=dict(top_p=0.9))
+    b = run(x, u=u, cfg=dict(top_p=0.9), logprobs=False)
+    assert np.array_equal(a[1], b[1])
+    c = dms.make_sample_config(3001, top_p=0.9)
+    stream = torch.cuda.Stream()
+    logits, ud = torch.from_numpy(x).cuda(), torch.from_numpy(u).cuda()
+    tokens = torch.empty(5, dtype=torch.int32, device="cuda")
+    ws = torch.empty(dms.dms_sample_workspace(c, 5), dtype=torch.uint8, device="cuda")
+    stream.wait_stream(torch.cuda.current_stream())
+    dms.dms_sample(c, 5, logits, None, None, None, None, ud, tokens, None, ws, stream=stream)
+    torch.cuda.synchronize()
+    assert np.array_equal(tokens.cpu().numpy(), a[1])
