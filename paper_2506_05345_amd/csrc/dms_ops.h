@@ -52,7 +52,7 @@ hipError_t launch_compact(const dms_config& c, const Layout& lo, void* meta, voi
 // Trees of drafted tokens.
 constexpr int kTreeMaxNodes = 256;     // nodes of a tree: a thread each in its preparation
 constexpr int kTreeWords = kTreeMaxNodes / 32;
-constexpr int kTreeWorkgroups = 256;   // attention workgroups at most (a workspace holds their partial results)
+constexpr int kTreeWorkgroups = 512;   // attention workgroups at most (a workspace holds their partial results)
 size_t tree_workspace_bytes(const dms_config& c, int n, int total, int max_nodes);
 // flags null: decisions from q, written to decisions_out where that is given.
 hipError_t launch_tree_attention(const dms_config& c, const Layout& lo, void* meta, void* pool, int layer, int n,

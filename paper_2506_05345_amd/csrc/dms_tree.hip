@@ -68,12 +68,14 @@ struct TreeArgs {
   int32_t* node_seq;       // [total]
   int32_t* deepest;        // [n]
   char* tiles;             // [H][tph] tiles of the drafted rows
+  uint32_t* tmeta;         // [H][tph][32] their rows (position | flag << 31), as the pool's slot owners
   float* part_o;           // [2 G][UC][D]
   float2* part_ml;         // [2 G][UC]
   size_t page_bytes;
   int n, H, g, w, P, log2P, maxp, max_slots, max_seqs, total, max_nodes, words, tph;
   int G, UC, min_tiles;    // workgroups, columns of a unit, flat tiles a workgroup takes at least
   int zero_neuron;
+  int once;                // every tile is read by one workgroup
   float bias, scale_log2;
 };
 
@@ -201,16 +203,33 @@ __device__ void tree_ancestors(const TreeArgs& a, int i) {
 template <int D, bool FP8>
 __device__ void tree_tile(const TreeArgs& a, int hh, int k) {
   __shared__ uint16_t vrows[32][D + 2];
-  const int i = hh / a.H, h = hh % a.H, tid = threadIdx.x;
+  __shared__ int up[kTreeMaxNodes];
+  const int i = hh / a.H, h = hh % a.H, tid = threadIdx.x, s = a.seq_ids[i];
   const int tok0 = a.cu[i], m = a.cu[i + 1] - tok0;
-  if (tok0 < 0 || m < 0 || m > a.max_nodes || tok0 + m > a.total || 32 * k >= m) return;
-  if (a.flags_out != nullptr && tid < 32 && 32 * k + tid < m) {
-    const size_t node = static_cast<size_t>(tok0) + 32 * k + tid;
-    const uint32_t bits = a.q[(node * a.H + h) * a.g * D];
-    a.flags_out[node * a.H + h] = (__uint_as_float(bits << 16) + a.bias) > 0.f;
+  if (tok0 < 0 || m < 0 || m > a.max_nodes || m > a.total - tok0 || 32 * k >= m || s < 0 || s >= a.max_seqs) return;
+  const int tile0 = h * a.tph + tok0 / 32 + i + k;
+  for (int x = tid; x < 32 * k + 32 && x < m; x += kPrepThreads) up[x] = a.parents[tok0 + x];
+  __syncthreads();
+  if (tid < 32) {
+    const int x = 32 * k + tid;
+    uint32_t row = 0;
+    if (x < m) {
+      const size_t node = static_cast<size_t>(tok0) + x;
+      bool flag;
+      if (a.flags_out != nullptr) {
+        const uint32_t bits = a.q[(node * a.H + h) * a.g * D];
+        flag = (__uint_as_float(bits << 16) + a.bias) > 0.f;
+        a.flags_out[node * a.H + h] = flag;
+      } else {
+        flag = a.flags[node * a.H + h] != 0;
+      }
+      int depth = 0;
+      for (int y = up[x], last = x; y >= 0 && y < last; last = y, y = up[y]) ++depth;   // (parents that break the rules end it)
+      row = static_cast<uint32_t>(a.pos[s] + depth) | (flag ? kFlagBit : 0u);
+    }
+    a.tmeta[static_cast<size_t>(tile0) * 32 + tid] = row;
   }
   constexpr int kPieces = 32 * D / 8;
-  const int tile0 = h * a.tph + tok0 / 32 + i + k;
   char* tile = a.tiles + static_cast<size_t>(tile0) * (FP8 ? fp8_tile_bytes(D) : tile_bytes(D));
   for (int pc = tid; pc < kPieces; pc += kPrepThreads) {
     const int j = pc / (D / 8), part = pc % (D / 8), e0 = 8 * part;
@@ -261,68 +280,36 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a) {
 // Attention
 // ---------------------------------------------------------------------------
 
-// The operands of one 32-row tile as a wave's 32x32x16 products take them:
-//   keys: lane l of k-step s holds dims 16 s + 8 (l / 32) .. + 7 of row
-//     row_token(l % 32);
-//   values: lane l of (32-dim block b, half y) holds rows 16 y + 8 (l / 32) .. + 7
-//     of dim 32 b + l % 32;
-// and the lane's row (position | flag << 31 of row l % 32).
-template <int D>
-struct TileRegs {
-  u32x4 k[D / 16], v[D / 32][2];
-  uint32_t meta;
-};
-// 8-bit tile: codes as stored, the key scale of the lane's key row, the value
-// scales of its 16 rows.
-template <int D>
-struct TileRegsF8 {
-  u32x4 k[D / 32];      // [p][y]: dims 64 p + 16 y + 8 (l / 32) .., then the same + 32
-  u32x2 v[D / 32][2];
-  u32x4 vs[2][2];
-  float ks;
-  uint32_t meta;
-};
-
-// NT: the tile is read by this wave alone
-template <bool NT>
-__device__ inline u32x4 ldt16(const char* p) {
-  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-  return *reinterpret_cast<const u32x4*>(p);
-}
-template <bool NT>
-__device__ inline u32x2 ldt8(const char* p) {
-  if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
-  return *reinterpret_cast<const u32x2*>(p);
-}
-
-struct LaneAt {
-  int k, v;     // byte offsets of the lane's first key and value piece in a tile
-  int ks, vs;   // and of its scales (8-bit pages)
+// How the four waves of a workgroup share a unit's columns (32 to a wave) and
+// tiles: CW side by side over the columns, KW = 4 / CW over the tiles.  Tiles go
+// through LDS by hardware copies, as they are stored: the products read their
+// operands from there, so that the registers are left to queries and sums, and
+// two workgroups fit a compute unit, each attending while the other waits.
+//   CW = 1: every wave attends tiles of its own and never waits for another
+//     before the end of a segment.  A tile's keys are copied as soon as the
+//     products have read those of the tile R before, its values likewise.
+//   else: stages of KW tiles in a ring of S, one barrier a stage.
+template <int D, bool FP8, int CW_>
+struct Shape {
+  static constexpr int CW = CW_, NW = 4, KW = NW / CW, UC = 32 * CW;
+  static constexpr bool PRIVATE = CW == 1;
+  static constexpr int kTile = FP8 ? D * 64 + 256 : D * 128;      // a stored tile
+  static constexpr int kFold = 32 * D * 4;                        // a wave's block of float32 sums
+  static constexpr int kSlots = FP8 ? 8 : 4;                      // tiles in LDS
+  static constexpr int R = kSlots / NW, S = kSlots / KW;
+  static constexpr int kWaveBytes = R * kTile > kFold ? R * kTile : kFold;
+  static constexpr int kLds = NW * kWaveBytes;
+  __device__ static constexpr int slot_at(int slot) { return PRIVATE ? slot / R * kWaveBytes + slot % R * kTile : slot * kTile; }
 };
 
-template <bool NT, int D>
-__device__ inline void load_tile(TileRegs<D>& r, const char* tile, const LaneAt& at) {
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) r.k[s] = ldt16<NT>(tile + at.k + (s >> 1) * 2048 + (s & 1) * 512);
-#pragma unroll
-  for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-    for (int y = 0; y < 2; ++y) r.v[b][y] = ldt16<NT>(tile + at.v + b * 2048 + y * 512);
+__device__ inline void copy16_once(const void* src, uint32_t m0) {   // a tile that this wave alone reads
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(m0), "v"(src) : "memory", "m0", "vcc");
 }
-template <bool NT, int D>
-__device__ inline void load_tile(TileRegsF8<D>& r, const char* tile, const LaneAt& at) {
-#pragma unroll
-  for (int x = 0; x < D / 32; ++x) r.k[x] = ldt16<NT>(tile + at.k + (x >> 1) * 2048 + (x & 1) * 512);
-#pragma unroll
-  for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-    for (int y = 0; y < 2; ++y) r.v[b][y] = ldt8<NT>(tile + at.v + b * 1024 + y * 512);
-  r.ks = *reinterpret_cast<const float*>(tile + at.ks);
-#pragma unroll
-  for (int y = 0; y < 2; ++y)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) r.vs[y][x] = ld16(tile + at.vs + y * 128 + x * 16);
+__device__ inline void copy4(const void* src, uint32_t m0) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" : : "s"(m0), "v"(src) : "memory", "m0", "vcc");
 }
+__device__ inline u32x4 lds16(uint32_t at) { return *reinterpret_cast<DMS_LDS const u32x4*>(at); }
+__device__ inline u32x2 lds8(uint32_t at) { return *reinterpret_cast<DMS_LDS const u32x2*>(at); }
 
 // 8 E4M3 codes to bf16 times a power of two (exact)
 __device__ inline u32x4 f8_bf16x8(uint32_t w0, uint32_t w1, float scale) {
@@ -333,134 +320,186 @@ __device__ inline u32x4 f8_bf16x8(uint32_t w0, uint32_t w1, float scale) {
   o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, scale, true));
   return o;
 }
-template <int D>
-__device__ inline void operands(const TileRegs<D>& r, u32x4 (&k)[D / 16], u32x4 (&v)[D / 32][2]) {
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s) k[s] = r.k[s];
-#pragma unroll
-  for (int b = 0; b < D / 32; ++b) v[b][0] = r.v[b][0], v[b][1] = r.v[b][1];
-}
-template <int D>
-__device__ inline void operands(const TileRegsF8<D>& r, u32x4 (&k)[D / 16], u32x4 (&v)[D / 32][2]) {
-  // piece (p, y) holds k-steps 4 p + y and 4 p + 2 + y
-#pragma unroll
-  for (int x = 0; x < D / 32; ++x) {
-    k[4 * (x >> 1) + (x & 1)] = f8_bf16x8(r.k[x][0], r.k[x][1], r.ks);
-    k[4 * (x >> 1) + 2 + (x & 1)] = f8_bf16x8(r.k[x][2], r.k[x][3], r.ks);
-  }
-#pragma unroll
-  for (int b = 0; b < D / 32; ++b)
-#pragma unroll
-    for (int y = 0; y < 2; ++y) v[b][y] = f8_bf16x8(r.v[b][y][0], r.v[b][y][1], 1.0f);
-}
-// value scale of the lane's row 8 (i / 8) + i % 8 of 16 (1 for bf16 pages)
-template <int D>
-__device__ inline float value_scale(const TileRegs<D>&, int) { return 1.0f; }
-template <int D>
-__device__ inline float value_scale(const TileRegsF8<D>& r, int i) {
-  return __uint_as_float(r.vs[i >> 3][(i >> 2) & 1][i & 3]);
-}
-// value (row j, dim e) of a stored tile; an 8-bit one without its scale
+
+// Byte offsets of the lane's first key and value piece in a tile, and of its
+// scales (8-bit pages).  The 32x32x16 products take
+//   keys: lane l of k-step s dims 16 s + 8 (l / 32) .. + 7 of row row_token(l % 32);
+//   values: lane l of (32-dim block b, half y) rows 16 y + 8 (l / 32) .. + 7 of
+//     dim 32 b + l % 32.
+struct LaneAt {
+  uint32_t k, v, ks, vs;
+};
 template <int D, bool FP8>
-__device__ inline float stored_value(const char* tile, int j, int e) {
-  if constexpr (FP8)
-    return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(*reinterpret_cast<const uint8_t*>(tile + fp8_v_off(j, e, D))), 0);
-  else
-    return __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(tile + v_elem_off(j, e, D))) << 16);
+__device__ inline LaneAt lane_at(int lane) {
+  const int hf = lane >> 5, kt = row_token(lane & 31), h = (kt >> 2) & 1, r = 4 * (kt >> 3) + (kt & 3);
+  LaneAt at;
+  at.k = h * 1024 + hf * 256 + r * 16;
+  if (FP8) {
+    at.v = D * 32 + hf * 256 + (lane & 15) * 16 + 8 * ((lane >> 4) & 1);
+    at.ks = D * 64 + (kt >> 3) * 64 + (kt & 7) * 4;
+    at.vs = D * 64 + hf * 64 + 32;
+  } else {
+    at.v = D * 64 + ((lane >> 4) & 1) * 1024 + hf * 256 + (lane & 15) * 16;
+    at.ks = at.vs = 0;
+  }
+  return at;
+}
+
+template <int D, bool FP8>
+__device__ inline u32x4 value_operand(uint32_t tile, const LaneAt& at, int b, int y) {
+  if constexpr (FP8) {
+    const u32x2 c = lds8(tile + at.v + b * 1024 + y * 512);
+    return f8_bf16x8(c[0], c[1], 1.0f);
+  } else {
+    return lds16(tile + at.v + b * 2048 + y * 512);
+  }
+}
+// value (row j, dim e) of a tile in LDS; an 8-bit one without its scale
+template <int D, bool FP8>
+__device__ inline float stored_value(uint32_t tile, int j, int e) {
+  if constexpr (FP8) {
+    const int code = *reinterpret_cast<DMS_LDS const uint8_t*>(tile + static_cast<uint32_t>(fp8_v_off(j, e, D)));
+    return __builtin_amdgcn_cvt_f32_fp8(code, 0);
+  } else {
+    return __uint_as_float(static_cast<uint32_t>(*reinterpret_cast<DMS_LDS const uint16_t*>(tile + static_cast<uint32_t>(v_elem_off(j, e, D)))) << 16);
+  }
 }
 
 // A segment of the flat list: tiles t0 .. t1 - 1 of unit `unit` of head hh.
 struct Segment {
-  TreeRow r;
+  int sh, L, tok0, m, p0, tile0;     // see TreeRow
   int hh, unit, t0, t1, T, nc, deep;
 };
 
 // The state of a wave's NC blocks of 32 columns; lane l: column l % 32.
-template <int D, int NC>
+template <int D, int NC = 1>
 struct Columns {
   u32x4 q[NC][D / 16];
   f32x16 o[NC][D / 32];
   float m[NC], l[NC];
-  int t[NC];              // position of the column's node
+  int t[NC];                 // position of the column's node
   const uint32_t* anc[NC];   // its ancestors, one word per tile of the tree
 };
 
-template <int D, bool FP8, int NC, class Regs>
-__device__ __forceinline__ void attend_tile(const TreeArgs& a, const Segment& sg, Columns<D, NC>& c, const Regs& r,
-                                            const char* tile, int t, int blocks, int lane) {
-  constexpr int KS = D / 16, OB = D / 32;
+// Rows of tile t that some column does not see, and what that takes.
+struct TileMask {
+  bool masked, tree;
+  uint32_t alive, old, odd;   // rows there; flagged and old enough for the deepest node; values not finite
+};
+
+// The masked tile's rows whose values are not finite.  A hidden row takes part
+// with weight 0, and 0 times an infinity or NaN is NaN: such rows are zeroed in
+// the products, as those past the end are, and added by hand to the columns that
+// see them.
+template <int D, bool FP8>
+__device__ __forceinline__ uint32_t odd_rows(uint32_t tile, int lane) {
+  const LaneAt at = lane_at<D, FP8>(fresh(lane));
+  uint32_t mine = 0;
+#pragma unroll 1
+  for (int z = 0; z < D / 16; ++z) {
+    const int b = z >> 1, y = z & 1;
+    const u32x4 v = value_operand<D, FP8>(tile, at, b, y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t x = (v[e >> 1] >> (16 * (e & 1))) & 0x7F80u;
+      mine |= (x == 0x7F80u ? 1u : 0u) << (16 * y + e);
+    }
+  }
+  mine <<= 8 * (lane >> 5);
+#pragma unroll
+  for (int off = 32; off; off >>= 1) mine |= __shfl_xor(mine, off, 64);
+  return __builtin_amdgcn_readfirstlane(mine);
+}
+
+template <int D, bool FP8>
+__device__ __forceinline__ TileMask tile_mask(const TreeArgs& a, const Segment& sg, uint32_t meta, uint32_t tile, int t, int lane) {
+  TileMask k;
+  k.tree = t >= sg.nc;
+  const int rows = k.tree ? sg.m - 32 * (t - sg.nc) : sg.L - 32 * t;
+  k.alive = rows >= 32 ? ~0u : (1u << rows) - 1u;
+  const bool soon = (meta & kFlagBit) != 0 && sg.deep - static_cast<int>(meta & ~kFlagBit) >= a.w;
+  k.old = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(soon)) & k.alive;
+  k.masked = k.tree || k.old != 0 || k.alive != ~0u;
+  k.odd = 0;
+  if (k.masked) k.odd = odd_rows<D, FP8>(tile, lane) & k.alive;
+  return k;
+}
+
+constexpr int kAhead = 4;   // products between an operand's LDS read and its use
+
+// Scores of the tile for every block of columns.
+template <int D, bool FP8, int NC>
+__device__ __forceinline__ void tile_scores(const Columns<D, NC>& c, f32x16 (&s)[NC], uint32_t tile, const LaneAt& at) {
+  constexpr int KS = D / 16;
+#pragma unroll
+  for (int x = 0; x < NC; ++x)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
+  if constexpr (FP8) {
+    const float ks = *reinterpret_cast<DMS_LDS const float*>(tile + at.ks);
+    // piece (p, y) holds k-steps 4 p + y and 4 p + 2 + y
+    u32x4 op[2] = {lds16(tile + at.k), lds16(tile + at.k + 512)};
+#pragma unroll
+    for (int e = 0; e < KS / 2; ++e) {
+      const u32x4 raw = op[e & 1];
+      if (e + 2 < KS / 2) op[e & 1] = lds16(tile + at.k + ((e + 2) >> 1) * 2048 + (e & 1) * 512);
+      const u32x4 k0 = f8_bf16x8(raw[0], raw[1], ks), k1 = f8_bf16x8(raw[2], raw[3], ks);
+#pragma unroll
+      for (int x = 0; x < NC; ++x) s[x] = mfma(k0, c.q[x][4 * (e >> 1) + (e & 1)], s[x]);
+#pragma unroll
+      for (int x = 0; x < NC; ++x) s[x] = mfma(k1, c.q[x][4 * (e >> 1) + 2 + (e & 1)], s[x]);
+    }
+  } else {
+    u32x4 op[kAhead];
+    auto read = [&](int e) { return lds16(tile + at.k + (e >> 1) * 2048 + (e & 1) * 512); };
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) op[e] = read(e);
+#pragma unroll
+    for (int e = 0; e < KS; ++e) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < NC; ++x) s[x] = mfma(op[e % kAhead], c.q[x][e], s[x]);
+      if (e + kAhead < KS) op[e % kAhead] = read(e + kAhead);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// Weights of the tile's rows (packed for the products) from the scores, and the
+// running maximum and sum.
+template <int D, bool FP8, int NC>
+__device__ __forceinline__ void tile_weights(const TreeArgs& a, const Segment& sg, Columns<D, NC>& c, f32x16 (&s)[NC], u32x4 (&pu)[NC][2],
+                                             uint32_t (&vis)[NC], const TileMask& k, uint32_t meta, uint32_t tile, const LaneAt& at,
+                                             int t, int lane) {
+  constexpr int OB = D / 32;
   const int hf = lane >> 5;
   const float sl2 = a.scale_log2, thr = kRescale / sl2;
   const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
-  u32x4 kf[KS], vf[OB][2];
-  operands(r, kf, vf);
-  // rows that some column does not see: none there, flagged and old enough for the
-  // deepest node, or any row of the tree
-  const bool tree = t >= sg.nc;
-  const int rows = tree ? sg.r.m - 32 * (t - sg.nc) : sg.r.L - 32 * t;
-  const uint32_t alive = rows >= 32 ? ~0u : (1u << rows) - 1u;
-  const bool soon = (r.meta & kFlagBit) != 0 && sg.deep - static_cast<int>(r.meta & ~kFlagBit) >= a.w;
-  const uint32_t old = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(soon)) & alive;
-  const bool masked = tree || old != 0 || alive != ~0u;
-  uint32_t odd = 0;       // rows whose values are not finite and which some column may not see
-  if (masked) {
-    // A hidden row takes part with weight 0, and 0 times an infinity or NaN is NaN:
-    // values of rows past the end are zeroed; those of rows that are not
-    // finite too, and are added by hand to the columns that see them.
-    uint32_t mine = 0;
+  u32x4 vs[2][2];
+  if constexpr (FP8) {
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        uint32_t any = 0;
-#pragma unroll
-        for (int b = 0; b < OB; ++b) {
-          const uint32_t x = (vf[b][y][e >> 1] >> (16 * (e & 1))) & 0x7F80u;
-          any |= x == 0x7F80u;
-        }
-        mine |= any << (16 * y + e);
-      }
-    mine <<= 8 * hf;
-#pragma unroll
-    for (int off = 32; off; off >>= 1) mine |= __shfl_xor(mine, off, 64);
-    odd = __builtin_amdgcn_readfirstlane(mine) & alive;
-    const uint32_t keep = (alive & ~odd) >> (8 * hf);
-    if ((alive & ~odd) != ~0u) {
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t bit = keep >> (16 * y + 2 * e);
-          const uint32_t and_ = ((bit & 1) ? 0x0000FFFFu : 0u) | ((bit & 2) ? 0xFFFF0000u : 0u);
-#pragma unroll
-          for (int b = 0; b < OB; ++b) vf[b][y][e] &= and_;
-        }
-    }
+      for (int x = 0; x < 2; ++x) vs[y][x] = lds16(tile + at.vs + y * 128 + x * 16);
   }
 #pragma unroll
   for (int x = 0; x < NC; ++x) {
-    if (x >= blocks) break;
-    f32x16 s;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.f;
-#pragma unroll
-    for (int e = 0; e < KS; ++e) s = mfma(kf[e], c.q[x][e], s);
-    uint32_t vis = ~0u;
-    if (masked) {
-      vis = alive;
-      if (tree) vis &= c.anc[x][t - sg.nc];
-      for (uint32_t left = old; left; left &= left - 1) {
+    vis[x] = ~0u;
+    if (k.masked) {
+      vis[x] = k.alive;
+      if (k.tree) vis[x] &= c.anc[x][t - sg.nc];
+      for (uint32_t left = k.old; left; left &= left - 1) {
         const int j = __builtin_ctz(left);
-        const int kp = static_cast<int>(__builtin_amdgcn_readlane(static_cast<int>(r.meta), j) & ~kFlagBit);
-        if (c.t[x] - kp >= a.w) vis &= ~(1u << j);
+        const int kp = static_cast<int>(__builtin_amdgcn_readlane(static_cast<int>(meta), j) & ~kFlagBit);
+        if (c.t[x] - kp >= a.w) vis[x] &= ~(1u << j);
       }
-      const uint32_t mine = vis >> (8 * hf);
+      const uint32_t mine = vis[x] >> (8 * hf);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = (mine >> (16 * (i >> 3) + (i & 7))) & 1 ? s[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) s[x][i] = (mine >> (16 * (i >> 3) + (i & 7))) & 1 ? s[x][i] : -INFINITY;
     }
-    float mx = s[0];
+    float mx = s[x][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
     mx = col_max(mx);
     const bool raise = mx > c.m[x] + thr;   // false while the column has seen no key
     if (__builtin_amdgcn_ballot_w64(raise)) {
@@ -474,66 +513,107 @@ __device__ __forceinline__ void attend_tile(const TreeArgs& a, const Segment& sg
     // weights 2^((s - m) scale), rounded to bf16 for the products; the
     // denominator adds the rounded values, so that one dominant key returns its
     // value row exactly.  8-bit pages: the weight of the product carries the
-    // value scale, a power of two
+    // value scale, a power of two, so that its rounding is the same
     const float mb = c.m[x] * sl2;
-    u32x4 pu[2];
-    float w[16];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const f32x2 pr = {__builtin_amdgcn_exp2f(fmaf(s[2 * j], sl2, -mb)),
-                        __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], sl2, -mb))};
+      f32x2 pr = {__builtin_amdgcn_exp2f(fmaf(s[x][2 * j], sl2, -mb)),
+                  __builtin_amdgcn_exp2f(fmaf(s[x][2 * j + 1], sl2, -mb))};
       const bf16x2 pb = __builtin_convertvector(pr, bf16x2);
       c.l[x] = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, c.l[x], false);
-      w[2 * j] = static_cast<float>(pb[0]);
-      w[2 * j + 1] = static_cast<float>(pb[1]);
       if constexpr (FP8) {
-        w[2 * j] *= value_scale(r, 2 * j);
-        w[2 * j + 1] *= value_scale(r, 2 * j + 1);
-        const f32x2 ws = {w[2 * j], w[2 * j + 1]};
-        pu[j >> 2][j & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(ws, bf16x2));
+        pr[0] *= __uint_as_float(vs[j >> 2][(j >> 1) & 1][2 * j & 3]);
+        pr[1] *= __uint_as_float(vs[j >> 2][(j >> 1) & 1][(2 * j + 1) & 3]);
+        pu[x][j >> 2][j & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
       } else {
-        pu[j >> 2][j & 3] = __builtin_bit_cast(uint32_t, pb);
+        pu[x][j >> 2][j & 3] = __builtin_bit_cast(uint32_t, pb);
       }
     }
+  }
+}
+
+// Rows whose values are not finite, added to the columns that see them.
+template <int D, bool FP8, int NC>
+__device__ __forceinline__ void odd_values(Columns<D, NC>& c, const u32x4 (&pu)[NC][2], const uint32_t (&vis)[NC], uint32_t odd,
+                                           uint32_t tile, int lane) {
+  for (uint32_t left = odd; left; left &= left - 1) {
+    const int j = __builtin_ctz(left), ln = fresh(lane);
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
+    for (int x = 0; x < NC; ++x) {
+      uint32_t pair = 0;
 #pragma unroll
-      for (int b = 0; b < OB; ++b) c.o[x][b] = mfma(vf[b][y], pu[y], c.o[x][b]);
-    for (uint32_t left = odd; left; left &= left - 1) {
-      const int j = __builtin_ctz(left);
-      float pj = 0.f;
+      for (int i = 0; i < 8; ++i)
+        if (i == (8 * (j >> 4) + (j & 7)) >> 1) pair = pu[x][i >> 2][i & 3];
+      float pj = __uint_as_float(j & 1 ? pair & 0xFFFF0000u : pair << 16);
+      pj = __shfl(pj, (ln & 31) + 32 * ((j >> 3) & 1), 64);
+      const bool seen = (vis[x] >> j) & 1;
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i == 8 * (j >> 4) + (j & 7)) pj = w[i];
-      pj = __shfl(pj, (lane & 31) + 32 * ((j >> 3) & 1), 64);
-      const bool seen = (vis >> j) & 1;
-#pragma unroll
-      for (int b = 0; b < OB; ++b)
+      for (int b = 0; b < D / 32; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float val = stored_value<D, FP8>(tile, j, 32 * b + 8 * (i >> 2) + 4 * hf + (i & 3));
+          const float val = stored_value<D, FP8>(tile, j, 32 * b + 8 * (i >> 2) + 4 * (ln >> 5) + (i & 3));
           c.o[x][b][i] = seen ? fmaf(pj, val, c.o[x][b][i]) : c.o[x][b][i];
+          asm volatile("" ::: "memory");     // one value at a time: this is rare, its registers are not
         }
     }
   }
 }
 
-// Workgroup: 4 waves, CW of them side by side over the columns of a unit (NC
-// blocks of 32 each), 4 / CW over its tiles.  A wave streams its tiles straight
-// into operand registers, the next one's loads in flight while it attends the
-// present one; waves meet only to fold their results at a segment's end.
-template <int D, bool FP8, int NC, int CW>
-__global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
-  constexpr int KW = 4 / CW, KS = D / 16, OB = D / 32, UC = 32 * NC * CW;
-  constexpr size_t TB = FP8 ? static_cast<size_t>(D) * 64 + 256 : static_cast<size_t>(D) * 128;
-  using Regs = typename std::conditional<FP8, TileRegsF8<D>, TileRegs<D>>::type;
-  __shared__ __attribute__((aligned(16))) float fold[4][32][D + 4];
-  __shared__ float2 ml_lds[4][32 * NC];
-  __shared__ int first[4];
+template <int D, bool FP8, int NC>
+__device__ __forceinline__ void tile_values(Columns<D, NC>& c, const u32x4 (&pu)[NC][2], const uint32_t (&vis)[NC], const TileMask& k,
+                                            uint32_t tile, const LaneAt& at, int lane) {
+  constexpr int OB = D / 32;
+  const uint32_t keep = k.alive & ~k.odd;
+  if (keep != ~0u) {
+    const uint32_t mine = keep >> (8 * (lane >> 5));
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      u32x4 and_;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t bit = mine >> (16 * y + 2 * e);
+        and_[e] = ((bit & 1) ? 0x0000FFFFu : 0u) | ((bit & 2) ? 0xFFFF0000u : 0u);
+      }
+#pragma unroll
+      for (int b = 0; b < OB; ++b) {
+        const u32x4 v = value_operand<D, FP8>(tile, at, b, y) & and_;
+#pragma unroll
+        for (int x = 0; x < NC; ++x) c.o[x][b] = mfma(v, pu[x][y], c.o[x][b]);
+      }
+    }
+    if (k.odd) odd_values<D, FP8, NC>(c, pu, vis, k.odd, tile, lane);
+    return;
+  }
+  u32x4 op[kAhead];
+  auto read = [&](int e) { return value_operand<D, FP8>(tile, at, e % OB, e / OB); };
+#pragma unroll
+  for (int e = 0; e < kAhead; ++e) op[e] = read(e);
+#pragma unroll
+  for (int e = 0; e < 2 * OB; ++e) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int x = 0; x < NC; ++x) c.o[x][e % OB] = mfma(op[e % kAhead], pu[x][e / OB], c.o[x][e % OB]);
+    if (e + kAhead < 2 * OB) op[e % kAhead] = read(e + kAhead);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// The workgroup's part of the flat list, segment by segment.
+template <int D, bool FP8, int CW>
+__global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
+  using Sh = Shape<D, FP8, CW>;
+  constexpr int NC = 1;
+  constexpr bool PRIVATE = Sh::PRIVATE;
+  constexpr int NW = Sh::NW, KW = Sh::KW, UC = Sh::UC, KS = D / 16, OB = D / 32, TB = Sh::kTile;
+  __shared__ __attribute__((aligned(1024))) char tiles_lds[Sh::kLds];
+  __shared__ __attribute__((aligned(16))) uint32_t meta_lds[Sh::kSlots][64];
+  __shared__ float2 ml_lds[NW][32];
+  __shared__ int first[NW];
   if (load_status(a.status) != 0) return;
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int cw = wave % CW, kw = wave / CW;
+  // waves of the same columns on different SIMDs: a unit with few columns leaves none idle
+  const int cw = wave / KW, kw = wave % KW;
   const int NH = a.n * a.H, Hq = a.H * a.g;
   const int total = *(const DMS_CONST int32_t*)(a.cum + NH);
   const int parts = parts_of(total, a.min_tiles, a.G);
@@ -542,147 +622,225 @@ __global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
   // the last head whose first flat tile is not past tb
   {
     int cnt = 0;
-    for (int x = tid; x < NH; x += 256) cnt += a.cum[x] <= tb;
+    for (int x = tid; x < NH; x += 64 * NW) cnt += a.cum[x] <= tb;
     for (int off = 32; off; off >>= 1) cnt += __shfl_xor(cnt, off, 64);
     if (lane == 0) first[wave] = cnt;
   }
   __syncthreads();
-  int hh = first[0] + first[1] + first[2] + first[3] - 1;
+  int hh = -1;
+  for (int x = 0; x < NW; ++x) hh += first[x];
   hh = __builtin_amdgcn_readfirstlane(hh);
-  LaneAt at;
-  {
-    const int kt = row_token(lane & 31), h = (kt >> 2) & 1, r = 4 * (kt >> 3) + (kt & 3);
-    if (FP8) {
-      at.k = h * 1024 + hf * 256 + r * 16;
-      at.v = D * 32 + hf * 256 + (lane & 15) * 16 + 8 * ((lane >> 4) & 1);
-      at.ks = D * 64 + (kt >> 3) * 64 + (kt & 7) * 4;
-      at.vs = D * 64 + hf * 64 + 32;
-    } else {
-      at.k = h * 1024 + hf * 256 + r * 16;
-      at.v = D * 64 + ((lane >> 4) & 1) * 1024 + hf * 256 + (lane & 15) * 16;
-      at.ks = at.vs = 0;
-    }
-  }
+  const LaneAt at = lane_at<D, FP8>(lane);
+  const uint32_t lds0 = lds_addr(tiles_lds), meta0 = lds_addr(meta_lds[0]);
+
   for (int f = tb; f < te;) {
     while (((const DMS_CONST int32_t*)a.cum)[hh + 1] <= f) ++hh;   // heads without nodes have no tiles
     Segment sg;
     {
       typedef int __attribute__((ext_vector_type(8))) i32x8;
       const i32x8 rd = *((const DMS_CONST i32x8*)(a.rows + hh));
-      sg.r.sh = rd[0];
-      sg.r.L = rd[1];
-      sg.r.tok0 = rd[2];
-      sg.r.m = rd[3];
-      sg.r.p0 = rd[4];
-      sg.r.tile0 = rd[5];
-      sg.r.seq = rd[6];
+      sg.sh = rd[0];
+      sg.L = rd[1];
+      sg.tok0 = rd[2];
+      sg.m = rd[3];
+      sg.p0 = rd[4];
+      sg.tile0 = rd[5];
+      sg.deep = rd[4] + ((const DMS_CONST int32_t*)a.deepest)[rd[6]];
     }
     const int at0 = f - ((const DMS_CONST int32_t*)a.cum)[hh];
     sg.hh = hh;
-    sg.T = tiles_of(sg.r.L, sg.r.m);
+    sg.T = tiles_of(sg.L, sg.m);
     sg.unit = at0 / sg.T;
     sg.t0 = at0 - sg.unit * sg.T;
     sg.t1 = min(sg.T, sg.t0 + te - f);
-    sg.nc = (sg.r.L + 31) >> 5;
-    sg.deep = sg.r.p0 + ((const DMS_CONST int32_t*)a.deepest)[sg.r.seq];
-    const int h = hh % a.H, cols = sg.r.m * a.g;
+    sg.nc = (sg.L + 31) >> 5;
+    const int h = hh % a.H, cols = sg.m * a.g;
+    const int nt = sg.t1 - sg.t0;
+
+    // ---- tiles: sources and copies
+    auto page_of = [&](int t) {
+      return t < sg.nc ? ((const DMS_CONST int32_t*)(a.page_table + static_cast<size_t>(sg.sh) * a.maxp))[(32 * t) >> a.log2P] : 0;
+    };
+    auto source = [&](int t, int page) -> const char* {
+      return t < sg.nc ? a.pool + static_cast<size_t>(page) * a.page_bytes + static_cast<size_t>(((32 * t) & (a.P - 1)) >> 5) * TB
+                       : a.tiles + (static_cast<size_t>(sg.tile0) + (t - sg.nc)) * TB;
+    };
+    auto meta_of = [&](int t) -> const uint32_t* {
+      return t < sg.nc ? reinterpret_cast<const uint32_t*>(a.slot_meta + static_cast<size_t>(sg.sh) * a.max_slots) + 32 * t
+                       : a.tmeta + (static_cast<size_t>(sg.tile0) + (t - sg.nc)) * 32;
+    };
+
     // ---- this wave's columns
     const int col0 = sg.unit * UC + cw * 32 * NC;
-    const int blocks = max(0, min(NC, (cols - col0 + 31) / 32));
+    const bool busy = col0 < cols;
     Columns<D, NC> c;
+    auto load_columns = [&]() {
 #pragma unroll
-    for (int x = 0; x < NC; ++x) {
-      const int col = col0 + 32 * x + (lane & 31);
-      const bool ok = col < cols;
-      const int node = ok ? col / a.g : 0, qh = ok ? col % a.g : 0;
-      const size_t tok = static_cast<size_t>(sg.r.tok0) + node;
-      const uint16_t* q = a.q + (tok * Hq + h * a.g + qh) * D + 8 * hf;
+      for (int x = 0; x < NC; ++x) {
+        const int ln = fresh(lane), col = col0 + 32 * x + (ln & 31);
+        const bool ok = col < cols;
+        const int node = ok ? col / a.g : 0, qh = ok ? col % a.g : 0;
+        const size_t tok = static_cast<size_t>(sg.tok0) + node;
+        const uint16_t* q = a.q + (tok * Hq + h * a.g + qh) * D + 8 * (ln >> 5);
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-        c.q[x][s] = ok ? *reinterpret_cast<const u32x4*>(q + 16 * s) : u32x4{0u, 0u, 0u, 0u};
-      // the borrowed decision neuron takes no part in attention (App. C)
-      if (a.zero_neuron && qh == 0 && hf == 0) c.q[x][0][0] &= 0xFFFF0000u;
-      c.t[x] = sg.r.p0 + a.depth[tok];
-      c.anc[x] = a.anc + tok * a.words;
-      c.m[x] = kMInit;
-      c.l[x] = 0.f;
+        for (int s = 0; s < KS; ++s)
+          c.q[x][s] = ok ? *reinterpret_cast<const u32x4*>(q + 16 * s) : u32x4{0u, 0u, 0u, 0u};
+        // the borrowed decision neuron takes no part in attention (App. C)
+        if (a.zero_neuron && qh == 0 && hf == 0) c.q[x][0][0] &= 0xFFFF0000u;
+        c.t[x] = sg.p0 + a.depth[tok];
+        c.anc[x] = a.anc + tok * a.words;
+        c.m[x] = kMInit;
+        c.l[x] = 0.f;
 #pragma unroll
-      for (int b = 0; b < OB; ++b)
+        for (int b = 0; b < OB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) c.o[x][b][i] = 0.f;
-    }
-    // ---- its tiles
-    auto source = [&](int t) -> const char* {
-      if (t >= sg.nc) return a.tiles + (static_cast<size_t>(sg.r.tile0) + (t - sg.nc)) * TB;
-      const int page = ((const DMS_CONST int32_t*)(a.page_table + static_cast<size_t>(sg.r.sh) * a.maxp))[(32 * t) >> a.log2P];
-      return a.pool + static_cast<size_t>(page) * a.page_bytes + static_cast<size_t>(((32 * t) & (a.P - 1)) >> 5) * TB;
-    };
-    auto load = [&](Regs& r, int t) -> const char* {
-      const char* tile = source(t);
-      load_tile<CW == 1>(r, tile, at);
-      if (t < sg.nc) {
-        r.meta = static_cast<uint32_t>(a.slot_meta[static_cast<size_t>(sg.r.sh) * a.max_slots + 32 * t + (lane & 31)]);
-      } else {
-        const int x = min(32 * (t - sg.nc) + (lane & 31), sg.r.m - 1);
-        const size_t node = static_cast<size_t>(sg.r.tok0) + x;
-        r.meta = static_cast<uint32_t>(sg.r.p0 + a.depth[node]) | (a.flags[node * a.H + h] ? kFlagBit : 0u);
+          for (int i = 0; i < 16; ++i) c.o[x][b][i] = 0.f;
       }
-      return tile;
     };
-    if (blocks > 0 && sg.t0 + kw < sg.t1) {
-      Regs ra, rb;
-      int t = sg.t0 + kw;
-      const int last = t + (sg.t1 - 1 - t) / KW * KW;
-      const char* ta = load(ra, t);
-      while (true) {
-        const char* tb2 = load(rb, min(t + KW, last));
-        attend_tile<D, FP8, NC>(a, sg, c, ra, ta, t, blocks, lane);
-        t += KW;
-        if (t > last) break;
-        ta = load(ra, min(t + KW, last));
-        attend_tile<D, FP8, NC>(a, sg, c, rb, tb2, t, blocks, lane);
-        t += KW;
-        if (t > last) break;
+
+    if constexpr (PRIVATE) {
+      constexpr int R = Sh::R, KC = (FP8 ? D / 32 + 1 : D / 16) + 1, VC = FP8 ? D / 32 : D / 16;
+      // keys of own tile u (with the row's owners; 8-bit pages: the scales too) and its values
+      auto copy_keys = [&](int u, const char* tile) {
+        const int slot = wave * R + u % R;
+        const uint32_t dst = lds0 + Sh::slot_at(slot);
+#pragma unroll
+        for (int x = 0; x < D * (FP8 ? 32 : 64) / 1024; ++x) copy16_once(tile + 16 * lane + 1024 * x, dst + 1024 * x);
+        if constexpr (FP8) copy4(tile + D * 64 + 4 * lane, dst + D * 64);
+        copy4(meta_of(sg.t0 + kw + u * KW) + (lane & 31), meta0 + 256 * slot);
+      };
+      auto copy_values = [&](int u, const char* tile) {
+        constexpr int V0 = D * (FP8 ? 32 : 64);
+        const uint32_t dst = lds0 + Sh::slot_at(wave * R + u % R) + V0;
+#pragma unroll
+        for (int x = 0; x < V0 / 1024; ++x) copy16_once(tile + V0 + 16 * lane + 1024 * x, dst + 1024 * x);
+      };
+      const int n = max(0, (nt - kw + KW - 1) / KW);   // own tiles: t0 + kw, + KW, ..
+      const char* src[R];
+#pragma unroll
+      for (int u = 0; u < R; ++u)
+        if (u < n) {
+          const int t = sg.t0 + kw + u * KW;
+          src[u] = source(t, page_of(t));
+          copy_keys(u, src[u]);
+          copy_values(u, src[u]);
+        }
+      load_columns();
+      int page = R < n ? page_of(sg.t0 + kw + R * KW) : 0;
+      for (int u = 0; u < n; ++u) {
+        const int t = sg.t0 + kw + u * KW, slot = wave * R + u % R;
+        const uint32_t tile = lds0 + Sh::slot_at(slot);
+        if (u + R - 1 < n) wait_copies_but<VC + (R - 1) * (KC + VC)>();
+        else wait_copies();
+        asm volatile("" ::: "memory");
+        const uint32_t meta = meta_lds[slot][lane & 31];
+        f32x16 s[NC];
+        tile_scores<D, FP8, NC>(c, s, tile, at);
+        u32x4 pu[NC][2];
+        uint32_t vis[NC];
+        const bool more = u + R < n;
+        const char* next = source(sg.t0 + kw + (u + R) * KW, page);
+        // 8-bit pages: the scales lie in the keys' copies and are read for the weights
+        if constexpr (!FP8) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (more) copy_keys(u + R, next);
+        }
+        if (more) wait_copies_but<(R - 1) * (KC + VC) + (FP8 ? 0 : KC)>();
+        else wait_copies();
+        asm volatile("" ::: "memory");
+        const TileMask k = tile_mask<D, FP8>(a, sg, meta, tile, t, lane);
+        tile_weights<D, FP8, NC>(a, sg, c, s, pu, vis, k, meta, tile, at, t, lane);
+        if constexpr (FP8) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (more) copy_keys(u + R, next);
+        }
+        tile_values<D, FP8, NC>(c, pu, vis, k, tile, at, lane);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) copy_values(u + R, next);
+        if (u + R + 1 < n) page = page_of(sg.t0 + kw + (u + R + 1) * KW);
+      }
+    } else {
+      // a stage's copies: KW tiles, CW waves to each (past the end: the last one again, not
+      // attended)
+      constexpr int S = Sh::S, kPieces = TB / 1024 / CW, PC = kPieces + 1 + FP8;
+      const int ns = (nt + KW - 1) / KW;
+      const int my = wave / CW, share = wave % CW;
+      auto copy_stage = [&](int st, int page) {
+        const int t = min(sg.t0 + st * KW + my, sg.t1 - 1), slot = st % S * KW + my;
+        const char* tile = source(t, page) + 16 * lane;
+        const uint32_t dst = lds0 + Sh::slot_at(slot);
+#pragma unroll
+        for (int x = 0; x < kPieces; ++x) {
+          const int at1 = 1024 * (kPieces * share + x);
+          if (a.once) copy16_once(tile + at1, dst + at1);
+          else lds_copy16(tile + at1, dst + at1);
+        }
+        if constexpr (FP8) copy4(tile + D * 64 - 12 * lane, dst + D * 64);
+        copy4(meta_of(t) + (lane & 31), meta0 + 256 * slot);
+      };
+      auto stage_page = [&](int st) { return page_of(min(sg.t0 + st * KW + my, sg.t1 - 1)); };
+#pragma unroll
+      for (int st = 0; st < S - 1; ++st)
+        if (st < ns) copy_stage(st, stage_page(st));
+      load_columns();
+      int page = stage_page(S - 1);
+      for (int st = 0; st < ns; ++st) {
+        // all but the stages after it have landed
+        if (st + S - 2 < ns) wait_copies_but<(S - 2) * PC>();
+        else wait_copies();
+        __syncthreads();     // the stage is there, and no wave reads the one before it
+        if (st + S - 1 < ns) copy_stage(st + S - 1, page);
+        const int t = sg.t0 + st * KW + kw, slot = st % S * KW + kw;
+        if (busy && t < sg.t1) {
+          const uint32_t tile = lds0 + Sh::slot_at(slot), meta = meta_lds[slot][lane & 31];
+          f32x16 s[NC];
+          tile_scores<D, FP8, NC>(c, s, tile, at);
+          const TileMask k = tile_mask<D, FP8>(a, sg, meta, tile, t, lane);
+          u32x4 pu[NC][2];
+          uint32_t vis[NC];
+          tile_weights<D, FP8, NC>(a, sg, c, s, pu, vis, k, meta, tile, at, t, lane);
+          tile_values<D, FP8, NC>(c, pu, vis, k, tile, at, lane);
+        }
+        page = stage_page(st + S);
       }
     }
+
     // ---- fold the waves of a column block and write it: the outputs of a whole
     // unit, else a partial (slot 2 w: a unit that began before this workgroup's
-    // part; 2 w + 1: one that ends after it)
+    // part; 2 w + 1: one that ends after it).  A wave's sums lie in its own share
+    // of the tiles' LDS, 16-byte pieces flipped by column to spread the banks.
     const bool whole = sg.t0 == 0 && sg.t1 == sg.T;
-    const int slot = 2 * blockIdx.x + (sg.t0 == 0);
+    const int part = 2 * blockIdx.x + (sg.t0 == 0);
+    auto fold_at = [&](int w, int cc, int piece) {
+      return reinterpret_cast<f32x4*>(tiles_lds + w * Sh::kWaveBytes + cc * (D * 4) + 16 * (piece ^ (cc & 7)));
+    };
 #pragma unroll
     for (int x = 0; x < NC; ++x) {
+      __syncthreads();     // tiles (the block before) are read
       const float l = col_sum(c.l[x]);
-      if (lane < 32) ml_lds[wave][32 * x + lane] = make_float2(c.m[x], l);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < NC; ++x) {
-      float M = kMInit;
-#pragma unroll
-      for (int y = 0; y < KW; ++y) M = fmaxf(M, ml_lds[y * CW + cw][32 * x + (lane & 31)].x);
-      const float scale = __builtin_amdgcn_exp2f((c.m[x] - M) * a.scale_log2);
+      const int ln = fresh(lane), th = fresh(tid);     // (addresses formed here, not held ahead of the loops)
+      if (ln < 32) ml_lds[wave][ln] = make_float2(c.m[x], l);
 #pragma unroll
       for (int b = 0; b < OB; ++b)
 #pragma unroll
         for (int y = 0; y < 4; ++y)
-          *reinterpret_cast<f32x4*>(&fold[wave][lane & 31][32 * b + 8 * y + 4 * hf]) =
-              f32x4{c.o[x][b][4 * y], c.o[x][b][4 * y + 1], c.o[x][b][4 * y + 2], c.o[x][b][4 * y + 3]} * scale;
+          *fold_at(wave, ln & 31, 8 * b + 2 * y + (ln >> 5)) = f32x4{c.o[x][b][4 * y], c.o[x][b][4 * y + 1], c.o[x][b][4 * y + 2], c.o[x][b][4 * y + 3]};
       __syncthreads();
       // CW blocks of 32 columns, D / 4 pieces each
-      for (int e = tid; e < CW * 32 * (D / 4); e += 256) {
+      for (int e = th; e < CW * 32 * (D / 4); e += 64 * NW) {
         const int piece = e % (D / 4), cc = e / (D / 4) % 32, cx = e / (D / 4) / 32;
         const int uc = (cx * NC + x) * 32 + cc, col = sg.unit * UC + uc;
         if (col >= cols) continue;
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        float Mc = kMInit, L = 0.f;
+        float M = kMInit, L = 0.f;
 #pragma unroll
-        for (int y = 0; y < KW; ++y) Mc = fmaxf(Mc, ml_lds[y * CW + cx][32 * x + cc].x);
+        for (int y = 0; y < KW; ++y) M = fmaxf(M, ml_lds[cx * KW + y][cc].x);
 #pragma unroll
         for (int y = 0; y < KW; ++y) {
-          const float2 ml = ml_lds[y * CW + cx][32 * x + cc];
-          L += ml.y * __builtin_amdgcn_exp2f((ml.x - Mc) * a.scale_log2);
-          sum += *reinterpret_cast<const f32x4*>(&fold[y * CW + cx][cc][4 * piece]);
+          const float2 ml = ml_lds[cx * KW + y][cc];
+          const float w = __builtin_amdgcn_exp2f((ml.x - M) * a.scale_log2);
+          L += ml.y * w;
+          sum += *fold_at(cx * KW + y, cc, piece) * w;
         }
         if (whole) {
           const int node = col / a.g, qh = col % a.g;
@@ -690,16 +848,16 @@ __global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
           const f32x2 lo = {sum[0] * inv, sum[1] * inv}, hi = {sum[2] * inv, sum[3] * inv};
           const u32x2 ob = {__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
                             __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
-          *reinterpret_cast<u32x2*>(a.out + ((static_cast<size_t>(sg.r.tok0) + node) * Hq + h * a.g + qh) * D + 4 * piece) = ob;
+          *reinterpret_cast<u32x2*>(a.out + ((static_cast<size_t>(sg.tok0) + node) * Hq + h * a.g + qh) * D + 4 * piece) = ob;
         } else {
-          const size_t pc = static_cast<size_t>(slot) * UC + uc;
+          const size_t pc = static_cast<size_t>(part) * UC + uc;
           *reinterpret_cast<f32x4*>(a.part_o + pc * D + 4 * piece) = sum;
-          if (piece == 0) a.part_ml[pc] = make_float2(Mc, L);
+          if (piece == 0) a.part_ml[pc] = make_float2(M, L);
         }
       }
-      __syncthreads();
     }
-    f += sg.t1 - sg.t0;
+    __syncthreads();       // the next segment's copies go where the sums are
+    f += nt;
   }
 }
 
@@ -1079,22 +1237,19 @@ __global__ __launch_bounds__(256) void commit_write_kernel(CommitArgs a) {
 // Launches
 // ---------------------------------------------------------------------------
 
-// compute units of the current device, at most what a workspace holds partials for
+// two workgroups a compute unit, at most what a workspace holds partials for
 int tree_workgroups() {
   int dev = 0, v = 0;
   if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v < 1)
     return kTreeWorkgroups;
-  return std::min(v, kTreeWorkgroups);
+  return std::min(2 * v, kTreeWorkgroups);
 }
 
-// Column blocks of a wave and waves side by side for the largest tree of a call.
-struct TreeShape {
-  int nc, cw;
-};
-TreeShape tree_shape(int cols) { return cols <= 32 ? TreeShape{1, 1} : cols <= 64 ? TreeShape{2, 1} : cols <= 128 ? TreeShape{2, 2} : TreeShape{2, 4}; }
+// Waves side by side over the columns, for the largest tree of a call.
+int tree_waves(int cols) { return cols <= 32 ? 1 : cols <= 64 ? 2 : 4; }
 
 struct TreeLayout {
-  size_t rows, cum, anc, depth, node_seq, deepest, flags, tiles, part_o, part_ml, need, fresh, base, before, bytes;
+  size_t rows, cum, anc, depth, node_seq, deepest, flags, tiles, tmeta, part_o, part_ml, need, fresh, base, before, bytes;
   int words, tph, UC;
 };
 TreeLayout tree_layout(const dms_config& c, int n, int total, int max_nodes) {
@@ -1107,10 +1262,9 @@ TreeLayout tree_layout(const dms_config& c, int n, int total, int max_nodes) {
   lo.base = take(NH * 4);
   lo.before = take((n + NH + 4) * 4);
   if (c.kv_format != DMS_KV_MLA) {
-    const TreeShape sh = tree_shape(max_nodes * c.group_size);
     lo.words = std::max(1, (max_nodes + 31) / 32);
     lo.tph = total / 32 + n + 1;
-    lo.UC = 32 * sh.nc * sh.cw;
+    lo.UC = 32 * tree_waves(max_nodes * c.group_size);
     lo.rows = take(NH * sizeof(TreeRow));
     lo.cum = take((NH + 1) * 4);
     lo.anc = take(T * lo.words * 4);
@@ -1119,6 +1273,7 @@ TreeLayout tree_layout(const dms_config& c, int n, int total, int max_nodes) {
     lo.deepest = take(static_cast<size_t>(n) * 4);
     lo.flags = take(T * H);
     lo.tiles = take(H * static_cast<size_t>(lo.tph) * (c.kv_format == DMS_KV_FP8 ? fp8_tile_bytes(c.head_dim) : tile_bytes(c.head_dim)));
+    lo.tmeta = take(H * static_cast<size_t>(lo.tph) * 32 * 4);
     lo.part_o = take(size_t(2) * kTreeWorkgroups * lo.UC * D * 4);
     lo.part_ml = take(size_t(2) * kTreeWorkgroups * lo.UC * 8);
   }
@@ -1127,13 +1282,12 @@ TreeLayout tree_layout(const dms_config& c, int n, int total, int max_nodes) {
 }
 
 template <int D, bool FP8>
-hipError_t launch_attention(const TreeArgs& a, const TreeShape& sh, hipStream_t st) {
+hipError_t launch_attention(const TreeArgs& a, hipStream_t st) {
   const unsigned prep = 1u + a.n + static_cast<unsigned>(a.n) * a.H * a.words;
   hipLaunchKernelGGL((tree_prep_kernel<D, FP8>), dim3(prep), dim3(kPrepThreads), 0, st, a);
-  if (sh.nc == 1) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 1, 1>), dim3(a.G), dim3(256), 0, st, a);
-  else if (sh.cw == 1) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 2, 1>), dim3(a.G), dim3(256), 0, st, a);
-  else if (sh.cw == 2) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 2, 2>), dim3(a.G), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 2, 4>), dim3(a.G), dim3(256), 0, st, a);
+  if (a.UC == 32) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 1>), dim3(a.G), dim3(256), 0, st, a);
+  else if (a.UC == 64) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 2>), dim3(a.G), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 4>), dim3(a.G), dim3(256), 0, st, a);
   const int64_t rows = static_cast<int64_t>(a.total) * a.H * a.g;
   const unsigned merge = static_cast<unsigned>(std::min<int64_t>((rows + 3) / 4, 1 << 20));
   hipLaunchKernelGGL((tree_merge_kernel<D>), dim3(merge), dim3(256), 0, st, a);
@@ -1151,7 +1305,6 @@ hipError_t launch_tree_attention(const dms_config& c, const Layout& lo, void* me
                                  const int32_t* parents, const void* q, const void* k, const void* v,
                                  const uint8_t* flags, uint8_t* decisions_out, void* out, void* ws, hipStream_t st) {
   const TreeLayout tl = tree_layout(c, n, total, max_nodes);
-  const TreeShape sh = tree_shape(max_nodes * c.group_size);
   char* w = static_cast<char*>(ws);
   const LayerState s = layer_state(lo, meta, layer);
   TreeArgs a{};
@@ -1180,6 +1333,7 @@ hipError_t launch_tree_attention(const dms_config& c, const Layout& lo, void* me
   a.node_seq = reinterpret_cast<int32_t*>(w + tl.node_seq);
   a.deepest = reinterpret_cast<int32_t*>(w + tl.deepest);
   a.tiles = w + tl.tiles;
+  a.tmeta = reinterpret_cast<uint32_t*>(w + tl.tmeta);
   a.part_o = reinterpret_cast<float*>(w + tl.part_o);
   a.part_ml = reinterpret_cast<float2*>(w + tl.part_ml);
   a.page_bytes = lo.page_bytes;
@@ -1198,13 +1352,14 @@ hipError_t launch_tree_attention(const dms_config& c, const Layout& lo, void* me
   a.tph = tl.tph;
   a.G = tree_workgroups();
   a.UC = tl.UC;
-  a.min_tiles = 2 * (4 / sh.cw);
+  a.min_tiles = 256 / a.UC;
+  a.once = max_nodes * c.group_size <= a.UC;
   a.zero_neuron = c.decision_source == DMS_DECIDE_QUERY;
   a.bias = c.decision_bias;
   a.scale_log2 = c.softmax_scale * 1.4426950408889634f;
   const bool fp8 = c.kv_format == DMS_KV_FP8;
-  if (c.head_dim == 64) return fp8 ? launch_attention<64, true>(a, sh, st) : launch_attention<64, false>(a, sh, st);
-  return fp8 ? launch_attention<128, true>(a, sh, st) : launch_attention<128, false>(a, sh, st);
+  if (c.head_dim == 64) return fp8 ? launch_attention<64, true>(a, st) : launch_attention<64, false>(a, st);
+  return fp8 ? launch_attention<128, true>(a, st) : launch_attention<128, false>(a, st);
 }
 
 hipError_t launch_tree_accept(int n, const int32_t* cu, int total, int max_nodes, const int32_t* parents,
