@@ -45,6 +45,13 @@ struct __attribute__((aligned(32))) TreeRow {
   int sh, L, tok0, m, p0, tile0, seq, pad;   // state head, live slots, first node, nodes, position, first tile of the tree
 };
 
+// One equal part of a call's tiles: the first head's row beside it, so that a
+// workgroup starts with one load.
+struct __attribute__((aligned(64))) TreePart {
+  int tb, te, hh, c0;      // flat tiles [tb, te), the head that holds tb, its first flat tile
+  TreeRow r;
+};
+
 struct TreeArgs {
   int32_t* status;
   const int32_t* seq_ids;
@@ -63,9 +70,9 @@ struct TreeArgs {
   uint16_t* out;           // [total, Hq, D] bf16
   TreeRow* rows;           // [n * H]
   int32_t* cum;            // [n * H + 1] flat tiles before each head
+  TreePart* part;          // [cells] (te = tb: no such part)
   uint32_t* anc;           // [total][words] ancestors and itself, bit a: node a of its tree
   int32_t* depth;          // [total]
-  int32_t* node_seq;       // [total]
   int32_t* deepest;        // [n]
   char* tiles;             // [H][tph] tiles of the drafted rows
   uint32_t* tmeta;         // [H][tph][32] their rows (position | flag << 31), as the pool's slot owners
@@ -73,16 +80,15 @@ struct TreeArgs {
   float2* part_ml;         // [2 G][UC]
   size_t page_bytes;
   int n, H, g, w, P, log2P, maxp, max_slots, max_seqs, total, max_nodes, words, tph;
-  int G, UC, min_tiles;    // workgroups, columns of a unit, flat tiles a workgroup takes at least
+  int cells, U, UC, min_tiles;   // parts at most, units (workgroups) to a part, columns of a unit, least tiles of a part
   int zero_neuron;
   int once;                // every tile is read by one workgroup
   float bias, scale_log2;
 };
 
-__host__ __device__ inline int units_of(int cols, int UC) { return (cols + UC - 1) / UC; }
-__device__ inline int tiles_of(int L, int m) { return ((L + 31) >> 5) + ((m + 31) >> 5); }
-// Workgroups that share `total` flat tiles, and where part w begins.
-__device__ inline int parts_of(int total, int min_tiles, int G) { return max(1, min(G, total / min_tiles)); }
+__device__ inline int tiles_of(int L, int m) { return m ? ((L + 31) >> 5) + ((m + 31) >> 5) : 0; }
+// Parts that share `total` flat tiles, and where part w begins.
+__device__ inline int parts_of(int total, int min_tiles, int cells) { return max(1, min(cells, total / min_tiles)); }
 __device__ inline int part_begin(int w, int total, int parts) {
   return static_cast<int>(static_cast<int64_t>(w) * total / parts);
 }
@@ -132,7 +138,7 @@ __device__ void tree_plan(const TreeArgs& a) {
       r.seq = i;
       r.pad = 0;
       a.rows[hh] = r;
-      tiles = r.m ? tiles_of(r.L, r.m) * units_of(r.m * a.g, a.UC) : 0;
+      tiles = tiles_of(r.L, r.m);
     }
     int tot;
     const int ex = block_exclusive_scan(tiles, lds, &tot);
@@ -140,6 +146,24 @@ __device__ void tree_plan(const TreeArgs& a) {
     run += tot;
   }
   if (threadIdx.x == 0) a.cum[NH] = run;
+  __syncthreads();
+  const int parts = parts_of(run, a.min_tiles, a.cells);
+  for (int w = threadIdx.x; w < a.cells; w += blockDim.x) {
+    TreePart p{};
+    if (w < parts && run > 0) {
+      p.tb = part_begin(w, run, parts);
+      p.te = part_begin(w + 1, run, parts);
+      int lo = 0, hi = NH - 1;      // the last head whose first tile is not past tb
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.cum[mid] <= p.tb) lo = mid; else hi = mid - 1;
+      }
+      p.hh = lo;
+      p.c0 = a.cum[lo];
+      p.r = a.rows[lo];
+    }
+    a.part[w] = p;
+  }
 }
 
 // The next n blocks: ancestors of a sequence's nodes.  Bits and jumps double
@@ -191,7 +215,6 @@ __device__ void tree_ancestors(const TreeArgs& a, int i) {
       a.anc[static_cast<size_t>(tok0 + x) * a.words + u] = b;
     }
     a.depth[tok0 + x] = d;
-    a.node_seq[tok0 + x] = i;
     atomicMax(&deepest, d);
   }
   __syncthreads();
@@ -288,7 +311,9 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a) {
 //   CW = 1: every wave attends tiles of its own and never waits for another
 //     before the end of a segment.  A tile's keys are copied as soon as the
 //     products have read those of the tile R before, its values likewise.
-//   else: stages of KW tiles in a ring of S, one barrier a stage.
+//   CW = 2: stages of KW tiles in a ring of S, one barrier a stage.
+//   CW = 4: a wave attends the two tiles of a stage together (TPS), their chains
+//     of products and exponentials side by side.
 template <int D, bool FP8, int CW_>
 struct Shape {
   static constexpr int CW = CW_, NW = 4, KW = NW / CW, UC = 32 * CW;
@@ -296,7 +321,8 @@ struct Shape {
   static constexpr int kTile = FP8 ? D * 64 + 256 : D * 128;      // a stored tile
   static constexpr int kFold = 32 * D * 4;                        // a wave's block of float32 sums
   static constexpr int kSlots = FP8 ? 8 : 4;                      // tiles in LDS
-  static constexpr int R = kSlots / NW, S = kSlots / KW;
+  static constexpr int TPS = CW == 4 ? 2 : 1;
+  static constexpr int R = kSlots / NW, S = kSlots / (KW * TPS);
   static constexpr int kWaveBytes = R * kTile > kFold ? R * kTile : kFold;
   static constexpr int kLds = NW * kWaveBytes;
   __device__ static constexpr int slot_at(int slot) { return PRIVATE ? slot / R * kWaveBytes + slot % R * kTile : slot * kTile; }
@@ -365,20 +391,20 @@ __device__ inline float stored_value(uint32_t tile, int j, int e) {
   }
 }
 
-// A segment of the flat list: tiles t0 .. t1 - 1 of unit `unit` of head hh.
+// A segment of a part: tiles t0 .. t1 - 1 of head hh.
 struct Segment {
   int sh, L, tok0, m, p0, tile0;     // see TreeRow
-  int hh, unit, t0, t1, T, nc, deep;
+  int hh, t0, t1, T, nc, deep;
 };
 
-// The state of a wave's NC blocks of 32 columns; lane l: column l % 32.
-template <int D, int NC = 1>
+// The state of a wave's 32 columns; lane l: column l % 32.
+template <int D>
 struct Columns {
-  u32x4 q[NC][D / 16];
-  f32x16 o[NC][D / 32];
-  float m[NC], l[NC];
-  int t[NC];                 // position of the column's node
-  const uint32_t* anc[NC];   // its ancestors, one word per tile of the tree
+  u32x4 q[D / 16];
+  f32x16 o[D / 32];
+  float m, l;
+  int t;                 // position of the column's node
+  const uint32_t* anc;   // its ancestors, one word per tile of the tree
 };
 
 // Rows of tile t that some column does not see, and what that takes.
@@ -387,10 +413,7 @@ struct TileMask {
   uint32_t alive, old, odd;   // rows there; flagged and old enough for the deepest node; values not finite
 };
 
-// The masked tile's rows whose values are not finite.  A hidden row takes part
-// with weight 0, and 0 times an infinity or NaN is NaN: such rows are zeroed in
-// the products, as those past the end are, and added by hand to the columns that
-// see them.
+// The tile's rows whose values are not finite.
 template <int D, bool FP8>
 __device__ __forceinline__ uint32_t odd_rows(uint32_t tile, int lane) {
   const LaneAt at = lane_at<D, FP8>(fresh(lane));
@@ -411,189 +434,201 @@ __device__ __forceinline__ uint32_t odd_rows(uint32_t tile, int lane) {
   return __builtin_amdgcn_readfirstlane(mine);
 }
 
+// `careful`: a hidden row takes part in the products with weight 0, and 0 times
+// an infinity or NaN is NaN.  Sums that end finite met none.  Where they do not,
+// the segment is attended again with such rows found (odd), zeroed in the products
+// as those past the end always are, and added by hand to the columns that see them.
 template <int D, bool FP8>
-__device__ __forceinline__ TileMask tile_mask(const TreeArgs& a, const Segment& sg, uint32_t meta, uint32_t tile, int t, int lane) {
+__device__ __forceinline__ TileMask tile_mask(const TreeArgs& a, const Segment& sg, uint32_t meta, uint32_t tile, int t, bool careful,
+                                              int lane) {
   TileMask k;
   k.tree = t >= sg.nc;
-  const int rows = k.tree ? sg.m - 32 * (t - sg.nc) : sg.L - 32 * t;
+  const int rows = t >= sg.t1 ? 0 : k.tree ? sg.m - 32 * (t - sg.nc) : sg.L - 32 * t;
   k.alive = rows >= 32 ? ~0u : (1u << rows) - 1u;
   const bool soon = (meta & kFlagBit) != 0 && sg.deep - static_cast<int>(meta & ~kFlagBit) >= a.w;
   k.old = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(soon)) & k.alive;
   k.masked = k.tree || k.old != 0 || k.alive != ~0u;
   k.odd = 0;
-  if (k.masked) k.odd = odd_rows<D, FP8>(tile, lane) & k.alive;
+  if (careful && k.masked) k.odd = odd_rows<D, FP8>(tile, lane) & k.alive;
   return k;
 }
 
 constexpr int kAhead = 4;   // products between an operand's LDS read and its use
 
-// Scores of the tile for every block of columns.
-template <int D, bool FP8, int NC>
-__device__ __forceinline__ void tile_scores(const Columns<D, NC>& c, f32x16 (&s)[NC], uint32_t tile, const LaneAt& at) {
+// Scores of TPS tiles; their chains of products take turns.
+template <int D, bool FP8, int TPS>
+__device__ __forceinline__ void tile_scores(const Columns<D>& c, f32x16 (&s)[TPS], const uint32_t (&tile)[TPS], const LaneAt& at) {
   constexpr int KS = D / 16;
 #pragma unroll
-  for (int x = 0; x < NC; ++x)
+  for (int x = 0; x < TPS; ++x)
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[x][i] = 0.f;
   if constexpr (FP8) {
-    const float ks = *reinterpret_cast<DMS_LDS const float*>(tile + at.ks);
-    // piece (p, y) holds k-steps 4 p + y and 4 p + 2 + y
-    u32x4 op[2] = {lds16(tile + at.k), lds16(tile + at.k + 512)};
+    float ks[TPS];
 #pragma unroll
-    for (int e = 0; e < KS / 2; ++e) {
+    for (int x = 0; x < TPS; ++x) ks[x] = *reinterpret_cast<DMS_LDS const float*>(tile[x] + at.ks);
+    // piece (p, y) of 16 codes holds k-steps 4 p + y and 4 p + 2 + y
+    u32x4 op[2];
+    auto read = [&](int e) { return lds16(tile[e % TPS] + at.k + (e / TPS >> 1) * 2048 + (e / TPS & 1) * 512); };
+    op[0] = read(0);
+    op[1] = read(1);
+#pragma unroll
+    for (int e = 0; e < TPS * KS / 2; ++e) {
       const u32x4 raw = op[e & 1];
-      if (e + 2 < KS / 2) op[e & 1] = lds16(tile + at.k + ((e + 2) >> 1) * 2048 + (e & 1) * 512);
-      const u32x4 k0 = f8_bf16x8(raw[0], raw[1], ks), k1 = f8_bf16x8(raw[2], raw[3], ks);
-#pragma unroll
-      for (int x = 0; x < NC; ++x) s[x] = mfma(k0, c.q[x][4 * (e >> 1) + (e & 1)], s[x]);
-#pragma unroll
-      for (int x = 0; x < NC; ++x) s[x] = mfma(k1, c.q[x][4 * (e >> 1) + 2 + (e & 1)], s[x]);
+      if (e + 2 < TPS * KS / 2) op[e & 1] = read(e + 2);
+      const int x = e % TPS, p = e / TPS;
+      s[x] = mfma(f8_bf16x8(raw[0], raw[1], ks[x]), c.q[4 * (p >> 1) + (p & 1)], s[x]);
+      s[x] = mfma(f8_bf16x8(raw[2], raw[3], ks[x]), c.q[4 * (p >> 1) + 2 + (p & 1)], s[x]);
     }
   } else {
     u32x4 op[kAhead];
-    auto read = [&](int e) { return lds16(tile + at.k + (e >> 1) * 2048 + (e & 1) * 512); };
+    auto read = [&](int e) { return lds16(tile[e % TPS] + at.k + (e / TPS >> 1) * 2048 + (e / TPS & 1) * 512); };
 #pragma unroll
     for (int e = 0; e < kAhead; ++e) op[e] = read(e);
 #pragma unroll
-    for (int e = 0; e < KS; ++e) {
+    for (int e = 0; e < TPS * KS; ++e) {
       __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int x = 0; x < NC; ++x) s[x] = mfma(op[e % kAhead], c.q[x][e], s[x]);
-      if (e + kAhead < KS) op[e % kAhead] = read(e + kAhead);
+      s[e % TPS] = mfma(op[e % kAhead], c.q[e / TPS], s[e % TPS]);
+      if (e + kAhead < TPS * KS) op[e % kAhead] = read(e + kAhead);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
 }
 
-// Weights of the tile's rows (packed for the products) from the scores, and the
-// running maximum and sum.
-template <int D, bool FP8, int NC>
-__device__ __forceinline__ void tile_weights(const TreeArgs& a, const Segment& sg, Columns<D, NC>& c, f32x16 (&s)[NC], u32x4 (&pu)[NC][2],
-                                             uint32_t (&vis)[NC], const TileMask& k, uint32_t meta, uint32_t tile, const LaneAt& at,
-                                             int t, int lane) {
+// Rows whose values are not finite, added to the columns that see them.
+template <int D, bool FP8>
+__device__ __forceinline__ void odd_values(Columns<D>& c, const u32x4 (&pu)[2], uint32_t vis, uint32_t odd, uint32_t tile, int lane) {
+  for (uint32_t left = odd; left; left &= left - 1) {
+    const int j = __builtin_ctz(left), ln = fresh(lane);
+    uint32_t pair = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i == (8 * (j >> 4) + (j & 7)) >> 1) pair = pu[i >> 2][i & 3];
+    float pj = __uint_as_float(j & 1 ? pair & 0xFFFF0000u : pair << 16);
+    pj = __shfl(pj, (ln & 31) + 32 * ((j >> 3) & 1), 64);
+    const bool seen = (vis >> j) & 1;
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float val = stored_value<D, FP8>(tile, j, 32 * b + 8 * (i >> 2) + 4 * (ln >> 5) + (i & 3));
+        c.o[b][i] = seen ? fmaf(pj, val, c.o[b][i]) : c.o[b][i];
+        asm volatile("" ::: "memory");     // one value at a time: this is rare, its registers are not
+      }
+  }
+}
+
+// TPS tiles from the products' scores on: masks, running maximum and sum, weights
+// and the products with the values.  keys_done() once nothing but the values (and,
+// for 8-bit pages, the values' scales) is read any more, values_ready() before
+// those are.
+template <int D, bool FP8, int TPS, class KeysDone, class ValuesReady>
+__device__ __forceinline__ void attend_tiles(const TreeArgs& a, const Segment& sg, Columns<D>& c, const uint32_t (&tile)[TPS],
+                                             const uint32_t (&meta)[TPS], int t, const LaneAt& at, bool careful, int lane,
+                                             KeysDone keys_done, ValuesReady values_ready) {
   constexpr int OB = D / 32;
   const int hf = lane >> 5;
   const float sl2 = a.scale_log2, thr = kRescale / sl2;
   const bf16x2 ones = __builtin_bit_cast(bf16x2, 0x3F803F80u);
-  u32x4 vs[2][2];
-  if constexpr (FP8) {
+  f32x16 s[TPS];
+  tile_scores<D, FP8, TPS>(c, s, tile, at);
+  keys_done();
+  if (careful) values_ready();
+  TileMask k[TPS];
+  uint32_t vis[TPS];
+  bool partial = false;
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) vs[y][x] = lds16(tile + at.vs + y * 128 + x * 16);
-  }
-#pragma unroll
-  for (int x = 0; x < NC; ++x) {
+  for (int x = 0; x < TPS; ++x) {
+    k[x] = tile_mask<D, FP8>(a, sg, meta[x], tile[x], t + x, careful, lane);
     vis[x] = ~0u;
-    if (k.masked) {
-      vis[x] = k.alive;
-      if (k.tree) vis[x] &= c.anc[x][t - sg.nc];
-      for (uint32_t left = k.old; left; left &= left - 1) {
+    partial |= (k[x].alive & ~k[x].odd) != ~0u;
+    if (k[x].masked) {
+      vis[x] = k[x].alive;
+      if (k[x].tree && k[x].alive) vis[x] &= c.anc[t + x - sg.nc];
+      for (uint32_t left = k[x].old; left; left &= left - 1) {
         const int j = __builtin_ctz(left);
-        const int kp = static_cast<int>(__builtin_amdgcn_readlane(static_cast<int>(meta), j) & ~kFlagBit);
-        if (c.t[x] - kp >= a.w) vis[x] &= ~(1u << j);
+        const int kp = static_cast<int>(__builtin_amdgcn_readlane(static_cast<int>(meta[x]), j) & ~kFlagBit);
+        if (c.t - kp >= a.w) vis[x] &= ~(1u << j);
       }
       const uint32_t mine = vis[x] >> (8 * hf);
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[x][i] = (mine >> (16 * (i >> 3) + (i & 7))) & 1 ? s[x][i] : -INFINITY;
     }
-    float mx = s[x][0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
-    mx = col_max(mx);
-    const bool raise = mx > c.m[x] + thr;   // false while the column has seen no key
-    if (__builtin_amdgcn_ballot_w64(raise)) {
-      const float m_new = raise ? mx : c.m[x];
-      const float alpha = __builtin_amdgcn_exp2f((c.m[x] - m_new) * sl2);
-      c.l[x] *= alpha;
-#pragma unroll
-      for (int b = 0; b < OB; ++b) c.o[x][b] *= alpha;
-      c.m[x] = m_new;
-    }
-    // weights 2^((s - m) scale), rounded to bf16 for the products; the
-    // denominator adds the rounded values, so that one dominant key returns its
-    // value row exactly.  8-bit pages: the weight of the product carries the
-    // value scale, a power of two, so that its rounding is the same
-    const float mb = c.m[x] * sl2;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      f32x2 pr = {__builtin_amdgcn_exp2f(fmaf(s[x][2 * j], sl2, -mb)),
-                  __builtin_amdgcn_exp2f(fmaf(s[x][2 * j + 1], sl2, -mb))};
-      const bf16x2 pb = __builtin_convertvector(pr, bf16x2);
-      c.l[x] = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, c.l[x], false);
-      if constexpr (FP8) {
-        pr[0] *= __uint_as_float(vs[j >> 2][(j >> 1) & 1][2 * j & 3]);
-        pr[1] *= __uint_as_float(vs[j >> 2][(j >> 1) & 1][(2 * j + 1) & 3]);
-        pu[x][j >> 2][j & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
-      } else {
-        pu[x][j >> 2][j & 3] = __builtin_bit_cast(uint32_t, pb);
-      }
-    }
   }
-}
-
-// Rows whose values are not finite, added to the columns that see them.
-template <int D, bool FP8, int NC>
-__device__ __forceinline__ void odd_values(Columns<D, NC>& c, const u32x4 (&pu)[NC][2], const uint32_t (&vis)[NC], uint32_t odd,
-                                           uint32_t tile, int lane) {
-  for (uint32_t left = odd; left; left &= left - 1) {
-    const int j = __builtin_ctz(left), ln = fresh(lane);
+  float mx = s[0][0];
 #pragma unroll
-    for (int x = 0; x < NC; ++x) {
-      uint32_t pair = 0;
+  for (int x = 0; x < TPS; ++x)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i == (8 * (j >> 4) + (j & 7)) >> 1) pair = pu[x][i >> 2][i & 3];
-      float pj = __uint_as_float(j & 1 ? pair & 0xFFFF0000u : pair << 16);
-      pj = __shfl(pj, (ln & 31) + 32 * ((j >> 3) & 1), 64);
-      const bool seen = (vis[x] >> j) & 1;
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][i]);
+  mx = col_max(mx);
+  const bool raise = mx > c.m + thr;   // false while the column has seen no key
+  if (__builtin_amdgcn_ballot_w64(raise)) {
+    const float m_new = raise ? mx : c.m;
+    const float alpha = __builtin_amdgcn_exp2f((c.m - m_new) * sl2);
+    c.l *= alpha;
 #pragma unroll
-      for (int b = 0; b < D / 32; ++b)
+    for (int b = 0; b < OB; ++b) c.o[b] *= alpha;
+    c.m = m_new;
+  }
+  // weights 2^((s - m) scale), rounded to bf16 for the products; the
+  // denominator adds the rounded values, so that one dominant key returns its
+  // value row exactly.  8-bit pages: the weight of the product carries the
+  // value scale, a power of two, so that its rounding is the same
+  const float mb = c.m * sl2;
+  u32x4 pu[TPS][2];
+  auto weight_pair = [&](int x, int j) {
+    f32x2 pr = {__builtin_amdgcn_exp2f(fmaf(s[x][2 * j], sl2, -mb)), __builtin_amdgcn_exp2f(fmaf(s[x][2 * j + 1], sl2, -mb))};
+    const bf16x2 pb = __builtin_convertvector(pr, bf16x2);
+    c.l = __builtin_amdgcn_fdot2_f32_bf16(pb, ones, c.l, false);
+    if constexpr (FP8) {
+      const f32x2 vs = *reinterpret_cast<DMS_LDS const f32x2*>(tile[x] + at.vs + (j >> 2) * 128 + (j & 3) * 8);
+      pr[0] *= vs[0];
+      pr[1] *= vs[1];
+      pu[x][j >> 2][j & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
+    } else {
+      pu[x][j >> 2][j & 3] = __builtin_bit_cast(uint32_t, pb);
+    }
+  };
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float val = stored_value<D, FP8>(tile, j, 32 * b + 8 * (i >> 2) + 4 * (ln >> 5) + (i & 3));
-          c.o[x][b][i] = seen ? fmaf(pj, val, c.o[x][b][i]) : c.o[x][b][i];
-          asm volatile("" ::: "memory");     // one value at a time: this is rare, its registers are not
+  for (int j = 0; j < 8; ++j) weight_pair(0, j);
+  if (!careful) values_ready();
+  if (partial) {
+#pragma unroll
+    for (int x = 0; x < TPS; ++x) {
+      if (x > 0)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) weight_pair(x, j);
+      const uint32_t mine = (k[x].alive & ~k[x].odd) >> (8 * hf);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        u32x4 keep;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t bit = mine >> (16 * y + 2 * e);
+          keep[e] = ((bit & 1) ? 0x0000FFFFu : 0u) | ((bit & 2) ? 0xFFFF0000u : 0u);
         }
-    }
-  }
-}
-
-template <int D, bool FP8, int NC>
-__device__ __forceinline__ void tile_values(Columns<D, NC>& c, const u32x4 (&pu)[NC][2], const uint32_t (&vis)[NC], const TileMask& k,
-                                            uint32_t tile, const LaneAt& at, int lane) {
-  constexpr int OB = D / 32;
-  const uint32_t keep = k.alive & ~k.odd;
-  if (keep != ~0u) {
-    const uint32_t mine = keep >> (8 * (lane >> 5));
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      u32x4 and_;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t bit = mine >> (16 * y + 2 * e);
-        and_[e] = ((bit & 1) ? 0x0000FFFFu : 0u) | ((bit & 2) ? 0xFFFF0000u : 0u);
+        for (int b = 0; b < OB; ++b) c.o[b] = mfma(value_operand<D, FP8>(tile[x], at, b, y) & keep, pu[x][y], c.o[b]);
       }
-#pragma unroll
-      for (int b = 0; b < OB; ++b) {
-        const u32x4 v = value_operand<D, FP8>(tile, at, b, y) & and_;
-#pragma unroll
-        for (int x = 0; x < NC; ++x) c.o[x][b] = mfma(v, pu[x][y], c.o[x][b]);
-      }
+      if (k[x].odd) odd_values<D, FP8>(c, pu[x], vis[x], k[x].odd, tile[x], lane);
     }
-    if (k.odd) odd_values<D, FP8, NC>(c, pu, vis, k.odd, tile, lane);
     return;
   }
+  // product e: tile e / (2 OB), row half (e / OB) % 2, dim block e % OB; the second
+  // tile's weights beside the first one's products
   u32x4 op[kAhead];
-  auto read = [&](int e) { return value_operand<D, FP8>(tile, at, e % OB, e / OB); };
+  auto read = [&](int e) { return value_operand<D, FP8>(tile[e / (2 * OB)], at, e % OB, e / OB % 2); };
 #pragma unroll
   for (int e = 0; e < kAhead; ++e) op[e] = read(e);
 #pragma unroll
-  for (int e = 0; e < 2 * OB; ++e) {
+  for (int e = 0; e < 2 * OB * TPS; ++e) {
     __builtin_amdgcn_sched_barrier(0);
+    c.o[e % OB] = mfma(op[e % kAhead], pu[e / (2 * OB)][e / OB % 2], c.o[e % OB]);
+    if (e + kAhead < 2 * OB * TPS) op[e % kAhead] = read(e + kAhead);
+    if (TPS > 1 && e < 2 * OB) {
 #pragma unroll
-    for (int x = 0; x < NC; ++x) c.o[x][e % OB] = mfma(op[e % kAhead], pu[x][e / OB], c.o[x][e % OB]);
-    if (e + kAhead < 2 * OB) op[e % kAhead] = read(e + kAhead);
+      for (int j = e * 8 / (2 * OB); j < (e + 1) * 8 / (2 * OB); ++j) weight_pair(TPS - 1, j);
+    }
   }
   __builtin_amdgcn_sched_barrier(0);
 }
@@ -602,59 +637,54 @@ __device__ __forceinline__ void tile_values(Columns<D, NC>& c, const u32x4 (&pu)
 template <int D, bool FP8, int CW>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
   using Sh = Shape<D, FP8, CW>;
-  constexpr int NC = 1;
-  constexpr bool PRIVATE = Sh::PRIVATE;
   constexpr int NW = Sh::NW, KW = Sh::KW, UC = Sh::UC, KS = D / 16, OB = D / 32, TB = Sh::kTile;
   __shared__ __attribute__((aligned(1024))) char tiles_lds[Sh::kLds];
   __shared__ __attribute__((aligned(16))) uint32_t meta_lds[Sh::kSlots][64];
   __shared__ float2 ml_lds[NW][32];
-  __shared__ int first[NW];
+  __shared__ float factor_lds[KW][UC];
+  __shared__ int row_lds[UC];
   if (load_status(a.status) != 0) return;
   const int tid = threadIdx.x, lane = tid & 63, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   // waves of the same columns on different SIMDs: a unit with few columns leaves none idle
   const int cw = wave / KW, kw = wave % KW;
-  const int NH = a.n * a.H, Hq = a.H * a.g;
-  const int total = *(const DMS_CONST int32_t*)(a.cum + NH);
-  const int parts = parts_of(total, a.min_tiles, a.G);
-  if (static_cast<int>(blockIdx.x) >= parts || total == 0) return;
-  const int tb = part_begin(blockIdx.x, total, parts), te = part_begin(blockIdx.x + 1, total, parts);
-  // the last head whose first flat tile is not past tb
-  {
-    int cnt = 0;
-    for (int x = tid; x < NH; x += 64 * NW) cnt += a.cum[x] <= tb;
-    for (int off = 32; off; off >>= 1) cnt += __shfl_xor(cnt, off, 64);
-    if (lane == 0) first[wave] = cnt;
-  }
-  __syncthreads();
-  int hh = -1;
-  for (int x = 0; x < NW; ++x) hh += first[x];
-  hh = __builtin_amdgcn_readfirstlane(hh);
+  const int Hq = a.H * a.g;
+  // the U units of a part (their columns) read the same tiles: workgroups of one XCD
+  // (the dispatcher deals them round-robin), dispatched next to each other
+  const int x8 = blockIdx.x % kXcds, y8 = blockIdx.x / kXcds;
+  const int unit = y8 % a.U, cell = kXcds * (y8 / a.U) + x8;
+  if (cell >= a.cells) return;
+  typedef int __attribute__((ext_vector_type(4))) i32x4;
+  typedef int __attribute__((ext_vector_type(8))) i32x8;
+  const i32x4 mine = *((const DMS_CONST i32x4*)(a.part + cell));
+  i32x8 rd = *((const DMS_CONST i32x8*)(&a.part[cell].r));
+  const int tb = mine[0], te = mine[1];
+  int hh = mine[2], c0 = mine[3];
   const LaneAt at = lane_at<D, FP8>(lane);
   const uint32_t lds0 = lds_addr(tiles_lds), meta0 = lds_addr(meta_lds[0]);
 
   for (int f = tb; f < te;) {
-    while (((const DMS_CONST int32_t*)a.cum)[hh + 1] <= f) ++hh;   // heads without nodes have no tiles
     Segment sg;
-    {
-      typedef int __attribute__((ext_vector_type(8))) i32x8;
-      const i32x8 rd = *((const DMS_CONST i32x8*)(a.rows + hh));
-      sg.sh = rd[0];
-      sg.L = rd[1];
-      sg.tok0 = rd[2];
-      sg.m = rd[3];
-      sg.p0 = rd[4];
-      sg.tile0 = rd[5];
-      sg.deep = rd[4] + ((const DMS_CONST int32_t*)a.deepest)[rd[6]];
-    }
-    const int at0 = f - ((const DMS_CONST int32_t*)a.cum)[hh];
+    sg.sh = rd[0];
+    sg.L = rd[1];
+    sg.tok0 = rd[2];
+    sg.m = rd[3];
+    sg.p0 = rd[4];
+    sg.tile0 = rd[5];
+    sg.deep = rd[4] + ((const DMS_CONST int32_t*)a.deepest)[rd[6]];
     sg.hh = hh;
     sg.T = tiles_of(sg.L, sg.m);
-    sg.unit = at0 / sg.T;
-    sg.t0 = at0 - sg.unit * sg.T;
+    sg.t0 = f - c0;
     sg.t1 = min(sg.T, sg.t0 + te - f);
     sg.nc = (sg.L + 31) >> 5;
-    const int h = hh % a.H, cols = sg.m * a.g;
+    f += sg.t1 - sg.t0;
+    if (f < te) {          // the next head with nodes
+      do c0 = ((const DMS_CONST int32_t*)a.cum)[++hh];
+      while (((const DMS_CONST int32_t*)a.cum)[hh + 1] <= f);
+      rd = *((const DMS_CONST i32x8*)(a.rows + hh));
+    }
+    if (unit * UC >= sg.m * a.g) continue;     // a smaller tree: no such columns
+    const int h = sg.hh % a.H, cols = sg.m * a.g;
     const int nt = sg.t1 - sg.t0;
 
     // ---- tiles: sources and copies
@@ -671,250 +701,251 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
     };
 
     // ---- this wave's columns
-    const int col0 = sg.unit * UC + cw * 32 * NC;
+    const int col0 = unit * UC + cw * 32;
     const bool busy = col0 < cols;
-    Columns<D, NC> c;
+    Columns<D> c;
     auto load_columns = [&]() {
+      const int ln = fresh(lane), col = col0 + (ln & 31);
+      const bool ok = col < cols;
+      const int node = ok ? col / a.g : 0, qh = ok ? col % a.g : 0;
+      const size_t tok = static_cast<size_t>(sg.tok0) + node;
+      const uint16_t* q = a.q + (tok * Hq + h * a.g + qh) * D + 8 * (ln >> 5);
 #pragma unroll
-      for (int x = 0; x < NC; ++x) {
-        const int ln = fresh(lane), col = col0 + 32 * x + (ln & 31);
-        const bool ok = col < cols;
-        const int node = ok ? col / a.g : 0, qh = ok ? col % a.g : 0;
-        const size_t tok = static_cast<size_t>(sg.tok0) + node;
-        const uint16_t* q = a.q + (tok * Hq + h * a.g + qh) * D + 8 * (ln >> 5);
-#pragma unroll
-        for (int s = 0; s < KS; ++s)
-          c.q[x][s] = ok ? *reinterpret_cast<const u32x4*>(q + 16 * s) : u32x4{0u, 0u, 0u, 0u};
-        // the borrowed decision neuron takes no part in attention (App. C)
-        if (a.zero_neuron && qh == 0 && hf == 0) c.q[x][0][0] &= 0xFFFF0000u;
-        c.t[x] = sg.p0 + a.depth[tok];
-        c.anc[x] = a.anc + tok * a.words;
-        c.m[x] = kMInit;
-        c.l[x] = 0.f;
-#pragma unroll
-        for (int b = 0; b < OB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) c.o[x][b][i] = 0.f;
-      }
-    };
-
-    if constexpr (PRIVATE) {
-      constexpr int R = Sh::R, KC = (FP8 ? D / 32 + 1 : D / 16) + 1, VC = FP8 ? D / 32 : D / 16;
-      // keys of own tile u (with the row's owners; 8-bit pages: the scales too) and its values
-      auto copy_keys = [&](int u, const char* tile) {
-        const int slot = wave * R + u % R;
-        const uint32_t dst = lds0 + Sh::slot_at(slot);
-#pragma unroll
-        for (int x = 0; x < D * (FP8 ? 32 : 64) / 1024; ++x) copy16_once(tile + 16 * lane + 1024 * x, dst + 1024 * x);
-        if constexpr (FP8) copy4(tile + D * 64 + 4 * lane, dst + D * 64);
-        copy4(meta_of(sg.t0 + kw + u * KW) + (lane & 31), meta0 + 256 * slot);
-      };
-      auto copy_values = [&](int u, const char* tile) {
-        constexpr int V0 = D * (FP8 ? 32 : 64);
-        const uint32_t dst = lds0 + Sh::slot_at(wave * R + u % R) + V0;
-#pragma unroll
-        for (int x = 0; x < V0 / 1024; ++x) copy16_once(tile + V0 + 16 * lane + 1024 * x, dst + 1024 * x);
-      };
-      const int n = max(0, (nt - kw + KW - 1) / KW);   // own tiles: t0 + kw, + KW, ..
-      const char* src[R];
-#pragma unroll
-      for (int u = 0; u < R; ++u)
-        if (u < n) {
-          const int t = sg.t0 + kw + u * KW;
-          src[u] = source(t, page_of(t));
-          copy_keys(u, src[u]);
-          copy_values(u, src[u]);
-        }
-      load_columns();
-      int page = R < n ? page_of(sg.t0 + kw + R * KW) : 0;
-      for (int u = 0; u < n; ++u) {
-        const int t = sg.t0 + kw + u * KW, slot = wave * R + u % R;
-        const uint32_t tile = lds0 + Sh::slot_at(slot);
-        if (u + R - 1 < n) wait_copies_but<VC + (R - 1) * (KC + VC)>();
-        else wait_copies();
-        asm volatile("" ::: "memory");
-        const uint32_t meta = meta_lds[slot][lane & 31];
-        f32x16 s[NC];
-        tile_scores<D, FP8, NC>(c, s, tile, at);
-        u32x4 pu[NC][2];
-        uint32_t vis[NC];
-        const bool more = u + R < n;
-        const char* next = source(sg.t0 + kw + (u + R) * KW, page);
-        // 8-bit pages: the scales lie in the keys' copies and are read for the weights
-        if constexpr (!FP8) {
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          if (more) copy_keys(u + R, next);
-        }
-        if (more) wait_copies_but<(R - 1) * (KC + VC) + (FP8 ? 0 : KC)>();
-        else wait_copies();
-        asm volatile("" ::: "memory");
-        const TileMask k = tile_mask<D, FP8>(a, sg, meta, tile, t, lane);
-        tile_weights<D, FP8, NC>(a, sg, c, s, pu, vis, k, meta, tile, at, t, lane);
-        if constexpr (FP8) {
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          if (more) copy_keys(u + R, next);
-        }
-        tile_values<D, FP8, NC>(c, pu, vis, k, tile, at, lane);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (more) copy_values(u + R, next);
-        if (u + R + 1 < n) page = page_of(sg.t0 + kw + (u + R + 1) * KW);
-      }
-    } else {
-      // a stage's copies: KW tiles, CW waves to each (past the end: the last one again, not
-      // attended)
-      constexpr int S = Sh::S, kPieces = TB / 1024 / CW, PC = kPieces + 1 + FP8;
-      const int ns = (nt + KW - 1) / KW;
-      const int my = wave / CW, share = wave % CW;
-      auto copy_stage = [&](int st, int page) {
-        const int t = min(sg.t0 + st * KW + my, sg.t1 - 1), slot = st % S * KW + my;
-        const char* tile = source(t, page) + 16 * lane;
-        const uint32_t dst = lds0 + Sh::slot_at(slot);
-#pragma unroll
-        for (int x = 0; x < kPieces; ++x) {
-          const int at1 = 1024 * (kPieces * share + x);
-          if (a.once) copy16_once(tile + at1, dst + at1);
-          else lds_copy16(tile + at1, dst + at1);
-        }
-        if constexpr (FP8) copy4(tile + D * 64 - 12 * lane, dst + D * 64);
-        copy4(meta_of(t) + (lane & 31), meta0 + 256 * slot);
-      };
-      auto stage_page = [&](int st) { return page_of(min(sg.t0 + st * KW + my, sg.t1 - 1)); };
-#pragma unroll
-      for (int st = 0; st < S - 1; ++st)
-        if (st < ns) copy_stage(st, stage_page(st));
-      load_columns();
-      int page = stage_page(S - 1);
-      for (int st = 0; st < ns; ++st) {
-        // all but the stages after it have landed
-        if (st + S - 2 < ns) wait_copies_but<(S - 2) * PC>();
-        else wait_copies();
-        __syncthreads();     // the stage is there, and no wave reads the one before it
-        if (st + S - 1 < ns) copy_stage(st + S - 1, page);
-        const int t = sg.t0 + st * KW + kw, slot = st % S * KW + kw;
-        if (busy && t < sg.t1) {
-          const uint32_t tile = lds0 + Sh::slot_at(slot), meta = meta_lds[slot][lane & 31];
-          f32x16 s[NC];
-          tile_scores<D, FP8, NC>(c, s, tile, at);
-          const TileMask k = tile_mask<D, FP8>(a, sg, meta, tile, t, lane);
-          u32x4 pu[NC][2];
-          uint32_t vis[NC];
-          tile_weights<D, FP8, NC>(a, sg, c, s, pu, vis, k, meta, tile, at, t, lane);
-          tile_values<D, FP8, NC>(c, pu, vis, k, tile, at, lane);
-        }
-        page = stage_page(st + S);
-      }
-    }
-
-    // ---- fold the waves of a column block and write it: the outputs of a whole
-    // unit, else a partial (slot 2 w: a unit that began before this workgroup's
-    // part; 2 w + 1: one that ends after it).  A wave's sums lie in its own share
-    // of the tiles' LDS, 16-byte pieces flipped by column to spread the banks.
-    const bool whole = sg.t0 == 0 && sg.t1 == sg.T;
-    const int part = 2 * blockIdx.x + (sg.t0 == 0);
-    auto fold_at = [&](int w, int cc, int piece) {
-      return reinterpret_cast<f32x4*>(tiles_lds + w * Sh::kWaveBytes + cc * (D * 4) + 16 * (piece ^ (cc & 7)));
-    };
-#pragma unroll
-    for (int x = 0; x < NC; ++x) {
-      __syncthreads();     // tiles (the block before) are read
-      const float l = col_sum(c.l[x]);
-      const int ln = fresh(lane), th = fresh(tid);     // (addresses formed here, not held ahead of the loops)
-      if (ln < 32) ml_lds[wave][ln] = make_float2(c.m[x], l);
+      for (int s = 0; s < KS; ++s) c.q[s] = ok ? *reinterpret_cast<const u32x4*>(q + 16 * s) : u32x4{0u, 0u, 0u, 0u};
+      // the borrowed decision neuron takes no part in attention (App. C)
+      if (a.zero_neuron && qh == 0 && hf == 0) c.q[0][0] &= 0xFFFF0000u;
+      c.t = sg.p0 + a.depth[tok];
+      c.anc = a.anc + tok * a.words;
+      c.m = kMInit;
+      c.l = 0.f;
 #pragma unroll
       for (int b = 0; b < OB; ++b)
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
-          *fold_at(wave, ln & 31, 8 * b + 2 * y + (ln >> 5)) = f32x4{c.o[x][b][4 * y], c.o[x][b][4 * y + 1], c.o[x][b][4 * y + 2], c.o[x][b][4 * y + 3]};
-      __syncthreads();
-      // CW blocks of 32 columns, D / 4 pieces each
-      for (int e = th; e < CW * 32 * (D / 4); e += 64 * NW) {
-        const int piece = e % (D / 4), cc = e / (D / 4) % 32, cx = e / (D / 4) / 32;
-        const int uc = (cx * NC + x) * 32 + cc, col = sg.unit * UC + uc;
-        if (col >= cols) continue;
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-        float M = kMInit, L = 0.f;
+        for (int i = 0; i < 16; ++i) c.o[b][i] = 0.f;
+    };
+
+    for (int careful = 0; careful < 2; ++careful) {
+      if constexpr (Sh::PRIVATE) {
+        constexpr int R = Sh::R, KC = (FP8 ? D / 32 + 1 : D / 16) + 1, VC = FP8 ? D / 32 : D / 16;
+        // keys of own tile u (with the rows' owners; 8-bit pages: the scales too) and its values
+        auto copy_keys = [&](int u, const char* tile) {
+          const int slot = wave * R + u % R;
+          const uint32_t dst = lds0 + Sh::slot_at(slot);
 #pragma unroll
-        for (int y = 0; y < KW; ++y) M = fmaxf(M, ml_lds[cx * KW + y][cc].x);
+          for (int x = 0; x < D * (FP8 ? 32 : 64) / 1024; ++x) copy16_once(tile + 16 * lane + 1024 * x, dst + 1024 * x);
+          if constexpr (FP8) copy4(tile + D * 64 + 4 * lane, dst + D * 64);
+          copy4(meta_of(sg.t0 + kw + u * KW) + (lane & 31), meta0 + 256 * slot);
+        };
+        auto copy_values = [&](int u, const char* tile) {
+          constexpr int V0 = D * (FP8 ? 32 : 64);
+          const uint32_t dst = lds0 + Sh::slot_at(wave * R + u % R) + V0;
 #pragma unroll
-        for (int y = 0; y < KW; ++y) {
-          const float2 ml = ml_lds[cx * KW + y][cc];
-          const float w = __builtin_amdgcn_exp2f((ml.x - M) * a.scale_log2);
-          L += ml.y * w;
-          sum += *fold_at(cx * KW + y, cc, piece) * w;
+          for (int x = 0; x < V0 / 1024; ++x) copy16_once(tile + V0 + 16 * lane + 1024 * x, dst + 1024 * x);
+        };
+        const int n = max(0, (nt - kw + KW - 1) / KW);   // own tiles: t0 + kw, + KW, ..
+#pragma unroll
+        for (int u = 0; u < R; ++u)
+          if (u < n) {
+            const int t = sg.t0 + kw + u * KW;
+            const char* src = source(t, page_of(t));
+            copy_keys(u, src);
+            copy_values(u, src);
+          }
+        load_columns();
+        int page = R < n ? page_of(sg.t0 + kw + R * KW) : 0;
+        for (int u = 0; u < n; ++u) {
+          const int t = sg.t0 + kw + u * KW, slot = wave * R + u % R;
+          const uint32_t tile[1] = {lds0 + static_cast<uint32_t>(Sh::slot_at(slot))};
+          if (u + R - 1 < n) wait_copies_but<VC + (R - 1) * (KC + VC)>();
+          else wait_copies();
+          asm volatile("" ::: "memory");
+          const uint32_t meta[1] = {meta_lds[slot][lane & 31]};
+          const bool more = u + R < n;
+          const char* next = source(sg.t0 + kw + (u + R) * KW, page);
+          attend_tiles<D, FP8, 1>(a, sg, c, tile, meta, t, at, careful, lane,
+              [&]() {
+                // 8-bit pages: the scales lie in the keys' copies and are read for the weights
+                if constexpr (!FP8) {
+                  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                  if (more) copy_keys(u + R, next);
+                }
+              },
+              [&]() {
+                if (more) wait_copies_but<(R - 1) * (KC + VC) + (FP8 ? 0 : KC)>();
+                else wait_copies();
+                asm volatile("" ::: "memory");
+              });
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (more) {
+            if constexpr (FP8) copy_keys(u + R, next);
+            copy_values(u + R, next);
+          }
+          if (u + R + 1 < n) page = page_of(sg.t0 + kw + (u + R + 1) * KW);
         }
-        if (whole) {
-          const int node = col / a.g, qh = col % a.g;
-          const float inv = 1.0f / L;
-          const f32x2 lo = {sum[0] * inv, sum[1] * inv}, hi = {sum[2] * inv, sum[3] * inv};
-          const u32x2 ob = {__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
-                            __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
-          *reinterpret_cast<u32x2*>(a.out + ((static_cast<size_t>(sg.tok0) + node) * Hq + h * a.g + qh) * D + 4 * piece) = ob;
-        } else {
-          const size_t pc = static_cast<size_t>(part) * UC + uc;
-          *reinterpret_cast<f32x4*>(a.part_o + pc * D + 4 * piece) = sum;
-          if (piece == 0) a.part_ml[pc] = make_float2(M, L);
+      } else {
+        // a stage's copies: KW TPS tiles, the waves' shares of its pieces alike (past the
+        // end: the last tile again, not attended)
+        constexpr int S = Sh::S, TPS = Sh::TPS, kTiles = KW * TPS, kShare = NW / kTiles;
+        constexpr int kPieces = TB / 1024 / kShare, PC = kPieces + 1 + FP8;
+        const int ns = (nt + kTiles - 1) / kTiles;
+        const int my = wave / kShare, share = wave % kShare;
+        auto copy_stage = [&](int st, int page) {
+          const int t = min(sg.t0 + st * kTiles + my, sg.t1 - 1), slot = st % S * kTiles + my;
+          const char* tile = source(t, page) + 16 * lane;
+          const uint32_t dst = lds0 + Sh::slot_at(slot);
+#pragma unroll
+          for (int x = 0; x < kPieces; ++x) {
+            const int at1 = 1024 * (kPieces * share + x);
+            if (CW < 4 && a.once) copy16_once(tile + at1, dst + at1);
+            else lds_copy16(tile + at1, dst + at1);
+          }
+          if constexpr (FP8) copy4(tile + D * 64 - 12 * lane, dst + D * 64);
+          copy4(meta_of(t) + (lane & 31), meta0 + 256 * slot);
+        };
+        auto stage_page = [&](int st) { return page_of(min(sg.t0 + st * kTiles + my, sg.t1 - 1)); };
+#pragma unroll
+        for (int st = 0; st < S - 1; ++st)
+          if (st < ns) copy_stage(st, stage_page(st));
+        load_columns();
+        int page = stage_page(S - 1);
+        for (int st = 0; st < ns; ++st) {
+          // all but the stages after it have landed
+          if (st + S - 2 < ns) wait_copies_but<(S - 2) * PC>();
+          else wait_copies();
+          __syncthreads();     // the stage is there, and no wave reads the one before it
+          if (st + S - 1 < ns) copy_stage(st + S - 1, page);
+          const int t = sg.t0 + st * kTiles + kw * TPS, slot = st % S * kTiles + kw * TPS;
+          if (busy && t < sg.t1) {
+            uint32_t tile[TPS], meta[TPS];
+#pragma unroll
+            for (int x = 0; x < TPS; ++x) {
+              tile[x] = lds0 + Sh::slot_at(slot + x);
+              meta[x] = meta_lds[slot + x][lane & 31];
+            }
+            attend_tiles<D, FP8, TPS>(a, sg, c, tile, meta, t, at, careful, lane, []() {}, []() {});
+          }
+          page = stage_page(st + S);
         }
+      }
+      if (careful) break;
+      float z = 0.f;
+#pragma unroll
+      for (int b = 0; b < OB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z = fmaf(c.o[b][i], 0.f, z);
+      if (!__syncthreads_or(z != 0.f)) break;    // (tiles are read)
+    }
+
+    // ---- fold the waves of a column block and write it: the outputs of a whole
+    // head, else a partial (slot 2 w: a head that began before this part; 2 w + 1:
+    // one that ends after it).  A wave's sums lie in its own share of the tiles'
+    // LDS, 16-byte pieces flipped by column to spread the banks.
+    const bool whole = sg.t0 == 0 && sg.t1 == sg.T;
+    const int part = 2 * (cell * a.U + unit) + (sg.t0 == 0);
+    auto fold_at = [&](int w, int cc, int piece) {
+      return reinterpret_cast<f32x4*>(tiles_lds + w * Sh::kWaveBytes + cc * (D * 4) + 16 * (piece ^ (cc & 7)));
+    };
+    const float l = col_sum(c.l);
+    const int ln = fresh(lane), th = fresh(tid);     // (addresses formed here, not held ahead of the loops)
+    __syncthreads();
+    if (ln < 32) ml_lds[wave][ln] = make_float2(c.m, l);
+#pragma unroll
+    for (int b = 0; b < OB; ++b)
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+        *fold_at(wave, ln & 31, 8 * b + 2 * y + (ln >> 5)) =
+            f32x4{c.o[b][4 * y], c.o[b][4 * y + 1], c.o[b][4 * y + 2], c.o[b][4 * y + 3]};
+    __syncthreads();
+    if (th < UC) {     // a thread a column: what its waves' sums are multiplied by, and where it goes
+      const int cx = th / 32, cc = th % 32, col = unit * UC + th;
+      float M = kMInit, L = 0.f, f[KW];
+#pragma unroll
+      for (int y = 0; y < KW; ++y) M = fmaxf(M, ml_lds[cx * KW + y][cc].x);
+#pragma unroll
+      for (int y = 0; y < KW; ++y) {
+        const float2 ml = ml_lds[cx * KW + y][cc];
+        f[y] = __builtin_amdgcn_exp2f((ml.x - M) * a.scale_log2);
+        L += ml.y * f[y];
+      }
+      const float inv = whole ? 1.0f / L : 1.0f;
+#pragma unroll
+      for (int y = 0; y < KW; ++y) factor_lds[y][th] = f[y] * inv;
+      const int node = col / a.g;
+      row_lds[th] = col >= cols ? -1 : whole ? (sg.tok0 + node) * Hq + h * a.g + (col - node * a.g) : part * UC + th;
+      if (!whole && col < cols) a.part_ml[static_cast<size_t>(part) * UC + th] = make_float2(M, L);
+    }
+    __syncthreads();
+    // UC columns, D / 4 pieces each
+    for (int e = th; e < UC * (D / 4); e += 64 * NW) {
+      const int piece = e % (D / 4), uc = e / (D / 4), row = row_lds[uc];
+      if (row < 0) continue;
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int y = 0; y < KW; ++y) sum += *fold_at(uc / 32 * KW + y, uc % 32, piece) * factor_lds[y][uc];
+      const size_t dst = static_cast<size_t>(row) * D + 4 * piece;
+      if (whole) {
+        const f32x2 lo = {sum[0], sum[1]}, hi = {sum[2], sum[3]};
+        *reinterpret_cast<u32x2*>(a.out + dst) = u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
+                                                       __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
+      } else {
+        *reinterpret_cast<f32x4*>(a.part_o + dst) = sum;
       }
     }
     __syncthreads();       // the next segment's copies go where the sums are
-    f += nt;
   }
 }
 
-// Joins the units that several workgroups attended, a wave per output row.
+// Joins the heads that several parts attended: D / 4 threads a column, a batch of
+// its partials in flight at a time, a workgroup for 1024 / D columns of a head.
 template <int D>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
-  if (load_status(a.status) != 0) return;
-  const int lane = threadIdx.x & 63, NH = a.n * a.H, Hq = a.H * a.g;
-  const int64_t rows = static_cast<int64_t>(a.total) * Hq;
-  const int total = a.cum[NH], parts = parts_of(total, a.min_tiles, a.G);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + wave; row < rows; row += static_cast<int64_t>(gridDim.x) * 4) {
-    const int node = static_cast<int>(row / Hq), hq = static_cast<int>(row % Hq);
-    const int i = a.node_seq[node], h = hq / a.g, hh = i * a.H + h;
+  constexpr int kCols = 1024 / D, kBatch = 8;
+  const int status = load_status(a.status);
+  const int NH = a.n * a.H, per = (a.max_nodes * a.g + kCols - 1) / kCols;
+  const int total = a.cum[NH], parts = parts_of(total, a.min_tiles, a.cells);
+  if (status != 0) return;
+  const int piece = threadIdx.x % (D / 4);
+  for (int64_t x = blockIdx.x; x < static_cast<int64_t>(NH) * per; x += gridDim.x) {
+    const int hh = static_cast<int>(x / per), col = static_cast<int>(x % per) * kCols + threadIdx.x / (D / 4);
     const TreeRow r = a.rows[hh];
-    const int T = tiles_of(r.L, r.m), col = (node - r.tok0) * a.g + hq % a.g, unit = col / a.UC, uc = col % a.UC;
-    const int u0 = a.cum[hh] + unit * T;
-    const int w0 = part_holding(u0, total, parts), w1 = part_holding(u0 + T - 1, total, parts);
-    if (w0 == w1) continue;   // one workgroup wrote it
-    auto slot = [&](int w) { return static_cast<size_t>(2 * w + (w == w0)) * a.UC + uc; };
-    float M = kMInit;
-    for (int w = w0 + lane; w <= w1; w += 64) M = fmaxf(M, a.part_ml[slot(w)].x);
-    for (int off = 32; off; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-    float L = 0.f;
-    constexpr int E = D / 64;
-    float acc[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    constexpr int kBatch = 8;
+    const int u0 = a.cum[hh], u1 = a.cum[hh + 1] - 1;
+    if (col >= r.m * a.g) continue;
+    const int w0 = part_holding(u0, total, parts), w1 = part_holding(u1, total, parts);
+    if (w0 == w1) continue;    // one part wrote it
+    const int unit = col / a.UC, uc = col - unit * a.UC;
+    float M = kMInit, L = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int w = w0; w <= w1; w += kBatch) {
-      float x[kBatch][E];
+      f32x4 v[kBatch];
       float2 ml[kBatch];
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
-        const size_t pc = slot(min(w + u, w1));
+        const int y = min(w + u, w1);
+        const size_t pc = (static_cast<size_t>(2) * (y * a.U + unit) + (y == w0)) * a.UC + uc;
         ml[u] = a.part_ml[pc];
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[u][e] = a.part_o[pc * D + E * lane + e];
+        v[u] = *reinterpret_cast<const f32x4*>(a.part_o + pc * D + 4 * piece);
       }
+      float m = M;
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) m = fmaxf(m, ml[u].x);
+      const float f0 = __builtin_amdgcn_exp2f((M - m) * a.scale_log2);
+      acc *= f0;
+      L *= f0;
+      M = m;
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
-        if (w + u > w1) continue;
+        if (w + u > w1) break;
         const float f = __builtin_amdgcn_exp2f((ml[u].x - M) * a.scale_log2);
         L += ml[u].y * f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = fmaf(x[u][e], f, acc[e]);
+        acc += v[u] * f;
       }
     }
-    const float inv = 1.0f / L;
-    uint16_t* dst = a.out + row * D + E * lane;
-    if constexpr (E == 2) {
-      const f32x2 pr = {acc[0] * inv, acc[1] * inv};
-      *reinterpret_cast<uint32_t*>(dst) = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
-    } else {
-      const f32x2 pr = {acc[0] * inv, 0.f};
-      *dst = static_cast<uint16_t>(__builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2)));
-    }
+    acc *= 1.0f / L;
+    const int h = hh % a.H, node = col / a.g;
+    const f32x2 lo = {acc[0], acc[1]}, hi = {acc[2], acc[3]};
+    *reinterpret_cast<u32x2*>(a.out + ((static_cast<size_t>(r.tok0) + node) * (a.H * a.g) + h * a.g + (col - node * a.g)) * D + 4 * piece) =
+        u32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(lo, bf16x2)),
+              __builtin_bit_cast(uint32_t, __builtin_convertvector(hi, bf16x2))};
   }
 }
 
@@ -1249,7 +1280,7 @@ int tree_workgroups() {
 int tree_waves(int cols) { return cols <= 32 ? 1 : cols <= 64 ? 2 : 4; }
 
 struct TreeLayout {
-  size_t rows, cum, anc, depth, node_seq, deepest, flags, tiles, tmeta, part_o, part_ml, need, fresh, base, before, bytes;
+  size_t rows, cum, part, anc, depth, deepest, flags, tiles, tmeta, part_o, part_ml, need, fresh, base, before, bytes;
   int words, tph, UC;
 };
 TreeLayout tree_layout(const dms_config& c, int n, int total, int max_nodes) {
@@ -1267,9 +1298,9 @@ TreeLayout tree_layout(const dms_config& c, int n, int total, int max_nodes) {
     lo.UC = 32 * tree_waves(max_nodes * c.group_size);
     lo.rows = take(NH * sizeof(TreeRow));
     lo.cum = take((NH + 1) * 4);
+    lo.part = take(kTreeWorkgroups * sizeof(TreePart));
     lo.anc = take(T * lo.words * 4);
     lo.depth = take(T * 4);
-    lo.node_seq = take(T * 4);
     lo.deepest = take(static_cast<size_t>(n) * 4);
     lo.flags = take(T * H);
     lo.tiles = take(H * static_cast<size_t>(lo.tph) * (c.kv_format == DMS_KV_FP8 ? fp8_tile_bytes(c.head_dim) : tile_bytes(c.head_dim)));
@@ -1285,11 +1316,11 @@ template <int D, bool FP8>
 hipError_t launch_attention(const TreeArgs& a, hipStream_t st) {
   const unsigned prep = 1u + a.n + static_cast<unsigned>(a.n) * a.H * a.words;
   hipLaunchKernelGGL((tree_prep_kernel<D, FP8>), dim3(prep), dim3(kPrepThreads), 0, st, a);
-  if (a.UC == 32) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 1>), dim3(a.G), dim3(256), 0, st, a);
-  else if (a.UC == 64) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 2>), dim3(a.G), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 4>), dim3(a.G), dim3(256), 0, st, a);
-  const int64_t rows = static_cast<int64_t>(a.total) * a.H * a.g;
-  const unsigned merge = static_cast<unsigned>(std::min<int64_t>((rows + 3) / 4, 1 << 20));
+  if (a.UC == 32) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 1>), dim3(a.cells * a.U), dim3(256), 0, st, a);
+  else if (a.UC == 64) hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 2>), dim3(a.cells * a.U), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((tree_attn_kernel<D, FP8, 4>), dim3(a.cells * a.U), dim3(256), 0, st, a);
+  const int64_t blocks = static_cast<int64_t>(a.n) * a.H * ((a.max_nodes * a.g + 1024 / D - 1) / (1024 / D));
+  const unsigned merge = static_cast<unsigned>(std::min<int64_t>(blocks, 1 << 20));
   hipLaunchKernelGGL((tree_merge_kernel<D>), dim3(merge), dim3(256), 0, st, a);
   return hipGetLastError();
 }
@@ -1328,9 +1359,9 @@ hipError_t launch_tree_attention(const dms_config& c, const Layout& lo, void* me
   a.out = static_cast<uint16_t*>(out);
   a.rows = reinterpret_cast<TreeRow*>(w + tl.rows);
   a.cum = reinterpret_cast<int32_t*>(w + tl.cum);
+  a.part = reinterpret_cast<TreePart*>(w + tl.part);
   a.anc = reinterpret_cast<uint32_t*>(w + tl.anc);
   a.depth = reinterpret_cast<int32_t*>(w + tl.depth);
-  a.node_seq = reinterpret_cast<int32_t*>(w + tl.node_seq);
   a.deepest = reinterpret_cast<int32_t*>(w + tl.deepest);
   a.tiles = w + tl.tiles;
   a.tmeta = reinterpret_cast<uint32_t*>(w + tl.tmeta);
@@ -1350,10 +1381,11 @@ hipError_t launch_tree_attention(const dms_config& c, const Layout& lo, void* me
   a.max_nodes = max_nodes;
   a.words = tl.words;
   a.tph = tl.tph;
-  a.G = tree_workgroups();
   a.UC = tl.UC;
+  a.U = (max_nodes * c.group_size + tl.UC - 1) / tl.UC;
+  a.cells = std::max(1, tree_workgroups() / kXcds / a.U) * kXcds;
   a.min_tiles = 256 / a.UC;
-  a.once = max_nodes * c.group_size <= a.UC;
+  a.once = a.U == 1;
   a.zero_neuron = c.decision_source == DMS_DECIDE_QUERY;
   a.bias = c.decision_bias;
   a.scale_log2 = c.softmax_scale * 1.4426950408889634f;
