@@ -1384,7 +1384,7 @@ hipError_t launch_tree_attention(const dms_config& c, const Layout& lo, void* me
   a.UC = tl.UC;
   a.U = (max_nodes * c.group_size + tl.UC - 1) / tl.UC;
   a.cells = std::max(1, tree_workgroups() / kXcds / a.U) * kXcds;
-  a.min_tiles = 256 / a.UC;
+  a.min_tiles = 8;
   a.once = a.U == 1;
   a.zero_neuron = c.decision_source == DMS_DECIDE_QUERY;
   a.bias = c.decision_bias;
