@@ -6,6 +6,20 @@
 // formed in float64: sums of a row are exact in 64 bits whatever their order
 // (at most 2^20 tokens), so that borders and picks depend on neither the split of a
 // row nor the order of atomics.  Tokens of weight 0 are never taken.
+//
+// Rows of more than kSmallVocab logits are cut into splits, so that few rows fill the
+// chip too, and take four launches:
+//   sample_max_kernel   the splits' largest values (reads the logits from memory;
+//                       the passes after it find them in the caches);
+//   sample_hist_kernel  the splits' weights, and each row's counts and weights by
+//                       distance from its largest value, 32 bins an octave over 20 octaves;
+//   sample_cut_kernel   from those the bins that hold the borders of top-k and
+//                       top-p: the weights ahead of them by split, and their tokens
+//                       listed;
+//   sample_pick_kernel  a workgroup a row sorts the listed tokens, cuts them, finds the
+//                       split that holds the picked token and walks it.
+// A row whose border lies past the bins or has too many tokens in its bins (many equal
+// logits) is done by the last launch alone, as shorter rows are (sample_row).
 #include <math.h>
 
 #include <algorithm>
@@ -17,6 +31,8 @@ namespace dms {
 namespace {
 
 typedef unsigned long long u64;
+
+struct RowState;
 
 struct SampleArgs {
   const void* logits;
@@ -31,6 +47,8 @@ struct SampleArgs {
   int rows, vocab;
   float temperature0, top_p0, min_p0;
   int top_k0;
+  RowState* state;            // [rows], rows in splits
+  int splits;
 };
 
 // Settings of one row.
@@ -79,11 +97,29 @@ __device__ inline float key_value(uint32_t k) {
 }
 constexpr uint32_t kKeyNone = 0x007FFFFFu;   // -inf
 
+// 2^43 2^((x - top) c), rounded.  2^f for |f| <= 1/2 is its Taylor sum to the 12th
+// power, (ln 2 / 2)^13 / 13! = 2e-16 off.
 __device__ inline u64 weight(float x, float top, double c) {
-  const double e = exp2((static_cast<double>(x) - static_cast<double>(top)) * c);
+  const double t = (static_cast<double>(x) - static_cast<double>(top)) * c;
+  if (!(t > -45.0)) return 0;
+  const double n = rint(t), f = t - n;
+  double p = 2.5678435993488196e-11;
+  p = fma(p, f, 4.44553827187081e-10);
+  p = fma(p, f, 7.054911620801121e-09);
+  p = fma(p, f, 1.0178086009239696e-07);
+  p = fma(p, f, 1.3215486790144305e-06);
+  p = fma(p, f, 1.5252733804059838e-05);
+  p = fma(p, f, 0.00015403530393381606);
+  p = fma(p, f, 0.0013333558146428441);
+  p = fma(p, f, 0.009618129107628477);
+  p = fma(p, f, 0.055504108664821576);
+  p = fma(p, f, 0.2402265069591007);
+  p = fma(p, f, 0.6931471805599453);
+  p = fma(p, f, 1.0);
+  const double scale = __longlong_as_double(static_cast<long long>(1023 + 43 + static_cast<int>(n)) << 52);
   // 2^52 and more have no fraction bits: the sum is rounded to an integer, half to even
-  const u64 b = static_cast<u64>(__double_as_longlong(fma(e, 0x1p43, 0x1p52)));
-  return x == -INFINITY ? 0ull : b & ((1ull << 52) - 1);
+  const u64 b = static_cast<u64>(__double_as_longlong(fma(p, scale, 0x1p52)));
+  return b & ((1ull << 52) - 1);
 }
 
 // ---------------------------------------------------------------------------
@@ -189,9 +225,8 @@ __device__ Border find_border(const SampleArgs& a, const void* row, float top, d
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
-  __shared__ RowLds s;
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.vocab;
+__device__ void sample_row(const SampleArgs& a, int r, RowLds& s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.vocab;
   const char* row = static_cast<const char*>(a.logits) + static_cast<int64_t>(r) * a.stride * (BF16 ? 2 : 4);
   const RowSetting set = row_setting(a, r);
   // ---- the largest value, and the weight of the row
@@ -321,10 +356,505 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
   }
 }
 
+template <bool BF16>
+__global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
+  __shared__ RowLds s;
+  sample_row<BF16>(a, blockIdx.x, s);
+}
+
+// ---------------------------------------------------------------------------
+// A row in splits
+// ---------------------------------------------------------------------------
+constexpr int kSplitThreads = 256, kMaxSplits = 64;
+constexpr int kPerOctave = 32, kHist = 20 * kPerOctave;   // bins of a row
+constexpr int kListed = 2048;                             // tokens that a row lists at most
+
+// What the launches of a row leave each other.
+struct RowState {
+  u64 mass[kHist];            // weights by bin
+  u64 split_mass[kMaxSplits], split_kept[kMaxSplits];
+  u64 list[kListed];          // key << 32 | ~index of the tokens in the borders' bins
+  uint32_t count[kHist];
+  uint32_t split_top[kMaxSplits];
+  uint32_t listed;
+};
+
+// The splits of a row: 16-byte groups of logits in equal parts; what lies before the
+// first aligned group belongs to the first split, what is left to the last.
+template <bool BF16>
+struct Splits {
+  static constexpr int VEC = BF16 ? 8 : 4;
+  const char* row;
+  int V, S, lead, groups;
+  __device__ Splits(const SampleArgs& a, int r) {
+    row = static_cast<const char*>(a.logits) + static_cast<int64_t>(r) * a.stride * (BF16 ? 2 : 4);
+    V = a.vocab;
+    S = a.splits;
+    lead = min(V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (BF16 ? 2 : 4));
+    groups = (V - lead) / VEC;
+  }
+  __device__ int first_group(int s) const { return static_cast<int>(static_cast<int64_t>(s) * groups / S); }
+  __device__ int begin(int s) const { return s == 0 ? 0 : lead + first_group(s) * VEC; }
+  __device__ int end(int s) const { return s == S - 1 ? V : lead + first_group(s + 1) * VEC; }
+  __device__ int holding(int i) const {
+    if (i < lead) return 0;
+    const int g = (i - lead) / VEC;
+    return g >= groups ? S - 1 : static_cast<int>((static_cast<int64_t>(g + 1) * S - 1) / groups);
+  }
+  // f(index, logit) of every token of split s, four 16-byte loads in flight
+  template <class F>
+  __device__ void each(int s, F f) const {
+    const int tid = threadIdx.x;
+    if (s == 0)
+      for (int i = tid; i < lead; i += kSplitThreads) f(i, logit<BF16>(row, i));
+    const int g1 = first_group(s + 1);
+    const uint4* p = reinterpret_cast<const uint4*>(row + static_cast<size_t>(lead) * (BF16 ? 2 : 4));
+    for (int g = first_group(s) + tid; g < g1; g += 4 * kSplitThreads) {
+      uint4 x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = p[min(g + u * kSplitThreads, g1 - 1)];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (g + u * kSplitThreads >= g1) break;
+        const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+        const int i = lead + (g + u * kSplitThreads) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          f(i + e, counted(BF16 ? __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16) : __uint_as_float(w[e & 3])));
+      }
+    }
+    if (s == S - 1)
+      for (int i = lead + groups * VEC + tid; i < V; i += kSplitThreads) f(i, logit<BF16>(row, i));
+  }
+};
+
+__device__ inline uint32_t wave_max32(uint32_t v) {
+  for (int off = 32; off; off >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), off, 64)));
+  return v;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kSplitThreads) void sample_max_kernel(SampleArgs a) {
+  __shared__ uint32_t top[kSplitThreads / 64];
+  const int r = blockIdx.x / a.splits, s = blockIdx.x % a.splits, tid = threadIdx.x;
+  RowState& st = a.state[r];
+  for (int x = s * kSplitThreads + tid; x < kHist; x += a.splits * kSplitThreads) st.mass[x] = 0, st.count[x] = 0;
+  if (s == 0 && tid == 0) st.listed = 0;
+  uint32_t key = kKeyNone;
+  Splits<BF16>(a, r).each(s, [&](int, float x) { key = max(key, order_key(x)); });
+  key = wave_max32(key);
+  if ((tid & 63) == 0) top[tid >> 6] = key;
+  __syncthreads();
+  if (tid == 0) {
+    for (int x = 1; x < kSplitThreads / 64; ++x) key = max(key, top[x]);
+    st.split_top[s] = key;
+  }
+}
+
+// The row's largest value, from its splits.
+__device__ inline uint32_t row_top(const RowState& st, int splits) {
+  const int lane = threadIdx.x & 63;
+  return wave_max32(lane < splits ? st.split_top[lane] : kKeyNone);
+}
+// Bin of a token: larger for smaller logits (each step is monotonous), kHist past the bins.
+__device__ inline int bin_of(float x, float top, float c) {
+  const float z = (top - x) * c * static_cast<float>(kPerOctave);
+  return z < static_cast<float>(kHist) ? static_cast<int>(z) : kHist;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kSplitThreads) void sample_hist_kernel(SampleArgs a) {
+  __shared__ u64 mass[kHist], part[kSplitThreads / 64];
+  __shared__ uint32_t count[kHist];
+  const int r = blockIdx.x / a.splits, s = blockIdx.x % a.splits, tid = threadIdx.x;
+  RowState& st = a.state[r];
+  const RowSetting set = row_setting(a, r);
+  const uint32_t key = row_top(st, a.splits);
+  if (key == kKeyNone) return;
+  const bool cut = set.k < a.vocab || set.p < 1.0;
+  if (cut) {
+    for (int x = tid; x < kHist; x += kSplitThreads) mass[x] = 0, count[x] = 0;
+    __syncthreads();
+  }
+  const float top = key_value(key), c = static_cast<float>(set.c);
+  u64 sum = 0;
+  Splits<BF16>(a, r).each(s, [&](int, float x) {
+    const u64 w = weight(x, top, set.c);
+    sum += w;
+    if (cut && w) {
+      const int b = bin_of(x, top, c);
+      if (b < kHist) {
+        atomicAdd(&mass[b], w);
+        atomicAdd(&count[b], 1u);
+      }
+    }
+  });
+  sum = wave_sum64(sum);
+  if ((tid & 63) == 0) part[tid >> 6] = sum;
+  __syncthreads();
+  if (tid == 0) {
+    for (int x = 1; x < kSplitThreads / 64; ++x) sum += part[x];
+    st.split_mass[s] = sum;
+  }
+  if (cut)
+    for (int x = tid; x < kHist; x += kSplitThreads)
+      if (count[x]) {
+        atomicAdd(&st.mass[x], mass[x]);
+        atomicAdd(&st.count[x], count[x]);
+      }
+}
+
+// Which bins hold a row's borders.
+struct Cut {
+  bool none, slow;     // nothing to cut by rank or weight; the row is left to sample_row
+  int from, to;        // bins whose tokens are listed; those before are kept
+  uint32_t ahead;      // tokens and weight before `from`
+  u64 ahead_mass, all; // weight of the row
+};
+struct CutLds {
+  u64 wave_mass[16];
+  uint32_t wave_count[16];
+  int k_bin, p_low, p_high;
+  u64 k_before, k_with;
+  uint32_t ahead, through;
+  u64 ahead_mass;
+};
+// Found by a whole workgroup of THREADS, three bins or fewer to a thread.
+template <int THREADS>
+__device__ Cut find_cut(const SampleArgs& a, const RowState& st, const RowSetting& set, CutLds& l) {
+  constexpr int PER = (kHist + THREADS - 1) / THREADS;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  Cut cut{};
+  cut.all = wave_sum64(lane < a.splits ? st.split_mass[lane] : 0);
+  cut.none = set.k >= a.vocab && !(set.p < 1.0);
+  if (cut.none) return cut;
+  u64 m[PER], sum = 0;
+  uint32_t n[PER], num = 0;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int b = tid * PER + u;
+    m[u] = b < kHist ? st.mass[b] : 0;
+    n[u] = b < kHist ? st.count[b] : 0;
+    sum += m[u];
+    num += n[u];
+  }
+  u64 im = sum;
+  uint32_t in = num;
+  for (int off = 1; off < 64; off <<= 1) {
+    const u64 um = __shfl_up(im, off, 64);
+    const uint32_t un = __shfl_up(in, off, 64);
+    if (lane >= off) im += um, in += un;
+  }
+  if (lane == 63) l.wave_mass[wave] = im, l.wave_count[wave] = in;
+  if (tid == 0) l.k_bin = l.p_low = l.p_high = kHist;
+  __syncthreads();
+  u64 before = im - sum, all_mass = 0;
+  uint32_t ahead = in - num, all_count = 0;
+  for (int x = 0; x < THREADS / 64; ++x) {
+    if (x < wave) before += l.wave_mass[x], ahead += l.wave_count[x];
+    all_mass += l.wave_mass[x];
+    all_count += l.wave_count[x];
+  }
+  // top-k: the bin with the k-th token.  Where the bins hold fewer and nothing lies past
+  // them, top-k takes all.
+  const uint32_t k = static_cast<uint32_t>(set.k);
+  const bool past = all_mass != cut.all;
+  const bool by_k = k < all_count || (past && set.k < a.vocab);
+  const bool by_p = set.p < 1.0;
+  if (by_k && k > all_count) cut.slow = true;
+  if (!by_k && !by_p) {
+    cut.none = true;
+    return cut;
+  }
+  {
+    u64 x = before;
+    uint32_t y = ahead;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      if (by_k && y < k && y + n[u] >= k) {
+        l.k_bin = tid * PER + u;
+        l.k_before = x;
+        l.k_with = x + m[u];
+      }
+      x += m[u];
+      y += n[u];
+    }
+  }
+  __syncthreads();
+  if (by_k && l.k_bin == kHist) cut.slow = true;
+  if (cut.slow) return cut;
+  if (by_p) {
+    // what top-k leaves weighs between the bins before its border and those with it
+    const double low = set.p * static_cast<double>(by_k ? l.k_before : cut.all);
+    const double high = set.p * static_cast<double>(by_k ? l.k_with : cut.all);
+    u64 x = before;
+    uint32_t y = ahead;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const bool was_low = y > 0 && static_cast<double>(x) >= low, was_high = y > 0 && static_cast<double>(x) >= high;
+      x += m[u];
+      y += n[u];
+      if (!was_low && y > 0 && static_cast<double>(x) >= low) l.p_low = tid * PER + u;
+      if (!was_high && y > 0 && static_cast<double>(x) >= high) l.p_high = tid * PER + u;
+    }
+    __syncthreads();
+    if (l.p_high == kHist || l.p_low == kHist) {
+      cut.slow = true;
+      return cut;
+    }
+  }
+  cut.from = by_p ? l.p_low : l.k_bin;
+  cut.to = by_k ? l.k_bin : l.p_high;
+  {
+    u64 x = before;
+    uint32_t y = ahead;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int b = tid * PER + u;
+      if (b == cut.from) l.ahead = y, l.ahead_mass = x;
+      x += m[u];
+      y += n[u];
+      if (b == cut.to) l.through = y;
+    }
+  }
+  __syncthreads();
+  cut.ahead = l.ahead;
+  cut.ahead_mass = l.ahead_mass;
+  cut.slow = l.through - l.ahead > kListed;
+  return cut;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kSplitThreads) void sample_cut_kernel(SampleArgs a) {
+  __shared__ CutLds l;
+  __shared__ u64 part[kSplitThreads / 64];
+  const int r = blockIdx.x / a.splits, s = blockIdx.x % a.splits, tid = threadIdx.x;
+  RowState& st = a.state[r];
+  const RowSetting set = row_setting(a, r);
+  const uint32_t key = row_top(st, a.splits);
+  if (key == kKeyNone) return;
+  const Cut cut = find_cut<kSplitThreads>(a, st, set, l);
+  if (cut.slow || (cut.none && set.least <= 0.0)) return;
+  const float top = key_value(key), c = static_cast<float>(set.c);
+  u64 sum = 0;
+  Splits<BF16>(a, r).each(s, [&](int i, float x) {
+    const int b = bin_of(x, top, c);
+    if (!cut.none && b > cut.to) return;
+    const u64 w = weight(x, top, set.c);
+    if (cut.none || b < cut.from) {
+      sum += static_cast<double>(w) >= set.least ? w : 0ull;
+    } else if (w) {
+      const uint32_t at = atomicAdd(&st.listed, 1u);
+      if (at < kListed) st.list[at] = static_cast<u64>(order_key(x)) << 32 | ~static_cast<uint32_t>(i);
+    }
+  });
+  sum = wave_sum64(sum);
+  if ((tid & 63) == 0) part[tid >> 6] = sum;
+  __syncthreads();
+  if (tid == 0) {
+    for (int x = 1; x < kSplitThreads / 64; ++x) sum += part[x];
+    st.split_kept[s] = sum;
+  }
+}
+
+struct PickLds {
+  CutLds cut;
+  u64 list[kListed];
+  u64 mass[kMaxSplits];
+  u64 wave_mass[kWaves];
+  u64 total, k_mass, before;
+  int last, split, k_last;
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) {
+  __shared__ union {
+    RowLds row;
+    PickLds pick;
+  } lds;
+  PickLds& l = lds.pick;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const RowState& st = a.state[r];
+  const RowSetting set = row_setting(a, r);
+  const uint32_t key = row_top(st, a.splits);
+  if (key == kKeyNone) {      // no token is left
+    if (tid == 0) {
+      a.tokens[r] = -1;
+      if (a.logprobs) a.logprobs[r] = NAN;
+    }
+    return;
+  }
+  const Cut cut = find_cut<kRowThreads>(a, st, set, l.cut);
+  if (cut.slow) {
+    __syncthreads();
+    sample_row<BF16>(a, r, lds.row);
+    return;
+  }
+  const float top = key_value(key);
+  const Splits<BF16> sp(a, r);
+  const bool whole = cut.none && set.least <= 0.0;
+  if (tid < kMaxSplits) l.mass[tid] = tid < a.splits ? (whole ? st.split_mass[tid] : st.split_kept[tid]) : 0;
+  u64 border = 0;              // the last kept token of the listed ones, as the list holds it
+  __syncthreads();
+  if (!cut.none) {
+    // ---- the listed tokens in falling order (equal ones by index)
+    const int n = min(static_cast<int>(st.listed), kListed);
+    int size = 64;
+    while (size < n) size *= 2;
+    for (int x = tid; x < size; x += kRowThreads) l.list[x] = x < n ? st.list[x] : 0;
+    __syncthreads();
+    for (int span = 2; span <= size; span *= 2)
+      for (int step = span / 2; step; step /= 2) {
+        for (int x = tid; x < size / 2; x += kRowThreads) {
+          const int i = 2 * x - (x & (step - 1)), j = i + step;   // pairs of this step
+          const u64 p = l.list[i], q = l.list[j];
+          if ((p < q) == ((i & span) == 0)) l.list[i] = q, l.list[j] = p;
+        }
+        __syncthreads();
+      }
+    // ---- running weights: thread t holds tokens 2 t and 2 t + 1
+    const int x0 = 2 * tid;
+    const u64 w0 = x0 < n ? weight(key_value(static_cast<uint32_t>(l.list[x0] >> 32)), top, set.c) : 0;
+    const u64 w1 = x0 + 1 < n ? weight(key_value(static_cast<uint32_t>(l.list[x0 + 1] >> 32)), top, set.c) : 0;
+    u64 run = w0 + w1;
+    for (int off = 1; off < 64; off <<= 1) {
+      const u64 up = __shfl_up(run, off, 64);
+      if (lane >= off) run += up;
+    }
+    if (lane == 63) l.wave_mass[wave] = run;
+    if (tid == 0) l.last = n - 1, l.k_last = n - 1, l.k_mass = cut.all;
+    __syncthreads();
+    for (int x = 0; x < wave; ++x) run += l.wave_mass[x];
+    const u64 r0 = cut.ahead_mass + run - w1, r1 = cut.ahead_mass + run;   // through token 2 t, 2 t + 1
+    const int64_t left = static_cast<int64_t>(set.k) - cut.ahead;         // listed tokens that top-k keeps
+    if (left >= 1 && left <= n && (left - 1) / 2 == tid) {
+      l.k_last = static_cast<int>(left) - 1;
+      l.k_mass = (left - 1) % 2 ? r1 : r0;
+    }
+    __syncthreads();
+    if (set.p < 1.0) {
+      const double least = set.p * static_cast<double>(l.k_mass);
+      // the first token at which the running weight is enough
+      const bool e0 = x0 < n && static_cast<double>(r0) >= least, e1 = x0 + 1 < n && static_cast<double>(r1) >= least;
+      const bool eb = x0 > 0 && x0 <= n && static_cast<double>(r0 - w0) >= least;
+      if (!eb && (e0 || e1)) atomicMin(&l.last, e0 ? x0 : x0 + 1);
+    }
+    __syncthreads();
+    const int last = min(l.last, l.k_last);
+    border = l.list[last];
+    // ---- kept ones, to their splits
+    if (x0 <= last && static_cast<double>(w0) >= set.least)
+      atomicAdd(&l.mass[sp.holding(static_cast<int>(~static_cast<uint32_t>(l.list[x0])))], w0);
+    if (x0 + 1 <= last && static_cast<double>(w1) >= set.least)
+      atomicAdd(&l.mass[sp.holding(static_cast<int>(~static_cast<uint32_t>(l.list[x0 + 1])))], w1);
+    __syncthreads();
+  }
+  // ---- the split that holds the picked token
+  if (wave == 0) {
+    const u64 m = l.mass[lane];
+    u64 run = m;
+    for (int off = 1; off < 64; off <<= 1) {
+      const u64 up = __shfl_up(run, off, 64);
+      if (lane >= off) run += up;
+    }
+    const u64 total = __shfl(run, 63, 64);
+    const u64 target = static_cast<u64>(static_cast<double>(set.u) * static_cast<double>(total));
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(run > target);
+    const int s = static_cast<int>(__builtin_ctzll(hit));
+    if (lane == s) {
+      l.split = s;
+      l.total = total;
+      l.before = run - m;
+    }
+  }
+  __syncthreads();
+  // ---- its tokens by index, four to a thread at a time
+  const u64 total = l.total, target = static_cast<u64>(static_cast<double>(set.u) * static_cast<double>(total));
+  u64 before = l.before;
+  const int end = sp.end(l.split);
+  for (int i0 = sp.begin(l.split); i0 < end; i0 += 4 * kRowThreads) {
+    u64 w[4], sum = 0;
+    float x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = i0 + 4 * tid + u;
+      x[u] = i < end ? logit<BF16>(sp.row, i) : -INFINITY;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const u64 as_listed = static_cast<u64>(order_key(x[u])) << 32 | ~static_cast<uint32_t>(i0 + 4 * tid + u);
+      w[u] = as_listed >= border ? weight(x[u], top, set.c) : 0;
+      if (!(static_cast<double>(w[u]) >= set.least)) w[u] = 0;
+      sum += w[u];
+    }
+    u64 run = sum;
+    for (int off = 1; off < 64; off <<= 1) {
+      const u64 up = __shfl_up(run, off, 64);
+      if (lane >= off) run += up;
+    }
+    __syncthreads();
+    if (lane == 63) l.wave_mass[wave] = run;
+    __syncthreads();
+    u64 all = 0;
+    run += before;
+    for (int y = 0; y < kWaves; ++y) {
+      if (y < wave) run += l.wave_mass[y];
+      all += l.wave_mass[y];
+    }
+    if (run > target && run - sum <= target) {     // one thread
+      u64 at = run - sum;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (at + w[u] > target) {
+          a.tokens[r] = i0 + 4 * tid + u;
+          if (a.logprobs)
+            a.logprobs[r] = static_cast<float>((static_cast<double>(x[u]) - static_cast<double>(top)) / set.t -
+                                               log(static_cast<double>(total) * 0x1p-43));
+          break;
+        }
+        at += w[u];
+      }
+    }
+    before += all;
+    if (before > target) break;
+  }
+}
+
+// Splits of a row: about four workgroups a compute unit in all, none of fewer than 2048
+// logits.
+int row_splits(int rows, int vocab) { return std::max(1, std::min({kMaxSplits, (1024 + rows - 1) / rows, vocab / 2048})); }
+
 }  // namespace
 
+// Up to here a row is one workgroup's: it takes fewer passes than there are launches.
+constexpr int kSmallVocab = 4096;
+// Rows of one round of launches (the workspace holds the state of so many).
+constexpr int kRowsAtOnce = 1024;
+
 size_t sample_workspace_bytes(const dms_sample_config& c, int rows) {
-  return kAlign;
+  return c.vocab <= kSmallVocab ? kAlign : align_up(sizeof(RowState) * std::max(1, std::min(rows, kRowsAtOnce)), kAlign);
+}
+
+template <bool BF16>
+hipError_t launch_rows(SampleArgs a, hipStream_t st) {
+  if (a.vocab <= kSmallVocab) {
+    hipLaunchKernelGGL(sample_row_kernel<BF16>, dim3(a.rows), dim3(kRowThreads), 0, st, a);
+    return hipGetLastError();
+  }
+  const int all = a.rows;
+  for (int r = 0; r < all; r += kRowsAtOnce) {
+    a.rows = std::min(kRowsAtOnce, all - r);
+    a.splits = row_splits(a.rows, a.vocab);
+    const dim3 grid(a.rows * a.splits), threads(kSplitThreads);
+    hipLaunchKernelGGL(sample_max_kernel<BF16>, grid, threads, 0, st, a);
+    hipLaunchKernelGGL(sample_hist_kernel<BF16>, grid, threads, 0, st, a);
+    hipLaunchKernelGGL(sample_cut_kernel<BF16>, grid, threads, 0, st, a);
+    hipLaunchKernelGGL(sample_pick_kernel<BF16>, dim3(a.rows), dim3(kRowThreads), 0, st, a);
+    a.logits = static_cast<const char*>(a.logits) + static_cast<int64_t>(a.rows) * a.stride * (BF16 ? 2 : 4);
+    auto on = [&](auto*& p) { if (p) p += a.rows; };
+    on(a.temperature), on(a.top_k), on(a.top_p), on(a.min_p), on(a.u), on(a.tokens), on(a.logprobs);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_sample(const dms_sample_config& c, int rows, const void* logits, int64_t stride, const float* temperature,
@@ -346,9 +876,8 @@ hipError_t launch_sample(const dms_sample_config& c, int rows, const void* logit
   a.top_k0 = c.top_k;
   a.top_p0 = c.top_p;
   a.min_p0 = c.min_p;
-  if (c.logits_type == DMS_TYPE_BF16) hipLaunchKernelGGL(sample_row_kernel<true>, dim3(rows), dim3(kRowThreads), 0, st, a);
-  else hipLaunchKernelGGL(sample_row_kernel<false>, dim3(rows), dim3(kRowThreads), 0, st, a);
-  return hipGetLastError();
+  a.state = static_cast<RowState*>(ws);
+  return c.logits_type == DMS_TYPE_BF16 ? launch_rows<true>(a, st) : launch_rows<false>(a, st);
 }
 
 }  // namespace dms
