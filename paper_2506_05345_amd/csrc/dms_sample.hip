@@ -7,19 +7,19 @@
 // (at most 2^20 tokens), so that borders and picks depend on neither the split of a
 // row nor the order of atomics.  Tokens of weight 0 are never taken.
 //
-// Rows of more than kSmallVocab logits are cut into splits, so that few rows fill the
+// Rows of more than kSmallVocab logits are cut into parts, so that few rows fill the
 // chip too, and take four launches:
-//   sample_max_kernel   the splits' largest values (reads the logits from memory;
+//   sample_max_kernel   the parts' largest values (reads the logits from memory;
 //                       the passes after it find them in the caches);
-//   sample_hist_kernel  the splits' weights, and each row's counts and weights by
-//                       distance from its largest value, 32 bins an octave over 20 octaves;
+//   sample_hist_kernel  the parts' weights, and each row's counts and weights by
+//                       distance from its largest value (bins of 1/32 octave of weight);
 //   sample_cut_kernel   from those the bins that hold the borders of top-k and
-//                       top-p: the weights ahead of them by split, and their tokens
+//                       top-p: the weights ahead of them by part, and their tokens
 //                       listed;
 //   sample_pick_kernel  a workgroup a row sorts the listed tokens, cuts them, finds the
-//                       split that holds the picked token and walks it.
-// A row whose border lies past the bins or has too many tokens in its bins (many equal
-// logits) is done by the last launch alone, as shorter rows are (sample_row).
+//                       part that holds the picked token and walks it.
+// A row whose borders' bins hold too many tokens (many equal logits) is done by the
+// last launch alone, as shorter rows are (sample_row).
 #include <math.h>
 
 #include <algorithm>
@@ -47,8 +47,8 @@ struct SampleArgs {
   int rows, vocab;
   float temperature0, top_p0, min_p0;
   int top_k0;
-  RowState* state;            // [rows], rows in splits
-  int splits;
+  RowState* state;            // [rows], rows in parts
+  int parts;
 };
 
 // Settings of one row.
@@ -98,25 +98,24 @@ __device__ inline float key_value(uint32_t k) {
 constexpr uint32_t kKeyNone = 0x007FFFFFu;   // -inf
 
 // 2^43 2^((x - top) c), rounded.  2^f for |f| <= 1/2 is its Taylor sum to the 12th
-// power, (ln 2 / 2)^13 / 13! = 2e-16 off.
+// power, (ln 2 / 2)^13 / 13! = 2e-16 off.  No branches: several weights are formed
+// side by side.
 __device__ inline u64 weight(float x, float top, double c) {
-  const double t = (static_cast<double>(x) - static_cast<double>(top)) * c;
-  if (!(t > -45.0)) return 0;
+  const double t = fmax((static_cast<double>(x) - static_cast<double>(top)) * c, -64.0);   // (NaN too: weight 0)
   const double n = rint(t), f = t - n;
-  double p = 2.5678435993488196e-11;
-  p = fma(p, f, 4.44553827187081e-10);
-  p = fma(p, f, 7.054911620801121e-09);
-  p = fma(p, f, 1.0178086009239696e-07);
-  p = fma(p, f, 1.3215486790144305e-06);
-  p = fma(p, f, 1.5252733804059838e-05);
-  p = fma(p, f, 0.00015403530393381606);
-  p = fma(p, f, 0.0013333558146428441);
-  p = fma(p, f, 0.009618129107628477);
-  p = fma(p, f, 0.055504108664821576);
-  p = fma(p, f, 0.2402265069591007);
-  p = fma(p, f, 0.6931471805599453);
+  constexpr double kTerms[12] = {2.5678435993488196e-11, 4.44553827187081e-10, 7.054911620801121e-09,
+                                 1.0178086009239696e-07, 1.3215486790144305e-06, 1.5252733804059838e-05,
+                                 0.00015403530393381606, 0.0013333558146428441, 0.009618129107628477,
+                                 0.055504108664821576, 0.2402265069591007, 0.6931471805599453};
+  double p = kTerms[0];
+#pragma unroll
+  for (int i = 1; i < 12; ++i) {
+    double term = kTerms[i];
+    asm("" : "+s"(term));      // in scalar registers: an addend is no move of its own
+    p = fma(p, f, term);
+  }
   p = fma(p, f, 1.0);
-  const double scale = __longlong_as_double(static_cast<long long>(1023 + 43 + static_cast<int>(n)) << 52);
+  const double scale = __hiloint2double((1023 + 43 + static_cast<int>(n)) << 20, 0);
   // 2^52 and more have no fraction bits: the sum is rounded to an integer, half to even
   const u64 b = static_cast<u64>(__double_as_longlong(fma(p, scale, 0x1p52)));
   return b & ((1ull << 52) - 1);
@@ -363,33 +362,34 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// A row in splits
+// A row in parts
 // ---------------------------------------------------------------------------
-constexpr int kSplitThreads = 256, kMaxSplits = 64;
-constexpr int kPerOctave = 32, kHist = 20 * kPerOctave;   // bins of a row
+constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64;
+constexpr int kMaxParts = 256;                            // parts of a row, a wave each
+constexpr int kFine = 20 * 32, kHist = kFine + 25 * 4;    // bins: 32 an octave over 20 octaves, then 4 over 25
 constexpr int kListed = 2048;                             // tokens that a row lists at most
 
 // What the launches of a row leave each other.
 struct RowState {
   u64 mass[kHist];            // weights by bin
-  u64 split_mass[kMaxSplits], split_kept[kMaxSplits];
+  u64 part_mass[kMaxParts], part_kept[kMaxParts];
   u64 list[kListed];          // key << 32 | ~index of the tokens in the borders' bins
   uint32_t count[kHist];
-  uint32_t split_top[kMaxSplits];
+  uint32_t part_top[kMaxParts];
   uint32_t listed;
 };
 
-// The splits of a row: 16-byte groups of logits in equal parts; what lies before the
-// first aligned group belongs to the first split, what is left to the last.
+// The parts of a row: 16-byte groups of logits in equal shares; what lies before the
+// first aligned group belongs to the first part, what is left to the last.
 template <bool BF16>
-struct Splits {
+struct Parts {
   static constexpr int VEC = BF16 ? 8 : 4;
   const char* row;
   int V, S, lead, groups;
-  __device__ Splits(const SampleArgs& a, int r) {
+  __device__ Parts(const SampleArgs& a, int r) {
     row = static_cast<const char*>(a.logits) + static_cast<int64_t>(r) * a.stride * (BF16 ? 2 : 4);
     V = a.vocab;
-    S = a.splits;
+    S = a.parts;
     lead = min(V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (BF16 ? 2 : 4));
     groups = (V - lead) / VEC;
   }
@@ -401,30 +401,40 @@ struct Splits {
     const int g = (i - lead) / VEC;
     return g >= groups ? S - 1 : static_cast<int>((static_cast<int64_t>(g + 1) * S - 1) / groups);
   }
-  // f(index, logit) of every token of split s, four 16-byte loads in flight
+  // f(first index, four logits, how many of them are there) over part s, by one wave; four 16-byte loads in flight
   template <class F>
   __device__ void each(int s, F f) const {
-    const int tid = threadIdx.x;
-    if (s == 0)
-      for (int i = tid; i < lead; i += kSplitThreads) f(i, logit<BF16>(row, i));
+    const int lane = threadIdx.x & 63;
+    auto edge = [&](int i0, int i1) {      // fewer than VEC tokens
+      if (i0 + lane < i1) {
+        const float x[4] = {logit<BF16>(row, i0 + lane), -INFINITY, -INFINITY, -INFINITY};
+        f(i0 + lane, x, 1);
+      }
+    };
+    if (s == 0) edge(0, lead);
     const int g1 = first_group(s + 1);
     const uint4* p = reinterpret_cast<const uint4*>(row + static_cast<size_t>(lead) * (BF16 ? 2 : 4));
-    for (int g = first_group(s) + tid; g < g1; g += 4 * kSplitThreads) {
-      uint4 x[4];
+    for (int g = first_group(s) + lane; g < g1; g += 4 * 64) {
+      uint4 v[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) x[u] = p[min(g + u * kSplitThreads, g1 - 1)];
+      for (int u = 0; u < 4; ++u) v[u] = p[min(g + u * 64, g1 - 1)];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        if (g + u * kSplitThreads >= g1) break;
-        const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-        const int i = lead + (g + u * kSplitThreads) * VEC;
+        if (g + u * 64 >= g1) break;
+        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        const int i = lead + (g + u * 64) * VEC;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          f(i + e, counted(BF16 ? __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16) : __uint_as_float(w[e & 3])));
+        for (int h = 0; h < VEC / 4; ++h) {
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[e] = counted(BF16 ? __uint_as_float(e & 1 ? w[2 * h + (e >> 1)] & 0xFFFF0000u : w[2 * h + (e >> 1)] << 16)
+                                : __uint_as_float(w[e]));
+          f(i + 4 * h, x, 4);
+        }
       }
     }
-    if (s == S - 1)
-      for (int i = lead + groups * VEC + tid; i < V; i += kSplitThreads) f(i, logit<BF16>(row, i));
+    if (s == S - 1) edge(lead + groups * VEC, V);
   }
 };
 
@@ -432,76 +442,111 @@ __device__ inline uint32_t wave_max32(uint32_t v) {
   for (int off = 32; off; off >>= 1) v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), off, 64)));
   return v;
 }
-
-template <bool BF16>
-__global__ __launch_bounds__(kSplitThreads) void sample_max_kernel(SampleArgs a) {
-  __shared__ uint32_t top[kSplitThreads / 64];
-  const int r = blockIdx.x / a.splits, s = blockIdx.x % a.splits, tid = threadIdx.x;
-  RowState& st = a.state[r];
-  for (int x = s * kSplitThreads + tid; x < kHist; x += a.splits * kSplitThreads) st.mass[x] = 0, st.count[x] = 0;
-  if (s == 0 && tid == 0) st.listed = 0;
-  uint32_t key = kKeyNone;
-  Splits<BF16>(a, r).each(s, [&](int, float x) { key = max(key, order_key(x)); });
-  key = wave_max32(key);
-  if ((tid & 63) == 0) top[tid >> 6] = key;
-  __syncthreads();
-  if (tid == 0) {
-    for (int x = 1; x < kSplitThreads / 64; ++x) key = max(key, top[x]);
-    st.split_top[s] = key;
+// Row and part of a wave.
+struct PartOf {
+  int r, s;
+  __device__ explicit PartOf(const SampleArgs& a) {
+    const int per = a.parts / kPartWaves;
+    r = blockIdx.x / per;
+    s = __builtin_amdgcn_readfirstlane((blockIdx.x % per) * kPartWaves + (threadIdx.x >> 6));
   }
-}
-
-// The row's largest value, from its splits.
-__device__ inline uint32_t row_top(const RowState& st, int splits) {
-  const int lane = threadIdx.x & 63;
-  return wave_max32(lane < splits ? st.split_top[lane] : kKeyNone);
-}
-// Bin of a token: larger for smaller logits (each step is monotonous), kHist past the bins.
-__device__ inline int bin_of(float x, float top, float c) {
-  const float z = (top - x) * c * static_cast<float>(kPerOctave);
-  return z < static_cast<float>(kHist) ? static_cast<int>(z) : kHist;
-}
+};
 
 template <bool BF16>
-__global__ __launch_bounds__(kSplitThreads) void sample_hist_kernel(SampleArgs a) {
-  __shared__ u64 mass[kHist], part[kSplitThreads / 64];
+__global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) {
+  const PartOf me(a);
+  RowState& st = a.state[me.r];
+  const int lane = threadIdx.x & 63;
+  for (int x = me.s * 64 + lane; x < kHist; x += a.parts * 64) st.mass[x] = 0, st.count[x] = 0;
+  if (me.s == 0 && lane == 0) st.listed = 0;
+  uint32_t key = kKeyNone;
+  Parts<BF16>(a, me.r).each(me.s, [&](int, const float (&x)[4], int) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) key = max(key, order_key(x[e]));
+  });
+  key = wave_max32(key);
+  if (lane == 0) st.part_top[me.s] = key;
+}
+
+// The row's largest value, from its parts (by every wave).
+__device__ inline uint32_t row_top(const RowState& st, int parts) {
+  uint32_t key = kKeyNone;
+  for (int x = threadIdx.x & 63; x < parts; x += 64) key = max(key, st.part_top[x]);
+  return wave_max32(key);
+}
+// Distance of a logit from the largest in octaves of weight, and its bin: larger for
+// smaller logits (each step is monotonous), kHist where the weight is 0.
+__device__ inline float octaves(float x, float top, float c) {
+  const float half = 0.5f * top - 0.5f * x;      // (two large values of either sign: no overflow)
+  return half == 0.f ? 0.f : half * (2.0f * c);
+}
+__device__ inline int bin_of(float z) {
+  return z < 20.f ? static_cast<int>(z * 32.f) : z < 45.f ? kFine + static_cast<int>((z - 20.f) * 4.f) : kHist;
+}
+
+// What a row asks of its passes: weights of its bins (top-p), of its parts (no cut by
+// rank or weight at all), counts (top-k).
+struct Asked {
+  bool by_k, by_p, least;
+  __device__ Asked(const SampleArgs& a, const RowSetting& s) : by_k(s.k < a.vocab), by_p(s.p < 1.0), least(s.least > 0.0) {}
+  __device__ bool weights() const { return by_p || !(by_k || least); }
+  __device__ bool bins() const { return by_k || by_p; }
+  __device__ bool whole() const { return !(by_k || by_p || least); }
+};
+
+template <bool BF16>
+__global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a) {
+  __shared__ u64 mass[kHist];
   __shared__ uint32_t count[kHist];
-  const int r = blockIdx.x / a.splits, s = blockIdx.x % a.splits, tid = threadIdx.x;
-  RowState& st = a.state[r];
-  const RowSetting set = row_setting(a, r);
-  const uint32_t key = row_top(st, a.splits);
-  if (key == kKeyNone) return;
-  const bool cut = set.k < a.vocab || set.p < 1.0;
-  if (cut) {
-    for (int x = tid; x < kHist; x += kSplitThreads) mass[x] = 0, count[x] = 0;
+  const PartOf me(a);
+  const int tid = threadIdx.x, lane = tid & 63;
+  RowState& st = a.state[me.r];
+  const RowSetting set = row_setting(a, me.r);
+  const Asked ask(a, set);
+  const uint32_t key = row_top(st, a.parts);
+  if (key == kKeyNone || !(ask.weights() || ask.bins())) return;
+  if (ask.bins()) {
+    for (int x = tid; x < kHist; x += kPartThreads) mass[x] = 0, count[x] = 0;
     __syncthreads();
   }
   const float top = key_value(key), c = static_cast<float>(set.c);
-  u64 sum = 0;
-  Splits<BF16>(a, r).each(s, [&](int, float x) {
-    const u64 w = weight(x, top, set.c);
-    sum += w;
-    if (cut && w) {
-      const int b = bin_of(x, top, c);
-      if (b < kHist) {
-        atomicAdd(&mass[b], w);
-        atomicAdd(&count[b], 1u);
+  const Parts<BF16> parts(a, me.r);
+  if (ask.weights()) {
+    u64 sum = 0;
+    parts.each(me.s, [&](int, const float (&x)[4], int) {
+      u64 w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = weight(x[e], top, set.c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += w[e];
+      if (ask.by_p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (w[e]) {
+            const int b = bin_of(octaves(x[e], top, c));
+            atomicAdd(&mass[b], w[e]);
+            atomicAdd(&count[b], 1u);
+          }
+    });
+    sum = wave_sum64(sum);
+    if (lane == 0) st.part_mass[me.s] = sum;
+  } else {
+    parts.each(me.s, [&](int, const float (&x)[4], int) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = octaves(x[e], top, c);
+        if (z < 45.f) atomicAdd(&count[bin_of(z)], 1u);
       }
-    }
-  });
-  sum = wave_sum64(sum);
-  if ((tid & 63) == 0) part[tid >> 6] = sum;
-  __syncthreads();
-  if (tid == 0) {
-    for (int x = 1; x < kSplitThreads / 64; ++x) sum += part[x];
-    st.split_mass[s] = sum;
+    });
   }
-  if (cut)
-    for (int x = tid; x < kHist; x += kSplitThreads)
+  if (ask.bins()) {
+    __syncthreads();
+    for (int x = tid; x < kHist; x += kPartThreads)
       if (count[x]) {
-        atomicAdd(&st.mass[x], mass[x]);
+        if (ask.by_p) atomicAdd(&st.mass[x], mass[x]);
         atomicAdd(&st.count[x], count[x]);
       }
+  }
 }
 
 // Which bins hold a row's borders.
@@ -509,24 +554,23 @@ struct Cut {
   bool none, slow;     // nothing to cut by rank or weight; the row is left to sample_row
   int from, to;        // bins whose tokens are listed; those before are kept
   uint32_t ahead;      // tokens and weight before `from`
-  u64 ahead_mass, all; // weight of the row
+  u64 ahead_mass, all; // weight of the bins
 };
 struct CutLds {
-  u64 wave_mass[16];
-  uint32_t wave_count[16];
+  u64 wave_mass[kRowThreads / 64];
+  uint32_t wave_count[kRowThreads / 64];
   int k_bin, p_low, p_high;
   u64 k_before, k_with;
   uint32_t ahead, through;
   u64 ahead_mass;
 };
-// Found by a whole workgroup of THREADS, three bins or fewer to a thread.
+// Found by a whole workgroup, a few bins to a thread.
 template <int THREADS>
-__device__ Cut find_cut(const SampleArgs& a, const RowState& st, const RowSetting& set, CutLds& l) {
+__device__ Cut find_cut(const RowState& st, const RowSetting& set, const Asked& ask, CutLds& l) {
   constexpr int PER = (kHist + THREADS - 1) / THREADS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   Cut cut{};
-  cut.all = wave_sum64(lane < a.splits ? st.split_mass[lane] : 0);
-  cut.none = set.k >= a.vocab && !(set.p < 1.0);
+  cut.none = !ask.bins();
   if (cut.none) return cut;
   u64 m[PER], sum = 0;
   uint32_t n[PER], num = 0;
@@ -548,21 +592,17 @@ __device__ Cut find_cut(const SampleArgs& a, const RowState& st, const RowSettin
   if (lane == 63) l.wave_mass[wave] = im, l.wave_count[wave] = in;
   if (tid == 0) l.k_bin = l.p_low = l.p_high = kHist;
   __syncthreads();
-  u64 before = im - sum, all_mass = 0;
+  u64 before = im - sum;
   uint32_t ahead = in - num, all_count = 0;
   for (int x = 0; x < THREADS / 64; ++x) {
     if (x < wave) before += l.wave_mass[x], ahead += l.wave_count[x];
-    all_mass += l.wave_mass[x];
+    cut.all += l.wave_mass[x];
     all_count += l.wave_count[x];
   }
-  // top-k: the bin with the k-th token.  Where the bins hold fewer and nothing lies past
-  // them, top-k takes all.
+  // top-k: the bin with the k-th token; fewer tokens than that have a weight: all of them
   const uint32_t k = static_cast<uint32_t>(set.k);
-  const bool past = all_mass != cut.all;
-  const bool by_k = k < all_count || (past && set.k < a.vocab);
-  const bool by_p = set.p < 1.0;
-  if (by_k && k > all_count) cut.slow = true;
-  if (!by_k && !by_p) {
+  const bool by_k = ask.by_k && k < all_count;
+  if (!by_k && !ask.by_p) {
     cut.none = true;
     return cut;
   }
@@ -581,9 +621,7 @@ __device__ Cut find_cut(const SampleArgs& a, const RowState& st, const RowSettin
     }
   }
   __syncthreads();
-  if (by_k && l.k_bin == kHist) cut.slow = true;
-  if (cut.slow) return cut;
-  if (by_p) {
+  if (ask.by_p) {
     // what top-k leaves weighs between the bins before its border and those with it
     const double low = set.p * static_cast<double>(by_k ? l.k_before : cut.all);
     const double high = set.p * static_cast<double>(by_k ? l.k_with : cut.all);
@@ -598,12 +636,8 @@ __device__ Cut find_cut(const SampleArgs& a, const RowState& st, const RowSettin
       if (!was_high && y > 0 && static_cast<double>(x) >= high) l.p_high = tid * PER + u;
     }
     __syncthreads();
-    if (l.p_high == kHist || l.p_low == kHist) {
-      cut.slow = true;
-      return cut;
-    }
   }
-  cut.from = by_p ? l.p_low : l.k_bin;
+  cut.from = ask.by_p ? l.p_low : l.k_bin;
   cut.to = by_k ? l.k_bin : l.p_high;
   {
     u64 x = before;
@@ -625,46 +659,79 @@ __device__ Cut find_cut(const SampleArgs& a, const RowState& st, const RowSettin
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(kSplitThreads) void sample_cut_kernel(SampleArgs a) {
+__global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) {
   __shared__ CutLds l;
-  __shared__ u64 part[kSplitThreads / 64];
-  const int r = blockIdx.x / a.splits, s = blockIdx.x % a.splits, tid = threadIdx.x;
-  RowState& st = a.state[r];
-  const RowSetting set = row_setting(a, r);
-  const uint32_t key = row_top(st, a.splits);
+  const PartOf me(a);
+  const int lane = threadIdx.x & 63;
+  RowState& st = a.state[me.r];
+  const RowSetting set = row_setting(a, me.r);
+  const Asked ask(a, set);
+  if (ask.whole()) return;
+  const uint32_t key = row_top(st, a.parts);
   if (key == kKeyNone) return;
-  const Cut cut = find_cut<kSplitThreads>(a, st, set, l);
-  if (cut.slow || (cut.none && set.least <= 0.0)) return;
+  const Cut cut = find_cut<kPartThreads>(st, set, ask, l);
+  if (cut.slow) return;
   const float top = key_value(key), c = static_cast<float>(set.c);
+  // past this distance no token passes min-p (2^-43 of the largest weight: no token has one)
+  const float far = ask.least ? 43.01f - log2f(static_cast<float>(set.least)) : 45.f;
   u64 sum = 0;
-  Splits<BF16>(a, r).each(s, [&](int i, float x) {
-    const int b = bin_of(x, top, c);
-    if (!cut.none && b > cut.to) return;
-    const u64 w = weight(x, top, set.c);
-    if (cut.none || b < cut.from) {
-      sum += static_cast<double>(w) >= set.least ? w : 0ull;
-    } else if (w) {
-      const uint32_t at = atomicAdd(&st.listed, 1u);
-      if (at < kListed) st.list[at] = static_cast<u64>(order_key(x)) << 32 | ~static_cast<uint32_t>(i);
+  Parts<BF16>(a, me.r).each(me.s, [&](int i, const float (&x)[4], int n) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float z = octaves(x[e], top, c);
+      const int b = bin_of(z);
+      if (cut.none ? !(z < far) : b > cut.to) continue;
+      const bool ahead = cut.none || b < cut.from;
+      if (ahead && !(z < far)) continue;
+      const u64 w = weight(x[e], top, set.c);
+      if (ahead) {
+        sum += static_cast<double>(w) >= set.least ? w : 0ull;
+      } else if (w && e < n) {
+        const uint32_t at = atomicAdd(&st.listed, 1u);
+        if (at < kListed) st.list[at] = static_cast<u64>(order_key(x[e])) << 32 | ~static_cast<uint32_t>(i + e);
+      }
     }
   });
   sum = wave_sum64(sum);
-  if ((tid & 63) == 0) part[tid >> 6] = sum;
-  __syncthreads();
-  if (tid == 0) {
-    for (int x = 1; x < kSplitThreads / 64; ++x) sum += part[x];
-    st.split_kept[s] = sum;
-  }
+  if (lane == 0) st.part_kept[me.s] = sum;
 }
 
 struct PickLds {
   CutLds cut;
-  u64 list[kListed];
-  u64 mass[kMaxSplits];
+  u64 list[2][kListed];
+  u64 mass[kMaxParts];
   u64 wave_mass[kWaves];
   u64 total, k_mass, before;
-  int last, split, k_last;
+  int last, part, k_last;
 };
+
+// Sorts the n tokens of l.list[0], largest first; returns which of the two lists holds
+// them.  Up to 1024 every thread counts those ahead of its own; more take a bitonic
+// network (1024 tokens: 55 barriers against one).
+__device__ int sort_listed(PickLds& l, int n) {
+  const int tid = threadIdx.x;
+  if (n <= kRowThreads) {
+    if (tid < n) {
+      const u64 mine = l.list[0][tid];
+      int rank = 0;
+#pragma unroll 8
+      for (int x = 0; x < n; ++x) rank += l.list[0][x] > mine;
+      l.list[1][rank] = mine;
+    }
+    __syncthreads();
+    return 1;
+  }
+  for (int x = n + tid; x < kListed; x += kRowThreads) l.list[0][x] = 0;
+  __syncthreads();
+  for (int span = 2; span <= kListed; span *= 2)
+    for (int step = span / 2; step; step /= 2) {
+      const int i = 2 * tid - (tid & (step - 1)), j = i + step;   // the pairs of this step
+      const u64 p = l.list[0][i], q = l.list[0][j];
+      if ((p < q) == ((i & span) == 0)) l.list[0][i] = q, l.list[0][j] = p;
+      __syncthreads();
+    }
+  return 0;
+}
 
 template <bool BF16>
 __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) {
@@ -676,7 +743,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const RowState& st = a.state[r];
   const RowSetting set = row_setting(a, r);
-  const uint32_t key = row_top(st, a.splits);
+  const Asked ask(a, set);
+  const uint32_t key = row_top(st, a.parts);
   if (key == kKeyNone) {      // no token is left
     if (tid == 0) {
       a.tokens[r] = -1;
@@ -684,38 +752,26 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
     }
     return;
   }
-  const Cut cut = find_cut<kRowThreads>(a, st, set, l.cut);
+  const u64 mine = tid < a.parts ? (ask.whole() ? st.part_mass[tid] : st.part_kept[tid]) : 0;
+  const int n = min(static_cast<int>(st.listed), kListed);
+  const Cut cut = find_cut<kRowThreads>(st, set, ask, l.cut);
   if (cut.slow) {
     __syncthreads();
     sample_row<BF16>(a, r, lds.row);
     return;
   }
   const float top = key_value(key);
-  const Splits<BF16> sp(a, r);
-  const bool whole = cut.none && set.least <= 0.0;
-  if (tid < kMaxSplits) l.mass[tid] = tid < a.splits ? (whole ? st.split_mass[tid] : st.split_kept[tid]) : 0;
+  const Parts<BF16> parts(a, r);
+  if (tid < kMaxParts) l.mass[tid] = mine;
   u64 border = 0;              // the last kept token of the listed ones, as the list holds it
-  __syncthreads();
   if (!cut.none) {
-    // ---- the listed tokens in falling order (equal ones by index)
-    const int n = min(static_cast<int>(st.listed), kListed);
-    int size = 64;
-    while (size < n) size *= 2;
-    for (int x = tid; x < size; x += kRowThreads) l.list[x] = x < n ? st.list[x] : 0;
+    for (int x = tid; x < n; x += kRowThreads) l.list[0][x] = st.list[x];
     __syncthreads();
-    for (int span = 2; span <= size; span *= 2)
-      for (int step = span / 2; step; step /= 2) {
-        for (int x = tid; x < size / 2; x += kRowThreads) {
-          const int i = 2 * x - (x & (step - 1)), j = i + step;   // pairs of this step
-          const u64 p = l.list[i], q = l.list[j];
-          if ((p < q) == ((i & span) == 0)) l.list[i] = q, l.list[j] = p;
-        }
-        __syncthreads();
-      }
+    const u64* list = l.list[sort_listed(l, n)];
     // ---- running weights: thread t holds tokens 2 t and 2 t + 1
     const int x0 = 2 * tid;
-    const u64 w0 = x0 < n ? weight(key_value(static_cast<uint32_t>(l.list[x0] >> 32)), top, set.c) : 0;
-    const u64 w1 = x0 + 1 < n ? weight(key_value(static_cast<uint32_t>(l.list[x0 + 1] >> 32)), top, set.c) : 0;
+    const u64 w0 = x0 < n ? weight(key_value(static_cast<uint32_t>(list[x0] >> 32)), top, set.c) : 0;
+    const u64 w1 = x0 + 1 < n ? weight(key_value(static_cast<uint32_t>(list[x0 + 1] >> 32)), top, set.c) : 0;
     u64 run = w0 + w1;
     for (int off = 1; off < 64; off <<= 1) {
       const u64 up = __shfl_up(run, off, 64);
@@ -732,59 +788,67 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
       l.k_mass = (left - 1) % 2 ? r1 : r0;
     }
     __syncthreads();
-    if (set.p < 1.0) {
+    if (ask.by_p) {
       const double least = set.p * static_cast<double>(l.k_mass);
       // the first token at which the running weight is enough
       const bool e0 = x0 < n && static_cast<double>(r0) >= least, e1 = x0 + 1 < n && static_cast<double>(r1) >= least;
       const bool eb = x0 > 0 && x0 <= n && static_cast<double>(r0 - w0) >= least;
       if (!eb && (e0 || e1)) atomicMin(&l.last, e0 ? x0 : x0 + 1);
+      __syncthreads();
     }
-    __syncthreads();
     const int last = min(l.last, l.k_last);
-    border = l.list[last];
-    // ---- kept ones, to their splits
+    border = list[last];
+    // ---- kept ones, to their parts
     if (x0 <= last && static_cast<double>(w0) >= set.least)
-      atomicAdd(&l.mass[sp.holding(static_cast<int>(~static_cast<uint32_t>(l.list[x0])))], w0);
+      atomicAdd(&l.mass[parts.holding(static_cast<int>(~static_cast<uint32_t>(list[x0])))], w0);
     if (x0 + 1 <= last && static_cast<double>(w1) >= set.least)
-      atomicAdd(&l.mass[sp.holding(static_cast<int>(~static_cast<uint32_t>(l.list[x0 + 1])))], w1);
-    __syncthreads();
+      atomicAdd(&l.mass[parts.holding(static_cast<int>(~static_cast<uint32_t>(list[x0 + 1])))], w1);
   }
-  // ---- the split that holds the picked token
+  __syncthreads();
+  // ---- the part that holds the picked token: lane t has parts 4 t .. 4 t + 3
   if (wave == 0) {
-    const u64 m = l.mass[lane];
-    u64 run = m;
+    u64 m[kMaxParts / 64], sum = 0;
+#pragma unroll
+    for (int u = 0; u < kMaxParts / 64; ++u) sum += m[u] = l.mass[lane * (kMaxParts / 64) + u];
+    u64 run = sum;
     for (int off = 1; off < 64; off <<= 1) {
       const u64 up = __shfl_up(run, off, 64);
       if (lane >= off) run += up;
     }
     const u64 total = __shfl(run, 63, 64);
     const u64 target = static_cast<u64>(static_cast<double>(set.u) * static_cast<double>(total));
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(run > target);
-    const int s = static_cast<int>(__builtin_ctzll(hit));
-    if (lane == s) {
-      l.split = s;
-      l.total = total;
-      l.before = run - m;
+    u64 at = run - sum;
+    if (run > target && at <= target) {     // one lane
+#pragma unroll
+      for (int u = 0; u < kMaxParts / 64; ++u) {
+        if (at + m[u] > target) {
+          l.part = lane * (kMaxParts / 64) + u;
+          l.total = total;
+          l.before = at;
+          break;
+        }
+        at += m[u];
+      }
     }
   }
   __syncthreads();
   // ---- its tokens by index, four to a thread at a time
   const u64 total = l.total, target = static_cast<u64>(static_cast<double>(set.u) * static_cast<double>(total));
   u64 before = l.before;
-  const int end = sp.end(l.split);
-  for (int i0 = sp.begin(l.split); i0 < end; i0 += 4 * kRowThreads) {
+  const int end = parts.end(l.part);
+  for (int i0 = parts.begin(l.part); i0 < end; i0 += 4 * kRowThreads) {
     u64 w[4], sum = 0;
     float x[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int i = i0 + 4 * tid + u;
-      x[u] = i < end ? logit<BF16>(sp.row, i) : -INFINITY;
+      x[u] = i < end ? logit<BF16>(parts.row, i) : -INFINITY;
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const u64 as_listed = static_cast<u64>(order_key(x[u])) << 32 | ~static_cast<uint32_t>(i0 + 4 * tid + u);
-      w[u] = as_listed >= border ? weight(x[u], top, set.c) : 0;
-      if (!(static_cast<double>(w[u]) >= set.least)) w[u] = 0;
+      w[u] = weight(x[u], top, set.c);
+      if (as_listed < border || !(static_cast<double>(w[u]) >= set.least)) w[u] = 0;
       sum += w[u];
     }
     u64 run = sum;
@@ -820,9 +884,11 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
   }
 }
 
-// Splits of a row: about four workgroups a compute unit in all, none of fewer than 2048
-// logits.
-int row_splits(int rows, int vocab) { return std::max(1, std::min({kMaxSplits, (1024 + rows - 1) / rows, vocab / 2048})); }
+// Parts of a row, a wave each: about four workgroups of four a compute unit in all, no
+// part of fewer than 512 logits.
+int row_parts(int rows, int vocab) {
+  return kPartWaves * std::max(1, std::min({kMaxParts / kPartWaves, (1024 + rows - 1) / rows, vocab / (512 * kPartWaves)}));
+}
 
 }  // namespace
 
@@ -844,8 +910,8 @@ hipError_t launch_rows(SampleArgs a, hipStream_t st) {
   const int all = a.rows;
   for (int r = 0; r < all; r += kRowsAtOnce) {
     a.rows = std::min(kRowsAtOnce, all - r);
-    a.splits = row_splits(a.rows, a.vocab);
-    const dim3 grid(a.rows * a.splits), threads(kSplitThreads);
+    a.parts = row_parts(a.rows, a.vocab);
+    const dim3 grid(a.rows * (a.parts / kPartWaves)), threads(kPartThreads);
     hipLaunchKernelGGL(sample_max_kernel<BF16>, grid, threads, 0, st, a);
     hipLaunchKernelGGL(sample_hist_kernel<BF16>, grid, threads, 0, st, a);
     hipLaunchKernelGGL(sample_cut_kernel<BF16>, grid, threads, 0, st, a);
