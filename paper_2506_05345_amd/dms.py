@@ -306,6 +306,24 @@ def _one_device(where, *tensors):
                 raise DmsError(DMS_ERR_INVALID, f"{where}: tensors must be on the current device")
 
 
+def _take(where, specs):
+    """The addresses of a call's tensors, given as in _args, after the checks of _args and
+    _one_device: one look at each tensor where all is well."""
+    here, out = -2, []
+    for x, _, kind, count in specs:
+        if x is None or type(x) is int:
+            out.append(x)
+            continue
+        if here == -2:
+            here = _torch().cuda.current_device()
+        if not (isinstance(x, torch.Tensor) and x.dtype is _KINDS[kind] and x.get_device() == here and
+                x.is_contiguous() and x.numel() >= count):
+            _args(where, *specs)
+            _one_device(where, *(s[0] for s in specs))
+        out.append(x.data_ptr())
+    return out
+
+
 def _rows_stride(x, heads, dim, stride):
     """Elements from a token's row to the next: `stride` if given; of a tensor [tokens, heads, dim]
     whose rows are dense, its own; None where the rows are not dense."""
@@ -848,64 +866,64 @@ def dms_tree_workspace(cfg: DmsConfig, n, total_nodes, max_nodes) -> int:
     return size.value
 
 
-def _check_tree_args(ctx, where, workspace, n, total, max_nodes, seq_ids, cu_nodes, **t):
-    specs = [(seq_ids, "seq_ids", _I32, n), (cu_nodes, "cu_nodes", _I32, n + 1)]
-    cfg, dims = _CTX_CFG.get(ctx), _dims(ctx)
-    if dims is not None:
-        H, Hq, D, _ = dims
-        of = {"q": (_BF16, total * Hq * D), "out": (_BF16, total * Hq * D), "k": (_BF16, total * H * D),
-              "v": (_BF16, total * H * D), "flags": (_U8, total * H), "decisions_out": (_U8, total * H),
-              "parents": (_I32, total), "path": (_I32, total), "path_len": (_I32, n)}
-        specs += [(x, name, *of[name]) for name, x in t.items()]
-        if workspace is not None and type(workspace) is not int:
-            # the size is only known for sizes that the library takes (else it refuses them)
-            size = _SZ()
-            ok = lib().dms_tree_workspace(ctypes.byref(cfg), n, total, max_nodes, ctypes.byref(size)) == DMS_OK
-            specs.append((workspace, "workspace", _U8, size.value if ok else 0))
-    _args(where, *specs)
-    _one_device(where, workspace, seq_ids, cu_nodes, *t.values())
+def _workspace_bytes(fn, *args):
+    """What a call's workspace has to hold; 0 for sizes that the library refuses (it says why)."""
+    size = _SZ()
+    return size.value if fn(*args, ctypes.byref(size)) == DMS_OK else 0
+
+
+def _tree_sizes(ctx, n, total, max_nodes, workspace):
+    """Element counts of a tree call's rows: queries, keys, flags; its workspace's bytes.  Zeros for a
+    handle this module did not create."""
+    cfg = _CTX_CFG.get(ctx)
+    if cfg is None:
+        return 0, 0, 0, 0
+    kv = total * cfg.num_kv_heads
+    need = 0 if workspace is None or type(workspace) is int else \
+        _workspace_bytes(lib().dms_tree_workspace, ctypes.byref(cfg), n, total, max_nodes)
+    return kv * cfg.group_size * cfg.head_dim, kv * cfg.head_dim, kv, need
 
 
 def dms_tree_attention(ctx, layer, n, seq_ids, cu_nodes, total_nodes, max_nodes, parents, q, k, v, flags, out,
                        workspace, stream=None):
-    w = "dms_tree_attention"
-    _check_tree_args(ctx, w, workspace, n, total_nodes, max_nodes, seq_ids, cu_nodes, parents=parents, q=q, k=k, v=v,
-                     flags=flags, out=out)
-    _check(lib().dms_tree_attention(ctx, layer, n, _ptr(seq_ids), _ptr(cu_nodes), total_nodes, max_nodes,
-                                    _ptr(parents), _ptr(q), _ptr(k), _ptr(v), _ptr(flags), _ptr(out),
-                                    _ptr(workspace), _stream(stream)), w)
+    rows_q, rows_k, rows, need = _tree_sizes(ctx, n, total_nodes, max_nodes, workspace)
+    ids, cu, *rest = _take("dms_tree_attention", (
+        (seq_ids, "seq_ids", _I32, n), (cu_nodes, "cu_nodes", _I32, n + 1), (parents, "parents", _I32, total_nodes),
+        (q, "q", _BF16, rows_q), (k, "k", _BF16, rows_k), (v, "v", _BF16, rows_k), (flags, "flags", _U8, rows),
+        (out, "out", _BF16, rows_q), (workspace, "workspace", _U8, need)))
+    _check(lib().dms_tree_attention(ctx, layer, n, ids, cu, total_nodes, max_nodes, *rest, _stream(stream)),
+           "dms_tree_attention")
 
 
 def dms_tree_attention_q(ctx, layer, n, seq_ids, cu_nodes, total_nodes, max_nodes, parents, q, k, v, decisions_out,
                          out, workspace, stream=None):
-    w = "dms_tree_attention_q"
-    _check_tree_args(ctx, w, workspace, n, total_nodes, max_nodes, seq_ids, cu_nodes, parents=parents, q=q, k=k, v=v,
-                     decisions_out=decisions_out, out=out)
-    _check(lib().dms_tree_attention_q(ctx, layer, n, _ptr(seq_ids), _ptr(cu_nodes), total_nodes, max_nodes,
-                                      _ptr(parents), _ptr(q), _ptr(k), _ptr(v), _ptr(decisions_out), _ptr(out),
-                                      _ptr(workspace), _stream(stream)), w)
+    rows_q, rows_k, rows, need = _tree_sizes(ctx, n, total_nodes, max_nodes, workspace)
+    ids, cu, *rest = _take("dms_tree_attention_q", (
+        (seq_ids, "seq_ids", _I32, n), (cu_nodes, "cu_nodes", _I32, n + 1), (parents, "parents", _I32, total_nodes),
+        (q, "q", _BF16, rows_q), (k, "k", _BF16, rows_k), (v, "v", _BF16, rows_k),
+        (decisions_out, "decisions_out", _U8, rows), (out, "out", _BF16, rows_q), (workspace, "workspace", _U8, need)))
+    _check(lib().dms_tree_attention_q(ctx, layer, n, ids, cu, total_nodes, max_nodes, *rest, _stream(stream)),
+           "dms_tree_attention_q")
 
 
 def dms_tree_accept(n, cu_nodes, total_nodes, max_nodes, parents, tokens, targets, first, path_out, path_len_out,
                     next_out, stream=None):
-    w = "dms_tree_accept"
-    _args(w, (cu_nodes, "cu_nodes", _I32, n + 1), (parents, "parents", _I32, total_nodes),
-          (tokens, "tokens", _I32, total_nodes), (targets, "targets", _I32, total_nodes), (first, "first", _I32, n),
-          (path_out, "path_out", _I32, total_nodes), (path_len_out, "path_len_out", _I32, n),
-          (next_out, "next_out", _I32, n))
-    _one_device(w, cu_nodes, parents, tokens, targets, first, path_out, path_len_out, next_out)
-    _check(lib().dms_tree_accept(n, _ptr(cu_nodes), total_nodes, max_nodes, _ptr(parents), _ptr(tokens),
-                                 _ptr(targets), _ptr(first), _ptr(path_out), _ptr(path_len_out), _ptr(next_out),
-                                 _stream(stream)), w)
+    cu, *rest = _take("dms_tree_accept", (
+        (cu_nodes, "cu_nodes", _I32, n + 1), (parents, "parents", _I32, total_nodes), (tokens, "tokens", _I32, total_nodes),
+        (targets, "targets", _I32, total_nodes), (first, "first", _I32, n), (path_out, "path_out", _I32, total_nodes),
+        (path_len_out, "path_len_out", _I32, n), (next_out, "next_out", _I32, n)))
+    _check(lib().dms_tree_accept(n, cu, total_nodes, max_nodes, *rest, _stream(stream)), "dms_tree_accept")
 
 
 def dms_tree_commit(ctx, layer, n, seq_ids, cu_nodes, total_nodes, max_nodes, path, path_len, k, v, flags, workspace,
                     stream=None):
-    w = "dms_tree_commit"
-    _check_tree_args(ctx, w, workspace, n, total_nodes, max_nodes, seq_ids, cu_nodes, path=path, path_len=path_len,
-                     k=k, v=v, flags=flags)
-    _check(lib().dms_tree_commit(ctx, layer, n, _ptr(seq_ids), _ptr(cu_nodes), total_nodes, max_nodes, _ptr(path),
-                                 _ptr(path_len), _ptr(k), _ptr(v), _ptr(flags), _ptr(workspace), _stream(stream)), w)
+    _, rows_k, rows, need = _tree_sizes(ctx, n, total_nodes, max_nodes, workspace)
+    ids, cu, *rest = _take("dms_tree_commit", (
+        (seq_ids, "seq_ids", _I32, n), (cu_nodes, "cu_nodes", _I32, n + 1), (path, "path", _I32, total_nodes),
+        (path_len, "path_len", _I32, n), (k, "k", _BF16, rows_k), (v, "v", _BF16, rows_k), (flags, "flags", _U8, rows),
+        (workspace, "workspace", _U8, need)))
+    _check(lib().dms_tree_commit(ctx, layer, n, ids, cu, total_nodes, max_nodes, *rest, _stream(stream)),
+           "dms_tree_commit")
 
 
 # ---------------------------------------------------------------------------
@@ -947,15 +965,11 @@ def dms_sample(cfg, rows, logits, temperature, top_k, top_p, min_p, u, tokens_ou
             raise DmsError(DMS_ERR_INVALID, f"{w}: logits must have dense rows of {cfg.vocab}")
         if rows > 0 and have < (rows - 1) * stride + cfg.vocab:
             raise DmsError(DMS_ERR_INVALID, f"{w}: logits holds fewer than {rows} rows")
-    specs = [(temperature, "temperature", _F32, rows), (top_k, "top_k", _I32, rows), (top_p, "top_p", _F32, rows),
-             (min_p, "min_p", _F32, rows), (u, "u", _F32, rows), (tokens_out, "tokens_out", _I32, rows),
-             (logprobs_out, "logprobs_out", _F32, rows)]
-    if workspace is not None and type(workspace) is not int:
-        size = _SZ()
-        ok = lib().dms_sample_workspace(ctypes.byref(cfg), rows, ctypes.byref(size)) == DMS_OK
-        specs.append((workspace, "workspace", _U8, size.value if ok else 0))
-    _args(w, *specs)
-    _one_device(w, logits, temperature, top_k, top_p, min_p, u, tokens_out, logprobs_out, workspace)
-    _check(lib().dms_sample(ctypes.byref(cfg), rows, _ptr(logits), stride, _ptr(temperature), _ptr(top_k),
-                            _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(tokens_out), _ptr(logprobs_out),
-                            _ptr(workspace), _stream(stream)), w)
+    need = 0 if workspace is None or type(workspace) is int else \
+        _workspace_bytes(lib().dms_sample_workspace, ctypes.byref(cfg), rows)
+    rest = _take(w, (
+        (temperature, "temperature", _F32, rows), (top_k, "top_k", _I32, rows), (top_p, "top_p", _F32, rows),
+        (min_p, "min_p", _F32, rows), (u, "u", _F32, rows), (tokens_out, "tokens_out", _I32, rows),
+        (logprobs_out, "logprobs_out", _F32, rows), (workspace, "workspace", _U8, need)))
+    _one_device(w, logits)
+    _check(lib().dms_sample(ctypes.byref(cfg), rows, _ptr(logits), stride, *rest, _stream(stream)), w)
