@@ -71,6 +71,7 @@ struct TreeArgs {
   TreeRow* rows;           // [n * H]
   int32_t* cum;            // [n * H + 1] flat tiles before each head
   TreePart* part;          // [cells] (te = tb: no such part)
+  int2* head_parts;        // [n * H] first and last part of each head
   uint32_t* anc;           // [total][words] ancestors and itself, bit a: node a of its tree
   int32_t* depth;          // [total]
   int32_t* deepest;        // [n]
@@ -100,18 +101,40 @@ __device__ inline int part_holding(int tile, int total, int parts) {
 // Preparation
 // ---------------------------------------------------------------------------
 
-// Block 0: the call's ids and sizes are checked, the heads described and their
-// flat tiles summed.
+// Block 0: the call's ids and sizes are checked, the heads described, their tiles
+// summed and cut into parts:
+//   few tiles in all: every head into slices of its own, of min_tiles or so, so that a
+//     workgroup starts and ends one head only (16 heads of 78 tiles: 18.7 us, cut
+//     without regard to heads 26.5);
+//   many: equal parts of the flat list whatever heads they meet, so that ragged heads
+//     cannot unbalance the chip.
+constexpr int kPlanHeads = 512;    // heads that the plan holds in LDS
+__device__ inline TreeRow tree_row(const TreeArgs& a, int hh) {
+  const int i = hh / a.H, s = a.seq_ids[i], c0 = a.cu[i];
+  TreeRow r;
+  r.sh = s * a.H + hh % a.H;
+  r.L = a.len[r.sh];
+  r.tok0 = c0;
+  r.m = a.cu[i + 1] - c0;
+  r.p0 = a.pos[s];
+  r.tile0 = (hh % a.H) * a.tph + c0 / 32 + i;
+  r.seq = i;
+  r.pad = 0;
+  return r;
+}
 __device__ void tree_plan(const TreeArgs& a) {
-  __shared__ uint32_t seen[kMaxSeqs / 32];
-  __shared__ int lds[17];
-  for (int i = threadIdx.x; i < (a.max_seqs + 31) / 32; i += blockDim.x) seen[i] = 0;
+  __shared__ union {
+    uint32_t seen[kMaxSeqs / 32];
+    TreeRow rows[kPlanHeads];
+  } u;
+  __shared__ int cum[kPlanHeads], first[kPlanHeads], lds[17];
+  for (int i = threadIdx.x; i < (a.max_seqs + 31) / 32; i += blockDim.x) u.seen[i] = 0;
   __syncthreads();
   int bad_id = 0, bad = 0;
   for (int i = threadIdx.x; i < a.n; i += blockDim.x) {
     const int s = a.seq_ids[i], c0 = a.cu[i], c1 = a.cu[i + 1];
     if (s < 0 || s >= a.max_seqs) bad_id = 1;
-    else if (atomicOr(&seen[s >> 5], 1u << (s & 31)) & (1u << (s & 31))) bad_id = 1;
+    else if (atomicOr(&u.seen[s >> 5], 1u << (s & 31)) & (1u << (s & 31))) bad_id = 1;
     bad |= c0 < 0 || c1 < c0 || c1 > a.total || c1 - c0 > a.max_nodes;
     bad |= (i == 0 && c0 != 0) || (i == a.n - 1 && c1 != a.total);
   }
@@ -122,47 +145,79 @@ __device__ void tree_plan(const TreeArgs& a) {
     return;
   }
   const int NH = a.n * a.H;
-  int run = 0;
+  const bool held = NH <= kPlanHeads;     // rows and sums in LDS for what follows
+  int total = 0;
   for (int base = 0; base < NH; base += blockDim.x) {
     const int hh = base + threadIdx.x;
     int tiles = 0;
     if (hh < NH) {
-      const int i = hh / a.H, s = a.seq_ids[i], c0 = a.cu[i];
-      TreeRow r;
-      r.sh = s * a.H + hh % a.H;
-      r.L = a.len[r.sh];
-      r.tok0 = c0;
-      r.m = a.cu[i + 1] - c0;
-      r.p0 = a.pos[s];
-      r.tile0 = (hh % a.H) * a.tph + c0 / 32 + i;
-      r.seq = i;
-      r.pad = 0;
+      const TreeRow r = tree_row(a, hh);
       a.rows[hh] = r;
+      if (held) u.rows[hh] = r;
       tiles = tiles_of(r.L, r.m);
     }
     int tot;
     const int ex = block_exclusive_scan(tiles, lds, &tot);
-    if (hh < NH) a.cum[hh] = run + ex;
-    run += tot;
+    if (hh < NH) {
+      a.cum[hh] = total + ex;
+      if (held) cum[hh] = total + ex;
+    }
+    total += tot;
   }
-  if (threadIdx.x == 0) a.cum[NH] = run;
+  if (threadIdx.x == 0) a.cum[NH] = total;
   __syncthreads();
-  const int parts = parts_of(run, a.min_tiles, a.cells);
-  for (int w = threadIdx.x; w < a.cells; w += blockDim.x) {
-    TreePart p{};
-    if (w < parts && run > 0) {
-      p.tb = part_begin(w, run, parts);
-      p.te = part_begin(w + 1, run, parts);
-      int lo = 0, hi = NH - 1;      // the last head whose first tile is not past tb
+  if (held && total < 2 * a.min_tiles * a.cells && NH <= a.cells / 2) {
+    // slices of ceil(total / (cells - NH)) tiles at most, min_tiles at least: no more than cells of them
+    const int slice = max(a.min_tiles, (total + a.cells - NH - 1) / (a.cells - NH));
+    int run = 0;
+    for (int base = 0; base < NH; base += blockDim.x) {
+      const int hh = base + threadIdx.x;
+      const int ns = hh < NH ? (tiles_of(u.rows[hh].L, u.rows[hh].m) + slice - 1) / slice : 0;
+      int tot;
+      const int w0 = run + block_exclusive_scan(ns, lds, &tot);
+      if (hh < NH) {
+        first[hh] = w0;
+        a.head_parts[hh] = make_int2(w0, w0 + ns - 1);
+      }
+      run += tot;
+    }
+    __syncthreads();
+    for (int w = threadIdx.x; w < a.cells; w += blockDim.x) {
+      int lo = 0, hi = NH - 1;      // the last head whose first part is not past w: one with tiles
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (a.cum[mid] <= p.tb) lo = mid; else hi = mid - 1;
+        if (first[mid] <= w) lo = mid; else hi = mid - 1;
       }
-      p.hh = lo;
-      p.c0 = a.cum[lo];
-      p.r = a.rows[lo];
+      const TreeRow r = u.rows[lo];
+      const int T = tiles_of(r.L, r.m), ns = (T + slice - 1) / slice, s = w - first[lo];
+      TreePart* p = a.part + w;
+      p->tb = w < run ? cum[lo] + part_begin(s, T, ns) : 0;
+      p->te = w < run ? cum[lo] + part_begin(s + 1, T, ns) : 0;
+      p->hh = lo;
+      p->c0 = cum[lo];
+      p->r = r;
     }
-    a.part[w] = p;
+    return;
+  }
+  const int parts = parts_of(total, a.min_tiles, a.cells);
+  for (int w = threadIdx.x; w < a.cells; w += blockDim.x) {
+    const bool on = w < parts && total > 0;
+    const int tb = on ? part_begin(w, total, parts) : 0, te = on ? part_begin(w + 1, total, parts) : 0;
+    int lo = 0, hi = NH - 1;      // the last head whose first tile is not past tb
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if ((held ? cum[mid] : a.cum[mid]) <= tb) lo = mid; else hi = mid - 1;
+    }
+    TreePart* p = a.part + w;
+    p->tb = tb;
+    p->te = te;
+    p->hh = lo;
+    p->c0 = held ? cum[lo] : a.cum[lo];
+    p->r = held ? u.rows[lo] : tree_row(a, lo);
+  }
+  for (int hh = threadIdx.x; hh < NH; hh += blockDim.x) {
+    const int c0 = a.cum[hh], c1 = a.cum[hh + 1];
+    a.head_parts[hh] = c1 > c0 ? make_int2(part_holding(c0, total, parts), part_holding(c1 - 1, total, parts)) : make_int2(0, 0);
   }
 }
 
@@ -902,16 +957,14 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
   constexpr int kCols = 1024 / D, kBatch = 8;
   const int status = load_status(a.status);
   const int NH = a.n * a.H, per = (a.max_nodes * a.g + kCols - 1) / kCols;
-  const int total = a.cum[NH], parts = parts_of(total, a.min_tiles, a.cells);
   if (status != 0) return;
   const int piece = threadIdx.x % (D / 4);
   for (int64_t x = blockIdx.x; x < static_cast<int64_t>(NH) * per; x += gridDim.x) {
     const int hh = static_cast<int>(x / per), col = static_cast<int>(x % per) * kCols + threadIdx.x / (D / 4);
     const TreeRow r = a.rows[hh];
-    const int u0 = a.cum[hh], u1 = a.cum[hh + 1] - 1;
-    if (col >= r.m * a.g) continue;
-    const int w0 = part_holding(u0, total, parts), w1 = part_holding(u1, total, parts);
-    if (w0 == w1) continue;    // one part wrote it
+    const int2 span = a.head_parts[hh];
+    const int w0 = __builtin_amdgcn_readfirstlane(span.x), w1 = __builtin_amdgcn_readfirstlane(span.y);
+    if (w0 == w1 || col >= r.m * a.g) continue;    // one part wrote it
     const int unit = col / a.UC, uc = col - unit * a.UC;
     float M = kMInit, L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -920,7 +973,10 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
       float2 ml[kBatch];
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
-        const int y = min(w + u, w1);
+        const int y = w + u;
+        ml[u] = make_float2(kMInit, 0.f);
+        v[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (y > w1) continue;
         const size_t pc = (static_cast<size_t>(2) * (y * a.U + unit) + (y == w0)) * a.UC + uc;
         ml[u] = a.part_ml[pc];
         v[u] = *reinterpret_cast<const f32x4*>(a.part_o + pc * D + 4 * piece);
@@ -934,7 +990,6 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
       M = m;
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
-        if (w + u > w1) break;
         const float f = __builtin_amdgcn_exp2f((ml[u].x - M) * a.scale_log2);
         L += ml[u].y * f;
         acc += v[u] * f;
@@ -1280,7 +1335,7 @@ int tree_workgroups() {
 int tree_waves(int cols) { return cols <= 32 ? 1 : cols <= 64 ? 2 : 4; }
 
 struct TreeLayout {
-  size_t rows, cum, part, anc, depth, deepest, flags, tiles, tmeta, part_o, part_ml, need, fresh, base, before, bytes;
+  size_t rows, cum, part, head_parts, anc, depth, deepest, flags, tiles, tmeta, part_o, part_ml, need, fresh, base, before, bytes;
   int words, tph, UC;
 };
 TreeLayout tree_layout(const dms_config& c, int n, int total, int max_nodes) {
@@ -1299,6 +1354,7 @@ TreeLayout tree_layout(const dms_config& c, int n, int total, int max_nodes) {
     lo.rows = take(NH * sizeof(TreeRow));
     lo.cum = take((NH + 1) * 4);
     lo.part = take(kTreeWorkgroups * sizeof(TreePart));
+    lo.head_parts = take(NH * sizeof(int2));
     lo.anc = take(T * lo.words * 4);
     lo.depth = take(T * 4);
     lo.deepest = take(static_cast<size_t>(n) * 4);
@@ -1360,6 +1416,7 @@ hipError_t launch_tree_attention(const dms_config& c, const Layout& lo, void* me
   a.rows = reinterpret_cast<TreeRow*>(w + tl.rows);
   a.cum = reinterpret_cast<int32_t*>(w + tl.cum);
   a.part = reinterpret_cast<TreePart*>(w + tl.part);
+  a.head_parts = reinterpret_cast<int2*>(w + tl.head_parts);
   a.anc = reinterpret_cast<uint32_t*>(w + tl.anc);
   a.depth = reinterpret_cast<int32_t*>(w + tl.depth);
   a.deepest = reinterpret_cast<int32_t*>(w + tl.deepest);

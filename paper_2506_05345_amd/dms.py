@@ -247,8 +247,10 @@ def _check(rc, where):
         raise DmsError(rc, where)
 
 
-# Configuration of every live context (by handle), for the argument checks.
+# Configuration of every live context (by handle), for the argument checks, and the tree
+# calls' workspace bytes by their sizes.
 _CTX_CFG = {}
+_TREE_BYTES = {}
 
 _BF16 = "bf16"
 _U8 = "uint8"
@@ -395,12 +397,14 @@ def dms_create(cfg: DmsConfig, meta, pools, workspace):
     _check(lib().dms_create(ctypes.byref(cfg), _ptr(meta), arr, _ptr(workspace),
                             ctypes.byref(out)), "dms_create")
     _CTX_CFG[out.value] = DmsConfig.from_buffer_copy(cfg)
+    _TREE_BYTES[out.value] = {}
     return out.value
 
 
 def dms_destroy(ctx):
     _check(lib().dms_destroy(ctx), "dms_destroy")
     _CTX_CFG.pop(ctx, None)
+    _TREE_BYTES.pop(ctx, None)
 
 
 def dms_init_state(ctx, stream=None):
@@ -879,8 +883,14 @@ def _tree_sizes(ctx, n, total, max_nodes, workspace):
     if cfg is None:
         return 0, 0, 0, 0
     kv = total * cfg.num_kv_heads
-    need = 0 if workspace is None or type(workspace) is int else \
-        _workspace_bytes(lib().dms_tree_workspace, ctypes.byref(cfg), n, total, max_nodes)
+    need = 0
+    if workspace is not None and type(workspace) is not int:
+        need = _TREE_BYTES[ctx].get((n, total, max_nodes))
+        if need is None:
+            need = _TREE_BYTES[ctx][n, total, max_nodes] = \
+                _workspace_bytes(lib().dms_tree_workspace, ctypes.byref(cfg), n, total, max_nodes)
+            if len(_TREE_BYTES[ctx]) > 4096:       # sizes of every kind: start over
+                _TREE_BYTES[ctx].clear()
     return kv * cfg.group_size * cfg.head_dim, kv * cfg.head_dim, kv, need
 
 
