@@ -489,13 +489,13 @@ __device__ __forceinline__ uint32_t odd_rows(uint32_t tile, int lane) {
   return __builtin_amdgcn_readfirstlane(mine);
 }
 
-// `careful`: a hidden row takes part in the products with weight 0, and 0 times
-// an infinity or NaN is NaN.  Sums that end finite met none.  Where they do not,
-// the segment is attended again with such rows found (odd), zeroed in the products
-// as those past the end always are, and added by hand to the columns that see them.
-template <int D, bool FP8>
-__device__ __forceinline__ TileMask tile_mask(const TreeArgs& a, const Segment& sg, uint32_t meta, uint32_t tile, int t, bool careful,
-                                              int lane) {
+// CAREFUL: a hidden row takes part in the products with weight 0, and 0 times an
+// infinity or NaN is NaN.  Sums that end finite met none.  Where they do not, the
+// segment is attended again with the rows whose values are not finite found (odd),
+// zeroed in the products, and added by hand to the columns that see them.  (Slots past
+// the live length, whose values may be anything, are zeroed in LDS beforehand.)
+template <int D, bool FP8, bool CAREFUL>
+__device__ __forceinline__ TileMask tile_mask(const TreeArgs& a, const Segment& sg, uint32_t meta, uint32_t tile, int t, int lane) {
   TileMask k;
   k.tree = t >= sg.nc;
   const int rows = t >= sg.t1 ? 0 : k.tree ? sg.m - 32 * (t - sg.nc) : sg.L - 32 * t;
@@ -504,8 +504,27 @@ __device__ __forceinline__ TileMask tile_mask(const TreeArgs& a, const Segment& 
   k.old = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(soon)) & k.alive;
   k.masked = k.tree || k.old != 0 || k.alive != ~0u;
   k.odd = 0;
-  if (careful && k.masked) k.odd = odd_rows<D, FP8>(tile, lane) & k.alive;
+  if (CAREFUL && k.masked) k.odd = odd_rows<D, FP8>(tile, lane) & k.alive;
   return k;
+}
+
+// Zeroes the values of rows `valid` on of a tile in LDS; threads t, t + n, ..
+template <int D, bool FP8>
+__device__ inline void zero_values(uint32_t tile, int valid, int t, int n) {
+  for (int P = t; P < D * (FP8 ? 2 : 4); P += n) {
+    const int nv = valid - 8 * ((P >> 4) & 3);       // rows of this 16-byte piece that stay
+    if (nv >= 8) continue;
+    u32x4 keep;
+    if (FP8) {       // two dims of eight codes
+      const uint64_t k8 = nv <= 0 ? 0ull : ~0ull >> (8 * (8 - nv));
+      keep = u32x4{static_cast<uint32_t>(k8), static_cast<uint32_t>(k8 >> 32), static_cast<uint32_t>(k8), static_cast<uint32_t>(k8 >> 32)};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) keep[e] = (2 * e < nv ? 0x0000FFFFu : 0u) | (2 * e + 1 < nv ? 0xFFFF0000u : 0u);
+    }
+    auto* x = reinterpret_cast<DMS_LDS u32x4*>(tile + D * (FP8 ? 32 : 64) + P * 16);
+    *x = *x & keep;
+  }
 }
 
 constexpr int kAhead = 4;   // products between an operand's LDS read and its use
@@ -577,10 +596,10 @@ __device__ __forceinline__ void odd_values(Columns<D>& c, const u32x4 (&pu)[2], 
 // and the products with the values.  keys_done() once nothing but the values (and,
 // for 8-bit pages, the values' scales) is read any more, values_ready() before
 // those are.
-template <int D, bool FP8, int TPS, class KeysDone, class ValuesReady>
+template <int D, bool FP8, int TPS, bool CAREFUL, class KeysDone, class ValuesReady>
 __device__ __forceinline__ void attend_tiles(const TreeArgs& a, const Segment& sg, Columns<D>& c, const uint32_t (&tile)[TPS],
-                                             const uint32_t (&meta)[TPS], int t, const LaneAt& at, bool careful, int lane,
-                                             KeysDone keys_done, ValuesReady values_ready) {
+                                             const uint32_t (&meta)[TPS], int t, const LaneAt& at, int lane, KeysDone keys_done,
+                                             ValuesReady values_ready) {
   constexpr int OB = D / 32;
   const int hf = lane >> 5;
   const float sl2 = a.scale_log2, thr = kRescale / sl2;
@@ -588,15 +607,13 @@ __device__ __forceinline__ void attend_tiles(const TreeArgs& a, const Segment& s
   f32x16 s[TPS];
   tile_scores<D, FP8, TPS>(c, s, tile, at);
   keys_done();
-  if (careful) values_ready();
+  if (CAREFUL) values_ready();
   TileMask k[TPS];
   uint32_t vis[TPS];
-  bool partial = false;
 #pragma unroll
   for (int x = 0; x < TPS; ++x) {
-    k[x] = tile_mask<D, FP8>(a, sg, meta[x], tile[x], t + x, careful, lane);
+    k[x] = tile_mask<D, FP8, CAREFUL>(a, sg, meta[x], tile[x], t + x, lane);
     vis[x] = ~0u;
-    partial |= (k[x].alive & ~k[x].odd) != ~0u;
     if (k[x].masked) {
       vis[x] = k[x].alive;
       if (k[x].tree && k[x].alive) vis[x] &= c.anc[t + x - sg.nc];
@@ -646,8 +663,8 @@ __device__ __forceinline__ void attend_tiles(const TreeArgs& a, const Segment& s
   };
 #pragma unroll
   for (int j = 0; j < 8; ++j) weight_pair(0, j);
-  if (!careful) values_ready();
-  if (partial) {
+  if (!CAREFUL) values_ready();
+  if constexpr (CAREFUL) {
 #pragma unroll
     for (int x = 0; x < TPS; ++x) {
       if (x > 0)
@@ -779,7 +796,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
         for (int i = 0; i < 16; ++i) c.o[b][i] = 0.f;
     };
 
-    for (int careful = 0; careful < 2; ++careful) {
+    auto attend = [&](auto careful_c) {
+      constexpr bool CAREFUL = decltype(careful_c)::value;
       if constexpr (Sh::PRIVATE) {
         constexpr int R = Sh::R, KC = (FP8 ? D / 32 + 1 : D / 16) + 1, VC = FP8 ? D / 32 : D / 16;
         // keys of own tile u (with the rows' owners; 8-bit pages: the scales too) and its values
@@ -817,7 +835,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
           const uint32_t meta[1] = {meta_lds[slot][lane & 31]};
           const bool more = u + R < n;
           const char* next = source(sg.t0 + kw + (u + R) * KW, page);
-          attend_tiles<D, FP8, 1>(a, sg, c, tile, meta, t, at, careful, lane,
+          attend_tiles<D, FP8, 1, CAREFUL>(a, sg, c, tile, meta, t, at, lane,
               [&]() {
                 // 8-bit pages: the scales lie in the keys' copies and are read for the weights
                 if constexpr (!FP8) {
@@ -829,6 +847,10 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
                 if (more) wait_copies_but<(R - 1) * (KC + VC) + (FP8 ? 0 : KC)>();
                 else wait_copies();
                 asm volatile("" ::: "memory");
+                if (t == sg.nc - 1 && (sg.L & 31)) {
+                  zero_values<D, FP8>(tile[0], sg.L & 31, fresh(lane), 64);
+                  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                }
               });
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           if (more) {
@@ -869,6 +891,11 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
           else wait_copies();
           __syncthreads();     // the stage is there, and no wave reads the one before it
           if (st + S - 1 < ns) copy_stage(st + S - 1, page);
+          const int last = sg.nc - 1 - (sg.t0 + st * kTiles);
+          if ((sg.L & 31) && last >= 0 && last < kTiles && sg.nc - 1 < sg.t1) {
+            zero_values<D, FP8>(lds0 + Sh::slot_at(st % S * kTiles + last), sg.L & 31, fresh(tid), 64 * NW);
+            __syncthreads();
+          }
           const int t = sg.t0 + st * kTiles + kw * TPS, slot = st % S * kTiles + kw * TPS;
           if (busy && t < sg.t1) {
             uint32_t tile[TPS], meta[TPS];
@@ -877,19 +904,19 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
               tile[x] = lds0 + Sh::slot_at(slot + x);
               meta[x] = meta_lds[slot + x][lane & 31];
             }
-            attend_tiles<D, FP8, TPS>(a, sg, c, tile, meta, t, at, careful, lane, []() {}, []() {});
+            attend_tiles<D, FP8, TPS, CAREFUL>(a, sg, c, tile, meta, t, at, lane, []() {}, []() {});
           }
           page = stage_page(st + S);
         }
       }
-      if (careful) break;
-      float z = 0.f;
+    };
+    attend(std::false_type{});
+    float z = 0.f;
 #pragma unroll
-      for (int b = 0; b < OB; ++b)
+    for (int b = 0; b < OB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) z = fmaf(c.o[b][i], 0.f, z);
-      if (!__syncthreads_or(z != 0.f)) break;    // (tiles are read)
-    }
+      for (int i = 0; i < 16; ++i) z = fmaf(c.o[b][i], 0.f, z);
+    if (__syncthreads_or(z != 0.f)) attend(std::true_type{});    // (tiles are read)
 
     // ---- fold the waves of a column block and write it: the outputs of a whole
     // head, else a partial (slot 2 w: a head that began before this part; 2 w + 1:
