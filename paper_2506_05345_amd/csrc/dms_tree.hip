@@ -508,7 +508,8 @@ __device__ __forceinline__ TileMask tile_mask(const TreeArgs& a, const Segment& 
   return k;
 }
 
-// Zeroes the values of rows `valid` on of a tile in LDS; threads t, t + n, ..
+// Zeroes the values (8-bit pages: and their scales) of rows `valid` on of a tile in
+// LDS; threads t, t + n, ..
 template <int D, bool FP8>
 __device__ inline void zero_values(uint32_t tile, int valid, int t, int n) {
   for (int P = t; P < D * (FP8 ? 2 : 4); P += n) {
@@ -525,6 +526,7 @@ __device__ inline void zero_values(uint32_t tile, int valid, int t, int n) {
     auto* x = reinterpret_cast<DMS_LDS u32x4*>(tile + D * (FP8 ? 32 : 64) + P * 16);
     *x = *x & keep;
   }
+  if (FP8 && t >= valid && t < 32) *reinterpret_cast<DMS_LDS float*>(tile + static_cast<uint32_t>(fp8_vs_off(t, D))) = 0.f;
 }
 
 constexpr int kAhead = 4;   // products between an operand's LDS read and its use
@@ -893,7 +895,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
           if (st + S - 1 < ns) copy_stage(st + S - 1, page);
           const int last = sg.nc - 1 - (sg.t0 + st * kTiles);
           if ((sg.L & 31) && last >= 0 && last < kTiles && sg.nc - 1 < sg.t1) {
-            zero_values<D, FP8>(lds0 + Sh::slot_at(st % S * kTiles + last), sg.L & 31, fresh(tid), 64 * NW);
+            for (int x = last; x < kTiles; ++x)    // (past the end: the last tile again)
+              if (x == last || sg.nc == sg.t1) zero_values<D, FP8>(lds0 + Sh::slot_at(st % S * kTiles + x), sg.L & 31, fresh(tid), 64 * NW);
             __syncthreads();
           }
           const int t = sg.t0 + st * kTiles + kw * TPS, slot = st % S * kTiles + kw * TPS;

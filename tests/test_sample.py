@@ -189,3 +189,53 @@ def test_log_probabilities_may_be_left_out_and_streams_differ():
     dms.dms_sample(c, 5, logits, None, None, None, None, ud, tokens, None, ws, stream=stream)
     torch.cuda.synchronize()
     assert np.array_equal(tokens.cpu().numpy(), a[1])
+
+
+@pytest.mark.parametrize("vocab", [257, 4500])
+def test_more_rows_than_run_at_once(vocab):
+    rng = np.random.default_rng(9)
+    rows = 1030
+    x = (rng.normal(size=(rows, vocab)) * 2).astype(np.float32)
+    T, k, p, m = mixed(rng, rows)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
+
+
+@pytest.mark.parametrize("vocab,values", [(4097, 1), (9000, 3), (50001, 7)])
+def test_few_distinct_logits(vocab, values):
+    """Thousands of equal logits at every border."""
+    rng = np.random.default_rng(vocab)
+    rows = 24
+    x = rng.choice(np.linspace(-1.0, 1.0, values), (rows, vocab)).astype(np.float32)
+    T, _, p, m = mixed(rng, rows)
+    k = rng.choice([0, 1, vocab // 3, vocab - 1, vocab, 3500], rows)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
+
+
+def test_many_kept_tokens_at_low_temperatures():
+    rng = np.random.default_rng(10)
+    rows, vocab = 12, 30000
+    x = (rng.normal(size=(rows, vocab)) * 3).astype(np.float32)
+    T = np.array([0.02, 0.05, 0.1, 0.2] * 3)
+    k, p = np.array([1000] * 6 + [0] * 3 + [20000] * 3), np.array([0.95, 0.999999, 1.0] * 4)
+    m = np.zeros(rows)
+    u = (1 - 2.0 ** -rng.integers(1, 25, rows)).astype(np.float32)
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
+
+
+def test_numbers_at_the_borders_of_equal_tokens():
+    """2^k equal tokens: token j from u = j 2^-k on."""
+    rows = 64
+    x = np.full((rows, 64), -np.inf, np.float32)
+    x[:, ::2] = 1.5
+    u = (np.arange(rows) / 64).astype(np.float32)
+    _, tokens, logp = run(x, u=u)
+    assert np.array_equal(tokens, 2 * (np.arange(rows) // 2))
+    assert np.allclose(logp, -np.log(32), atol=1e-6)
+    below = np.nextafter(u[2:], np.float32(0))
+    _, tokens, _ = run(x[2:], u=below)
+    assert np.array_equal(tokens, 2 * (np.ceil(u[2:] * 32).astype(int) - 1))

@@ -474,3 +474,18 @@ def test_refused_commits_change_nothing(how):
     for name in ("pos", "L", "ring_slot", "ring_flag", "page_table", "slot_pos", "slot_flag", "stack"):
         assert np.array_equal(getattr(before, name), getattr(after, name)), name
     assert before.top == after.top and np.array_equal(pool, pool_words(c))
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("byte", [0xFF, 0x7F, 0x00])
+def test_slots_past_the_live_length_hold_anything(kv, byte):
+    """A pool that held other bytes before its slots were written (0xFF and 0x7F: NaN keys, values and scales)."""
+    import torch
+    for lens, nodes, g in (([5, 40], [3, 9], 2), ([333], [40], 2), ([33, 95], [70, 5], 4), ([0, 500], [1, 100], 2),
+                           ([45, 100], [20, 5], 3)):
+        c = Call(41, lens, nodes, 2, g, 128, 16, 64, kv)
+        c.cache.pools[0].view(torch.uint8).fill_(byte)
+        c.dms.dms_init_state(c.cache.ctx)
+        c.dms.dms_append_chunk(c.cache.ctx, 0, c.n, dev(c.ids), dev(c.cu_ctx), sum(lens), max(lens), dev(c.k0, "bf16"),
+                               dev(c.v0, "bf16"), dev(c.f0))
+        c.check(c.attend())
