@@ -9,15 +9,19 @@
 //
 // Rows of more than kSmallVocab logits are cut into parts, so that few rows fill the
 // chip too, and take four launches:
-//   sample_max_kernel   the parts' largest values (reads the logits from memory;
-//                       the passes after it find them in the caches);
-//   sample_hist_kernel  the parts' weights, and each row's counts and weights by
-//                       distance from its largest value (bins of 1/32 octave of weight);
-//   sample_cut_kernel   from those the bins that hold the borders of top-k and
-//                       top-p: the weights ahead of them by part, and their tokens
-//                       listed;
-//   sample_pick_kernel  a workgroup a row sorts the listed tokens, cuts them, finds the
-//                       part that holds the picked token and walks it.
+//   sample_max_kernel   the largest values of the parts and of up to 2048 groups of a
+//                       row's tokens (reads the logits from memory; the passes after
+//                       it find them in the caches);
+//   sample_hist_kernel  top-k of at most half the groups: the k-th largest of the
+//                       groups' values, which k tokens reach.  Else the parts' weights,
+//                       and each row's counts and weights by distance from its largest
+//                       value (bins of 1/32 octave of weight);
+//   sample_cut_kernel   lists the tokens that reach that value, or those of the bins
+//                       that hold the borders of top-k and top-p, with the weights
+//                       ahead of them by part;
+//   sample_pick_kernel  a workgroup a row sorts the listed tokens, cuts them, and finds
+//                       the picked one: among them, if few are kept and all are
+//                       listed, else in the part that holds it, by walking that.
 // A row whose borders' bins hold too many tokens (many equal logits) is done by the
 // last launch alone, as shorter rows are (sample_row).
 #include <math.h>
@@ -128,7 +132,7 @@ __device__ inline u64 weight(float x, float top, double c) {
 // are found by their keys' digits (11, 11 and 10 bits), from the counts and
 // weights of each digit's values.
 // ---------------------------------------------------------------------------
-constexpr int kRowThreads = 1024, kWaves = kRowThreads / 64, kBins = 2048;
+constexpr int kRowThreads = 512, kWaves = kRowThreads / 64, kBins = 2048;
 
 struct RowLds {
   u64 mass[kBins];
@@ -180,12 +184,15 @@ __device__ Border find_border(const SampleArgs& a, const void* row, float top, d
       atomicAdd(&s.count[(key >> kShift[level]) & digits], 1u);
     }
     __syncthreads();
-    // thread t: the two bins 2047 - 2 t, 2046 - 2 t, in falling order
-    const int b0 = kBins - 1 - 2 * tid;
-    const uint32_t n0 = s.count[b0], n1 = s.count[b0 - 1];
-    const u64 m0 = s.mass[b0], m1 = s.mass[b0 - 1];
-    uint32_t n = n0 + n1;
-    u64 m = m0 + m1;
+    // thread t: bins 2047 - BINS t, .. in falling order
+    constexpr int BINS = kBins / kRowThreads;
+    const int b0 = kBins - 1 - BINS * tid;
+    uint32_t nb[BINS], num = 0;
+    u64 mb[BINS], sum = 0;
+#pragma unroll
+    for (int x = 0; x < BINS; ++x) num += nb[x] = s.count[b0 - x], sum += mb[x] = s.mass[b0 - x];
+    uint32_t n = num;
+    u64 m = sum;
     for (int off = 1; off < 64; off <<= 1) {
       const uint32_t un = __shfl_up(n, off, 64);
       const u64 um = __shfl_up(m, off, 64);
@@ -193,17 +200,23 @@ __device__ Border find_border(const SampleArgs& a, const void* row, float top, d
     }
     if (lane == 63) s.wave_count[wave] = n, s.wave_mass[wave] = m;
     __syncthreads();
-    uint32_t en = n - n0 - n1 + above_count;
-    u64 em = m - m0 - m1 + above_mass;
+    uint32_t en = n - num + above_count;
+    u64 em = m - sum + above_mass;
     for (int x = 0; x < wave; ++x) en += s.wave_count[x], em += s.wave_mass[x];
     // the first bin whose end reaches the border
-    auto reached = [&](uint32_t cn, u64 cm) { return by_mass ? static_cast<double>(cm) >= least : cn >= want; };
-    const bool r_before = reached(en, em) && en > 0;
-    const bool r0 = reached(en + n0, em + m0) && en + n0 > 0, r1 = reached(en + n0 + n1, em + m0 + m1) && en + n0 + n1 > 0;
-    if (!r_before && (r0 || r1)) {
-      s.digit = r0 ? b0 : b0 - 1;
-      s.above_count = r0 ? en : en + n0;
-      s.above_mass = r0 ? em : em + m0;
+    auto reached = [&](uint32_t cn, u64 cm) { return cn > 0 && (by_mass ? static_cast<double>(cm) >= least : cn >= want); };
+    bool before = reached(en, em);
+#pragma unroll
+    for (int x = 0; x < BINS; ++x) {
+      const bool now = reached(en + nb[x], em + mb[x]);
+      if (!before && now) {
+        s.digit = b0 - x;
+        s.above_count = en;
+        s.above_mass = em;
+      }
+      before = now;
+      en += nb[x];
+      em += mb[x];
     }
     __syncthreads();
     prefix |= s.digit << kShift[level];
@@ -369,21 +382,33 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleArgs a) {
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64;
 constexpr int kMaxParts = 256;                            // parts of a row, a wave each
 // Bins: 32 an octave over 20 octaves, then 4 over 25.  A row with top-p and no top-k
-// fills the first ones alone: a border past them is left to sample_row, and the rest of
-// the row, most of it, needs no atomics (128 x 152064, T = 0.6: the pass takes 35.6 us
-// with them, 30.6 without).
+// fills the weights of the first ones alone: a border past them is left to sample_row,
+// and the rest of the row, most of it, needs no atomics (128 x 152064, T = 0.6: the pass
+// took 35.6 us with them, 30.6 without).
 constexpr int kFine = 20 * 32, kHist = kFine + 25 * 4;
 constexpr int kListed = 2048;                             // tokens that a row lists at most
+constexpr int kFew = 256;     // kept tokens among which the picked one is found by sorting them by index
+constexpr int kGroups = 2048;                             // groups whose largest values a row keeps at most
 
 // What the launches of a row leave each other.
-struct RowState {
+struct alignas(16) RowState {
   u64 mass[kHist];            // weights by bin
   u64 part_mass[kMaxParts], part_kept[kMaxParts];
   u64 list[kListed];          // key << 32 | ~index of the tokens in the borders' bins
   uint32_t count[kHist];
   uint32_t part_top[kMaxParts];
+  uint32_t group_top[kGroups];
   uint32_t listed;
+  uint32_t near;              // key that at least top-k tokens reach (Asked::near)
 };
+
+// Groups of a part: a power of two, of the part's 256 pairs of a lane and a place in its
+// fours.
+__host__ __device__ inline int groups_of_part(int parts) {
+  int n = 256;
+  while (n * parts > kGroups) n >>= 1;
+  return n;
+}
 
 // The parts of a row: 16-byte groups of logits in equal shares; what lies before the
 // first aligned group belongs to the first part, what is left to the last.
@@ -465,13 +490,23 @@ __global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) 
   const int lane = threadIdx.x & 63;
   for (int x = me.s * 64 + lane; x < kHist; x += a.parts * 64) st.mass[x] = 0, st.count[x] = 0;
   if (me.s == 0 && lane == 0) st.listed = 0;
-  uint32_t key = kKeyNone;
+  uint32_t key[4] = {kKeyNone, kKeyNone, kKeyNone, kKeyNone};
   Parts<BF16>(a, me.r).each(me.s, [&](int, const float (&x)[4], int) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) key = max(key, order_key(x[e]));
+    for (int e = 0; e < 4; ++e) key[e] = max(key[e], order_key(x[e]));
   });
-  key = wave_max32(key);
-  if (lane == 0) st.part_top[me.s] = key;
+  const int groups = groups_of_part(a.parts);
+  uint32_t* group_top = st.group_top + me.s * groups;
+  if (groups == 256) *reinterpret_cast<uint4*>(group_top + 4 * lane) = make_uint4(key[0], key[1], key[2], key[3]);
+  key[0] = max(key[0], key[1]);
+  key[2] = max(key[2], key[3]);
+  if (groups == 128) *reinterpret_cast<uint2*>(group_top + 2 * lane) = make_uint2(key[0], key[2]);
+  uint32_t top = max(key[0], key[2]);
+  for (int off = 32, n = 64; off; off >>= 1, n >>= 1) {     // n groups: lanes alike in their low bits
+    if (n == groups && lane < n) group_top[lane] = top;
+    top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off, 64)));
+  }
+  if (lane == 0) st.part_top[me.s] = top;
 }
 
 // What a workgroup of THREADS reads of a row's state, in one round of loads: the
@@ -522,15 +557,44 @@ __device__ inline float bin_edge(int b) {
   return b <= kFine ? static_cast<float>(b) * (1.0f / 32.f) : 20.f + static_cast<float>(b - kFine) * 0.25f;
 }
 
-// What a row asks of its passes: weights of its bins (top-p), of its parts (no cut by
-// rank or weight at all), counts (top-k).
+// What a row asks of its passes: nothing but the groups (near: then every kept token is
+// listed), weights of its bins (top-p), of its parts (no cut by rank or weight at all),
+// counts (top-k).  Near: half the groups' values are reached by 1.4 tokens to a group
+// where tokens are spread over the groups at random, so that the list holds them.
 struct Asked {
-  bool by_k, by_p, least;
-  __device__ Asked(const SampleArgs& a, const RowSetting& s) : by_k(s.k < a.vocab), by_p(s.p < 1.0), least(s.least > 0.0) {}
-  __device__ bool weights() const { return by_p || !(by_k || least); }
-  __device__ bool bins() const { return by_k || by_p; }
+  bool by_k, by_p, least, near;
+  __device__ Asked(const SampleArgs& a, const RowSetting& s)
+      : by_k(s.k < a.vocab), by_p(s.p < 1.0), least(s.least > 0.0), near(by_k && 2 * s.k <= a.parts * groups_of_part(a.parts)) {}
+  __device__ bool weights() const { return !near && (by_p || !(by_k || least)); }
+  __device__ bool bins() const { return !near && (by_k || by_p); }
   __device__ bool whole() const { return !(by_k || by_p || least); }
 };
+
+// A key that at least k of the groups' largest values reach: the k-th largest one's upper
+// 16 bits (bf16 logits: all of it).  By the whole workgroup.
+__device__ uint32_t near_key(const SampleArgs& a, const RowState& st, int k) {
+  constexpr int PER = kGroups / kPartThreads;
+  __shared__ int counts[16][kPartWaves];
+  const int tid = threadIdx.x, n = a.parts * groups_of_part(a.parts);
+  uint32_t keys[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) keys[u] = tid + u * kPartThreads < n ? st.group_top[tid + u * kPartThreads] : 0u;
+  uint32_t found = 0;
+#pragma unroll 1
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t at_least = found | 0x10000u << bit;
+    int reached = 0;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) reached += __builtin_popcountll(__builtin_amdgcn_ballot_w64(keys[u] >= at_least));
+    if ((tid & 63) == 0) counts[bit][tid >> 6] = reached;
+    __syncthreads();
+    reached = 0;
+#pragma unroll
+    for (int x = 0; x < kPartWaves; ++x) reached += counts[bit][x];
+    if (reached >= k) found = at_least;
+  }
+  return found;
+}
 
 template <bool BF16>
 __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a) {
@@ -541,8 +605,15 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
   RowState& st = a.state[me.r];
   const RowSetting set = row_setting(a, me.r);
   const Asked ask(a, set);
+  if (ask.near) {
+    if (blockIdx.x % (a.parts / kPartWaves) != 0) return;
+    const uint32_t near = near_key(a, st, set.k);
+    if (tid == 0) st.near = near;
+    return;
+  }
+  if (!(ask.weights() || ask.bins())) return;
   const uint32_t key = RowView<kPartThreads>(a, st, false).key;
-  if (key == kKeyNone || !(ask.weights() || ask.bins())) return;
+  if (key == kKeyNone) return;
   if (ask.bins()) {
     for (int x = tid; x < kHist; x += kPartThreads) mass[x] = 0, count[x] = 0;
     __syncthreads();
@@ -551,7 +622,8 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
   const Parts<BF16> parts(a, me.r);
   if (ask.weights()) {
     u64 sum = 0;
-    const float most = ask.by_k ? 45.f : 20.f;
+    const bool by_k = ask.by_k;
+    const float most = by_k ? 45.f : 20.f;
     parts.each(me.s, [&](int, const float (&x)[4], int) {
       u64 w[4];
 #pragma unroll
@@ -565,7 +637,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
           if (z < most) {
             const int b = bin_of(z);
             atomicAdd(&mass[b], w[e]);
-            atomicAdd(&count[b], 1u);
+            if (by_k) atomicAdd(&count[b], 1u);
           }
         }
     });
@@ -582,17 +654,16 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
   }
   if (ask.bins()) {
     __syncthreads();
-    for (int x = tid; x < kHist; x += kPartThreads)
-      if (count[x]) {
-        if (ask.by_p) atomicAdd(&st.mass[x], mass[x]);
-        atomicAdd(&st.count[x], count[x]);
-      }
+    for (int x = tid; x < kHist; x += kPartThreads) {
+      if (mass[x]) atomicAdd(&st.mass[x], mass[x]);
+      if (count[x]) atomicAdd(&st.count[x], count[x]);
+    }
   }
 }
 
 // Which bins hold a row's borders.
 struct Cut {
-  bool none, slow;     // nothing to cut by rank or weight; the row is left to sample_row
+  bool none, slow;     // nothing to cut by bins; the row is left to sample_row
   int from, to;        // bins whose tokens are listed; those before are kept
   uint32_t ahead;      // tokens and weight before `from`
   u64 ahead_mass, all; // weight of the row
@@ -612,7 +683,7 @@ __device__ Cut find_cut(const RowView<THREADS>& v, const RowSetting& set, const 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   Cut cut{};
   cut.none = !ask.bins();
-  if (cut.none) return cut;
+  if (cut.none) return cut;     // (near: what is listed is known already)
   cut.all = v.all;
   const u64 (&m)[PER] = v.m;
   const uint32_t (&n)[PER] = v.n;
@@ -668,15 +739,14 @@ __device__ Cut find_cut(const RowView<THREADS>& v, const RowSetting& set, const 
     // what top-k leaves weighs between the bins before its border and those with it
     const double low = set.p * static_cast<double>(by_k ? l.k_before : cut.all);
     const double high = set.p * static_cast<double>(by_k ? l.k_with : cut.all);
+    // (the largest logit's weight lies in the first bin)
     u64 x = before;
-    uint32_t y = ahead;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      const bool was_low = y > 0 && static_cast<double>(x) >= low, was_high = y > 0 && static_cast<double>(x) >= high;
+      const bool was_low = x > 0 && static_cast<double>(x) >= low, was_high = x > 0 && static_cast<double>(x) >= high;
       x += m[u];
-      y += n[u];
-      if (!was_low && y > 0 && static_cast<double>(x) >= low) l.p_low = tid * PER + u;
-      if (!was_high && y > 0 && static_cast<double>(x) >= high) l.p_high = tid * PER + u;
+      if (!was_low && x > 0 && static_cast<double>(x) >= low) l.p_low = tid * PER + u;
+      if (!was_high && x > 0 && static_cast<double>(x) >= high) l.p_high = tid * PER + u;
     }
     __syncthreads();
     if (l.p_high == kHist || l.p_low == kHist) {
@@ -701,7 +771,14 @@ __device__ Cut find_cut(const RowView<THREADS>& v, const RowSetting& set, const 
   __syncthreads();
   cut.ahead = l.ahead;
   cut.ahead_mass = l.ahead_mass;
-  cut.slow = l.through - l.ahead > kListed;
+  // the tokens ahead weigh more than 2^43 2^-(where bin `from` begins) each: few of
+  // them are listed too
+  if (ask.by_p && static_cast<double>(cut.ahead_mass) * exp2f(bin_edge(cut.from) - 43.f) < 2.0 * kFew) {
+    cut.from = 0;
+    cut.ahead = 0;
+    cut.ahead_mass = 0;
+  }
+  cut.slow = l.through - cut.ahead > kListed;      // (without top-k: known when they are listed)
   return cut;
 }
 
@@ -724,6 +801,20 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
   // out; no token past `far` passes min-p (and none past 45 octaves has a weight)
   const float far = ask.least ? 43.01f - log2f(static_cast<float>(set.least)) : 45.f;
   const float keep = cut.none ? 64.f : bin_edge(cut.from), end = cut.none ? far : bin_edge(cut.to + 1);
+  auto list = [&](float x, int i) {
+    const uint32_t at = atomicAdd(&st.listed, 1u);
+    if (at < kListed) st.list[at] = static_cast<u64>(order_key(x)) << 32 | ~static_cast<uint32_t>(i);
+  };
+  if (ask.near) {
+    const float least = key_value(max(st.near, kKeyNone));
+    Parts<BF16>(a, me.r).each(me.s, [&](int i, const float (&x)[4], int n) {
+      if (!(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= least)) return;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (x[e] >= least && octaves(x[e], top, c) < 45.f && e < n) list(x[e], i + e);
+    });
+    return;
+  }
   u64 sum = 0;
   Parts<BF16>(a, me.r).each(me.s, [&](int i, const float (&x)[4], int n) {
     const float nearest = octaves(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), top, c);
@@ -736,8 +827,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
       if (z < keep) {
         sum += static_cast<double>(w) >= set.least ? w : 0ull;
       } else if (w && e < n) {
-        const uint32_t at = atomicAdd(&st.listed, 1u);
-        if (at < kListed) st.list[at] = static_cast<u64>(order_key(x[e])) << 32 | ~static_cast<uint32_t>(i + e);
+        list(x[e], i + e);
       }
     }
   });
@@ -754,32 +844,36 @@ struct PickLds {
   int last, part, k_last;
 };
 
-// Sorts the n tokens of l.list[0], largest first; returns which of the two lists holds
-// them.  Up to 1024 every thread counts those ahead of its own; more take a bitonic
-// network (1024 tokens: 55 barriers against one).
-__device__ int sort_listed(PickLds& l, int n) {
-  const int tid = threadIdx.x;
-  if (n <= kRowThreads) {
-    if (tid < n) {
-      const u64 mine = l.list[0][tid];
-      int rank = 0;
+// Sorts the n different numbers of l.list[0], largest first, into it: waves sort chunks
+// of 64 by counting those ahead of each, and a number's place is the sum of its places in
+// all chunks, each found by halving.  l.list[1] holds the chunks in between.
+__device__ void sort_listed(PickLds& l, int n) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, chunks = (n + 63) / 64;
+  for (int c = wave; c < chunks; c += kWaves) {
+    const u64* of = l.list[0] + 64 * c;
+    const u64 mine = 64 * c + lane < n ? of[lane] : 0;
+    const int there = min(64, n - 64 * c);
+    int rank = 0;
 #pragma unroll 8
-      for (int x = 0; x < n; ++x) rank += l.list[0][x] > mine;
-      l.list[1][rank] = mine;
-    }
-    __syncthreads();
-    return 1;
+    for (int x = 0; x < there; ++x) rank += of[x] > mine;
+    l.list[1][64 * c + (lane < there ? rank : lane)] = mine;
   }
-  for (int x = n + tid; x < kListed; x += kRowThreads) l.list[0][x] = 0;
   __syncthreads();
-  for (int span = 2; span <= kListed; span *= 2)
-    for (int step = span / 2; step; step /= 2) {
-      const int i = 2 * tid - (tid & (step - 1)), j = i + step;   // the pairs of this step
-      const u64 p = l.list[0][i], q = l.list[0][j];
-      if ((p < q) == ((i & span) == 0)) l.list[0][i] = q, l.list[0][j] = p;
-      __syncthreads();
+  for (int x = tid; x < n; x += kRowThreads) {
+    const u64 mine = l.list[1][x];
+    int rank = x & 63;
+#pragma unroll 4
+    for (int c = 0; c < chunks; ++c) {
+      const u64* of = l.list[1] + 64 * c;
+      int p = 0;
+#pragma unroll
+      for (int step = 32; step; step >>= 1) p += of[p + step - 1] > mine ? step : 0;
+      p += of[p] > mine;
+      rank += c == x >> 6 ? 0 : p;
     }
-  return 0;
+    l.list[0][rank] = mine;
+  }
+  __syncthreads();
 }
 
 template <bool BF16>
@@ -795,7 +889,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
   const Asked ask(a, set);
   const RowView<kRowThreads> view(a, st, ask.bins());
   const u64 mine = tid < a.parts ? (ask.whole() ? st.part_mass[tid] : st.part_kept[tid]) : 0;
-  const int n = min(static_cast<int>(st.listed), kListed);
+  const uint32_t listed = st.listed;
+  const int n = min(listed, static_cast<uint32_t>(kListed));
   const uint32_t key = view.key;
   if (key == kKeyNone) {      // no token is left
     if (tid == 0) {
@@ -805,24 +900,35 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
     return;
   }
   const Cut cut = find_cut(view, set, ask, l.cut);
-  if (cut.slow) {
+  if (cut.slow || listed > kListed) {
     __syncthreads();
     sample_row<BF16>(a, r, lds.row);
     return;
   }
   const float top = key_value(key);
   const Parts<BF16> parts(a, r);
-  if (tid < kMaxParts) l.mass[tid] = mine;
+  auto picked = [&](int i, u64 total) {
+    a.tokens[r] = i;
+    if (a.logprobs)
+      a.logprobs[r] = static_cast<float>((static_cast<double>(logit<BF16>(parts.row, i)) - static_cast<double>(top)) / set.t -
+                                         log(static_cast<double>(total) * 0x1p-43));
+  };
+  if (tid < kMaxParts) l.mass[tid] = ask.near ? 0 : mine;
   u64 border = 0;              // the last kept token of the listed ones, as the list holds it
-  if (!cut.none) {
+  if (ask.near || !cut.none) {
     for (int x = tid; x < n; x += kRowThreads) l.list[0][x] = st.list[x];
     __syncthreads();
-    const u64* list = l.list[sort_listed(l, n)];
-    // ---- running weights: thread t holds tokens 2 t and 2 t + 1
-    const int x0 = 2 * tid;
-    const u64 w0 = x0 < n ? weight(key_value(static_cast<uint32_t>(list[x0] >> 32)), top, set.c) : 0;
-    const u64 w1 = x0 + 1 < n ? weight(key_value(static_cast<uint32_t>(list[x0 + 1] >> 32)), top, set.c) : 0;
-    u64 run = w0 + w1;
+    sort_listed(l, n);
+    const u64* list = l.list[0];
+    // ---- running weights: thread t holds PER tokens from PER t on
+    constexpr int PER = kListed / kRowThreads;
+    const int x0 = PER * tid;
+    u64 w[PER], sum = 0;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) w[x] = x0 + x < n ? weight(key_value(static_cast<uint32_t>(list[x0 + x] >> 32)), top, set.c) : 0;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) sum += w[x];
+    u64 run = sum;
     for (int off = 1; off < 64; off <<= 1) {
       const u64 up = __shfl_up(run, off, 64);
       if (lane >= off) run += up;
@@ -831,28 +937,70 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
     if (tid == 0) l.last = n - 1, l.k_last = n - 1, l.k_mass = cut.all;
     __syncthreads();
     for (int x = 0; x < wave; ++x) run += l.wave_mass[x];
-    const u64 r0 = cut.ahead_mass + run - w1, r1 = cut.ahead_mass + run;   // through token 2 t, 2 t + 1
-    const int64_t left = static_cast<int64_t>(set.k) - cut.ahead;         // listed tokens that top-k keeps
-    if (left >= 1 && left <= n && (left - 1) / 2 == tid) {
+    run += cut.ahead_mass - sum;       // ahead of the thread's tokens
+    // listed tokens that top-k keeps (near: those that are not listed have no weight)
+    const int64_t left = ask.near ? min(set.k, n) : static_cast<int64_t>(set.k) - cut.ahead;
+    if (left >= 1 && left <= n && (left - 1) / PER == tid) {
+      u64 through = run;
+#pragma unroll
+      for (int x = 0; x < PER; ++x)
+        if (x0 + x < left) through += w[x];
       l.k_last = static_cast<int>(left) - 1;
-      l.k_mass = (left - 1) % 2 ? r1 : r0;
+      l.k_mass = through;
     }
     __syncthreads();
     if (ask.by_p) {
       const double least = set.p * static_cast<double>(l.k_mass);
       // the first token at which the running weight is enough
-      const bool e0 = x0 < n && static_cast<double>(r0) >= least, e1 = x0 + 1 < n && static_cast<double>(r1) >= least;
-      const bool eb = x0 > 0 && x0 <= n && static_cast<double>(r0 - w0) >= least;
-      if (!eb && (e0 || e1)) atomicMin(&l.last, e0 ? x0 : x0 + 1);
+      bool before = x0 > 0 && static_cast<double>(run) >= least;
+      u64 through = run;
+#pragma unroll
+      for (int x = 0; x < PER; ++x) {
+        through += w[x];
+        if (!before && x0 + x < n && static_cast<double>(through) >= least) {
+          atomicMin(&l.last, x0 + x);
+          before = true;
+        }
+      }
       __syncthreads();
     }
     const int last = min(l.last, l.k_last);
     border = list[last];
+    if (last < kFew && cut.from == 0) {      // every kept token is listed: by index
+      __syncthreads();
+      const bool mine = tid <= last;
+      const u64 as_listed = mine ? list[tid] : 0;
+      u64 wk = mine ? weight(key_value(static_cast<uint32_t>(as_listed >> 32)), top, set.c) : 0;
+      if (!(static_cast<double>(wk) >= set.least)) wk = 0;
+      __syncthreads();
+      // 20 bits of index (falling), 44 of weight
+      if (mine) l.list[0][tid] = static_cast<u64>(static_cast<uint32_t>(as_listed) & 0xFFFFFu) << 44 | wk;
+      __syncthreads();
+      sort_listed(l, last + 1);
+      const u64 item = mine ? l.list[0][tid] : 0;
+      wk = item & ((1ull << 44) - 1);
+      u64 run = wk;
+      for (int off = 1; off < 64; off <<= 1) {
+        const u64 up = __shfl_up(run, off, 64);
+        if (lane >= off) run += up;
+      }
+      if (lane == 63) l.wave_mass[wave] = run;
+      __syncthreads();
+      u64 total = 0;
+      for (int x = 0; x < kFew / 64; ++x) {
+        if (x < wave) run += l.wave_mass[x];
+        total += l.wave_mass[x];
+      }
+      const u64 target = static_cast<u64>(static_cast<double>(set.u) * static_cast<double>(total));
+      if (mine && run > target && run - wk <= target)      // one thread
+        picked(static_cast<int>(~static_cast<uint32_t>(item >> 44) & 0xFFFFFu), total);
+      return;
+    }
     // ---- kept ones, to their parts
-    if (x0 <= last && static_cast<double>(w0) >= set.least)
-      atomicAdd(&l.mass[parts.holding(static_cast<int>(~static_cast<uint32_t>(list[x0])))], w0);
-    if (x0 + 1 <= last && static_cast<double>(w1) >= set.least)
-      atomicAdd(&l.mass[parts.holding(static_cast<int>(~static_cast<uint32_t>(list[x0 + 1])))], w1);
+#pragma unroll
+    for (int x = 0; x < PER; ++x)
+      if (x0 + x <= last && static_cast<double>(w[x]) >= set.least)
+        atomicAdd(&l.mass[parts.holding(static_cast<int>(~static_cast<uint32_t>(list[x0 + x])))], w[x]);
   }
   __syncthreads();
   // ---- the part that holds the picked token: lane t has parts 4 t .. 4 t + 3
@@ -920,10 +1068,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         if (at + w[u] > target) {
-          a.tokens[r] = i0 + 4 * tid + u;
-          if (a.logprobs)
-            a.logprobs[r] = static_cast<float>((static_cast<double>(x[u]) - static_cast<double>(top)) / set.t -
-                                               log(static_cast<double>(total) * 0x1p-43));
+          picked(i0 + 4 * tid + u, total);
           break;
         }
         at += w[u];
@@ -937,7 +1082,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
 // Parts of a row, a wave each: about four workgroups of four a compute unit in all, no
 // part of fewer than 512 logits.
 int row_parts(int rows, int vocab) {
-  return kPartWaves * std::max(1, std::min({kMaxParts / kPartWaves, (1024 + rows - 1) / rows, vocab / (512 * kPartWaves)}));
+  return kPartWaves * std::max(1, std::min({kMaxParts / kPartWaves, (2048 + rows - 1) / rows, vocab / (512 * kPartWaves)}));
 }
 
 }  // namespace

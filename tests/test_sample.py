@@ -239,3 +239,45 @@ def test_numbers_at_the_borders_of_equal_tokens():
     below = np.nextafter(u[2:], np.float32(0))
     _, tokens, _ = run(x[2:], u=below)
     assert np.array_equal(tokens, 2 * (np.ceil(u[2:] * 32).astype(int) - 1))
+
+
+@pytest.mark.parametrize("vocab", [4100, 20000])
+def test_top_k_past_half_the_vocabulary_and_small_nuclei(vocab):
+    rng = np.random.default_rng(vocab + 1)
+    rows = 40
+    x = (rng.normal(size=(rows, vocab)) * 3).astype(np.float32)
+    T = rng.choice([0.7, 1.0, 3.0], rows)
+    k = rng.choice([500, 1024, 1025, 2050, vocab - 5], rows)
+    p = rng.choice([1.0, 1.0, 0.5, 0.99], rows)
+    m = rng.choice([0.0, 0.0, 0.01], rows)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
+
+
+def test_few_tokens_left_by_a_mask():
+    """Rows of -inf and of the type's lowest value but for a few tokens, with cuts at, above and below their number."""
+    rng = np.random.default_rng(12)
+    rows, vocab = 48, 9001
+    x = np.full((rows, vocab), -np.inf, np.float32)
+    x[::3] = np.finfo(np.float32).min
+    x[2::3] = -1e9
+    for r in range(rows):
+        at = rng.choice(vocab, 5, replace=False)
+        x[r, at] = rng.normal(size=5)
+    k, p, m = rng.choice([0, 1, 4, 5, 6, 300, 6000], rows), rng.choice([1.0, 0.4, 0.999], rows), rng.choice([0.0, 0.3], rows)
+    T = np.ones(rows)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
+
+
+def test_sorted_logits():
+    """The largest tokens side by side."""
+    rng = np.random.default_rng(13)
+    rows, vocab = 12, 33000
+    x = -np.sort(-rng.normal(size=(rows, vocab)) * 3, axis=1).astype(np.float32)
+    k, p, m = rng.choice([20, 200, 900], rows), np.ones(rows), np.zeros(rows)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, "f32", np.ones(rows), k, p, m, u)
+    check(x, u, got, np.ones(rows), k, p, m)
