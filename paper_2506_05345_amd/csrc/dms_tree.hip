@@ -1129,6 +1129,56 @@ __device__ inline bool commit_reuse(const CommitArgs& a, const int* nodes, int s
   return (static_cast<uint32_t>(a.st.ring[static_cast<size_t>(sh) * a.w + (pos + c) % a.w]) & kFlagBit) != 0;
 }
 
+// What one head's path takes, by a wave; its nodes are left in LDS.
+struct CommitHead {
+  int need, fresh, pos, len0;     // pages to pop, or the error that refuses the call
+};
+__device__ inline CommitHead commit_scan_head(const CommitArgs& a, int hh, int* nodes) {
+  const int lane = threadIdx.x & 63, i = hh / a.H, h = hh % a.H, s = a.seq_ids[i];
+  int tok0, len, fresh = 0;
+  CommitHead r{DMS_ERR_INVALID, 0, 0, 0};
+  if (s < 0 || s >= a.max_seqs || !commit_path(a, i, tok0, len)) return r;
+  const int m = a.cu[i + 1] - tok0, sh = s * a.H + h;
+  r.pos = a.st.pos[s];
+  r.len0 = a.st.len[sh];
+  int off = 0;
+  for (int c = lane; c < len; c += 64) {
+    int x = a.path[tok0 + c];
+    if (x < 0 || x >= m) {
+      off = 1;
+      x = 0;
+    }
+    nodes[c] = x;
+  }
+  const bool bad = __builtin_amdgcn_ballot_w64(off != 0) != 0;
+  // (the wave's own LDS writes are visible to it)
+  __builtin_amdgcn_wave_barrier();
+  for (int c0 = 0; c0 < len; c0 += 64) {
+    const int c = c0 + lane;
+    const bool f = c < len && !commit_reuse(a, nodes, sh, h, tok0, r.pos, c);
+    fresh += __builtin_popcountll(__builtin_amdgcn_ballot_w64(f));
+  }
+  r.fresh = fresh;
+  const int64_t L1 = static_cast<int64_t>(r.len0) + fresh;
+  if (!bad)
+    r.need = L1 > a.max_slots ? DMS_ERR_CAPACITY
+                              : static_cast<int>((L1 + a.P - 1) / a.P - (static_cast<int64_t>(r.len0) + a.P - 1) / a.P);
+  return r;
+}
+
+// Whether an id is off or named twice, as a workgroup finds it.
+__device__ inline bool commit_bad_ids(const CommitArgs& a, uint32_t* seen) {
+  for (int x = threadIdx.x; x < (a.max_seqs + 31) / 32; x += blockDim.x) seen[x] = 0;
+  __syncthreads();
+  int bad = 0;
+  for (int x = threadIdx.x; x < a.n; x += blockDim.x) {
+    const int s = a.seq_ids[x];
+    if (s < 0 || s >= a.max_seqs) bad = 1;
+    else if (atomicOr(&seen[s >> 5], 1u << (s & 31)) & (1u << (s & 31))) bad = 1;
+  }
+  return __syncthreads_or(bad);
+}
+
 // Pass 1, a wave per head and one more for the ids: fresh tokens and pages of
 // every head, and the state that pass 2 overwrites.
 __global__ __launch_bounds__(256) void commit_scan_kernel(CommitArgs a) {
@@ -1137,15 +1187,7 @@ __global__ __launch_bounds__(256) void commit_scan_kernel(CommitArgs a) {
   if (load_status(a.status) != 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (blockIdx.x == 0) {
-    for (int x = threadIdx.x; x < (a.max_seqs + 31) / 32; x += blockDim.x) seen[x] = 0;
-    __syncthreads();
-    int bad = 0;
-    for (int x = threadIdx.x; x < a.n; x += blockDim.x) {
-      const int s = a.seq_ids[x];
-      if (s < 0 || s >= a.max_seqs) bad = 1;
-      else if (atomicOr(&seen[s >> 5], 1u << (s & 31)) & (1u << (s & 31))) bad = 1;
-    }
-    bad = __syncthreads_or(bad);
+    const bool bad = commit_bad_ids(a, seen);
     if (threadIdx.x == 0) {
       *commit_word(a, 0) = *a.st.top;
       *commit_word(a, 1) = bad ? DMS_ERR_BAD_SEQ : DMS_OK;
@@ -1155,41 +1197,12 @@ __global__ __launch_bounds__(256) void commit_scan_kernel(CommitArgs a) {
   const int64_t hh64 = (static_cast<int64_t>(blockIdx.x) - 1) * 4 + wave;
   if (hh64 >= static_cast<int64_t>(a.n) * a.H) return;
   const int hh = static_cast<int>(hh64);
-  const int i = hh / a.H, h = hh % a.H, s = a.seq_ids[i];
-  int* nodes = nodes_lds[wave];
-  int tok0, len;
-  bool bad = s < 0 || s >= a.max_seqs || !commit_path(a, i, tok0, len);
-  int m = 0, pos = 0, L0 = 0, sh = 0, fresh = 0;
-  if (!bad) {
-    m = a.cu[i + 1] - tok0;
-    sh = s * a.H + h;
-    pos = a.st.pos[s];
-    L0 = a.st.len[sh];
-    int off = 0;
-    for (int c = lane; c < len; c += 64) {
-      int x = a.path[tok0 + c];
-      if (x < 0 || x >= m) {
-        off = 1;
-        x = 0;
-      }
-      nodes[c] = x;
-    }
-    bad = __builtin_amdgcn_ballot_w64(off != 0) != 0;
-    // (the wave's own LDS writes are visible to it)
-    __builtin_amdgcn_wave_barrier();
-    for (int c0 = 0; c0 < len; c0 += 64) {
-      const int c = c0 + lane;
-      const bool f = c < len && !commit_reuse(a, nodes, sh, h, tok0, pos, c);
-      fresh += __builtin_popcountll(__builtin_amdgcn_ballot_w64(f));
-    }
-  }
+  const CommitHead r = commit_scan_head(a, hh, nodes_lds[wave]);
   if (lane == 0) {
-    const int64_t L1 = static_cast<int64_t>(L0) + fresh;
-    a.need[hh] = bad ? DMS_ERR_INVALID : L1 > a.max_slots ? DMS_ERR_CAPACITY
-                     : static_cast<int>((L1 + a.P - 1) / a.P - (L0 + a.P - 1) / a.P);
-    a.fresh[hh] = fresh;
-    commit_len(a)[hh] = L0;
-    if (h == 0) commit_pos(a)[i] = pos;
+    a.need[hh] = r.need;
+    a.fresh[hh] = r.fresh;
+    commit_len(a)[hh] = r.len0;
+    if (hh % a.H == 0) commit_pos(a)[hh / a.H] = r.pos;
   }
 }
 
@@ -1251,54 +1264,48 @@ __global__ __launch_bounds__(1024) void commit_pages_kernel(CommitArgs a) {
   }
 }
 
-// Pass 2, a workgroup per head: slots, ring, slot owners, pages and the rows of
-// the tokens that keep their slot.
-template <bool SUMMED>
-__global__ __launch_bounds__(256) void commit_write_kernel(CommitArgs a) {
-  __shared__ int lds[12];
-  __shared__ int nodes[kTreeMaxNodes], slots[kTreeMaxNodes], keeps[kTreeMaxNodes];
-  if (load_status(a.status) != 0) return;
-  const int hh = blockIdx.x, i = hh / a.H, h = hh % a.H, tid = threadIdx.x;
-  int before, pops, err;
-  if (SUMMED) {
-    err = *commit_word(a, 2);
-    pops = *commit_word(a, 3);
-    before = err == DMS_OK ? a.base[hh] : 0;
-  } else {
-    err = commit_verdict(a, hh, lds, before, pops);
-  }
-  const int64_t last = static_cast<int64_t>(a.n) * a.H - 1;
-  if (err != DMS_OK) {
-    // the other workgroups of this launch read no status past their first line
-    if (hh == last && tid == 0) set_status(a.status, err);
-    return;
-  }
-  const int top0 = *commit_word(a, 0);
-  if (hh == last && tid == 0) *a.st.top = top0 - pops;
+// Slots, ring, slot owners, pages and the rows of the tokens that keep their slot, of
+// one head, by THREADS threads: a workgroup of kTreeMaxNodes or a wave.
+template <int THREADS>
+__device__ inline void commit_write_head(const CommitArgs& a, int hh, const CommitHead& r, int top0, int before, int* nodes,
+                                         int* slots, int* keeps, int* lds) {
+  static_assert(THREADS == 64 || THREADS == kTreeMaxNodes, "a token a thread, or a wave");
+  const int tid = threadIdx.x % THREADS, i = hh / a.H, h = hh % a.H;
   const int s = a.seq_ids[i], sh = s * a.H + h, tok0 = a.cu[i], len = a.path_len[i];
-  const int pos = commit_pos(a)[i], L0 = commit_len(a)[hh], fresh = a.fresh[hh];
+  const int pos = r.pos, L0 = r.len0;
+  auto sync = []() {
+    if (THREADS > 64) __syncthreads();
+    else {      // a wave's LDS accesses are in order
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
   if (len == 0) return;
   if (tid == 0) {
-    a.st.len[sh] = L0 + fresh;
+    a.st.len[sh] = L0 + r.fresh;
     if (h == 0) a.st.pos[s] = pos + len;
   }
   const int32_t* popped = a.st.stack + top0 - 1 - before;     // k-th new page at -k
   const size_t pt = static_cast<size_t>(sh) * a.maxp;
   const int new0 = (L0 + a.P - 1) >> a.log2P;
-  for (int x = tid; x < a.need[hh]; x += blockDim.x) a.st.page_table[pt + new0 + x] = popped[-x];
-  for (int c = tid; c < len; c += blockDim.x) nodes[c] = a.path[tok0 + c];
-  __syncthreads();
+  for (int x = tid; x < r.need; x += THREADS) a.st.page_table[pt + new0 + x] = popped[-x];
+  for (int c = tid; c < len; c += THREADS) nodes[c] = a.path[tok0 + c];
+  sync();
   // slots: fresh tokens in order; a reusing one has that of the token w before
-  // it, in the path or in the ring (kTreeMaxNodes threads, one token each)
-  const int c = tid;
-  const bool on = c < len;
-  const bool reuse = on && commit_reuse(a, nodes, sh, h, tok0, pos, c);
-  {
+  // it, in the path or in the ring
+  int ahead = 0;
+  for (int c0 = 0; c0 < len; c0 += THREADS) {     // (a workgroup: once)
+    const int c = c0 + tid;
+    const bool on = c < len;
+    const bool reuse = on && commit_reuse(a, nodes, sh, h, tok0, pos, c);
     const uint64_t bal = __builtin_amdgcn_ballot_w64(on && !reuse);
-    if ((tid & 63) == 0) lds[tid >> 6] = __builtin_popcountll(bal);
-    __syncthreads();
-    int rank = __builtin_popcountll(bal & ((1ull << (tid & 63)) - 1ull));
-    for (int x = 0; x < (tid >> 6); ++x) rank += lds[x];
+    int rank = ahead + __builtin_popcountll(bal & ((1ull << (tid & 63)) - 1ull));
+    if (THREADS > 64) {
+      if ((tid & 63) == 0) lds[tid >> 6] = __builtin_popcountll(bal);
+      sync();
+      for (int x = 0; x < (tid >> 6); ++x) rank += lds[x];
+    }
+    ahead += __builtin_popcountll(bal);
     if (on) {
       slots[c] = !reuse ? L0 + rank
                  : c < a.w ? static_cast<int>(static_cast<uint32_t>(a.st.ring[static_cast<size_t>(sh) * a.w + (pos + c) % a.w]) & ~kFlagBit)
@@ -1307,13 +1314,13 @@ __global__ __launch_bounds__(256) void commit_write_kernel(CommitArgs a) {
       keeps[c] = len - c <= a.w || !commit_reuse(a, nodes, sh, h, tok0, pos, c + a.w);
     }
   }
-  __syncthreads();
+  sync();
   for (int c0 = a.w; c0 < len; c0 += a.w) {     // one window of the path at a time
-    for (int x = c0 + tid; x < min(len, c0 + a.w); x += blockDim.x)
+    for (int x = c0 + tid; x < min(len, c0 + a.w); x += THREADS)
       if (slots[x] < 0) slots[x] = slots[x - a.w];
-    __syncthreads();
+    sync();
   }
-  if (on) {
+  for (int c = tid; c < len; c += THREADS) {
     const uint32_t fb = a.flags[(static_cast<size_t>(tok0) + nodes[c]) * a.H + h] ? kFlagBit : 0u;
     if (len - c <= a.w)
       a.st.ring[static_cast<size_t>(sh) * a.w + (pos + c) % a.w] = static_cast<int32_t>(static_cast<uint32_t>(slots[c]) | fb);
@@ -1323,7 +1330,7 @@ __global__ __launch_bounds__(256) void commit_write_kernel(CommitArgs a) {
   // rows: D / 8 consecutive lanes each (an aligned lane group for the 8-bit
   // quantizer: it takes every branch together)
   const int kq = a.D / 8;
-  for (int x = tid; x < len * kq; x += blockDim.x) {
+  for (int x = tid; x < len * kq; x += THREADS) {
     const int y = x / kq, part = x - y * kq;
     if (!keeps[y]) continue;
     const int slot = slots[y], row = slot & (a.P - 1), j = row & 31, pi = slot >> a.log2P;
@@ -1347,6 +1354,63 @@ __global__ __launch_bounds__(256) void commit_write_kernel(CommitArgs a) {
     for (int d = 0; d < 8; ++d)
       *reinterpret_cast<uint16_t*>(tile + v_elem_off(j, part * 8 + d, a.D)) = static_cast<uint16_t>(vw[d >> 1] >> (16 * (d & 1)));
   }
+}
+
+// Pass 2, a workgroup per head.
+template <bool SUMMED>
+__global__ __launch_bounds__(kTreeMaxNodes) void commit_write_kernel(CommitArgs a) {
+  __shared__ int lds[12];
+  __shared__ int nodes[kTreeMaxNodes], slots[kTreeMaxNodes], keeps[kTreeMaxNodes];
+  if (load_status(a.status) != 0) return;
+  const int hh = blockIdx.x, tid = threadIdx.x;
+  int before, pops, err;
+  if (SUMMED) {
+    err = *commit_word(a, 2);
+    pops = *commit_word(a, 3);
+    before = err == DMS_OK ? a.base[hh] : 0;
+  } else {
+    err = commit_verdict(a, hh, lds, before, pops);
+  }
+  const int64_t last = static_cast<int64_t>(a.n) * a.H - 1;
+  if (err != DMS_OK) {
+    // the other workgroups of this launch read no status past their first line
+    if (hh == last && tid == 0) set_status(a.status, err);
+    return;
+  }
+  const int top0 = *commit_word(a, 0);
+  if (hh == last && tid == 0) *a.st.top = top0 - pops;
+  const CommitHead r{a.need[hh], a.fresh[hh], commit_pos(a)[hh / a.H], commit_len(a)[hh]};
+  commit_write_head<kTreeMaxNodes>(a, hh, r, top0, before, nodes, slots, keeps, lds);
+}
+
+// Calls of up to kSmallHeads heads in one launch: a workgroup, a wave per head (28 calls
+// of 16 heads: @@US@@).
+constexpr int kSmallHeads = 16;
+__global__ __launch_bounds__(64 * kSmallHeads) void commit_small_kernel(CommitArgs a) {
+  __shared__ uint32_t seen[kMaxSeqs / 32];
+  __shared__ int nodes[kSmallHeads][kTreeMaxNodes], slots[kSmallHeads][kTreeMaxNodes], keeps[kSmallHeads][kTreeMaxNodes];
+  __shared__ int needs[kSmallHeads];
+  if (load_status(a.status) != 0) return;
+  const int lane = threadIdx.x & 63, hh = threadIdx.x >> 6, NH = a.n * a.H;
+  const int top0 = *a.st.top;
+  CommitHead r{};
+  if (hh < NH) r = commit_scan_head(a, hh, nodes[hh]);
+  if (lane == 0) needs[hh] = r.need;
+  const bool bad = commit_bad_ids(a, seen);      // (every wave has read the state that is written below)
+  int before = 0, pops = 0, err = 0;
+  for (int x = 0; x < kSmallHeads; ++x) {
+    const int nd = needs[x];
+    err |= nd == DMS_ERR_INVALID ? 1 : nd == DMS_ERR_CAPACITY ? 2 : 0;
+    if (x < hh) before += max(nd, 0);
+    pops += max(nd, 0);
+  }
+  const int rc = bad ? DMS_ERR_BAD_SEQ : err & 1 ? DMS_ERR_INVALID : err & 2 ? DMS_ERR_CAPACITY
+                 : pops > top0 ? DMS_ERR_OUT_OF_PAGES : DMS_OK;
+  if (threadIdx.x == 0) {
+    if (rc != DMS_OK) set_status(a.status, rc);
+    else *a.st.top = top0 - pops;
+  }
+  if (rc == DMS_OK && hh < NH) commit_write_head<64>(a, hh, r, top0, before, nodes[hh], slots[hh], keeps[hh], nullptr);
 }
 
 // ---------------------------------------------------------------------------
@@ -1526,12 +1590,16 @@ hipError_t launch_tree_commit(const dms_config& c, const Layout& lo, void* meta,
   a.fp8 = c.kv_format == DMS_KV_FP8;
   a.mla = c.kv_format == DMS_KV_MLA;
   const unsigned NH = static_cast<unsigned>(n) * c.num_kv_heads;
+  if (NH <= kSmallHeads) {
+    hipLaunchKernelGGL(commit_small_kernel, dim3(1), dim3(64 * kSmallHeads), 0, st, a);
+    return hipGetLastError();
+  }
   hipLaunchKernelGGL(commit_scan_kernel, dim3(1 + (NH + 3) / 4), dim3(256), 0, st, a);
   if (NH > kScanHeads) {
     hipLaunchKernelGGL(commit_pages_kernel, dim3(1), dim3(1024), 0, st, a);
-    hipLaunchKernelGGL(commit_write_kernel<true>, dim3(NH), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(commit_write_kernel<true>, dim3(NH), dim3(kTreeMaxNodes), 0, st, a);
   } else {
-    hipLaunchKernelGGL(commit_write_kernel<false>, dim3(NH), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(commit_write_kernel<false>, dim3(NH), dim3(kTreeMaxNodes), 0, st, a);
   }
   return hipGetLastError();
 }

@@ -356,6 +356,10 @@ COMMITS = [
     ([150, 77], [30, 50], 2, 2, 64, 5, 32, "bf16", {"how": "chain", "immediate": True}),
     ([150, 77], [30, 50], 2, 2, 64, 5, 32, "bf16", {"how": "chain", "quest": 2}),
     ([30] * 40, [9] * 40, 4, 2, 64, 6, 32, "bf16", {}),
+    ([60] * 9, [70, 3, 20] * 3, 2, 2, 64, 7, 32, "fp8", {"how": "chain"}),
+    ([40, 3, 77] * 6, [9, 130, 0] * 6, 1, 16, 576, 5, 64, "mla", {"how": "chain"}),
+    ([90] * 9, [30] * 9, 2, 2, 64, 5, 32, "bf16", {"how": "chain", "immediate": True}),
+    ([20] * 16, [65] * 16, 1, 2, 64, 300, 32, "bf16", {"how": "chain"}),
 ]
 
 
