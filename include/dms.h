@@ -664,7 +664,8 @@ int dms_tree_attention(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_de
 
 /* dms_tree_attention with decisions read from the queries (DMS_DECIDE_QUERY
  * only); the decisions taken are also written to decisions_out_dev (uint8
- * [total_nodes, Hkv], may be NULL): the flags of the commit. */
+ * [total_nodes, Hkv], may be NULL): the flags of the commit.  (A call that device
+ * arrays which break the rules refuse may have written some.) */
 int dms_tree_attention_q(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev,
                          const int32_t* cu_nodes_dev, int total_nodes, int max_nodes,
                          const int32_t* parents_dev, const void* q_dev, const void* k_dev,

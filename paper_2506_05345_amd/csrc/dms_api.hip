@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "dms_common.h"
+#include "dms_draft.h"
 #include "dms_fp8.h"
 #include "dms_ops.h"
 #include "dms_train.h"

@@ -24,12 +24,19 @@
 //                       listed, else in the part that holds it, by walking that.
 // A row whose borders' bins hold too many tokens (many equal logits) is done by the
 // last launch alone, as shorter rows are (sample_row).
+//
+// Kernel times on one MI355X in this order: 1 x 151936 float32, T = 0.6, top-p 0.95: 3.6 +
+// 6.8 + 6.7 + 10.2 us, chains of dependent loads; 128 x 152064 of those: 14.7 (5.3 TB/s) +
+// 32.3 + 23 + 13.6; 500 x 151936 bf16, every row its own settings: 29.4 (5.2 TB/s) + 61 + 64
+// + 25.  The second pass is bound by forming weights (20 float64 instructions a token), the
+// third by the workgroups of rows that keep much of the vocabulary.  Before the groups, with
+// counts for every top-k: 106, 81 and 69 us for the last three of the 500 rows.
 #include <math.h>
 
 #include <algorithm>
 
 #include "dms_common.h"
-#include "dms_ops.h"
+#include "dms_draft.h"
 
 namespace dms {
 namespace {
@@ -132,6 +139,8 @@ __device__ inline u64 weight(float x, float top, double c) {
 // are found by their keys' digits (11, 11 and 10 bits), from the counts and
 // weights of each digit's values.
 // ---------------------------------------------------------------------------
+// 512: two to three workgroups of the last launch fit a compute unit (of 1024, one: 500
+// mixed rows 40 us against 25, one row 13.4 against 10.2).
 constexpr int kRowThreads = 512, kWaves = kRowThreads / 64, kBins = 2048;
 
 struct RowLds {
@@ -383,8 +392,8 @@ constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64;
 constexpr int kMaxParts = 256;                            // parts of a row, a wave each
 // Bins: 32 an octave over 20 octaves, then 4 over 25.  A row with top-p and no top-k
 // fills the weights of the first ones alone: a border past them is left to sample_row,
-// and the rest of the row, most of it, needs no atomics (128 x 152064, T = 0.6: the pass
-// took 35.6 us with them, 30.6 without).
+// and the rest of the row, most of it, needs no atomics (128 x 152064, T = 0.6: 35.6 us
+// with them and 30.6 without, counts of the bins included in both).
 constexpr int kFine = 20 * 32, kHist = kFine + 25 * 4;
 constexpr int kListed = 2048;                             // tokens that a row lists at most
 constexpr int kFew = 256;     // kept tokens among which the picked one is found by sorting them by index
@@ -1079,8 +1088,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
   }
 }
 
-// Parts of a row, a wave each: about four workgroups of four a compute unit in all, no
-// part of fewer than 512 logits.
+// Parts of a row, a wave each: about eight workgroups of four a compute unit in all, no
+// part of fewer than 512 logits.  (Passes two to four of 500 mixed rows with 1024, 2048 and
+// 4096 workgroups: 208, 166 and 149 us; of 128 rows alike: 71, 70 and 77.)
 int row_parts(int rows, int vocab) {
   return kPartWaves * std::max(1, std::min({kMaxParts / kPartWaves, (2048 + rows - 1) / rows, vocab / (512 * kPartWaves)}));
 }

@@ -17,16 +17,19 @@
 //   tree_prep_kernel    ancestors of every node as bits, depths, the drafted
 //                       rows as tiles in the pool's layout (8-bit pages: in
 //                       their stored form), prefix sums of the heads' tiles;
-//   tree_attn_kernel    workgroup w takes the w-th equal part of the flat list;
-//   tree_merge_kernel   joins the heads that several workgroups attended.
+//   tree_attn_kernel    U workgroups, of 128 columns at most, take a part of the list;
+//   tree_merge_kernel   joins the heads that several parts attended.
+// Times below are of kernels on one MI355X; the sizes: "deep" 48 sequences of 8 KV heads
+// at 32768 tokens (8 times fewer kept) with trees of 12 nodes, 60 columns a head; "wide" 8
+// of those with 64 nodes, 320 columns.
 #include <math.h>
 
 #include <algorithm>
 #include <type_traits>
 
 #include "dms_common.h"
+#include "dms_draft.h"
 #include "dms_fp8.h"
-#include "dms_ops.h"
 #include "dms_tiles.h"
 
 namespace dms {
@@ -77,8 +80,8 @@ struct TreeArgs {
   int32_t* deepest;        // [n]
   char* tiles;             // [H][tph] tiles of the drafted rows
   uint32_t* tmeta;         // [H][tph][32] their rows (position | flag << 31), as the pool's slot owners
-  float* part_o;           // [2 G][UC][D]
-  float2* part_ml;         // [2 G][UC]
+  float* part_o;           // [2 cells U][UC][D]: the sums of a part's first and last head
+  float2* part_ml;         // [2 cells U][UC] their maxima and denominators
   size_t page_bytes;
   int n, H, g, w, P, log2P, maxp, max_slots, max_seqs, total, max_nodes, words, tph;
   int cells, U, UC, min_tiles;   // parts at most, units (workgroups) to a part, columns of a unit, least tiles of a part
@@ -340,6 +343,8 @@ __device__ void tree_tile(const TreeArgs& a, int hh, int k) {
   }
 }
 
+// One launch for all of it, bound by the plan's chain of dependent loads (ids, sizes,
+// lengths, parts): 5.4 us with one sequence, 6.3 with 64 heads, 10 with 384.
 template <int D, bool FP8>
 __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a) {
   if (load_status(a.status) != 0) return;
@@ -369,6 +374,12 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a) {
 //   CW = 2: stages of KW tiles in a ring of S, one barrier a stage.
 //   CW = 4: a wave attends the two tiles of a stage together (TPS), their chains
 //     of products and exponentials side by side.
+// Deep calls are bound by memory: 165 us for 0.85 GB, 5.1 TB/s, what a large copy reaches;
+// while tiles stream it is 7, the rest goes into a segment's start and its fold.  Wide ones
+// are bound by the chain of a step (scores, maximum, exponentials, values) at two waves a
+// SIMD: 82 us, 0.55 PFLOP/s, matrix units busy 28 % of it.  Two column blocks a wave, for
+// half the LDS reads, leave one wave a SIMD: 159 us.  Three 2-wave workgroups a compute unit
+// for CW = 2: 168 against 166.  Parts of 4 or 16 tiles at least: no faster than 8.
 template <int D, bool FP8, int CW_>
 struct Shape {
   static constexpr int CW = CW_, NW = 4, KW = NW / CW, UC = 32 * CW;
@@ -707,7 +718,8 @@ __device__ __forceinline__ void attend_tiles(const TreeArgs& a, const Segment& s
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// The workgroup's part of the flat list, segment by segment.
+// The workgroup's part of the flat list, segment by segment (a segment: what a part holds
+// of one head).  U units of the same part lie side by side on one XCD and share its L2.
 template <int D, bool FP8, int CW>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
   using Sh = Shape<D, FP8, CW>;
@@ -981,7 +993,10 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(TreeArgs a) {
 }
 
 // Joins the heads that several parts attended: D / 4 threads a column, a batch of
-// its partials in flight at a time, a workgroup for 1024 / D columns of a head.
+// its partials in flight at a time, a workgroup for 1024 / D columns of a head.  Two
+// rounds of dependent loads: 2 us for one head, 6 for 16 heads of 10 parts, 11.5 deep and
+// wide (14 and 19 MB of partials).  One wave to several columns, a column after the other,
+// took 64 us.
 template <int D>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
   constexpr int kCols = 1024 / D, kBatch = 8;
@@ -1040,7 +1055,8 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a) {
 
 // A wave per sequence; lane l holds nodes l, l + 64, ..  Each step finds the
 // lowest child of the present node whose token is the wanted one; a child's
-// index is past its parent's, so the walk ends.
+// index is past its parent's, so the walk ends.  Latency: 1.8 us for one tree of 16
+// nodes, 6.2 for 512 of up to 128.
 __global__ __launch_bounds__(256) void tree_accept_kernel(const int32_t* cu, const int32_t* parents, const int32_t* tokens,
                                                           const int32_t* targets, const int32_t* first, int n, int total,
                                                           int max_nodes, int32_t* path, int32_t* path_len, int32_t* next) {
@@ -1132,13 +1148,17 @@ __device__ inline bool commit_reuse(const CommitArgs& a, const int* nodes, int s
 // What one head's path takes, by a wave; its nodes are left in LDS.
 struct CommitHead {
   int need, fresh, pos, len0;     // pages to pop, or the error that refuses the call
+  int s, tok0, len;
 };
 __device__ inline CommitHead commit_scan_head(const CommitArgs& a, int hh, int* nodes) {
   const int lane = threadIdx.x & 63, i = hh / a.H, h = hh % a.H, s = a.seq_ids[i];
   int tok0, len, fresh = 0;
-  CommitHead r{DMS_ERR_INVALID, 0, 0, 0};
+  CommitHead r{DMS_ERR_INVALID, 0, 0, 0, 0, 0, 0};
   if (s < 0 || s >= a.max_seqs || !commit_path(a, i, tok0, len)) return r;
   const int m = a.cu[i + 1] - tok0, sh = s * a.H + h;
+  r.s = s;
+  r.tok0 = tok0;
+  r.len = len;
   r.pos = a.st.pos[s];
   r.len0 = a.st.len[sh];
   int off = 0;
@@ -1180,7 +1200,9 @@ __device__ inline bool commit_bad_ids(const CommitArgs& a, uint32_t* seen) {
 }
 
 // Pass 1, a wave per head and one more for the ids: fresh tokens and pages of
-// every head, and the state that pass 2 overwrites.
+// every head, and the state that pass 2 overwrites.  (Two launches, for no workgroup may
+// write before all heads are known to fit.  64 sequences of 8 heads, up to 24 tokens a
+// path: 4.3 + 7.9 us, dependent loads and scattered stores.)
 __global__ __launch_bounds__(256) void commit_scan_kernel(CommitArgs a) {
   __shared__ uint32_t seen[kMaxSeqs / 32];
   __shared__ int nodes_lds[4][kTreeMaxNodes];
@@ -1270,9 +1292,8 @@ template <int THREADS>
 __device__ inline void commit_write_head(const CommitArgs& a, int hh, const CommitHead& r, int top0, int before, int* nodes,
                                          int* slots, int* keeps, int* lds) {
   static_assert(THREADS == 64 || THREADS == kTreeMaxNodes, "a token a thread, or a wave");
-  const int tid = threadIdx.x % THREADS, i = hh / a.H, h = hh % a.H;
-  const int s = a.seq_ids[i], sh = s * a.H + h, tok0 = a.cu[i], len = a.path_len[i];
-  const int pos = r.pos, L0 = r.len0;
+  const int tid = threadIdx.x % THREADS, h = hh % a.H;
+  const int s = r.s, sh = s * a.H + h, tok0 = r.tok0, len = r.len, pos = r.pos, L0 = r.len0;
   auto sync = []() {
     if (THREADS > 64) __syncthreads();
     else {      // a wave's LDS accesses are in order
@@ -1289,8 +1310,10 @@ __device__ inline void commit_write_head(const CommitArgs& a, int hh, const Comm
   const size_t pt = static_cast<size_t>(sh) * a.maxp;
   const int new0 = (L0 + a.P - 1) >> a.log2P;
   for (int x = tid; x < r.need; x += THREADS) a.st.page_table[pt + new0 + x] = popped[-x];
-  for (int c = tid; c < len; c += THREADS) nodes[c] = a.path[tok0 + c];
-  sync();
+  if (THREADS > 64) {      // (a wave has them from its scan)
+    for (int c = tid; c < len; c += THREADS) nodes[c] = a.path[tok0 + c];
+    sync();
+  }
   // slots: fresh tokens in order; a reusing one has that of the token w before
   // it, in the path or in the ring
   int ahead = 0;
@@ -1379,12 +1402,13 @@ __global__ __launch_bounds__(kTreeMaxNodes) void commit_write_kernel(CommitArgs 
   }
   const int top0 = *commit_word(a, 0);
   if (hh == last && tid == 0) *a.st.top = top0 - pops;
-  const CommitHead r{a.need[hh], a.fresh[hh], commit_pos(a)[hh / a.H], commit_len(a)[hh]};
+  const int i = hh / a.H;
+  const CommitHead r{a.need[hh], a.fresh[hh], commit_pos(a)[i], commit_len(a)[hh], a.seq_ids[i], a.cu[i], a.path_len[i]};
   commit_write_head<kTreeMaxNodes>(a, hh, r, top0, before, nodes, slots, keeps, lds);
 }
 
-// Calls of up to kSmallHeads heads in one launch: a workgroup, a wave per head (28 calls
-// of 16 heads: @@US@@).
+// Calls of up to kSmallHeads heads in one launch: a workgroup, a wave per head (one call
+// of 16 heads: 10.7 us, in two launches 4.4 + 6.0 and the pause between them).
 constexpr int kSmallHeads = 16;
 __global__ __launch_bounds__(64 * kSmallHeads) void commit_small_kernel(CommitArgs a) {
   __shared__ uint32_t seen[kMaxSeqs / 32];
