@@ -26,11 +26,12 @@
 // last launch alone, as shorter rows are (sample_row).
 //
 // Kernel times on one MI355X in this order: 1 x 151936 float32, T = 0.6, top-p 0.95: 3.6 +
-// 6.8 + 6.7 + 10.2 us, chains of dependent loads; 128 x 152064 of those: 14.7 (5.3 TB/s) +
-// 32.3 + 23 + 13.6; 500 x 151936 bf16, every row its own settings: 29.4 (5.2 TB/s) + 61 + 64
-// + 25.  The second pass is bound by forming weights (20 float64 instructions a token), the
-// third by the workgroups of rows that keep much of the vocabulary.  Before the groups, with
-// counts for every top-k: 106, 81 and 69 us for the last three of the 500 rows.
+// 6.6 + 6.1 + 10.0 us, chains of dependent loads; 128 x 152064 of those: 14.7 (5.3 TB/s) +
+// 31.4 + 22.7 + 13.2; 500 x 151936 bf16, every row its own settings: 30 (5.1 TB/s) + 58 + 62
+// + 25.  The second pass is bound by forming weights (18 float64 instructions a token; all
+// vector instructions keep its units busy 82 % of 128 alike rows), the third by the
+// workgroups of rows that keep much of the vocabulary.  Before the groups, with counts for
+// every top-k: 106, 81 and 69 us for the last three of the 500 rows.
 #include <math.h>
 
 #include <algorithm>
@@ -91,6 +92,9 @@ __device__ inline float counted(float x) {
   x = x != x ? -INFINITY : fminf(x, 0x1.fffffep127f);
   return x + 0.0f;
 }
+// The same but for NaN and -0, in two instructions of five: NaN has no weight and lies
+// nowhere (comparisons are false), -0 weighs what 0 does.
+__device__ inline float finite(float x) { return x == INFINITY ? 0x1.fffffep127f : x; }
 template <bool BF16>
 __device__ inline float logit(const void* row, int i) {
   if constexpr (BF16)
@@ -108,21 +112,21 @@ __device__ inline float key_value(uint32_t k) {
 }
 constexpr uint32_t kKeyNone = 0x007FFFFFu;   // -inf
 
-// 2^43 2^((x - top) c), rounded.  2^f for |f| <= 1/2 is its Taylor sum to the 12th
-// power, (ln 2 / 2)^13 / 13! = 2e-16 off.  No branches: several weights are formed
-// side by side.
+// 2^43 2^((x - top) c), rounded.  2^f for |f| <= 1/2 is 1 + f P(f), P the polynomial of
+// degree 9 that meets (2^f - 1) / f at the ten Chebyshev nodes of the range: 6.4e-16 off
+// with its roundings, 0.006 of a unit.  No branches: several weights are formed side by side.
 __device__ inline u64 weight(float x, float top, double c) {
   const double t = fmax((static_cast<double>(x) - static_cast<double>(top)) * c, -64.0);   // (NaN too: weight 0)
   // t + 1.5 2^52 has t's nearest integer in its low bits (a conversion and a rounding
   // instruction take four additions' time each)
   const double shifted = t + 0x1.8p52, f = t - (shifted - 0x1.8p52);
-  constexpr double kTerms[12] = {2.5678435993488196e-11, 4.44553827187081e-10, 7.054911620801121e-09,
-                                 1.0178086009239696e-07, 1.3215486790144305e-06, 1.5252733804059838e-05,
-                                 0.00015403530393381606, 0.0013333558146428441, 0.009618129107628477,
-                                 0.055504108664821576, 0.2402265069591007, 0.6931471805599453};
+  constexpr double kTerms[10] = {7.070977866508138e-09,  1.0205905413765595e-07, 1.3215451633221434e-06,
+                                 1.5252672924850737e-05, 0.00015403530424776529, 0.0013333558200794592,
+                                 0.009618129107618665,   0.05550410866465167,    0.24022650695910075,
+                                 0.6931471805599462};
   double p = kTerms[0];
 #pragma unroll
-  for (int i = 1; i < 12; ++i) {
+  for (int i = 1; i < 10; ++i) {
     double term = kTerms[i];
     asm("" : "+s"(term));      // in scalar registers: an addend is no move of its own
     p = fma(p, f, term);
@@ -441,7 +445,8 @@ struct Parts {
     const int g = (i - lead) / VEC;
     return g >= groups ? S - 1 : static_cast<int>((static_cast<int64_t>(g + 1) * S - 1) / groups);
   }
-  // f(first index, four logits, how many of them are there) over part s, by one wave; four 16-byte loads in flight
+  // f(first index, four logits as they are, how many of them are there) over part s, by one wave; four 16-byte
+  // loads in flight
   template <class F>
   __device__ void each(int s, F f) const {
     const int lane = threadIdx.x & 63;
@@ -468,8 +473,7 @@ struct Parts {
           float x[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            x[e] = counted(BF16 ? __uint_as_float(e & 1 ? w[2 * h + (e >> 1)] & 0xFFFF0000u : w[2 * h + (e >> 1)] << 16)
-                                : __uint_as_float(w[e]));
+            x[e] = __uint_as_float(!BF16 ? w[e] : e & 1 ? w[2 * h + (e >> 1)] & 0xFFFF0000u : w[2 * h + (e >> 1)] << 16);
           f(i + 4 * h, x, 4);
         }
       }
@@ -502,7 +506,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) 
   uint32_t key[4] = {kKeyNone, kKeyNone, kKeyNone, kKeyNone};
   Parts<BF16>(a, me.r).each(me.s, [&](int, const float (&x)[4], int) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) key[e] = max(key[e], order_key(x[e]));
+    for (int e = 0; e < 4; ++e) key[e] = max(key[e], order_key(counted(x[e])));
   });
   const int groups = groups_of_part(a.parts);
   uint32_t* group_top = st.group_top + me.s * groups;
@@ -633,7 +637,8 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
     u64 sum = 0;
     const bool by_k = ask.by_k;
     const float most = by_k ? 45.f : 20.f;
-    parts.each(me.s, [&](int, const float (&x)[4], int) {
+    parts.each(me.s, [&](int, const float (&given)[4], int) {
+      const float x[4] = {finite(given[0]), finite(given[1]), finite(given[2]), finite(given[3])};
       u64 w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) w[e] = weight(x[e], top, set.c);
@@ -656,7 +661,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
     parts.each(me.s, [&](int, const float (&x)[4], int) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float z = octaves(x[e], top, c);
+        const float z = octaves(finite(x[e]), top, c);
         if (z < 45.f) atomicAdd(&count[bin_of(z)], 1u);
       }
     });
@@ -812,11 +817,12 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
   const float keep = cut.none ? 64.f : bin_edge(cut.from), end = cut.none ? far : bin_edge(cut.to + 1);
   auto list = [&](float x, int i) {
     const uint32_t at = atomicAdd(&st.listed, 1u);
-    if (at < kListed) st.list[at] = static_cast<u64>(order_key(x)) << 32 | ~static_cast<uint32_t>(i);
+    if (at < kListed) st.list[at] = static_cast<u64>(order_key(x + 0.0f)) << 32 | ~static_cast<uint32_t>(i);   // (-0 as 0)
   };
   if (ask.near) {
     const float least = key_value(max(st.near, kKeyNone));
-    Parts<BF16>(a, me.r).each(me.s, [&](int i, const float (&x)[4], int n) {
+    Parts<BF16>(a, me.r).each(me.s, [&](int i, const float (&given)[4], int n) {
+      const float x[4] = {finite(given[0]), finite(given[1]), finite(given[2]), finite(given[3])};
       if (!(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= least)) return;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -825,7 +831,8 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
     return;
   }
   u64 sum = 0;
-  Parts<BF16>(a, me.r).each(me.s, [&](int i, const float (&x)[4], int n) {
+  Parts<BF16>(a, me.r).each(me.s, [&](int i, const float (&given)[4], int n) {
+    const float x[4] = {finite(given[0]), finite(given[1]), finite(given[2]), finite(given[3])};
     const float nearest = octaves(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), top, c);
     if (!(nearest < end)) return;      // four at once: nearly all of most rows
 #pragma unroll
