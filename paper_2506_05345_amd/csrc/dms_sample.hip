@@ -29,7 +29,7 @@
 // 6.6 + 6.1 + 10.0 us, chains of dependent loads; 128 x 152064 of those: 14.7 (5.3 TB/s) +
 // 31.4 + 22.7 + 13.2; 500 x 151936 bf16, every row its own settings: 30 (5.1 TB/s) + 58 + 62
 // + 25.  The second pass is bound by forming weights (18 float64 instructions a token; all
-// vector instructions keep its units busy 82 % of 128 alike rows), the third by the
+// vector instructions keep its units busy 78 % of 128 alike rows), the third by the
 // workgroups of rows that keep much of the vocabulary.  Before the groups, with counts for
 // every top-k: 106, 81 and 69 us for the last three of the 500 rows.
 #include <math.h>
