@@ -27,8 +27,8 @@
 //
 // Kernel times on one MI355X in this order: 1 x 151936 float32, T = 0.6, top-p 0.95: 3.6 +
 // 6.6 + 6.1 + 10.0 us, chains of dependent loads; 128 x 152064 of those: 14.7 (5.3 TB/s) +
-// 31.4 + 22.7 + 13.2; 500 x 151936 bf16, every row its own settings: 30 (5.1 TB/s) + 58 + 62
-// + 25.  The second pass is bound by forming weights (18 float64 instructions a token; all
+// 31.4 + 22.7 + 13.2; 500 x 151936 bf16, every row its own settings: 31.5 (4.8 TB/s) + 52 + 52
+// + 22.  The second pass is bound by forming weights (18 float64 instructions a token; all
 // vector instructions keep its units busy 78 % of 128 alike rows), the third by the
 // workgroups of rows that keep much of the vocabulary.  Before the groups, with counts for
 // every top-k: 106, 81 and 69 us for the last three of the 500 rows.
@@ -1095,11 +1095,15 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
   }
 }
 
-// Parts of a row, a wave each: about eight workgroups of four a compute unit in all, no
-// part of fewer than 512 logits.  (Passes two to four of 500 mixed rows with 1024, 2048 and
-// 4096 workgroups: 208, 166 and 149 us; of 128 rows alike: 71, 70 and 77.)
+// Parts of a row, a wave each, four to a workgroup: workgroups of 16384 logits, so that
+// rows that ask for little and rows that ask for much even out, more of them where all
+// would be fewer than eight a compute unit, no part of fewer than 512 logits.  (All four
+// passes of 500 mixed rows with workgroups of 75968, 37984, 24576, 16384 and 8192 logits:
+// 238, 175, 170, 158 and 164 us; of 128 rows alike, whose every workgroup finds the border
+// again, with 19008, 9504 and 4752: 86, 82 and 93.)
 int row_parts(int rows, int vocab) {
-  return kPartWaves * std::max(1, std::min({kMaxParts / kPartWaves, (2048 + rows - 1) / rows, vocab / (512 * kPartWaves)}));
+  const int groups = std::max((2048 + rows - 1) / rows, vocab / 16384);
+  return kPartWaves * std::max(1, std::min({kMaxParts / kPartWaves, groups, vocab / (512 * kPartWaves)}));
 }
 
 }  // namespace
