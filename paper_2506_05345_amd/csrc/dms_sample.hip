@@ -447,8 +447,10 @@ struct Parts {
   }
   // f(first index, four logits as they are, how many of them are there) over part s, by one wave; four 16-byte
   // loads in flight
+  // (the caller's lane takes part: its loads are left out otherwise)
   template <class F>
-  __device__ void each(int s, F f) const {
+  __device__ void each(int s, F f, bool on = true) const {
+    if (!on) return;
     const int lane = threadIdx.x & 63;
     auto edge = [&](int i0, int i1) {      // fewer than VEC tokens
       if (i0 + lane < i1) {
@@ -568,6 +570,24 @@ __device__ inline int bin_of(float z) {
 // Distance at which bin b begins (exact: bins are powers of two wide).
 __device__ inline float bin_edge(int b) {
   return b <= kFine ? static_cast<float>(b) * (1.0f / 32.f) : 20.f + static_cast<float>(b - kFine) * 0.25f;
+}
+
+// The largest value of the logits that a lane of part s reads (in sample_max_kernel and in
+// every pass after it), or of a few lanes.
+__device__ inline float lane_top(const SampleArgs& a, const RowState& st, int s) {
+  const int lane = threadIdx.x & 63, groups = groups_of_part(a.parts);
+  const uint32_t* top = st.group_top + s * groups;
+  uint32_t key;
+  if (groups == 256) {
+    const uint4 k = *reinterpret_cast<const uint4*>(top + 4 * lane);
+    key = max(max(k.x, k.y), max(k.z, k.w));
+  } else if (groups == 128) {
+    const uint2 k = *reinterpret_cast<const uint2*>(top + 2 * lane);
+    key = max(k.x, k.y);
+  } else {
+    key = top[lane & (groups - 1)];
+  }
+  return key_value(key);
 }
 
 // What a row asks of its passes: nothing but the groups (near: then every kept token is
@@ -805,6 +825,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
   const RowSetting set = row_setting(a, me.r);
   const Asked ask(a, set);
   if (ask.whole()) return;
+  const float mine = lane_top(a, st, me.s);     // lanes without a token to list or keep read none
   const RowView<kPartThreads> view(a, st, ask.bins());
   const uint32_t key = view.key;
   if (key == kKeyNone) return;
@@ -827,7 +848,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (x[e] >= least && octaves(x[e], top, c) < 45.f && e < n) list(x[e], i + e);
-    });
+    }, mine >= least && octaves(mine, top, c) < 45.f);
     return;
   }
   u64 sum = 0;
@@ -846,7 +867,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
         list(x[e], i + e);
       }
     }
-  });
+  }, octaves(mine, top, c) < end);
   sum = wave_sum64(sum);
   if (lane == 0) st.part_kept[me.s] = sum;
 }
@@ -1098,9 +1119,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
 // Parts of a row, a wave each, four to a workgroup: workgroups of 16384 logits, so that
 // rows that ask for little and rows that ask for much even out, more of them where all
 // would be fewer than eight a compute unit, no part of fewer than 512 logits.  (All four
-// passes of 500 mixed rows with workgroups of 75968, 37984, 24576, 16384 and 8192 logits:
-// 238, 175, 170, 158 and 164 us; of 128 rows alike, whose every workgroup finds the border
-// again, with 19008, 9504 and 4752: 86, 82 and 93.)
+// passes of 500 mixed rows with workgroups of 37984, 24576, 16384 and 8192 logits: 175, 170,
+// 158 and 164 us; of 128 rows alike, whose every workgroup finds the border again, with
+// 19008, 9504 and 4752: 86, 85 and 93.)
 int row_parts(int rows, int vocab) {
   const int groups = std::max((2048 + rows - 1) / rows, vocab / 16384);
   return kPartWaves * std::max(1, std::min({kMaxParts / kPartWaves, groups, vocab / (512 * kPartWaves)}));
