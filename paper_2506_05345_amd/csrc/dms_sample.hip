@@ -15,23 +15,24 @@
 //   sample_hist_kernel  top-k of at most half the groups: the k-th largest of the
 //                       groups' values, which k tokens reach.  Else the parts' weights,
 //                       and each row's counts and weights by distance from its largest
-//                       value (bins of 1/32 octave of weight);
-//   sample_cut_kernel   lists the tokens that reach that value, or those of the bins
-//                       that hold the borders of top-k and top-p, with the weights
-//                       ahead of them by part;
+//                       value (bins of 1/32 octave of weight); the row's last workgroup
+//                       finds the bins that hold the borders of top-k and top-p;
+//   sample_cut_kernel   lists the tokens that reach that value, or those of the borders'
+//                       bins, with the weights ahead of them by part;
 //   sample_pick_kernel  a workgroup a row sorts the listed tokens, cuts them, and finds
 //                       the picked one: among them, if few are kept and all are
 //                       listed, else in the part that holds it, by walking that.
 // A row whose borders' bins hold too many tokens (many equal logits) is done by the
 // last launch alone, as shorter rows are (sample_row).
 //
-// Kernel times on one MI355X in this order: 1 x 151936 float32, T = 0.6, top-p 0.95: 3.6 +
-// 6.6 + 6.1 + 10.0 us, chains of dependent loads; 128 x 152064 of those: 14.7 (5.3 TB/s) +
-// 31.4 + 22.7 + 13.2; 500 x 151936 bf16, every row its own settings: 31.5 (4.8 TB/s) + 52 + 52
-// + 22.  The second pass is bound by forming weights (18 float64 instructions a token; all
-// vector instructions keep its units busy 78 % of 128 alike rows), the third by the
+// Kernel times on one MI355X in this order: 1 x 151936 float32, T = 0.6, top-p 0.95: 3.7 +
+// 11.0 + 4.4 + 7.3 us, chains of dependent loads; 128 x 152064 of those: 14.7 (5.3 TB/s) +
+// 35.8 + 14.9 + 10.7; 500 x 151936 bf16, every row its own settings: 32 (4.7 TB/s) + 55 + 40
+// + 19.5.  The second pass is bound by forming weights (18 float64 instructions a token; all
+// vector instructions keep its units busy three quarters of the time), the third by the
 // workgroups of rows that keep much of the vocabulary.  Before the groups, with counts for
-// every top-k: 106, 81 and 69 us for the last three of the 500 rows.
+// every top-k and the borders found by every workgroup of the third pass: 106, 81 and 69 us
+// for the last three of the 500 rows.
 #include <math.h>
 
 #include <algorithm>
@@ -400,8 +401,18 @@ constexpr int kMaxParts = 256;                            // parts of a row, a w
 // with them and 30.6 without, counts of the bins included in both).
 constexpr int kFine = 20 * 32, kHist = kFine + 25 * 4;
 constexpr int kListed = 2048;                             // tokens that a row lists at most
+constexpr int kWaitVmcnt0 = 0x0F70;                       // s_waitcnt vmcnt(0): the wave's memory operations are done
 constexpr int kFew = 256;     // kept tokens among which the picked one is found by sorting them by index
 constexpr int kGroups = 2048;                             // groups whose largest values a row keeps at most
+
+// What a row's second pass finds: its largest value and which bins hold its borders.
+struct Cut {
+  uint32_t key;        // of the largest value
+  bool none, slow;     // nothing to cut by bins; the row is left to sample_row
+  int from, to;        // bins whose tokens are listed; those before are kept
+  uint32_t ahead;      // tokens and weight before `from`
+  u64 ahead_mass, all; // weight of the row
+};
 
 // What the launches of a row leave each other.
 struct alignas(16) RowState {
@@ -413,6 +424,8 @@ struct alignas(16) RowState {
   uint32_t group_top[kGroups];
   uint32_t listed;
   uint32_t near;              // key that at least top-k tokens reach (Asked::near)
+  uint32_t arrived;           // workgroups of the second pass that are done
+  Cut cut;
 };
 
 // Groups of a part: a power of two, of the part's 256 pairs of a lane and a place in its
@@ -504,7 +517,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) 
   RowState& st = a.state[me.r];
   const int lane = threadIdx.x & 63;
   for (int x = me.s * 64 + lane; x < kHist; x += a.parts * 64) st.mass[x] = 0, st.count[x] = 0;
-  if (me.s == 0 && lane == 0) st.listed = 0;
+  if (me.s == 0 && lane == 0) st.listed = 0, st.arrived = 0;
   uint32_t key[4] = {kKeyNone, kKeyNone, kKeyNone, kKeyNone};
   Parts<BF16>(a, me.r).each(me.s, [&](int, const float (&x)[4], int) {
 #pragma unroll
@@ -524,39 +537,42 @@ __global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) 
   if (lane == 0) st.part_top[me.s] = top;
 }
 
-// What a workgroup of THREADS reads of a row's state, in one round of loads: the
-// largest logit and the weight of its parts (every wave) and a few bins to a thread.
-template <int THREADS>
+// What the workgroup that finds a row's borders reads of its state, in one round of loads:
+// the weight of its parts (every wave) and a few bins to a thread.  Other workgroups of the
+// same launch wrote it: loads that no cache of this XCD answers.
+template <class T>
+__device__ inline T load_shared(const T* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 struct RowView {
-  static constexpr int PER = (kHist + THREADS - 1) / THREADS;
-  uint32_t key;
+  static constexpr int PER = (kHist + kPartThreads - 1) / kPartThreads;
   u64 all;
   u64 m[PER];
   uint32_t n[PER];
-  __device__ RowView(const SampleArgs& a, const RowState& st, bool bins) {
+  __device__ RowView(const SampleArgs& a, const RowState& st) {
     constexpr int LANE = kMaxParts / 64;
     const int lane = threadIdx.x & 63;
-    uint32_t top[LANE];
     u64 part[LANE];
 #pragma unroll
-    for (int u = 0; u < LANE; ++u) {
-      top[u] = lane + 64 * u < a.parts ? st.part_top[lane + 64 * u] : kKeyNone;
-      part[u] = bins && lane + 64 * u < a.parts ? st.part_mass[lane + 64 * u] : 0;
-    }
+    for (int u = 0; u < LANE; ++u) part[u] = lane + 64 * u < a.parts ? load_shared(&st.part_mass[lane + 64 * u]) : 0;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
       const int b = threadIdx.x * PER + u;
-      m[u] = bins && b < kHist ? st.mass[b] : 0;
-      n[u] = bins && b < kHist ? st.count[b] : 0;
+      m[u] = b < kHist ? load_shared(&st.mass[b]) : 0;
+      n[u] = b < kHist ? load_shared(&st.count[b]) : 0;
     }
-    key = top[0];
     all = part[0];
 #pragma unroll
-    for (int u = 1; u < LANE; ++u) key = max(key, top[u]), all += part[u];
-    key = wave_max32(key);
+    for (int u = 1; u < LANE; ++u) all += part[u];
     all = wave_sum64(all);
   }
 };
+// Key of a row's largest logit, of its parts' (every wave).
+__device__ inline uint32_t row_top(const SampleArgs& a, const RowState& st) {
+  const int lane = threadIdx.x & 63;
+  uint32_t key = kKeyNone;
+#pragma unroll
+  for (int u = 0; u < kMaxParts / 64; ++u) key = max(key, lane + 64 * u < a.parts ? st.part_top[lane + 64 * u] : kKeyNone);
+  return wave_max32(key);
+}
 // Distance of a logit from the largest in octaves of weight, and its bin: larger for
 // smaller logits (each step is monotonous), kHist where the weight is 0.
 __device__ inline float octaves(float x, float top, float c) {
@@ -629,95 +645,19 @@ __device__ uint32_t near_key(const SampleArgs& a, const RowState& st, int k) {
   return found;
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a) {
-  __shared__ u64 mass[kHist];
-  __shared__ uint32_t count[kHist];
-  const PartOf me(a);
-  const int tid = threadIdx.x, lane = tid & 63;
-  RowState& st = a.state[me.r];
-  const RowSetting set = row_setting(a, me.r);
-  const Asked ask(a, set);
-  if (ask.near) {
-    if (blockIdx.x % (a.parts / kPartWaves) != 0) return;
-    const uint32_t near = near_key(a, st, set.k);
-    if (tid == 0) st.near = near;
-    return;
-  }
-  if (!(ask.weights() || ask.bins())) return;
-  const uint32_t key = RowView<kPartThreads>(a, st, false).key;
-  if (key == kKeyNone) return;
-  if (ask.bins()) {
-    for (int x = tid; x < kHist; x += kPartThreads) mass[x] = 0, count[x] = 0;
-    __syncthreads();
-  }
-  const float top = key_value(key), c = static_cast<float>(set.c);
-  const Parts<BF16> parts(a, me.r);
-  if (ask.weights()) {
-    u64 sum = 0;
-    const bool by_k = ask.by_k;
-    const float most = by_k ? 45.f : 20.f;
-    parts.each(me.s, [&](int, const float (&given)[4], int) {
-      const float x[4] = {finite(given[0]), finite(given[1]), finite(given[2]), finite(given[3])};
-      u64 w[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = weight(x[e], top, set.c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum += w[e];
-      if (ask.by_p)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float z = octaves(x[e], top, c);
-          if (z < most) {
-            const int b = bin_of(z);
-            atomicAdd(&mass[b], w[e]);
-            if (by_k) atomicAdd(&count[b], 1u);
-          }
-        }
-    });
-    sum = wave_sum64(sum);
-    if (lane == 0) st.part_mass[me.s] = sum;
-  } else {
-    parts.each(me.s, [&](int, const float (&x)[4], int) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float z = octaves(finite(x[e]), top, c);
-        if (z < 45.f) atomicAdd(&count[bin_of(z)], 1u);
-      }
-    });
-  }
-  if (ask.bins()) {
-    __syncthreads();
-    for (int x = tid; x < kHist; x += kPartThreads) {
-      if (mass[x]) atomicAdd(&st.mass[x], mass[x]);
-      if (count[x]) atomicAdd(&st.count[x], count[x]);
-    }
-  }
-}
-
-// Which bins hold a row's borders.
-struct Cut {
-  bool none, slow;     // nothing to cut by bins; the row is left to sample_row
-  int from, to;        // bins whose tokens are listed; those before are kept
-  uint32_t ahead;      // tokens and weight before `from`
-  u64 ahead_mass, all; // weight of the row
-};
 struct CutLds {
-  u64 wave_mass[kRowThreads / 64];
-  uint32_t wave_count[kRowThreads / 64];
+  u64 wave_mass[kPartWaves];
+  uint32_t wave_count[kPartWaves];
   int k_bin, p_low, p_high;
   u64 k_before, k_with;
   uint32_t ahead, through;
   u64 ahead_mass;
 };
-// Found by a whole workgroup, a few bins to a thread.
-template <int THREADS>
-__device__ Cut find_cut(const RowView<THREADS>& v, const RowSetting& set, const Asked& ask, CutLds& l) {
-  constexpr int PER = RowView<THREADS>::PER;
+// Found by a whole workgroup, a few bins to a thread, for a row that asks for bins.
+__device__ Cut find_cut(const RowView& v, const RowSetting& set, const Asked& ask, CutLds& l) {
+  constexpr int PER = RowView::PER;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   Cut cut{};
-  cut.none = !ask.bins();
-  if (cut.none) return cut;     // (near: what is listed is known already)
   cut.all = v.all;
   const u64 (&m)[PER] = v.m;
   const uint32_t (&n)[PER] = v.n;
@@ -737,7 +677,7 @@ __device__ Cut find_cut(const RowView<THREADS>& v, const RowSetting& set, const 
   __syncthreads();
   u64 before = im - sum, in_bins = 0;
   uint32_t ahead = in - num, all_count = 0;
-  for (int x = 0; x < THREADS / 64; ++x) {
+  for (int x = 0; x < kPartWaves; ++x) {
     if (x < wave) before += l.wave_mass[x], ahead += l.wave_count[x];
     in_bins += l.wave_mass[x];
     all_count += l.wave_count[x];
@@ -817,8 +757,90 @@ __device__ Cut find_cut(const RowView<THREADS>& v, const RowSetting& set, const 
 }
 
 template <bool BF16>
+__global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a) {
+  __shared__ u64 mass[kHist];
+  __shared__ uint32_t count[kHist];
+  __shared__ CutLds cut_lds;
+  __shared__ int last;
+  const PartOf me(a);
+  const int tid = threadIdx.x, lane = tid & 63;
+  RowState& st = a.state[me.r];
+  const RowSetting set = row_setting(a, me.r);
+  const Asked ask(a, set);
+  const int groups = a.parts / kPartWaves;       // workgroups of the row
+  const bool lead = blockIdx.x % groups == 0;
+  if (!lead && !(ask.weights() || ask.bins())) return;
+  const uint32_t key = row_top(a, st);
+  if (lead && (!ask.bins() || key == kKeyNone)) {
+    const uint32_t near = ask.near ? near_key(a, st, set.k) : 0u;
+    if (tid == 0) {
+      st.near = near;
+      st.cut = Cut{key, true, false, 0, 0, 0u, 0, 0};
+    }
+  }
+  if (key == kKeyNone || !(ask.weights() || ask.bins())) return;
+  if (ask.bins()) {
+    for (int x = tid; x < kHist; x += kPartThreads) mass[x] = 0, count[x] = 0;
+    __syncthreads();
+  }
+  const float top = key_value(key), c = static_cast<float>(set.c);
+  const Parts<BF16> parts(a, me.r);
+  if (ask.weights()) {
+    u64 sum = 0;
+    const bool by_k = ask.by_k;
+    const float most = by_k ? 45.f : 20.f;
+    parts.each(me.s, [&](int, const float (&given)[4], int) {
+      const float x[4] = {finite(given[0]), finite(given[1]), finite(given[2]), finite(given[3])};
+      u64 w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = weight(x[e], top, set.c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += w[e];
+      if (ask.by_p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float z = octaves(x[e], top, c);
+          if (z < most) {
+            const int b = bin_of(z);
+            atomicAdd(&mass[b], w[e]);
+            if (by_k) atomicAdd(&count[b], 1u);
+          }
+        }
+    });
+    sum = wave_sum64(sum);
+    if (lane == 0) __hip_atomic_store(&st.part_mass[me.s], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  } else {
+    parts.each(me.s, [&](int, const float (&x)[4], int) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float z = octaves(finite(x[e]), top, c);
+        if (z < 45.f) atomicAdd(&count[bin_of(z)], 1u);
+      }
+    });
+  }
+  if (ask.bins()) {
+    __syncthreads();
+    for (int x = tid; x < kHist; x += kPartThreads) {
+      if (mass[x]) atomicAdd(&st.mass[x], mass[x]);
+      if (count[x]) atomicAdd(&st.count[x], count[x]);
+    }
+    // the row's last workgroup finds the borders.  What the others leave it they write
+    // and it reads by device-wide atomics, past the caches of the XCDs: every wave waits
+    // until its own are done, then the workgroup arrives (fences of that scope, which write
+    // back and drop those caches, took the pass of 128 rows from 31 us to 230)
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+    __syncthreads();
+    if (tid == 0) last = atomicAdd(&st.arrived, 1u) == static_cast<uint32_t>(groups) - 1;
+    __syncthreads();
+    if (!last) return;
+    Cut cut = find_cut(RowView(a, st), set, ask, cut_lds);
+    cut.key = key;
+    if (tid == 0) st.cut = cut;
+  }
+}
+
+template <bool BF16>
 __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) {
-  __shared__ CutLds l;
   const PartOf me(a);
   const int lane = threadIdx.x & 63;
   RowState& st = a.state[me.r];
@@ -826,11 +848,9 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
   const Asked ask(a, set);
   if (ask.whole()) return;
   const float mine = lane_top(a, st, me.s);     // lanes without a token to list or keep read none
-  const RowView<kPartThreads> view(a, st, ask.bins());
-  const uint32_t key = view.key;
-  if (key == kKeyNone) return;
-  const Cut cut = find_cut(view, set, ask, l);
-  if (cut.slow) return;
+  const Cut cut = st.cut;
+  const uint32_t key = cut.key;
+  if (key == kKeyNone || cut.slow) return;
   const float top = key_value(key), c = static_cast<float>(set.c);
   // tokens nearer than `keep` are ahead of the listed bins, those from `end` on are
   // out; no token past `far` passes min-p (and none past 45 octaves has a weight)
@@ -873,7 +893,6 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
 }
 
 struct PickLds {
-  CutLds cut;
   u64 list[2][kListed];
   u64 mass[kMaxParts];
   u64 wave_mass[kWaves];
@@ -924,11 +943,11 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
   const RowState& st = a.state[r];
   const RowSetting set = row_setting(a, r);
   const Asked ask(a, set);
-  const RowView<kRowThreads> view(a, st, ask.bins());
+  const Cut cut = st.cut;
   const u64 mine = tid < a.parts ? (ask.whole() ? st.part_mass[tid] : st.part_kept[tid]) : 0;
   const uint32_t listed = st.listed;
   const int n = min(listed, static_cast<uint32_t>(kListed));
-  const uint32_t key = view.key;
+  const uint32_t key = cut.key;
   if (key == kKeyNone) {      // no token is left
     if (tid == 0) {
       a.tokens[r] = -1;
@@ -936,7 +955,6 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
     }
     return;
   }
-  const Cut cut = find_cut(view, set, ask, l.cut);
   if (cut.slow || listed > kListed) {
     __syncthreads();
     sample_row<BF16>(a, r, lds.row);
