@@ -1137,9 +1137,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
 // Parts of a row, a wave each, four to a workgroup: workgroups of 16384 logits, so that
 // rows that ask for little and rows that ask for much even out, more of them where all
 // would be fewer than eight a compute unit, no part of fewer than 512 logits.  (All four
-// passes of 500 mixed rows with workgroups of 37984, 24576, 16384 and 8192 logits: 175, 170,
-// 158 and 164 us; of 128 rows alike, whose every workgroup finds the border again, with
-// 19008, 9504 and 4752: 86, 85 and 93.)
+// passes of 500 mixed rows with workgroups of 37984, 16384 and 8192 logits: 160, 147 and 149
+// us; of 128 rows alike with 9504, 8448 and 4752: 76, 80 and 81.)
 int row_parts(int rows, int vocab) {
   const int groups = std::max((2048 + rows - 1) / rows, vocab / 16384);
   return kPartWaves * std::max(1, std::min({kMaxParts / kPartWaves, groups, vocab / (512 * kPartWaves)}));
