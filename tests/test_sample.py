@@ -281,3 +281,24 @@ def test_sorted_logits():
     u = rng.random(rows).astype(np.float32)
     got = run(x, "f32", np.ones(rows), k, p, m, u)
     check(x, u, got, np.ones(rows), k, p, m)
+
+
+def test_rows_far_apart():
+    """Rows 2^30 logits apart: offsets past 32 bits."""
+    import torch
+    from paper_2506_05345_amd import dms
+    rng = np.random.default_rng(14)
+    vocab = 9000
+    x = (rng.normal(size=(3, vocab)) * 3).astype(np.float32)
+    wide = torch.empty(2 * (1 << 30) + vocab, dtype=torch.bfloat16, device="cuda")
+    logits = wide.as_strided((3, vocab), (1 << 30, 1))
+    logits.copy_(torch.from_numpy(x))
+    c = dms.make_sample_config(vocab, dms.DMS_TYPE_BF16, top_p=0.9, temperature=0.8)
+    u = torch.tensor([0.1, 0.5, 0.9], device="cuda")
+    tokens, logp = torch.empty(3, dtype=torch.int32, device="cuda"), torch.empty(3, device="cuda")
+    ws = torch.empty(dms.dms_sample_workspace(c, 3), dtype=torch.uint8, device="cuda")
+    dms.dms_sample(c, 3, logits, None, None, None, None, u, tokens, logp, ws)
+    held = logits.float().cpu().numpy()
+    one = lambda v: np.full(3, v)
+    check(held, u.cpu().numpy(), (held, tokens.cpu().numpy(), logp.cpu().numpy()), one(np.float32(0.8)), one(0), one(np.float32(0.9)),
+          one(0.0))

@@ -493,3 +493,59 @@ def test_slots_past_the_live_length_hold_anything(kv, byte):
         c.dms.dms_append_chunk(c.cache.ctx, 0, c.n, dev(c.ids), dev(c.cu_ctx), sum(lens), max(lens), dev(c.k0, "bf16"),
                                dev(c.v0, "bf16"), dev(c.f0))
         c.check(c.attend())
+
+
+def test_commit_of_a_repeated_node():
+    """A path may name a node more than once: its rows are appended as often."""
+    for n in (2, 12):
+        a, b = (Call(51, [40] * n, [6] * n, 2, 2, 64, 4, 32) for _ in range(2))
+        path, plen = np.full(a.total, -1, np.int32), np.full(n, 4, np.int32)
+        for i in range(n):
+            path[a.cu[i]:a.cu[i] + 4] = [1, 1, 5, 1]
+        t = a.tensors()
+        a.dms.dms_tree_commit(a.cache.ctx, 0, n, t["ids"], t["cu"], a.total, a.most, dev(path), dev(plen), t["k"], t["v"], t["f"],
+                              a.ws)
+        rows = np.concatenate([a.cu[i] + np.array([1, 1, 5, 1]) for i in range(n)])
+        cu = 4 * np.arange(n + 1, dtype=np.int32)
+        b.dms.dms_append_chunk(b.cache.ctx, 0, n, dev(b.ids), dev(cu), 4 * n, 4, dev(b.k[rows], "bf16"), dev(b.v[rows], "bf16"),
+                               dev(b.f[rows]))
+        va, vb = a.cache.export(0), b.cache.export(0)
+        assert a.dms.dms_status(a.cache.ctx) == 0
+        for s in a.ids:
+            for h in range(2):
+                L = int(vb.L[s, h])
+                assert va.L[s, h] == L and va.pos[s] == vb.pos[s]
+                assert np.array_equal(va.slot_pos[s, h, :L], vb.slot_pos[s, h, :L])
+                assert np.array_equal(va.page_table[s, h, :-(-L // 32)], vb.page_table[s, h, :-(-L // 32)])
+
+
+def test_pages_past_four_gigabytes():
+    """A pool of 6 GB whose last pages come first."""
+    import torch
+    from paper_2506_05345_amd import dms
+    c = Call(52, [700, 90], [40, 7], 2, 3, 128, 16, 64)
+    base = c.attend()
+    cfg = dms.make_config(1, 3, 2, 3, 128, 16, 64, 190000, 16, 790)
+    big = dms.DmsCache(cfg)
+    o = big.offsets
+    stack = big.meta[o.layer0 + o.stack:o.layer0 + o.stack + 4 * 190000].view(torch.int32)
+    assert int(stack[-1]) == 0
+    stack.copy_(stack.flip(0).clone())
+    dms.dms_append_chunk(big.ctx, 0, 2, dev(c.ids), dev(c.cu_ctx), 790, 700, dev(c.k0, "bf16"), dev(c.v0, "bf16"), dev(c.f0))
+    assert int(big.export(0).page_table[c.ids[0], 0, 0]) * 32768 > 1 << 32
+    c.cache = big
+    assert torch.equal(c.attend(), base)
+    path, plen = some_paths(c.rng, c, "longest")
+    t = c.tensors()
+    dms.dms_tree_commit(big.ctx, 0, 2, t["ids"], t["cu"], c.total, c.most, dev(path), dev(plen), t["k"], t["v"], t["f"], c.ws)
+    assert dms.dms_status(big.ctx) == 0
+    out = torch.empty((2, 6, 128), device="cuda")
+    step = lambda cache: dms.dms_decode_step(cache.ctx, 0, 2, dev(c.ids), t["q"][:2].contiguous(), t["k"][:2].contiguous(),
+                                             t["v"][:2].contiguous(), t["f"][:2].contiguous(), out)
+    step(big)
+    got = out.clone()
+    small = Call(52, [700, 90], [40, 7], 2, 3, 128, 16, 64)
+    dms.dms_tree_commit(small.cache.ctx, 0, 2, t["ids"], t["cu"], c.total, c.most, dev(path), dev(plen), t["k"], t["v"], t["f"],
+                        small.ws)
+    step(small.cache)
+    assert torch.equal(got, out)
