@@ -410,6 +410,7 @@ struct Cut {
   uint32_t key;        // of the largest value
   bool none, slow;     // nothing to cut by bins; the row is left to sample_row
   int from, to;        // bins whose tokens are listed; those before are kept
+  float keep, end;     // distances at which they begin and end
   uint32_t ahead;      // tokens and weight before `from`
   u64 ahead_mass, all; // weight of the row
 };
@@ -421,6 +422,7 @@ struct alignas(16) RowState {
   u64 list[kListed];          // key << 32 | ~index of the tokens in the borders' bins
   uint32_t count[kHist];
   uint32_t part_top[kMaxParts];
+  uint32_t part_low[kMaxParts];   // smallest keys above kKeyNone, less kKeyNone + 1
   uint32_t group_top[kGroups];
   uint32_t listed;
   uint32_t near;              // key that at least top-k tokens reach (Asked::near)
@@ -518,11 +520,16 @@ __global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) 
   const int lane = threadIdx.x & 63;
   for (int x = me.s * 64 + lane; x < kHist; x += a.parts * 64) st.mass[x] = 0, st.count[x] = 0;
   if (me.s == 0 && lane == 0) st.listed = 0, st.arrived = 0;
-  uint32_t key[4] = {kKeyNone, kKeyNone, kKeyNone, kKeyNone};
+  uint32_t key[4] = {kKeyNone, kKeyNone, kKeyNone, kKeyNone}, low = 0xFFFFFFFFu;
   Parts<BF16>(a, me.r).each(me.s, [&](int, const float (&x)[4], int) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) key[e] = max(key[e], order_key(counted(x[e])));
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t k = order_key(counted(x[e]));
+      key[e] = max(key[e], k);
+      low = min(low, k - (kKeyNone + 1));
+    }
   });
+  low = ~wave_max32(~low);
   const int groups = groups_of_part(a.parts);
   uint32_t* group_top = st.group_top + me.s * groups;
   if (groups == 256) *reinterpret_cast<uint4*>(group_top + 4 * lane) = make_uint4(key[0], key[1], key[2], key[3]);
@@ -534,7 +541,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) 
     if (n == groups && lane < n) group_top[lane] = top;
     top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off, 64)));
   }
-  if (lane == 0) st.part_top[me.s] = top;
+  if (lane == 0) st.part_top[me.s] = top, st.part_low[me.s] = low;
 }
 
 // What the workgroup that finds a row's borders reads of its state, in one round of loads:
@@ -579,13 +586,27 @@ __device__ inline float octaves(float x, float top, float c) {
   const float half = 0.5f * top - 0.5f * x;      // (two large values of either sign: no overflow)
   return half == 0.f ? 0.f : half * (2.0f * c);
 }
-__device__ inline int bin_of(float z) {
-  return z < 20.f ? static_cast<int>(z * 32.f) : z < 45.f ? kFine + static_cast<int>((z - 20.f) * 4.f) : kHist;
+// Bins to an octave of a row: 32, or so many more, a power of two, that the fine bins hold
+// all of a flat row (152064 logits of deviation 0.5 at T = 1.7, top-p 0.5: lists of 32 bins
+// an octave overflow, 434 us; 49 with 128).
+__device__ inline float bins_an_octave(const SampleArgs& a, const RowState& st, uint32_t top, float c) {
+  const int lane = threadIdx.x & 63;
+  uint32_t low = 0xFFFFFFFFu;
+#pragma unroll
+  for (int u = 0; u < kMaxParts / 64; ++u) low = min(low, lane + 64 * u < a.parts ? st.part_low[lane + 64 * u] : 0xFFFFFFFFu);
+  low = ~wave_max32(~low) + (kKeyNone + 1);
+  const float range = octaves(key_value(low), key_value(top), c);
+  float f = 32.f;
+  while (f < 32.f * 1024.f && range * f < 0.49f * kFine) f *= 2.f;
+  return f;
+}
+__device__ inline int bin_of(float z, float f) {
+  return z * f < kFine ? static_cast<int>(z * f) : z < 45.f ? kFine + static_cast<int>((z - 20.f) * 4.f) : kHist;
 }
 
 // Distance at which bin b begins (exact: bins are powers of two wide).
-__device__ inline float bin_edge(int b) {
-  return b <= kFine ? static_cast<float>(b) * (1.0f / 32.f) : 20.f + static_cast<float>(b - kFine) * 0.25f;
+__device__ inline float bin_edge(int b, float f) {
+  return b < kFine || f > 32.f ? static_cast<float>(b) / f : 20.f + static_cast<float>(b - kFine) * 0.25f;
 }
 
 // The largest value of the logits that a lane of part s reads (in sample_max_kernel and in
@@ -654,7 +675,7 @@ struct CutLds {
   u64 ahead_mass;
 };
 // Found by a whole workgroup, a few bins to a thread, for a row that asks for bins.
-__device__ Cut find_cut(const RowView& v, const RowSetting& set, const Asked& ask, CutLds& l) {
+__device__ Cut find_cut(const RowView& v, const RowSetting& set, const Asked& ask, float f, CutLds& l) {
   constexpr int PER = RowView::PER;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   Cut cut{};
@@ -747,11 +768,13 @@ __device__ Cut find_cut(const RowView& v, const RowSetting& set, const Asked& as
   cut.ahead_mass = l.ahead_mass;
   // the tokens ahead weigh more than 2^43 2^-(where bin `from` begins) each: few of
   // them are listed too
-  if (ask.by_p && static_cast<double>(cut.ahead_mass) * exp2f(bin_edge(cut.from) - 43.f) < 2.0 * kFew) {
+  if (ask.by_p && static_cast<double>(cut.ahead_mass) * exp2f(bin_edge(cut.from, f) - 43.f) < 2.0 * kFew) {
     cut.from = 0;
     cut.ahead = 0;
     cut.ahead_mass = 0;
   }
+  cut.keep = bin_edge(cut.from, f);
+  cut.end = bin_edge(cut.to + 1, f);
   cut.slow = l.through - cut.ahead > kListed;      // (without top-k: known when they are listed)
   return cut;
 }
@@ -775,7 +798,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
     const uint32_t near = ask.near ? near_key(a, st, set.k) : 0u;
     if (tid == 0) {
       st.near = near;
-      st.cut = Cut{key, true, false, 0, 0, 0u, 0, 0};
+      st.cut = Cut{key, true, false, 0, 0, 0.f, 0.f, 0u, 0, 0};
     }
   }
   if (key == kKeyNone || !(ask.weights() || ask.bins())) return;
@@ -783,12 +806,12 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
     for (int x = tid; x < kHist; x += kPartThreads) mass[x] = 0, count[x] = 0;
     __syncthreads();
   }
-  const float top = key_value(key), c = static_cast<float>(set.c);
+  const float top = key_value(key), c = static_cast<float>(set.c), f = ask.bins() ? bins_an_octave(a, st, key, c) : 32.f;
   const Parts<BF16> parts(a, me.r);
   if (ask.weights()) {
     u64 sum = 0;
     const bool by_k = ask.by_k;
-    const float most = by_k ? 45.f : 20.f;
+    const float most = by_k ? 45.f : 20.f;       // (a flat row ends before)
     parts.each(me.s, [&](int, const float (&given)[4], int) {
       const float x[4] = {finite(given[0]), finite(given[1]), finite(given[2]), finite(given[3])};
       u64 w[4];
@@ -801,7 +824,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
         for (int e = 0; e < 4; ++e) {
           const float z = octaves(x[e], top, c);
           if (z < most) {
-            const int b = bin_of(z);
+            const int b = bin_of(z, f);
             atomicAdd(&mass[b], w[e]);
             if (by_k) atomicAdd(&count[b], 1u);
           }
@@ -814,7 +837,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float z = octaves(finite(x[e]), top, c);
-        if (z < 45.f) atomicAdd(&count[bin_of(z)], 1u);
+        if (z < 45.f) atomicAdd(&count[bin_of(z, f)], 1u);
       }
     });
   }
@@ -833,7 +856,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_hist_kernel(SampleArgs a)
     if (tid == 0) last = atomicAdd(&st.arrived, 1u) == static_cast<uint32_t>(groups) - 1;
     __syncthreads();
     if (!last) return;
-    Cut cut = find_cut(RowView(a, st), set, ask, cut_lds);
+    Cut cut = find_cut(RowView(a, st), set, ask, f, cut_lds);
     cut.key = key;
     if (tid == 0) st.cut = cut;
   }
@@ -855,7 +878,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
   // tokens nearer than `keep` are ahead of the listed bins, those from `end` on are
   // out; no token past `far` passes min-p (and none past 45 octaves has a weight)
   const float far = ask.least ? 43.01f - log2f(static_cast<float>(set.least)) : 45.f;
-  const float keep = cut.none ? 64.f : bin_edge(cut.from), end = cut.none ? far : bin_edge(cut.to + 1);
+  const float keep = cut.none ? 64.f : cut.keep, end = cut.none ? far : cut.end;
   auto list = [&](float x, int i) {
     const uint32_t at = atomicAdd(&st.listed, 1u);
     if (at < kListed) st.list[at] = static_cast<u64>(order_key(x + 0.0f)) << 32 | ~static_cast<uint32_t>(i);   // (-0 as 0)

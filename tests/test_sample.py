@@ -302,3 +302,19 @@ def test_rows_far_apart():
     one = lambda v: np.full(3, v)
     check(held, u.cpu().numpy(), (held, tokens.cpu().numpy(), logp.cpu().numpy()), one(np.float32(0.8)), one(0), one(np.float32(0.9)),
           one(0.0))
+
+
+@pytest.mark.parametrize("spread", [1e-4, 0.02, 0.5, 2.0])
+def test_flat_rows(spread):
+    """Logits close to each other: many tokens to a share of the weight, with and without masked ones far below."""
+    rng = np.random.default_rng(15)
+    rows, vocab = 24, 60000
+    x = (rng.normal(size=(rows, vocab)) * spread).astype(np.float32)
+    x[::4, 1000:50000] = -np.inf
+    x[1::4, :100] = -1e6
+    T, _, p, m = mixed(rng, rows)
+    T = np.where(T <= 0, 1.7, T)
+    k = rng.choice([0, 0, 0, 2000, 40000], rows)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
