@@ -25,11 +25,11 @@
 // A row whose borders' bins hold too many tokens (many equal logits) is done by the
 // last launch alone, as shorter rows are (sample_row).
 //
-// Kernel times on one MI355X in this order: 1 x 151936 float32, T = 0.6, top-p 0.95: 3.7 +
-// 11.0 + 4.4 + 7.3 us, chains of dependent loads; 128 x 152064 of those: 14.7 (5.3 TB/s) +
-// 35.8 + 14.9 + 10.7; 500 x 151936 bf16, every row its own settings: 32 (4.7 TB/s) + 55 + 40
-// + 19.5.  The second pass is bound by forming weights (18 float64 instructions a token; all
-// vector instructions keep its units busy three quarters of the time), the third by the
+// Kernel times on one MI355X in this order: 1 x 151936 float32, T = 0.6, top-p 0.95: 4.1 +
+// 11.8 + 4.0 + 7.2 us, chains of dependent loads; 128 x 152064 of those: 14.9 (5.2 TB/s) +
+// 36.2 + 14.8 + 10.9; 500 x 151936 bf16, every row its own settings: 28.2 (5.4 TB/s) + 54.7 +
+// 39.9 + 19.2.  The second pass is bound by forming weights (18 float64 instructions a token;
+// all vector instructions keep its units busy three quarters of the time), the third by the
 // workgroups of rows that keep much of the vocabulary.  Before the groups, with counts for
 // every top-k and the borders found by every workgroup of the third pass: 106, 81 and 69 us
 // for the last three of the 500 rows.
@@ -422,7 +422,7 @@ struct alignas(16) RowState {
   u64 list[kListed];          // key << 32 | ~index of the tokens in the borders' bins
   uint32_t count[kHist];
   uint32_t part_top[kMaxParts];
-  uint32_t part_low[kMaxParts];   // smallest keys above kKeyNone, less kKeyNone + 1
+  float part_low[kMaxParts];      // smallest finite values (inf: none)
   uint32_t group_top[kGroups];
   uint32_t listed;
   uint32_t near;              // key that at least top-k tokens reach (Asked::near)
@@ -520,16 +520,19 @@ __global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) 
   const int lane = threadIdx.x & 63;
   for (int x = me.s * 64 + lane; x < kHist; x += a.parts * 64) st.mass[x] = 0, st.count[x] = 0;
   if (me.s == 0 && lane == 0) st.listed = 0, st.arrived = 0;
-  uint32_t key[4] = {kKeyNone, kKeyNone, kKeyNone, kKeyNone}, low = 0xFFFFFFFFu;
+  // (in floats: NaN is neither, -inf is no smallest value; counted at the end)
+  float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, least = INFINITY;
   Parts<BF16>(a, me.r).each(me.s, [&](int, const float (&x)[4], int) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t k = order_key(counted(x[e]));
-      key[e] = max(key[e], k);
-      low = min(low, k - (kKeyNone + 1));
+      most[e] = fmaxf(most[e], x[e]);
+      least = fminf(least, x[e] > -INFINITY ? x[e] : INFINITY);
     }
   });
-  low = ~wave_max32(~low);
+  uint32_t key[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) key[e] = order_key(counted(most[e]));
+  for (int off = 32; off; off >>= 1) least = fminf(least, __shfl_xor(least, off, 64));
   const int groups = groups_of_part(a.parts);
   uint32_t* group_top = st.group_top + me.s * groups;
   if (groups == 256) *reinterpret_cast<uint4*>(group_top + 4 * lane) = make_uint4(key[0], key[1], key[2], key[3]);
@@ -541,7 +544,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) 
     if (n == groups && lane < n) group_top[lane] = top;
     top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), off, 64)));
   }
-  if (lane == 0) st.part_top[me.s] = top, st.part_low[me.s] = low;
+  if (lane == 0) st.part_top[me.s] = top, st.part_low[me.s] = least;
 }
 
 // What the workgroup that finds a row's borders reads of its state, in one round of loads:
@@ -591,11 +594,11 @@ __device__ inline float octaves(float x, float top, float c) {
 // an octave overflow, 434 us; 49 with 128).
 __device__ inline float bins_an_octave(const SampleArgs& a, const RowState& st, uint32_t top, float c) {
   const int lane = threadIdx.x & 63;
-  uint32_t low = 0xFFFFFFFFu;
+  float low = INFINITY;
 #pragma unroll
-  for (int u = 0; u < kMaxParts / 64; ++u) low = min(low, lane + 64 * u < a.parts ? st.part_low[lane + 64 * u] : 0xFFFFFFFFu);
-  low = ~wave_max32(~low) + (kKeyNone + 1);
-  const float range = octaves(key_value(low), key_value(top), c);
+  for (int u = 0; u < kMaxParts / 64; ++u) low = fminf(low, lane + 64 * u < a.parts ? st.part_low[lane + 64 * u] : INFINITY);
+  for (int off = 32; off; off >>= 1) low = fminf(low, __shfl_xor(low, off, 64));
+  const float range = octaves(finite(low), key_value(top), c);
   float f = 32.f;
   while (f < 32.f * 1024.f && range * f < 0.49f * kFine) f *= 2.f;
   return f;
@@ -1161,7 +1164,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
 // rows that ask for little and rows that ask for much even out, more of them where all
 // would be fewer than eight a compute unit, no part of fewer than 512 logits.  (All four
 // passes of 500 mixed rows with workgroups of 37984, 16384 and 8192 logits: 160, 147 and 149
-// us; of 128 rows alike with 9504, 8448 and 4752: 76, 80 and 81.)
+// us before the bins of flat rows; of 128 rows alike with 9504, 8448 and 4752: 76, 80 and 81.)
 int row_parts(int rows, int vocab) {
   const int groups = std::max((2048 + rows - 1) / rows, vocab / 16384);
   return kPartWaves * std::max(1, std::min({kMaxParts / kPartWaves, groups, vocab / (512 * kPartWaves)}));

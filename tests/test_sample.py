@@ -318,3 +318,16 @@ def test_flat_rows(spread):
     u = rng.random(rows).astype(np.float32)
     got = run(x, "f32", T, k, p, m, u)
     check(x, u, got, T, k, p, m)
+
+
+@pytest.mark.parametrize("vocab", [300, 5003])
+def test_signalling_nan(vocab):
+    rng = np.random.default_rng(16)
+    x = (rng.normal(size=(8, vocab)) * 2).astype(np.float32)
+    bits = x.view(np.uint32)
+    for r in range(8):
+        bits[r, rng.choice(vocab, 200, replace=False)] = [0x7F800001, 0xFF800001, 0x7FC00000, 0xFFFFFFFF][r % 4]
+    T, k, p, m = np.ones(8), np.array([0, 5, 0, 1000] * 2), np.array([1.0, 0.9] * 4), np.zeros(8)
+    u = rng.random(8).astype(np.float32)
+    got = run(x, "f32", T, k, p, m, u)
+    check(x, u, got, T, k, p, m)
