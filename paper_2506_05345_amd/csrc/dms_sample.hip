@@ -96,6 +96,8 @@ __device__ inline float counted(float x) {
 // The same but for NaN and -0, in two instructions of five: NaN has no weight and lies
 // nowhere (comparisons are false), -0 weighs what 0 does.
 __device__ inline float finite(float x) { return x == INFINITY ? 0x1.fffffep127f : x; }
+// And with NaN such as fmaxf passes over: it answers a signalling one with NaN.
+__device__ inline float quiet(float x) { return __builtin_canonicalizef(finite(x)); }
 template <bool BF16>
 __device__ inline float logit(const void* row, int i) {
   if constexpr (BF16)
@@ -525,7 +527,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_max_kernel(SampleArgs a) 
   Parts<BF16>(a, me.r).each(me.s, [&](int, const float (&x)[4], int) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      most[e] = fmaxf(most[e], x[e]);
+      most[e] = x[e] > most[e] ? x[e] : most[e];     // (fmaxf of a signalling NaN is NaN)
       least = fminf(least, x[e] > -INFINITY ? x[e] : INFINITY);
     }
   });
@@ -889,7 +891,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
   if (ask.near) {
     const float least = key_value(max(st.near, kKeyNone));
     Parts<BF16>(a, me.r).each(me.s, [&](int i, const float (&given)[4], int n) {
-      const float x[4] = {finite(given[0]), finite(given[1]), finite(given[2]), finite(given[3])};
+      const float x[4] = {quiet(given[0]), quiet(given[1]), quiet(given[2]), quiet(given[3])};
       if (!(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= least)) return;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -899,7 +901,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
   }
   u64 sum = 0;
   Parts<BF16>(a, me.r).each(me.s, [&](int i, const float (&given)[4], int n) {
-    const float x[4] = {finite(given[0]), finite(given[1]), finite(given[2]), finite(given[3])};
+    const float x[4] = {quiet(given[0]), quiet(given[1]), quiet(given[2]), quiet(given[3])};
     const float nearest = octaves(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), top, c);
     if (!(nearest < end)) return;      // four at once: nearly all of most rows
 #pragma unroll
