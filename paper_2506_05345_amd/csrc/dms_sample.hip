@@ -998,7 +998,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(SampleArgs a) 
   };
   if (tid < kMaxParts) l.mass[tid] = ask.near ? 0 : mine;
   u64 border = 0;              // the last kept token of the listed ones, as the list holds it
-  if (ask.near || !cut.none) {
+  // (nothing listed: the k-th token is past all that have a weight, and those are ahead of
+  // the border's bin)
+  if (n > 0 && (ask.near || !cut.none)) {
     for (int x = tid; x < n; x += kRowThreads) l.list[0][x] = st.list[x];
     __syncthreads();
     sort_listed(l, n);

@@ -331,3 +331,24 @@ def test_signalling_nan(vocab):
     u = rng.random(8).astype(np.float32)
     got = run(x, "f32", T, k, p, m, u)
     check(x, u, got, T, k, p, m)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [4099, 5003, 30000])
+def test_top_k_that_ends_among_tokens_without_weight(vocab, dtype):
+    """2000 tokens with a weight, 1000 that lie 44 to 45 octaves below the largest and weigh nothing, others further
+    below; the k-th one before, at, among and past the weightless, without top-p: a border whose bin lists nothing."""
+    rng = np.random.default_rng(vocab + 17)
+    rows = 16
+    z = np.concatenate([[0.0], rng.uniform(0.5, 43.4, 1999), rng.uniform(44.3, 44.7, 1000),
+                        rng.uniform(46, 60, vocab - 3000)])
+    x = np.stack([rng.permutation(-z) for _ in range(rows)])
+    x[::4] = -z[::-1]                                   # the largest last
+    x = (x * math.log(2.0)).astype(np.float32)
+    k = np.array([1999, 2000, 2001, 2400, 2500, 2999, 3000, 3001] * 2)
+    m = np.where(np.arange(rows) < 8, 0.0, 1e-3)
+    u = rng.random(rows).astype(np.float32)
+    u[[0, 3, 4]] = 0.0
+    one = np.ones(rows)
+    got = run(x, dtype, one, k, one, m, u)
+    check(got[0], u, got, one, k, one, m)
