@@ -881,8 +881,10 @@ __global__ __launch_bounds__(kPartThreads) void sample_cut_kernel(SampleArgs a) 
   if (key == kKeyNone || cut.slow) return;
   const float top = key_value(key), c = static_cast<float>(set.c);
   // tokens nearer than `keep` are ahead of the listed bins, those from `end` on are
-  // out; no token past `far` passes min-p (and none past 45 octaves has a weight)
-  const float far = ask.least ? 43.01f - log2f(static_cast<float>(set.least)) : 45.f;
+  // out; no token past `far` passes min-p (and none past 45 octaves has a weight): a
+  // weight of 128 units and more is rounded by 1/256 of it, 0.0057 octaves, at most;
+  // smaller ones by up to all of it
+  const float far = ask.least && set.least >= 128.0 ? 43.01f - log2f(static_cast<float>(set.least)) : 45.f;
   const float keep = cut.none ? 64.f : cut.keep, end = cut.none ? far : cut.end;
   auto list = [&](float x, int i) {
     const uint32_t at = atomicAdd(&st.listed, 1u);

@@ -352,3 +352,21 @@ def test_top_k_that_ends_among_tokens_without_weight(vocab, dtype):
     one = np.ones(rows)
     got = run(x, dtype, one, k, one, m, u)
     check(got[0], u, got, one, k, one, m)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [300, 5003, 30000])
+def test_min_p_among_weights_of_few_units(vocab, dtype):
+    """min-p of 1e-14 to 1e-10: weights are rounded to integers before they are compared.  Tokens in the order of their
+    weights, the largest last, and u = 0: the first token kept is the one taken."""
+    rng = np.random.default_rng(vocab + 18)
+    m = np.array([1e-14, 5e-14, 1e-13, 1.2e-13, 2e-13, 3e-13, 1e-12, 4e-12, 7e-12, 8e-12, 1e-11, 1e-10])
+    rows = 3 * len(m)
+    z = np.sort(rng.uniform(33.5, 44.6, (rows, vocab)))[:, ::-1].copy()
+    z[:, -1] = 0
+    x = (-z * math.log(2.0)).astype(np.float32)
+    m = np.tile(m, 3)
+    k = np.repeat([0, vocab - 9, 7 * vocab // 8], len(m))
+    one, u = np.ones(rows), np.zeros(rows, np.float32)
+    got = run(x, dtype, one, k, one, m, u)
+    check(got[0], u, got, one, k, one, m)
