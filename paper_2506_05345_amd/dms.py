@@ -953,8 +953,8 @@ def dms_sample_workspace(cfg: DmsSampleConfig, rows) -> int:
 
 def dms_sample(cfg, rows, logits, temperature, top_k, top_p, min_p, u, tokens_out, logprobs_out, workspace,
                row_stride=None, stream=None):
-    """logits [rows, vocab] may be part of wider rows: the stride is its own, or given (device
-    addresses)."""
+    """logits [rows, vocab] or wider, the first vocab of each row: from a row to the next is the
+    tensor's own stride (flat tensors, device addresses: vocab), or row_stride."""
     w = "dms_sample"
     kind = _TYPE_KIND.get(cfg.logits_type)
     if logits is None or type(logits) is int:
@@ -966,13 +966,17 @@ def dms_sample(cfg, rows, logits, temperature, top_k, top_p, min_p, u, tokens_ou
             raise DmsError(DMS_ERR_INVALID, f"{w}: logits must be {kind}, got {logits.dtype}")
         if not logits.is_cuda:
             raise DmsError(DMS_ERR_INVALID, f"{w}: logits must be a GPU tensor")
+        flat = logits.dim() < 2 or logits.numel() == 0     # rows of the vocabulary, one after the other
+        if not flat and row_stride is None and logits.shape[-1] < cfg.vocab:
+            raise DmsError(DMS_ERR_INVALID, f"{w}: logits must have rows of {cfg.vocab}, got {logits.shape[-1]}")
         if logits.is_contiguous():
-            stride, have = cfg.vocab if row_stride is None else row_stride, logits.numel()
-        elif logits.dim() == 2 and logits.shape[1] == cfg.vocab and (cfg.vocab == 1 or logits.stride(1) == 1):
-            stride = row_stride if row_stride is not None else logits.stride(0) if logits.shape[0] > 1 else cfg.vocab
-            have = (logits.shape[0] - 1) * logits.stride(0) + cfg.vocab if logits.shape[0] else 0
+            stride, have = cfg.vocab if flat else logits.shape[-1], logits.numel()
+        elif logits.dim() == 2 and logits.shape[1] >= cfg.vocab and (logits.shape[1] == 1 or logits.stride(1) == 1):
+            stride = logits.stride(0) if logits.shape[0] > 1 else cfg.vocab
+            have = (logits.shape[0] - 1) * logits.stride(0) + logits.shape[1] if logits.shape[0] else 0
         else:
             raise DmsError(DMS_ERR_INVALID, f"{w}: logits must have dense rows of {cfg.vocab}")
+        stride = stride if row_stride is None else row_stride
         if rows > 0 and have < (rows - 1) * stride + cfg.vocab:
             raise DmsError(DMS_ERR_INVALID, f"{w}: logits holds fewer than {rows} rows")
     need = 0 if workspace is None or type(workspace) is int else \

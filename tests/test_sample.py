@@ -370,3 +370,41 @@ def test_min_p_among_weights_of_few_units(vocab, dtype):
     one, u = np.ones(rows), np.zeros(rows, np.float32)
     got = run(x, dtype, one, k, one, m, u)
     check(got[0], u, got, one, k, one, m)
+
+
+@pytest.mark.parametrize("vocab", [1000, 5003])
+def test_tensors_wider_than_the_vocabulary(vocab):
+    """Logits of a padded output layer, whole: rows begin where the tensor's own rows do.  Flat tensors are rows of the
+    vocabulary; narrower rows are refused."""
+    import torch
+    from paper_2506_05345_amd import dms
+    rng = np.random.default_rng(vocab + 19)
+    rows, wide = 12, vocab + 137
+    x = (rng.normal(size=(rows, vocab)) * 2).astype(np.float32)
+    u = rng.random(rows).astype(np.float32)
+    want = [oracle.sample_token(x[r], 0.8, 0, 0.9, 0.0, u[r])[0] for r in range(rows)]
+    cfg = dms.make_sample_config(vocab, temperature=0.8, top_p=0.9)
+    ws = torch.empty(dms.dms_sample_workspace(cfg, rows), dtype=torch.uint8, device="cuda")
+    ud = torch.from_numpy(u).cuda()
+    padded = torch.full((rows, wide), 50.0, device="cuda")
+    padded[:, :vocab] = torch.from_numpy(x)
+    dense = padded[:, :vocab].contiguous()
+    wider = torch.full((rows, wide + 5), 50.0, device="cuda")
+    wider[:, 2:2 + wide] = padded
+
+    def tokens(logits, count=rows, **kw):
+        out = torch.full((rows,), -7, dtype=torch.int32, device="cuda")
+        dms.dms_sample(cfg, count, logits, None, None, None, None, ud, out, None, ws, **kw)
+        return out[:count].tolist()
+
+    assert tokens(padded) == tokens(padded, row_stride=wide) == want
+    assert tokens(padded.view(3, 4, wide)) == tokens(padded.view(rows, 1, wide)) == want
+    assert tokens(wider[:, 2:2 + wide]) == tokens(padded[:, :vocab]) == tokens(padded.view(-1), row_stride=wide) == want
+    assert tokens(dense) == tokens(dense.view(-1)) == tokens(dense.view(4, 3, vocab)) == want
+    assert tokens(padded[:0], 0) == tokens(padded[:0, :7], 0) == tokens(padded[0, :0], 0) == []
+    assert tokens(padded[:5], 5) == tokens(padded, 5) == want[:5]
+    assert tokens(padded[3], 1) == [oracle.sample_token(x[3], 0.8, 0, 0.9, 0.0, u[0])[0]]
+    narrow = torch.zeros((2 * rows, vocab - 1), device="cuda")
+    for logits in (narrow, narrow.view(rows, 2 * vocab - 2)[:, ::2], padded.t().contiguous().t(), padded[:rows - 1]):
+        with pytest.raises(dms.DmsError):
+            tokens(logits)
