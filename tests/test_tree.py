@@ -549,3 +549,74 @@ def test_pages_past_four_gigabytes():
                         small.ws)
     step(small.cache)
     assert torch.equal(got, out)
+
+
+def ragged(n, lens, nodes):
+    """n sequences that take their lengths and trees from two cycles; the first and the last have no nodes."""
+    a, b = [lens[i % len(lens)] for i in range(n)], [nodes[i % len(nodes)] for i in range(n)]
+    b[0] = b[-1] = 0
+    return a, b
+
+
+LISTS = {
+    # 12 heads, 400 columns of 25 units each at most: 16 parts, cut without regard to heads
+    "units": ([700, 40, 333, 5, 64, 129], [200, 0, 130, 5, 0, 64], 2, 16, 64, 16, 64, 0.6),
+    # four long heads in 16 parts: every head over several of them
+    "long": ([3100, 2500], [200, 3], 2, 16, 64, 256, 64, 0.3),
+    # many short heads, several to a part, of 32, 64 and 128 columns a unit
+    "32": (*ragged(72, [300, 0, 40, 1, 95, 130, 33], [6, 1, 0, 3, 0]), 4, 5, 128, 16, 32, 0.6),
+    "64": (*ragged(70, [260, 31, 0, 150, 64], [16, 0, 2, 7]), 4, 4, 64, 9, 64, 0.6),
+    "128": (*ragged(66, [200, 90, 3, 0, 420], [18, 0, 0, 5, 1, 11]), 4, 7, 128, 20, 64, 0.5),
+    # more heads than the plan holds in LDS (512)
+    "heads": (*ragged(150, [120, 0, 33, 64], [2, 0, 1, 3, 0, 0]), 4, 2, 64, 8, 32, 0.6),
+}
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("name", LISTS)
+def test_tiles_cut_without_regard_to_heads(name, kv):
+    """Calls of many heads or tiles: the tiles of all heads are one list in equal parts, which begin and end anywhere in a
+    head and go on past heads without nodes."""
+    import torch
+    lens, nodes, H, g, d, w, P, p = LISTS[name]
+    c = Call(61 + len(name), lens, nodes, H, g, d, w, P, kv, p=p)
+    out = c.attend()
+    c.check(out)
+    # the sizes do ask for such a list: two workgroups a compute unit, at least eight tiles a part
+    view = c.cache.export(0)
+    tiles = sum(-(-int(view.L[s, h]) // 32) + -(-m // 32) for s, m in zip(c.ids, nodes) if m for h in range(H))
+    cols = max(nodes) * g
+    units = -(-cols // (32 if cols <= 32 else 64 if cols <= 64 else 128))
+    most = 2 * torch.cuda.get_device_properties(0).multi_processor_count // 8 // units * 8
+    assert c.n * H > 512 or c.n * H > most // 2 or tiles >= 16 * most
+    assert tiles > 2 * 8
+    c.ws.random_(0, 256)
+    assert torch.equal(out, c.attend())
+
+
+@pytest.mark.parametrize("kv", ["bf16", "fp8"])
+@pytest.mark.parametrize("name", ["units", "32", "64", "128"])
+def test_hidden_infinities_where_heads_share_a_part(name, kv):
+    """Dead slots of NaN bytes, and a node of infinite values in one head: only its descendants and that head change,
+    whatever else the workgroup attends before and after."""
+    import torch
+    lens, nodes, H, g, d, w, P, p = LISTS[name]
+    c = Call(71 + len(name), lens, nodes, H, g, d, w, P, kv, p=p)
+    c.cache.pools[0].view(torch.uint8).fill_(0xFF)
+    c.dms.dms_init_state(c.cache.ctx)
+    c.dms.dms_append_chunk(c.cache.ctx, 0, c.n, dev(c.ids), dev(c.cu_ctx), sum(lens), max(lens), dev(c.k0, "bf16"),
+                           dev(c.v0, "bf16"), dev(c.f0))
+    base = c.attend()
+    c.check(base)
+    t = c.tensors()
+    i = int(np.argmax(c.nodes))
+    x = c.cu[i] + 1
+    below = [c.cu[i] + y for y, q in enumerate(oracle.tree_paths(c.parents[c.cu[i]:c.cu[i + 1]])) if 1 in q]
+    bad = t["v"].clone()
+    bad[x, 1, 9] = np.inf
+    out = c.attend(dict(t, v=bad))
+    changed = (out != base) | ~torch.isfinite(out.float())
+    allowed = torch.zeros_like(changed)
+    allowed[below, g:2 * g] = True
+    assert not (changed & ~allowed).any()
+    assert not torch.isfinite(out[x, g:2 * g, 9].float()).any()
