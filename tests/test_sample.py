@@ -408,3 +408,85 @@ def test_tensors_wider_than_the_vocabulary(vocab):
     for logits in (narrow, narrow.view(rows, 2 * vocab - 2)[:, ::2], padded.t().contiguous().t(), padded[:rows - 1]):
         with pytest.raises(dms.DmsError):
             tokens(logits)
+
+
+SETTINGS = {
+    "none": dict(), "k": dict(k=9), "many": dict(k=3000), "p": dict(p=0.8), "min": dict(m=0.1),
+    "kp": dict(k=3000, p=0.8), "all": dict(k=20, p=0.9, m=0.05),
+}
+
+
+def among_others(rng, special, vocab, **fixed):
+    """Special rows with an ordinary one before and after each, and settings for all of them."""
+    x = (rng.normal(size=(2 * len(special) + 1, vocab)) * 2).astype(np.float32)
+    x[1::2] = special
+    rows = len(x)
+    return x, np.full(rows, fixed.get("k", 0)), np.full(rows, fixed.get("p", 1.0)), np.full(rows, fixed.get("m", 0.0)), \
+        rng.random(rows).astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("what", SETTINGS)
+@pytest.mark.parametrize("vocab", [5003, 20000])
+def test_special_values_of_rows_in_parts(vocab, what, dtype):
+    """Masked, NaN, infinite, lowest, largest and smallest logits in the launches of large vocabularies, between ordinary
+    rows of the same call."""
+    rng = np.random.default_rng(vocab + len(what))
+    low, most = (np.finfo(np.float32).min, np.finfo(np.float32).max) if dtype == "f32" else (-3.3895314e38, 3.3895314e38)
+    x = rng.normal(size=(16, vocab)).astype(np.float32)
+    x[0] = -np.inf
+    x[1] = np.nan
+    x[2] = -np.inf
+    x[2, vocab - 3] = 3
+    x[3, ::2] = -np.inf
+    x[4, ::3] = np.nan
+    x[5, 4100] = np.inf
+    x[6, [20, 4500]] = np.inf
+    x[7] = low
+    x[8, 1:] = low
+    x[9, 5:] = -np.inf
+    x[10] = most
+    x[11] = np.float32(1e-45) if dtype == "f32" else 0
+    x[12, ::2] = np.nan
+    x[12, 1::2] = -np.inf
+    x[12, 4098] = low
+    x[13] = np.where(rng.random(vocab) < 0.5, low, most)
+    x[14] = rng.normal(size=vocab) * 1e-38              # denormal, most of them
+    x[15, :4099] = np.inf
+    x, k, p, m, u = among_others(rng, x, vocab, **SETTINGS[what])
+    u[3::4], u[1] = 5.0, -1.0
+    T = np.full(len(x), 0.9)
+    got = run(x, dtype, T, k, p, m, u)
+    check(got[0], u, got, T, k, p, m)
+    assert got[1][1] == -1 and got[1][3] == -1 and got[1][5] == vocab - 3
+    nan = np.full(len(x), np.nan)
+    got = run(x, dtype, nan, None, nan, nan, nan)       # greedy, no cuts
+    check(got[0], np.zeros(len(x)), got, nan, k * 0, nan, nan)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("what", SETTINGS)
+@pytest.mark.parametrize("vocab", [5003, 20000])
+def test_extreme_temperatures_of_rows_in_parts(vocab, what, dtype):
+    rng = np.random.default_rng(vocab + len(what) + 1)
+    T = np.array([1e-38, 1e-45, 1e-6, 0.01, 100.0, 1e30, 3e38, np.inf])
+    x, k, p, m, u = among_others(rng, rng.normal(size=(len(T), vocab)), vocab, **SETTINGS[what])
+    x[1::2, ::7] = -np.inf
+    T = np.concatenate([[1.0], np.stack([T, np.ones(len(T))], 1).ravel()])
+    got = run(x, dtype, T, k, p, m, u)
+    check(got[0], u, got, T, k, p, m)
+
+
+@pytest.mark.parametrize("vocab", [30011, 262144])
+def test_flat_rows_with_a_few_large_logits(vocab):
+    """Eight logits far above the rest of a flat row: thousands of tokens within a bin of the border, which no list holds."""
+    rng = np.random.default_rng(vocab + 20)
+    T, p = np.array([0.6, 1.0, 1.0, 1.7, 1.7, 1.0]), np.array([0.3, 0.8, 0.95, 0.5, 0.95, 0.9])
+    rows = len(T)
+    x = (rng.normal(size=(rows, vocab)) * 0.5).astype(np.float32)
+    for r in range(rows):
+        x[r, rng.choice(vocab, 8, replace=False)] += 6
+    k, m = np.array([0, 0, 0, 0, 0, vocab // 3]), np.zeros(rows)
+    u = rng.random(rows).astype(np.float32)
+    got = run(x, "f32", T, k, p, m, u)
+    check(got[0], u, got, T, k, p, m)
