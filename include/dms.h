@@ -693,7 +693,10 @@ int dms_tree_accept(int n, const int32_t* cu_nodes_dev, int total_nodes, int max
  * any page format and eviction mode, with counts that only the device knows.
  * path_dev int32 [total_nodes] and path_len_dev int32 [n] as dms_tree_accept
  * writes them (any path of nodes of the tree is taken); k_dev, v_dev, flags_dev:
- * of all nodes, 16-byte aligned (latent rows: v_dev is ignored). */
+ * of all nodes, 16-byte aligned (latent rows: v_dev is ignored).  A refused call
+ * changes nothing in its layer.  Layers have pages and lengths of their own: the
+ * call of a later layer may be refused (DMS_ERR_CAPACITY, DMS_ERR_OUT_OF_PAGES)
+ * after those of earlier ones appended, as with appends. */
 int dms_tree_commit(dms_ctx* ctx, int layer, int n, const int32_t* seq_ids_dev,
                     const int32_t* cu_nodes_dev, int total_nodes, int max_nodes,
                     const int32_t* path_dev, const int32_t* path_len_dev, const void* k_dev,

@@ -22,13 +22,16 @@
 //   sample_pick_kernel  a workgroup a row sorts the listed tokens, cuts them, and finds
 //                       the picked one: among them, if few are kept and all are
 //                       listed, else in the part that holds it, by walking that.
-// A row whose borders' bins hold too many tokens (many equal logits) is done by the
-// last launch alone, as shorter rows are (sample_row).
+// A row whose borders' bins hold too many tokens is done by the last launch alone, as
+// shorter rows are (sample_row): equal logits, and flat rows with a few large ones, for
+// bins are as fine as the range of a row allows.  Deviation 0.5 and eight logits 6 higher,
+// T = 1, top-p 0.8: 151936 logits 390 us of that launch, 64 such rows 700; 262144 logits
+// 660, 64 rows 1190.
 //
 // Kernel times on one MI355X in this order: 1 x 151936 float32, T = 0.6, top-p 0.95: 4.1 +
-// 11.8 + 4.0 + 7.2 us, chains of dependent loads; 128 x 152064 of those: 14.9 (5.2 TB/s) +
-// 36.2 + 14.8 + 10.9; 500 x 151936 bf16, every row its own settings: 28.2 (5.4 TB/s) + 54.7 +
-// 39.9 + 19.2.  The second pass is bound by forming weights (18 float64 instructions a token;
+// 11.7 + 3.9 + 7.3 us, chains of dependent loads; 128 x 152064 of those: 14.3 (5.4 TB/s) +
+// 37.3 + 15.0 + 11.0; 500 x 151936 bf16, every row its own settings: 29.0 (5.2 TB/s) + 55.8 +
+// 39.5 + 19.0.  The second pass is bound by forming weights (18 float64 instructions a token;
 // all vector instructions keep its units busy three quarters of the time), the third by the
 // workgroups of rows that keep much of the vocabulary.  Before the groups, with counts for
 // every top-k and the borders found by every workgroup of the third pass: 106, 81 and 69 us
@@ -593,7 +596,8 @@ __device__ inline float octaves(float x, float top, float c) {
 }
 // Bins to an octave of a row: 32, or so many more, a power of two, that the fine bins hold
 // all of a flat row (152064 logits of deviation 0.5 at T = 1.7, top-p 0.5: lists of 32 bins
-// an octave overflow, 434 us; 49 with 128).
+// an octave overflow, 434 us; 49 with 128).  By the range of the row: a single large logit
+// keeps them coarse.
 __device__ inline float bins_an_octave(const SampleArgs& a, const RowState& st, uint32_t top, float c) {
   const int lane = threadIdx.x & 63;
   float low = INFINITY;
